@@ -305,6 +305,157 @@ int qeft_linear_bwd(const qeft_desc_t* desc, const qeft_weight_t* w, const void*
 int qeft_weak_grad_noalloc(const qeft_desc_t* desc, const void* dY, int64_t M, int64_t lddy,
                            const void* Xw, int64_t ldxw, void* dW, int out_dtype, int accumulate, void* stream);
 
+/* ==== between a decoder block's linear layers: a paged key-value cache, the attention of one new token per sequence
+ * over it, eviction by accumulated attention weight, and the norms on both sides of a block ====
+ *
+ * The conventions above hold: device pointers, the caller's workspace, one stream, checks before any launch.  Whole-number
+ * inputs that lie in device memory (page tables, lengths, indices) cannot be checked by the host: the kernels clamp or skip
+ * what is out of range as stated at each call, so that no value leads to an access outside the buffers described.
+ *
+ * The cache: `pages` pages of page_size tokens, each of kv_heads heads of head_dim fp16 values (head_dim a multiple of 8,
+ * at most QEFT_MAX_HEAD_DIM), keys and values in two pools of the same layout.  Head h of slot s of page p starts at element
+ * p * page_stride + h * head_stride + s * token_stride of a pool (strides are multiples of 8; any order of the three axes).
+ * A sequence's tokens lie in the pages that its row of the page table (int32 [seqs][ld_table], table_pages entries used)
+ * names: token t in slot t % page_size of page table[b][t / page_size].  page_size is any number from 1; a multiple of 8
+ * is fastest (one table entry then serves 8 tokens of a wave). */
+#define QEFT_MAX_HEAD_DIM 256
+/* Most rows (a grid's workgroups) of one of these calls: tokens appended, rows normed, seqs * kv_heads of an eviction (and its possible moves, seqs *
+ * kv_heads * longest / 2 / 64, four times that); seqs * heads of an attention an eighth of it.  More is QEFT_ERR_SHAPE. */
+#define QEFT_MAX_ROWS (1 << 21)
+typedef struct {
+    int32_t pages, page_size, kv_heads, head_dim;
+    int64_t page_stride, head_stride, token_stride;   /* elements */
+} qeft_cache_desc_t;
+typedef struct {
+    void* k;
+    void* v;
+} qeft_cache_t;
+typedef struct {
+    const int32_t* table;   /* int32 [seqs][ld_table] */
+    int64_t ld_table;
+    int32_t table_pages;    /* entries per sequence */
+    int32_t seqs;
+} qeft_table_t;
+
+/* New tokens enter the cache: token t of the call (0 <= t < tokens) belongs to sequence seq[t] (seq NULL: sequence t) and
+ * becomes its cached token index[t].  k and v, fp16 [tokens][ldk] / [ldv] with kv_heads * head_dim values per row, are written to
+ * its slot, keys rotated; q (optional, fp16 [tokens][ldq], heads * head_dim values) is rotated into q_out (which may be q).
+ * Rotation: rot (fp32 [positions][ld_rot]) holds rot_dim / 2 cosines and then as many sines for every position; the first rot_dim
+ * values of a head (rot_dim even, at most head_dim) are pairs rot_dim / 2 apart: (a, b) -> (a c - b s, b c + a s), in fp32, rounded
+ * once.  Position of token t: pos[t], or index[t] where pos is NULL, clamped to 0 .. positions - 1.  rot_dim == 0: no rotation.
+ * A token whose sequence, index or page is out of range is not stored (its q is rotated all the same).  Two tokens of one
+ * call for the same slot: either may end up there. */
+typedef struct {
+    const void *q, *k, *v;
+    void* q_out;
+    int64_t ldq, ldq_out, ldk, ldv;
+    const int32_t *seq, *index, *pos;
+    const float* rot;
+    int64_t ld_rot;
+    int32_t positions, rot_dim, heads;
+    int64_t tokens;
+} qeft_append_t;
+int qeft_cache_append(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, const qeft_table_t* table, const qeft_append_t* a,
+                      void* stream);
+
+/* Attention of one new token per sequence over its cached tokens: out[b][h] = sum_t p[t] V[t], p = softmax_t(scale * q[b][h] . K[t])
+ * over t < lens[b], with kv head h / (heads / kv_heads); q and out fp16 [seqs][ldq] / [ldo], heads * head_dim values per row.
+ * lens int32 [seqs] on the device; `longest` is the host's upper bound of it (a longer sequence is cut there and at
+ * table_pages * page_size; at most QEFT_MAX_DIM).  lens[b] <= 0: zeros.  Slots at or behind the length are never used, whatever they hold.
+ * Table entries of used tokens are clamped to the pool.  Products of fp16 values, sums and the softmax are fp32; a probability enters the
+ * product with V as the sum of two fp16 values (22 bits), the result is rounded once.  Not-a-number or infinite keys and
+ * values among a sequence's own tokens give non-finite results in the channels they reach.
+ * score (optional, fp32 [seqs][kv_heads][ld_score], ld_score >= min(longest, table_pages * page_size)): the weight of every
+ * token, sum of p[t] over the query heads of the kv head, is written there, or added if accumulate != 0; entries behind the
+ * length keep their values.
+ * ws: qeft_attn_workspace bytes, 16-byte aligned (QEFT_ERR_WORKSPACE otherwise; 0 bytes: NULL).  The results do not depend on the
+ * order in which workgroups run. */
+size_t qeft_attn_workspace(const qeft_cache_desc_t* desc, int64_t seqs, int32_t heads, int64_t longest, int weights);
+typedef struct {
+    const int32_t* lens;
+    int64_t longest;
+    const void* q;
+    void* out;
+    int64_t ldq, ldo;
+    int32_t heads;
+    float scale;
+    float* score;
+    int64_t ld_score;
+    int32_t accumulate;
+    void* ws;
+    size_t ws_bytes;
+} qeft_attn_t;
+int qeft_attn_decode(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, const qeft_table_t* table, const qeft_attn_t* a,
+                     void* stream);
+
+/* Eviction: every head of a sequence of more than `budget` tokens keeps `budget` of them, which end up in its first `budget`
+ * slots.  score (fp32) and pos (int32), both [seqs][kv_heads][ld], hold the accumulated weight and the position of every cached
+ * token of a head; seen int32 [seqs] the number of positions a sequence has seen.  Always preferred: tokens with
+ * pos < keep_first or pos >= seen - keep_last (they rank as a score of +infinity); the others by score.  Equal ranks: the lower slot
+ * stays; -0 equals +0; not-a-number ranks above infinity.  Kept tokens in slots < budget stay where they are; the i-th kept token of
+ * the others (in slot order) moves, keys, values, score and position, into the i-th freed slot.  score_out and pos_out
+ * (each the same array as score / pos, or one that does not overlap it; pitch ld_out) receive the entries of slots < min(lens, budget), lens_out
+ * (int32 [seqs], may be lens) that number; entries behind it keep their values.  Sequences within the budget keep everything.
+ * lens is clamped to 0 .. min(longest, table_pages * page_size); ld >= that bound, ld_out >= min(that, budget).
+ * Rows are seqs * kv_heads; table entries of moved tokens are clamped to the pool; pages must not be shared between sequences.
+ * ws: qeft_evict_workspace bytes, 16-byte aligned. */
+size_t qeft_evict_workspace(const qeft_cache_desc_t* desc, int64_t seqs, int64_t longest, int64_t budget);
+typedef struct {
+    const int32_t *lens, *seen;
+    int64_t longest, budget;
+    const float* score;
+    const int32_t* pos;
+    int64_t ld;
+    int32_t keep_first, keep_last;
+    float* score_out;
+    int32_t* pos_out;
+    int64_t ld_out;
+    int32_t* lens_out;
+    void* ws;
+    size_t ws_bytes;
+} qeft_evict_t;
+int qeft_cache_evict(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, const qeft_table_t* table, const qeft_evict_t* a,
+                     void* stream);
+
+/* Norms around a block.  With unit(z) = z / sqrt(mean(z^2) + eps) over the n values of a row and u = y, or unit(y) * w_post
+ * where w_post is given (the norm after the block),
+ *     h = r + scale * gate * u        x = unit(h) * w_pre  (the norm before the next block; of h as stored)
+ * y, x fp16 and r, h of residual dtype (QEFT_DTYPE_F16 or _F32), [m][ld]; weights fp16 [n]; gate: none (NULL), fp16 [n] (CHANNEL) or fp16
+ * [m][ldg] (TOKEN).  y NULL: h is r itself and only x is computed (h, w_post and gate must be NULL).  h may be r; x may be y.
+ * The arithmetic is fp32 with one rounding per output.  n from 1 to QEFT_MAX_DIM, any number; rows and weights are 16-byte
+ * aligned, pitches multiples of 8.
+ * qeft_norm_bwd: with t = dh + unit's gradient of (dx * w_pre) at h (dh, residual dtype, NULL: zero),
+ *     dr = t    dy = scale * gate * t through u's gradient    dw_pre = sum_rows dx * unit(h)
+ *     dw_post = sum_rows scale * gate * t * unit(y)           dgate = scale * u * t, summed over the rows for a CHANNEL gate
+ * dr of residual dtype (may be dh), dy fp16 (may be dx), dw_pre, dw_post fp32 [n]; dgate fp32 [n] (CHANNEL) or fp16 [m][ldg] (TOKEN).
+ * Every gradient may be NULL (not computed).  accumulate != 0 adds dw_pre, dw_post and a CHANNEL gate's dgate to what is there.  Sums over rows are
+ * taken in a fixed order.  m == 0: a no-op, but for the sums, which are set to zero unless accumulated.
+ * ws: qeft_norm_workspace bytes, 16-byte aligned, needed where one of those sums is asked for. */
+enum { QEFT_GATE_NONE = 0, QEFT_GATE_CHANNEL = 1, QEFT_GATE_TOKEN = 2 };
+typedef struct {
+    int32_t n, residual_dtype, gate;
+    float scale, eps;
+} qeft_norm_desc_t;
+typedef struct {
+    const void *r, *y, *gate, *w_pre, *w_post;
+    void *h, *x;
+    int64_t ldr, ldy, ldg, ldh, ldx;
+    int64_t m;
+} qeft_norm_fwd_t;
+typedef struct {
+    const void *dx, *dh, *h, *y, *gate, *w_pre, *w_post;
+    void *dr, *dy, *dgate;
+    float *dw_pre, *dw_post;
+    int64_t lddx, lddh, ldh, ldy, ldg, lddr, lddy, lddg;
+    int64_t m;
+    int32_t accumulate;
+    void* ws;
+    size_t ws_bytes;
+} qeft_norm_bwd_t;
+int qeft_norm_fwd(const qeft_norm_desc_t* desc, const qeft_norm_fwd_t* a, void* stream);
+size_t qeft_norm_workspace(const qeft_norm_desc_t* desc, int64_t m);
+int qeft_norm_bwd(const qeft_norm_desc_t* desc, const qeft_norm_bwd_t* a, void* stream);
+
 /* Static, never NULL. */
 const char* qeft_status_string(int status);
 

@@ -24,6 +24,7 @@ QEFT_ERR_WORKSPACE, QEFT_ERR_UNSUPPORTED, QEFT_ERR_HIP = -5, -6, -7
 QEFT_OP_FWD, QEFT_OP_BWD_DX, QEFT_OP_WEAK_GRAD, QEFT_OP_FWD_IRREGULAR, QEFT_OP_BWD_DX_IRREGULAR, QEFT_OP_BWD = 0, 1, 2, 3, 4, 5
 QEFT_DTYPE_F16, QEFT_DTYPE_F32 = 0, 1
 QEFT_LAYOUT_CANONICAL, QEFT_LAYOUT_DENSE3 = 0, 1
+QEFT_GATE_NONE, QEFT_GATE_CHANNEL, QEFT_GATE_TOKEN = 0, 1, 2
 _DTYPES = {torch.float16: QEFT_DTYPE_F16, torch.float32: QEFT_DTYPE_F32}
 
 
@@ -41,6 +42,52 @@ class qeft_layout_t(C.Structure):
 
 class qeft_weight_t(C.Structure):
     _fields_ = [("qweight", C.c_void_p), ("scales", C.c_void_p), ("zeros", C.c_void_p), ("weak", C.c_void_p)]
+
+
+class qeft_cache_desc_t(C.Structure):
+    _fields_ = [("pages", C.c_int32), ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64)]
+
+
+class qeft_cache_t(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)]
+
+
+class qeft_table_t(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("ld_table", C.c_int64), ("table_pages", C.c_int32), ("seqs", C.c_int32)]
+
+
+class qeft_append_t(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_out", C.c_void_p), ("ldq", C.c_int64), ("ldq_out", C.c_int64),
+                ("ldk", C.c_int64), ("ldv", C.c_int64), ("seq", C.c_void_p), ("index", C.c_void_p), ("pos", C.c_void_p), ("rot", C.c_void_p),
+                ("ld_rot", C.c_int64), ("positions", C.c_int32), ("rot_dim", C.c_int32), ("heads", C.c_int32), ("tokens", C.c_int64)]
+
+
+class qeft_attn_t(C.Structure):
+    _fields_ = [("lens", C.c_void_p), ("longest", C.c_int64), ("q", C.c_void_p), ("out", C.c_void_p), ("ldq", C.c_int64), ("ldo", C.c_int64),
+                ("heads", C.c_int32), ("scale", C.c_float), ("score", C.c_void_p), ("ld_score", C.c_int64), ("accumulate", C.c_int32),
+                ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
+class qeft_evict_t(C.Structure):
+    _fields_ = [("lens", C.c_void_p), ("seen", C.c_void_p), ("longest", C.c_int64), ("budget", C.c_int64), ("score", C.c_void_p),
+                ("pos", C.c_void_p), ("ld", C.c_int64), ("keep_first", C.c_int32), ("keep_last", C.c_int32), ("score_out", C.c_void_p),
+                ("pos_out", C.c_void_p), ("ld_out", C.c_int64), ("lens_out", C.c_void_p), ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
+class qeft_norm_desc_t(C.Structure):
+    _fields_ = [("n", C.c_int32), ("residual_dtype", C.c_int32), ("gate", C.c_int32), ("scale", C.c_float), ("eps", C.c_float)]
+
+
+class qeft_norm_fwd_t(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("r", "y", "gate", "w_pre", "w_post", "h", "x")] + \
+               [(f, C.c_int64) for f in ("ldr", "ldy", "ldg", "ldh", "ldx", "m")]
+
+
+class qeft_norm_bwd_t(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("dx", "dh", "h", "y", "gate", "w_pre", "w_post", "dr", "dy", "dgate", "dw_pre", "dw_post")] + \
+               [(f, C.c_int64) for f in ("lddx", "lddh", "ldh", "ldy", "ldg", "lddr", "lddy", "lddg", "m")] + \
+               [("accumulate", C.c_int32), ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
 
 
 EXPORTS = {
@@ -78,6 +125,17 @@ EXPORTS = {
                                   C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "qeft_weak_grad_noalloc": (C.c_int, [C.POINTER(qeft_desc_t), C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64,
                                          C.c_void_p, C.c_int, C.c_int, C.c_void_p]),
+    "qeft_cache_append": (C.c_int, [C.POINTER(qeft_cache_desc_t), C.POINTER(qeft_cache_t), C.POINTER(qeft_table_t), C.POINTER(qeft_append_t),
+                                    C.c_void_p]),
+    "qeft_attn_workspace": (C.c_size_t, [C.POINTER(qeft_cache_desc_t), C.c_int64, C.c_int32, C.c_int64, C.c_int]),
+    "qeft_attn_decode": (C.c_int, [C.POINTER(qeft_cache_desc_t), C.POINTER(qeft_cache_t), C.POINTER(qeft_table_t), C.POINTER(qeft_attn_t),
+                                   C.c_void_p]),
+    "qeft_evict_workspace": (C.c_size_t, [C.POINTER(qeft_cache_desc_t), C.c_int64, C.c_int64, C.c_int64]),
+    "qeft_cache_evict": (C.c_int, [C.POINTER(qeft_cache_desc_t), C.POINTER(qeft_cache_t), C.POINTER(qeft_table_t), C.POINTER(qeft_evict_t),
+                                   C.c_void_p]),
+    "qeft_norm_fwd": (C.c_int, [C.POINTER(qeft_norm_desc_t), C.POINTER(qeft_norm_fwd_t), C.c_void_p]),
+    "qeft_norm_workspace": (C.c_size_t, [C.POINTER(qeft_norm_desc_t), C.c_int64]),
+    "qeft_norm_bwd": (C.c_int, [C.POINTER(qeft_norm_desc_t), C.POINTER(qeft_norm_bwd_t), C.c_void_p]),
     "qeft_status_string": (C.c_char_p, [C.c_int]),
 }
 
@@ -148,7 +206,8 @@ class Weight:
 
 
 _MARSHALLED = ("qeft_linear_fwd", "qeft_linear_fwd_group", "qeft_linear_bwd_dx", "qeft_linear_bwd", "qeft_linear_fwd_irregular",
-               "qeft_linear_bwd_dx_irregular", "qeft_weak_grad")
+               "qeft_linear_bwd_dx_irregular", "qeft_weak_grad", "qeft_cache_append", "qeft_attn_decode", "qeft_cache_evict", "qeft_norm_fwd",
+               "qeft_norm_bwd")
 
 
 def _load_marshal():
@@ -156,7 +215,7 @@ def _load_marshal():
         from . import _marshal as m
     except ImportError:   # not built, or not for this torch: every call is ctypes'
         return types.SimpleNamespace(**{n.removeprefix("qeft_"): lambda *args: None for n in _MARSHALLED})
-    m.init(tuple(C.cast(getattr(raw, n), C.c_void_p).value for n in _MARSHALLED), qeft_desc_t, Weight)
+    m.init(tuple(C.cast(getattr(raw, n), C.c_void_p).value for n in _MARSHALLED), qeft_desc_t, Weight, qeft_cache_desc_t, qeft_norm_desc_t)
     return m
 
 
@@ -408,3 +467,265 @@ def qeft_linear_bwd(desc, w: Weight, dY: torch.Tensor, Xw: torch.Tensor, dX: tor
     _check(st, "qeft_linear_bwd")
     return dX, dW
 
+
+
+# ---- between the linear layers: paged cache, attention of one token, eviction, norms ---------------------------------------------------------
+#
+# These calls check what the C functions cannot see, the types and shapes of tensors, and raise QeftError for what does not fit.
+
+def _fail(status: int, where: str, what: str):
+    e = QeftError(status, where)
+    e.args = (f"{e.args[0]}: {what}",)
+    raise e
+
+
+def _take(where, name, t, dtype, shape, optional=False):
+    """Pointer and row pitch of tensor t of this type and shape (entries None: any), whose rows are contiguous and whose leading axes, if there are
+    three, lie one behind the other."""
+    if t is None:
+        if not optional:
+            _fail(QEFT_ERR_NULL, where, f"{name} is missing")
+        return 0, 0
+    if t.dtype != dtype or t.dim() != len(shape):
+        _fail(QEFT_ERR_UNSUPPORTED, where, f"{name} is {t.dtype} of {t.dim()} axes, not {dtype} of {len(shape)}")
+    if any(want is not None and have != want for have, want in zip(t.shape, shape)):
+        _fail(QEFT_ERR_SHAPE, where, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        _fail(QEFT_ERR_UNSUPPORTED, where, f"{name} is not on the current GPU")
+    if t.numel() == 0:   # (an empty tensor's pitch says nothing)
+        return t.data_ptr(), max(t.shape[-1], 1) + 7 & ~7
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        _fail(QEFT_ERR_UNSUPPORTED, where, f"{name}'s rows are not contiguous")
+    ld = t.stride(-2) if t.dim() > 1 and t.shape[-2] > 1 else None
+    if t.dim() == 3 and t.shape[0] > 1:
+        if ld is None:
+            ld = t.stride(0)
+        elif t.stride(0) != ld * t.shape[1]:
+            _fail(QEFT_ERR_UNSUPPORTED, where, f"{name}'s leading axes do not lie one behind the other")
+    elif ld is None:   # one row: any pitch it may have
+        ld = t.shape[-1] + 7 & ~7
+    return t.data_ptr(), ld
+
+
+def make_cache_desc(pages, page_size, kv_heads, head_dim, page_stride=None, head_stride=None, token_stride=None) -> qeft_cache_desc_t:
+    """Strides in elements; by default a pool is [pages][kv_heads][page_size][head_dim], contiguous."""
+    return qeft_cache_desc_t(pages, page_size, kv_heads, head_dim, kv_heads * page_size * head_dim if page_stride is None else page_stride,
+                             page_size * head_dim if head_stride is None else head_stride, head_dim if token_stride is None else token_stride)
+
+
+class Cache:
+    """The two pools of a paged cache: fp16 tensors [pages][kv_heads][page_size][head_dim] with the description's strides (made here if not given)."""
+
+    def __init__(self, desc: qeft_cache_desc_t, k: torch.Tensor | None = None, v: torch.Tensor | None = None, device="cuda"):
+        self.desc = desc
+        shape = (desc.pages, desc.kv_heads, desc.page_size, desc.head_dim)
+        strides = (desc.page_stride, desc.head_stride, desc.token_stride, 1)
+        self.k, self.v = (torch.empty_strided(shape, strides, dtype=torch.float16, device=device).zero_() if t is None else t for t in (k, v))
+        for name, t in (("k", self.k), ("v", self.v)):
+            self._pool(name, t)
+
+    def _pool(self, name, t):
+        d = self.desc
+        shape = (d.pages, d.kv_heads, d.page_size, d.head_dim)
+        if t.dtype != torch.float16 or tuple(t.shape) != shape:
+            _fail(QEFT_ERR_SHAPE, "Cache", f"{name} is {t.dtype} {tuple(t.shape)}, not float16 {shape}")
+        if any(n > 1 and have != want for n, have, want in zip(shape, t.stride(), (d.page_stride, d.head_stride, d.token_stride, 1))):
+            _fail(QEFT_ERR_SHAPE, "Cache", f"{name}'s strides {t.stride()} are not the description's")
+        return t.data_ptr()
+
+    def c_struct(self) -> qeft_cache_t:
+        for name, t in (("k", self.k), ("v", self.v)):
+            if not t.is_cuda or t.device.index != torch.cuda.current_device():
+                _fail(QEFT_ERR_UNSUPPORTED, "Cache", f"{name} is not on the current GPU")
+        return qeft_cache_t(self._pool("k", self.k), self._pool("v", self.v))
+
+
+def _c_table(where, table):
+    p, ld = _take(where, "table", table, torch.int32, (None, None))
+    return qeft_table_t(p, max(ld, table.shape[1]), table.shape[1], table.shape[0])
+
+
+def _c_workspace(where, ws):
+    if ws is None:
+        return 0, 0
+    p, _ = _take(where, "ws", ws, torch.uint8, (None,))
+    return p, ws.numel()
+
+
+def qeft_cache_append(cache: Cache, table: torch.Tensor, k: torch.Tensor, v: torch.Tensor, index: torch.Tensor, seq: torch.Tensor | None = None,
+                      q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, rot: torch.Tensor | None = None,
+                      pos: torch.Tensor | None = None) -> torch.Tensor | None:
+    """k, v fp16 [tokens][kv_heads * head_dim] into the cache, k rotated; q fp16 [tokens][heads * head_dim] rotated into q_out, which is returned
+    (None without q).  index, seq, pos int32 [tokens]; rot fp32 [positions][rot_dim]; table int32 [seqs][pages]."""
+    if q is not None and q_out is None:
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    st = _native.cache_append(cache.desc, cache.k, cache.v, table, k, v, index, seq, q, q_out, rot, pos)
+    if st is None:
+        at, d = "qeft_cache_append", cache.desc
+        pools, tab = cache.c_struct(), _c_table(at, table)
+        n = k.shape[0] if k is not None and k.dim() == 2 else None
+        width = d.kv_heads * d.head_dim
+        pk, ldk = _take(at, "k", k, torch.float16, (n, width))
+        pv, ldv = _take(at, "v", v, torch.float16, (n, width))
+        pq, ldq = _take(at, "q", q, torch.float16, (n, None), True)
+        heads = 0 if q is None else q.shape[1] // d.head_dim
+        if q is not None and heads * d.head_dim != q.shape[1]:
+            _fail(QEFT_ERR_SHAPE, at, "q's rows are not whole heads")
+        po, ldo = _take(at, "q_out", q_out if q is not None else None, torch.float16, (n, heads * d.head_dim), q is None)
+        pi, ps, pp = (_take(at, name, t, torch.int32, (n,), t is not index)[0] for name, t in (("index", index), ("seq", seq), ("pos", pos)))
+        pr, ldr = _take(at, "rot", rot, torch.float32, (None, None), True)
+        a = qeft_append_t(pq, pk, pv, po, ldq, ldo, ldk, ldv, ps, pi, pp, pr, max(ldr, rot.shape[1]) if rot is not None else 0,
+                          rot.shape[0] if rot is not None else 0, rot.shape[1] if rot is not None else 0, heads, n)
+        st = raw.qeft_cache_append(C.byref(d), C.byref(pools), C.byref(tab), C.byref(a), _stream())
+    _check(st, "qeft_cache_append")
+    return q_out
+
+
+def qeft_attn_workspace(desc: qeft_cache_desc_t, seqs: int, heads: int, longest: int, weights=False) -> int:
+    return int(raw.qeft_attn_workspace(C.byref(desc), seqs, heads, longest, int(bool(weights))))
+
+
+def qeft_attn_decode(cache: Cache, table: torch.Tensor, lens: torch.Tensor, longest: int, q: torch.Tensor, out: torch.Tensor | None = None,
+                     score: torch.Tensor | None = None, accumulate=False, scale: float | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
+    """Attention of one token per sequence: q, out fp16 [seqs][heads * head_dim], lens int32 [seqs] on the GPU, longest the host's bound of them.
+    score fp32 [seqs][kv_heads][tokens]: every token's weight is written there (added with accumulate).  scale: head_dim ** -0.5 by default.
+    ws: uint8, qeft_attn_workspace bytes; None allocates it."""
+    d = cache.desc
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if scale is None:
+        scale = d.head_dim ** -0.5
+    if ws is None:
+        n = qeft_attn_workspace(d, q.shape[0], q.shape[1] // d.head_dim, longest, score is not None)
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    st = _native.attn_decode(d, cache.k, cache.v, table, lens, longest, q, out, score, accumulate, scale, ws)
+    if st is None:
+        at = "qeft_attn_decode"
+        pools, tab = cache.c_struct(), _c_table(at, table)
+        n = table.shape[0]
+        pq, ldq = _take(at, "q", q, torch.float16, (n, None))
+        heads = q.shape[1] // d.head_dim
+        if heads * d.head_dim != q.shape[1]:
+            _fail(QEFT_ERR_SHAPE, at, "q's rows are not whole heads")
+        po, ldo = _take(at, "out", out, torch.float16, (n, q.shape[1]))
+        pl, _ = _take(at, "lens", lens, torch.int32, (n,))
+        ps, lds = _take(at, "score", score, torch.float32, (n, d.kv_heads, None), True)
+        pw, nw = _c_workspace(at, ws)
+        a = qeft_attn_t(pl, int(longest), pq, po, ldq, ldo, heads, float(scale), ps, score.shape[2] if ps and lds < score.shape[2] else lds,
+                        int(bool(accumulate)), pw, nw)
+        st = raw.qeft_attn_decode(C.byref(d), C.byref(pools), C.byref(tab), C.byref(a), _stream())
+    _check(st, "qeft_attn_decode")
+    return out
+
+
+def qeft_evict_workspace(desc: qeft_cache_desc_t, seqs: int, longest: int, budget: int) -> int:
+    return int(raw.qeft_evict_workspace(C.byref(desc), seqs, longest, budget))
+
+
+def qeft_cache_evict(cache: Cache, table: torch.Tensor, lens: torch.Tensor, longest: int, budget: int, score: torch.Tensor, pos: torch.Tensor,
+                     seen: torch.Tensor, keep_first=0, keep_last=0, score_out: torch.Tensor | None = None, pos_out: torch.Tensor | None = None,
+                     lens_out: torch.Tensor | None = None, ws: torch.Tensor | None = None):
+    """Every head keeps `budget` tokens, moved into the first slots; returns (score_out, pos_out, lens_out).  score fp32 and pos int32
+    [seqs][kv_heads][tokens]; by default they are updated in place, lens_out is new."""
+    d = cache.desc
+    score_out, pos_out = score if score_out is None else score_out, pos if pos_out is None else pos_out
+    if lens_out is None:
+        lens_out = torch.empty_like(lens)
+    if ws is None:
+        n = qeft_evict_workspace(d, table.shape[0], longest, budget)
+        ws = torch.empty(n, dtype=torch.uint8, device=lens.device) if n else None
+    st = _native.cache_evict(d, cache.k, cache.v, table, lens, longest, budget, score, pos, seen, keep_first, keep_last, score_out, pos_out, lens_out, ws)
+    if st is None:
+        at = "qeft_cache_evict"
+        pools, tab = cache.c_struct(), _c_table(at, table)
+        n = table.shape[0]
+        pl, pn, po = (_take(at, name, t, torch.int32, (n,))[0] for name, t in (("lens", lens), ("seen", seen), ("lens_out", lens_out)))
+        (ps, lds), (pso, ldso) = (_take(at, name, t, torch.float32, (n, d.kv_heads, None)) for name, t in (("score", score), ("score_out", score_out)))
+        (pp, ldp), (ppo, ldpo) = (_take(at, name, t, torch.int32, (n, d.kv_heads, None)) for name, t in (("pos", pos), ("pos_out", pos_out)))
+        if score.shape != pos.shape or lds != ldp or score_out.shape != pos_out.shape or ldso != ldpo:
+            _fail(QEFT_ERR_SHAPE, at, "score and pos differ in shape or pitch")
+        one = n * d.kv_heads == 1   # (one row: its width is all there is)
+        pw, nw = _c_workspace(at, ws)
+        a = qeft_evict_t(pl, pn, int(longest), int(budget), ps, pp, score.shape[2] if one else lds, int(keep_first), int(keep_last), pso, ppo,
+                         score_out.shape[2] if one else ldso, po, pw, nw)
+        st = raw.qeft_cache_evict(C.byref(d), C.byref(pools), C.byref(tab), C.byref(a), _stream())
+    _check(st, "qeft_cache_evict")
+    return score_out, pos_out, lens_out
+
+
+def make_norm_desc(n, residual_dtype=torch.float16, gate=QEFT_GATE_NONE, scale=1.0, eps=1e-5) -> qeft_norm_desc_t:
+    return qeft_norm_desc_t(n, _DTYPES[residual_dtype], gate, scale, eps)
+
+
+def _residual(desc):
+    return torch.float32 if desc.residual_dtype == QEFT_DTYPE_F32 else torch.float16
+
+
+def qeft_norm_fwd(desc: qeft_norm_desc_t, r: torch.Tensor, w_pre: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | None = None,
+                  gate: torch.Tensor | None = None, h: torch.Tensor | None = None, x: torch.Tensor | None = None):
+    """(h, x): h = r + scale * gate * (y, normed with w_post if given), x = unit(h) * w_pre.  Without y only x is computed, from r; h is r then."""
+    if x is None:
+        x = _empty_rows(r.shape[0], desc.n, torch.float16, r.device)
+    if h is None and y is not None:
+        h = _empty_rows(r.shape[0], desc.n, _residual(desc), r.device)
+    st = _native.norm_fwd(desc, r, w_pre, y, w_post, gate, h, x)
+    if st is None:
+        at, m, n = "qeft_norm_fwd", r.shape[0], desc.n
+        pr, ldr = _take(at, "r", r, _residual(desc), (m, n))
+        px, ldx = _take(at, "x", x, torch.float16, (m, n))
+        py, ldy = _take(at, "y", y, torch.float16, (m, n), True)
+        ph, ldh = _take(at, "h", h, _residual(desc), (m, n), True)
+        pg, ldg = _take(at, "gate", gate, torch.float16, (m, n) if desc.gate == QEFT_GATE_TOKEN else (n,), True)
+        pw, po = _take(at, "w_pre", w_pre, torch.float16, (n,))[0], _take(at, "w_post", w_post, torch.float16, (n,), True)[0]
+        a = qeft_norm_fwd_t(pr, py, pg, pw, po, ph, px, ldr, ldy, ldg, ldh, ldx, m)
+        st = raw.qeft_norm_fwd(C.byref(desc), C.byref(a), _stream())
+    _check(st, "qeft_norm_fwd")
+    return (r if y is None else h), x
+
+
+def qeft_norm_workspace(desc: qeft_norm_desc_t, m: int) -> int:
+    return int(raw.qeft_norm_workspace(C.byref(desc), m))
+
+
+def qeft_norm_bwd(desc: qeft_norm_desc_t, dx: torch.Tensor, h: torch.Tensor, w_pre: torch.Tensor, dh: torch.Tensor | None = None,
+                  y: torch.Tensor | None = None, w_post: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                  dr: torch.Tensor | None = None, dy: torch.Tensor | None = None, dw_pre: torch.Tensor | None = None,
+                  dw_post: torch.Tensor | None = None, dgate: torch.Tensor | None = None, accumulate=False, ws: torch.Tensor | None = None):
+    """(dr, dy, dw_pre, dw_post, dgate) of qeft_norm_fwd's r, y, w_pre, w_post and gate, from the gradients of x and h and the stored h.
+    Gradients of what the call does not have are None; those not given are allocated, False leaves one out.  accumulate: the sums over rows (dw_pre, dw_post, a
+    channel gate's dgate) are added to what the given tensors hold."""
+    m, n, dev = dx.shape[0], desc.n, dx.device
+    sums = torch.zeros if accumulate else torch.empty
+
+    def out(t, has, make):
+        return None if t is False or not has else make() if t is None else t
+
+    dr = out(dr, True, lambda: _empty_rows(m, n, _residual(desc), dev))
+    dy = out(dy, y is not None, lambda: _empty_rows(m, n, torch.float16, dev))
+    dw_pre = out(dw_pre, True, lambda: sums(n, dtype=torch.float32, device=dev))
+    dw_post = out(dw_post, w_post is not None, lambda: sums(n, dtype=torch.float32, device=dev))
+    token = desc.gate == QEFT_GATE_TOKEN
+    dgate = out(dgate, gate is not None, lambda: _empty_rows(m, n, torch.float16, dev) if token else sums(n, dtype=torch.float32, device=dev))
+    if ws is None:
+        size = qeft_norm_workspace(desc, m)
+        ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
+    st = _native.norm_bwd(desc, dx, h, w_pre, dh, y, w_post, gate, dr, dy, dw_pre, dw_post, dgate, accumulate, ws)
+    if st is None:
+        at, res = "qeft_norm_bwd", _residual(desc)
+        half, f32 = torch.float16, torch.float32
+        pdx, lddx = _take(at, "dx", dx, half, (m, n))
+        ph, ldh = _take(at, "h", h, res, (m, n))
+        pdh, lddh = _take(at, "dh", dh, res, (m, n), True)
+        py, ldy = _take(at, "y", y, half, (m, n), True)
+        pg, ldg = _take(at, "gate", gate, half, (m, n) if token else (n,), True)
+        pw, po = _take(at, "w_pre", w_pre, half, (n,))[0], _take(at, "w_post", w_post, half, (n,), True)[0]
+        pdr, lddr = _take(at, "dr", dr, res, (m, n), True)
+        pdy, lddy = _take(at, "dy", dy, half, (m, n), True)
+        pdg, lddg = _take(at, "dgate", dgate, half, (m, n), True) if token else _take(at, "dgate", dgate, f32, (n,), True)
+        pdw, pdo = _take(at, "dw_pre", dw_pre, f32, (n,), True)[0], _take(at, "dw_post", dw_post, f32, (n,), True)[0]
+        pws, nws = _c_workspace(at, ws)
+        a = qeft_norm_bwd_t(pdx, pdh, ph, py, pg, pw, po, pdr, pdy, pdg, pdw, pdo, lddx, lddh, ldh, ldy, ldg, lddr, lddy, lddg, m,
+                            int(bool(accumulate)), pws, nws)
+        st = raw.qeft_norm_bwd(C.byref(desc), C.byref(a), _stream())
+    _check(st, "qeft_norm_bwd")
+    return dr, dy, dw_pre, dw_post, dgate

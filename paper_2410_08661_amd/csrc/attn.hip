@@ -1,0 +1,455 @@
+// Attention of one new token per sequence over its paged cache (qeft_attn_decode).
+//
+//   out[b][h] = sum_t p_t V_t,  p = softmax_t(scale q[b][h] . K_t),  t < lens[b]
+//
+// What bounds it: every cached byte is read once and used for 2 flops per query head of its kv head, so HBM for up to about a hundred heads per kv
+// head.  One pass: a wave takes 32 tokens at a time, keeps the running maximum m and sum l of its softmax and the unnormalised output, and rescales
+// those when a maximum grows by more than 8 in log2 (between, exponents are taken against the older maximum: p then is at most 2^8 too large,
+// in numerator and denominator alike).
+//
+// Both products run on the matrix units for any number of heads (a single head uses one of 16 columns, which costs nothing a bandwidth-bound
+// kernel misses), on fragments that come straight from global memory:
+//   S^T = K q^T     K's rows are tokens.  The two 16-row tiles of a step take their rows so that lane (c, grp) = (lane & 15, lane >> 4) ends up with
+//                   the scores of head column c for the 8 consecutive tokens t0 + 8 grp ..: tile u's row r is token t0 + 8 (r >> 2) + 4 u + (r & 3).
+//   O = P V         those 8 probabilities are then the lane's piece of the left operand as they stand, without a shuffle.  V is read by rows (4 rows
+//                   of 256 bytes per load at head_dim 128) so that a lane holds 8 tokens x NV dimensions; one v_perm per register makes the columns.
+// P enters as hi + lo, two fp16 values (22 bits): rounding it once would add half of the output's own rounding error again.  Exponents carry
+// an offset of 2^7 so that lo keeps its bits down to p = 2^-21 of the largest; the offset cancels in O / l.
+//
+// Work: a workgroup of 8 waves takes a chunk of one sequence's tokens for one kv head (16 query heads at a time; more heads read the chunk again, from L2),
+// joins its waves through LDS and writes out, or, where the sequence is cut in several chunks, m, l and O to the workspace for a second launch.
+#include "qeft_internal.h"
+
+namespace qeft {
+namespace {
+
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef __fp16 hr2 __attribute__((ext_vector_type(2)));   // (what the conversion builtin returns)
+typedef float f4 __attribute__((ext_vector_type(4)));
+
+constexpr int WAVES = 8;
+constexpr int STEP = 32;                // tokens of a wave's step
+constexpr int ROUND = WAVES * STEP;     // tokens a workgroup takes per round of its waves
+constexpr float OFFSET = 7.f;           // log2: exponents are taken against m - OFFSET
+constexpr float SLACK = 8.f;            // log2: growth of a maximum that is let pass without rescaling (2^(OFFSET + SLACK) is below fp16's largest)
+constexpr float NEG_INF = -__builtin_inff();
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// what exponents are taken against for a maximum of m (a maximum of -inf: every score so far was -inf, their weight is 0)
+__device__ __forceinline__ float base_of(float m) { return m == NEG_INF ? 0.f : m - OFFSET; }
+
+// Partial results of one (sequence, query head, chunk): base, l, and O[d], in arrays of their own.
+struct Partials {
+    float* base;   // [seqs][heads][chunks]
+    float* l;
+    float* o;      // [seqs][heads][chunks][d]
+    float* raw;    // scores in log2 units, [seqs][heads][pitch] (only where weights are asked for)
+    int64_t pitch;
+    int chunks, chunk;
+};
+
+// NV dimensions of a lane's V rows; 16 lanes cover DP
+template <int DP> struct VReg;
+template <> struct VReg<64> { typedef u2 type; static constexpr int n = 1; };
+template <> struct VReg<128> { typedef u4 type; static constexpr int n = 1; };
+template <> struct VReg<256> { typedef u4 type; static constexpr int n = 2; };
+
+// DP: head_dim padded to 64, 128 or 256; FULL: head_dim is DP; OCT: page_size is a multiple of 8, one table entry serves an octet of tokens
+template <int DP, bool FULL, bool OCT>
+__global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Attention a, Partials ps, int g, int tiles) {
+    constexpr int KS = DP / 32, NV = DP / 16;
+    typedef typename VReg<DP>::type vreg;
+    constexpr int VN = VReg<DP>::n, VW = sizeof(vreg) / 4;
+    __shared__ float sm[WAVES][16], sl[WAVES][16], sf[WAVES][16], sL[16], sB[16];
+    __shared__ __align__(16) float so[WAVES][4][DP];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, grp = lane >> 4;
+    int id = blockIdx.x;
+    const int tile = id % tiles;
+    id /= tiles;
+    const int chunk = id % ps.chunks;
+    id /= ps.chunks;
+    const int kvh = id % c.kv, b = id / c.kv;
+    const int head0 = kvh * g + 16 * tile, nh = min(16, g - 16 * tile);   // this workgroup's query heads
+    const int n = min(a.lens[b], a.longest);
+    const int begin = chunk * ps.chunk, end = min(n, begin + ps.chunk);
+    if (end <= begin && chunk > 0) return;   // (an empty sequence's first chunk writes the zeros)
+
+    // head slot of a column or row r of the products: r = 4 (h % 4) + h / 4, so that up to 4 heads lie in one register of O
+    const int my_head = (col >> 2) + 4 * (col & 3);
+    h8 q[KS];
+    {
+        const __half* qp = a.q + (size_t)b * a.ldq + (size_t)(head0 + my_head) * c.d;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            u4 v = {0, 0, 0, 0};
+            const int dim = 32 * s + 8 * grp;
+            if (my_head < nh && (FULL || dim < c.d)) v = *reinterpret_cast<const u4*>(qp + dim);
+            q[s] = __builtin_bit_cast(h8, v);
+        }
+    }
+    const int* row = c.table + (size_t)b * c.ld_table;
+    const size_t head_at = (size_t)kvh * c.head_stride;
+    const __half* kbase = c.k + head_at;
+    const __half* vbase = c.v + head_at;
+    const float unit = a.scale * 1.44269504088896340736f;
+
+    // element offset of token t's slot (t is below the length)
+    auto slot_at = [&](int t) -> size_t {
+        const int p = c.by_page.of(t);
+        const int page = min(max(row[p], 0), c.pages - 1);
+        return (size_t)page * c.page_stride + (size_t)(t - p * c.page_size) * c.token_stride;
+    };
+    u4 K[2][KS];
+    vreg V[8][VN];
+    auto load_k = [&](int t0) {
+        const int oct = t0 + 8 * (col >> 2), r = col & 3;
+        const __half* p[2];
+        if (OCT) {   // an octet beyond the length: the last one's rows (their scores are masked)
+            p[0] = kbase + slot_at(min(oct, (n - 1) & ~7)) + r * c.token_stride;
+            p[1] = p[0] + 4 * c.token_stride;
+        } else {
+            p[0] = kbase + slot_at(min(oct + r, n - 1));
+            p[1] = kbase + slot_at(min(oct + 4 + r, n - 1));
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int dim = 32 * s + 8 * grp;
+                if (FULL) K[u][s] = *reinterpret_cast<const u4*>(p[u] + dim);
+                else {
+                    K[u][s] = u4{0, 0, 0, 0};
+                    if (dim < c.d) K[u][s] = *reinterpret_cast<const u4*>(p[u] + dim);
+                }
+            }
+    };
+    auto load_v = [&](int t0) {
+        const int oct = t0 + 8 * grp, dim = NV * col;
+        const __half* p0 = OCT ? vbase + slot_at(min(oct, (n - 1) & ~7)) : nullptr;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const __half* p = OCT ? p0 + i * c.token_stride : vbase + slot_at(min(oct + i, n - 1));
+#pragma unroll
+            for (int x = 0; x < VN; ++x) {
+                if (FULL) V[i][x] = *reinterpret_cast<const vreg*>(p + dim + 8 * x);
+                else {
+                    V[i][x] = vreg{};
+                    if (dim + 8 * x < c.d) V[i][x] = *reinterpret_cast<const vreg*>(p + dim + 8 * x);
+                }
+            }
+        }
+    };
+
+    float m = NEG_INF, l = 0.f;   // of head column col; l: this lane's tokens only
+    f4 acc[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) acc[j] = f4{0.f, 0.f, 0.f, 0.f};
+
+    int t0 = begin + STEP * wave;
+    if (t0 < end) {
+        load_k(t0);
+        load_v(t0);
+    }
+    for (; t0 < end; t0 += ROUND) {
+        f4 st[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) st[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, K[u][s]), q[s], st[u], 0, 0, 0);
+        const bool more = t0 + ROUND < end;
+        if (more) load_k(t0 + ROUND);   // K's registers are free: the next step's rows fly during the softmax and the second product
+
+        float x[8];   // log2 of the weight, unnormalised; token t0 + 8 grp + e
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = st[e >> 2][e & 3] * unit;
+        const bool tail = t0 + STEP > end;
+        if (tail) {
+            const int left = end - (t0 + 8 * grp);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = e < left ? x[e] : NEG_INF;
+#pragma unroll
+                for (int y = 0; y < VN; ++y) V[e][y] = e < left ? V[e][y] : vreg{};   // whatever lies behind the end: 0 x NaN is NaN
+            }
+        }
+        if (ps.raw && my_head < nh) {
+            float* rp = ps.raw + ((size_t)b * a.heads + head0 + my_head) * ps.pitch + t0 + 8 * grp;
+            *reinterpret_cast<f4*>(rp) = f4{x[0], x[1], x[2], x[3]};
+            *reinterpret_cast<f4*>(rp + 4) = f4{x[4], x[5], x[6], x[7]};
+        }
+        float mx = x[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
+        if (__ballot(mx > m + SLACK)) {   // (m = -inf at first: taken for any score above it)
+            mx = fmaxf(mx, __shfl_xor(mx, 16));
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            mx = fmaxf(mx, m);
+            const float f = m == NEG_INF ? 0.f : exp2_fast(m - mx);   // (nothing but zeros to scale before the first score)
+            m = mx;
+            l = l == 0.f ? 0.f : l * f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float fr = __shfl(f, 4 * grp + i);
+#pragma unroll
+                for (int j = 0; j < NV; ++j) acc[j][i] *= fr;
+            }
+        }
+        const float base = base_of(m);
+        h8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const float p0 = exp2_fast(x[e] - base), p1 = exp2_fast(x[e + 1] - base);
+            l += p0;
+            l += p1;
+            const hr2 h = __builtin_amdgcn_cvt_pkrtz(p0, p1);   // (rounded towards zero: lo takes what is cut off)
+            const hr2 r = __builtin_amdgcn_cvt_pkrtz(p0 - (float)h.x, p1 - (float)h.y);
+            hi[e] = (_Float16)h.x, hi[e + 1] = (_Float16)h.y;
+            lo[e] = (_Float16)r.x, lo[e + 1] = (_Float16)r.y;
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            u4 col8;   // dimension NV col + j of the lane's 8 tokens
+            const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) col8[y] = __builtin_amdgcn_perm(V[2 * y + 1][j / (2 * VW)][(j / 2) % VW], V[2 * y][j / (2 * VW)][(j / 2) % VW], sel);
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, __builtin_bit_cast(h8, col8), acc[j], 0, 0, 0);
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, __builtin_bit_cast(h8, col8), acc[j], 0, 0, 0);
+        }
+        if (more) load_v(t0 + ROUND);
+    }
+
+    // ---- join the waves ----
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (lane < 16) {
+        sm[wave][lane] = m;
+        sl[wave][lane] = l;
+    }
+    __syncthreads();
+    if (threadIdx.x < 16) {
+        float M = NEG_INF, L = 0.f;
+        for (int w = 0; w < WAVES; ++w) M = fmaxf(M, sm[w][threadIdx.x]);
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = sm[w][threadIdx.x] == NEG_INF ? 0.f : exp2_fast(sm[w][threadIdx.x] - M);
+            sf[w][threadIdx.x] = f;
+            L += sl[w][threadIdx.x] * (sl[w][threadIdx.x] == 0.f ? 0.f : f);
+        }
+        sL[threadIdx.x] = L;
+        sB[threadIdx.x] = base_of(M);
+    }
+    __syncthreads();
+    const bool direct = ps.chunks == 1 && ps.base == nullptr;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (4 * i >= nh) break;   // heads 4 i .. 4 i + 3
+        const float f = sf[wave][4 * grp + i];
+#pragma unroll
+        for (int j = 0; j < NV; j += 4)
+            *reinterpret_cast<f4*>(&so[wave][grp][NV * col + j]) = f4{acc[j][i] * f, acc[j + 1][i] * f, acc[j + 2][i] * f, acc[j + 3][i] * f};
+        __syncthreads();
+        for (int e = threadIdx.x; e < 4 * DP; e += 64 * WAVES) {
+            const int hl = e / DP, dim = e % DP, h = hl + 4 * i;
+            if (h < nh && (FULL || dim < c.d)) {
+                float o = 0.f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) o += so[w][hl][dim];
+                if (direct) {
+                    a.out[(size_t)b * a.ldo + (size_t)(head0 + h) * c.d + dim] = __float2half_rn(n > 0 ? o / sL[4 * hl + i] : 0.f);
+                } else {
+                    const size_t at = ((size_t)b * a.heads + head0 + h) * ps.chunks + chunk;
+                    ps.o[at * c.d + dim] = o;
+                    if (dim == 0) {
+                        ps.base[at] = sB[4 * hl + i];
+                        ps.l[at] = sL[4 * hl + i];
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (direct && a.score) {   // all of the kv head's query heads are this workgroup's; its scores were written before the barriers above
+        const float* rp = ps.raw + ((size_t)b * a.heads + head0) * ps.pitch;
+        float* out = a.score + ((size_t)b * c.kv + kvh) * a.ld_score;
+        for (int t = threadIdx.x; t < n; t += 64 * WAVES) {
+            float w = 0.f;
+            for (int h = 0; h < nh; ++h) {
+                const int at = 4 * (h & 3) + (h >> 2);
+                w += exp2_fast(rp[(size_t)h * ps.pitch + t] - sB[at]) / sL[at];
+            }
+            out[t] = a.accumulate ? out[t] + w : w;
+        }
+    }
+}
+
+// Base and sum of a query head over its used chunks (a wave's work; the same in every lane).
+__device__ __forceinline__ void join_stats(const Partials& ps, size_t at, int used, float& B, float& L) {
+    const int lane = threadIdx.x & 63;
+    B = NEG_INF;
+    for (int i = lane; i < used; i += 64) B = fmaxf(B, ps.l[at + i] == 0.f ? NEG_INF : ps.base[at + i]);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) B = fmaxf(B, __shfl_xor(B, x));
+    L = 0.f;
+    for (int i = lane; i < used; i += 64) L += ps.l[at + i] == 0.f ? 0.f : ps.l[at + i] * exp2_fast(ps.base[at + i] - B);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) L += __shfl_xor(L, x);
+}
+
+constexpr int JOIN_TOKENS = 1024;   // tokens whose weights one workgroup of the second launch makes
+
+// The second launch.  Its first seqs x heads workgroups join the chunks of one query head: 8 lanes of chunks x 32 lanes of dimensions.  The others
+// make the weights of one kv head's tokens, JOIN_TOKENS at a time (weight_shares of them divide a kv head's), from the scores in the workspace.  Chunks are taken in order: the sums do not depend on who ran first.
+__global__ __launch_bounds__(256) void attn_join_kernel(Cache c, Attention a, Partials ps, int g, int weight_shares) {
+    const int64_t outs = (int64_t)c.seqs * a.heads;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ float red[8][QEFT_MAX_HEAD_DIM];
+    __shared__ float part[8];
+    if ((int64_t)blockIdx.x < outs) {
+        const int b = (int)(blockIdx.x / a.heads), h = (int)(blockIdx.x % a.heads);
+        const int n = min(a.lens[b], a.longest);
+        __half* out = a.out + (size_t)b * a.ldo + (size_t)h * c.d;
+        if (n <= 0) {
+            for (int d = tid; d < c.d; d += 256) out[d] = __float2half_rn(0.f);
+            return;
+        }
+        const int used = (n + ps.chunk - 1) / ps.chunk;
+        const size_t at = ((size_t)b * a.heads + h) * ps.chunks;
+        float B, L;
+        join_stats(ps, at, used, B, L);
+        const int quads = c.d / 4, ql = tid & 31, cl = tid >> 5;
+        for (int qd = ql; qd < quads; qd += 32) {
+            f4 o = {0.f, 0.f, 0.f, 0.f};
+            for (int i = cl; i < used; i += 8) {
+                const float f = ps.l[at + i] == 0.f ? 0.f : exp2_fast(ps.base[at + i] - B);
+                const f4 v = *reinterpret_cast<const f4*>(ps.o + (at + i) * c.d + 4 * qd);
+                o += v * f;
+            }
+            *reinterpret_cast<f4*>(&red[cl][4 * qd]) = o;
+        }
+        __syncthreads();
+        for (int d = tid; d < c.d; d += 256) {
+            float o = red[0][d];
+#pragma unroll
+            for (int x = 1; x < 8; ++x) o += red[x][d];
+            out[d] = __float2half_rn(o / L);
+        }
+        return;
+    }
+    int64_t id = (int64_t)blockIdx.x - outs;
+    const int first = (int)(id % weight_shares);
+    id /= weight_shares;
+    const int kvh = (int)(id % c.kv), b = (int)(id / c.kv);
+    const int n = min(a.lens[b], a.longest), used = (n + ps.chunk - 1) / ps.chunk;
+    float* out = a.score + ((size_t)b * c.kv + kvh) * a.ld_score;
+    for (int begin = first * JOIN_TOKENS; begin < n; begin += weight_shares * JOIN_TOKENS) {
+        const int end = min(n, begin + JOIN_TOKENS);
+        float w[JOIN_TOKENS / 256] = {};
+        for (int h0 = 0; h0 < g; h0 += 4) {   // a wave for the statistics of each of four heads
+            const int h = h0 + wave;
+            if (h < g) {
+                float B, L;
+                join_stats(ps, ((size_t)b * a.heads + (size_t)kvh * g + h) * ps.chunks, used, B, L);
+                if (lane == 0) {
+                    part[wave] = B;
+                    part[4 + wave] = L;
+                }
+            }
+            __syncthreads();
+            for (int y = 0; y < 4 && h0 + y < g; ++y) {
+                const float* rp = ps.raw + ((size_t)b * a.heads + (size_t)kvh * g + h0 + y) * ps.pitch;
+                const float B = part[y], L = part[4 + y];
+#pragma unroll
+                for (int x = 0; x < JOIN_TOKENS / 256; ++x) {
+                    const int t = begin + 256 * x + tid;
+                    if (t < end) w[x] += exp2_fast(rp[t] - B) / L;
+                }
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int x = 0; x < JOIN_TOKENS / 256; ++x) {
+            const int t = begin + 256 * x + tid;
+            if (t < end) out[t] = a.accumulate ? out[t] + w[x] : w[x];
+        }
+    }
+}
+
+struct Plan {
+    int chunk, chunks, tiles;
+    bool direct;
+    size_t at_l, at_o, at_raw, bytes;
+    int64_t pitch;
+};
+
+Plan plan_of(int kv, int d, int64_t seqs, int heads, int longest, bool weights) {
+    Plan p;
+    const int g = heads / kv;
+    p.tiles = (g + 15) / 16;
+    const int64_t rows = seqs * kv * p.tiles;
+    // Chunks of whole rounds.  One chunk, and no second launch, up to 512 tokens; else about 2048 workgroups (4 to a CU's two, so that the last ones to end
+    // leave little idle), as short as one round where there are few rows.
+    const int64_t rounds = ((int64_t)longest + ROUND - 1) / ROUND;
+    int64_t per = longest <= 2 * ROUND ? rounds : rows * rounds / 2048;
+    if (per < 1) per = 1;
+    p.chunk = (int)(per * ROUND);
+    p.chunks = rounds > 0 ? (int)((rounds + per - 1) / per) : 1;   // (longest 0: the chunk that writes the zeros)
+    p.direct = p.chunks == 1 && (p.tiles == 1 || !weights);
+    const size_t parts = p.direct ? 0 : (size_t)seqs * heads * p.chunks;
+    const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    p.at_l = up(parts * 4);
+    p.at_o = 2 * p.at_l;
+    p.at_raw = p.at_o + up(parts * d * 4);
+    p.pitch = weights ? rounds * ROUND : 0;
+    p.bytes = p.at_raw + (size_t)seqs * heads * p.pitch * 4;
+    return p;
+}
+
+template <int DP, bool FULL, bool OCT>
+void launch(const Cache& c, const Attention& a, const Partials& ps, int g, int tiles, unsigned grid, hipStream_t s) {
+    attn_chunk_kernel<DP, FULL, OCT><<<grid, 64 * WAVES, 0, s>>>(c, a, ps, g, tiles);
+}
+template <int DP>
+void launch_dim(const Cache& c, const Attention& a, const Partials& ps, int g, int tiles, unsigned grid, hipStream_t s) {
+    if (c.page_size % 8 != 0) return launch<DP, false, false>(c, a, ps, g, tiles, grid, s);
+    if (c.d == DP) return launch<DP, true, true>(c, a, ps, g, tiles, grid, s);
+    launch<DP, false, true>(c, a, ps, g, tiles, grid, s);
+}
+
+}  // namespace
+
+size_t attn_workspace(int kv, int d, int64_t seqs, int heads, int bound, bool weights) {
+    return plan_of(kv, d, seqs, heads, bound, weights).bytes;
+}
+
+hipError_t attn_decode(const Cache& c, const Attention& a, hipStream_t s) {
+    const bool weights = a.score != nullptr;
+    const Plan p = plan_of(c.kv, c.d, c.seqs, a.heads, a.bound, weights);
+    const int g = a.heads / c.kv;
+    Partials ps{};
+    ps.chunk = p.chunk;
+    ps.chunks = p.chunks;
+    if (!p.direct) {
+        ps.base = (float*)a.ws;
+        ps.l = (float*)(a.ws + p.at_l);
+        ps.o = (float*)(a.ws + p.at_o);
+    }
+    if (weights) {
+        ps.raw = (float*)(a.ws + p.at_raw);
+        ps.pitch = p.pitch;
+    }
+    const unsigned grid = (unsigned)((int64_t)c.seqs * c.kv * ps.chunks * p.tiles);
+    if (c.d <= 64) launch_dim<64>(c, a, ps, g, p.tiles, grid, s);
+    else if (c.d <= 128) launch_dim<128>(c, a, ps, g, p.tiles, grid, s);
+    else launch_dim<256>(c, a, ps, g, p.tiles, grid, s);
+    if (!p.direct) {
+        const int64_t rows = (int64_t)c.seqs * c.kv, most = rows < 32768 ? 65536 / rows : 1;   // (workgroups enough to fill the GPU, and a grid of bounded size)
+        const int tiles = weights ? (a.longest + JOIN_TOKENS - 1) / JOIN_TOKENS : 0, shares = tiles < most ? tiles : (int)most;
+        attn_join_kernel<<<(unsigned)((int64_t)c.seqs * a.heads + rows * shares), 256, 0, s>>>(c, a, ps, g, shares);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace qeft

@@ -174,4 +174,90 @@ hipError_t weak_grad_mfma(int oc, int k, const __half* dY, int64_t M, int64_t ld
 // dW = the sum of the strips' partial slabs, in their order
 hipError_t weak_grad_reduce(const float* part, int splits, int64_t n, void* dW, int out_f32, int accumulate, hipStream_t s);
 
+// ---- between the linear layers: paged cache, attention of one token, eviction, norms (block_api.hip checks the arguments) ----
+// t / d for 0 <= t < 2^31 and 1 <= d < 2^31 by a product: with 2^(c-1) < d <= 2^c and m = ceil(2^(31+c) / d) <= 2^32 - 1, the excess of m d over
+// 2^(31+c) is below d <= 2^c, so t times it stays below 2^(31+c) and the quotient is exact.
+struct Divider {
+    uint32_t m;
+    int shift;
+    __host__ __device__ __forceinline__ int of(int t) const { return (int)(((uint64_t)(uint32_t)t * m) >> shift); }
+};
+inline Divider divider(int d) {
+    int c = 0;
+    while (((int64_t)1 << c) < d) ++c;
+    return Divider{(uint32_t)((((uint64_t)1 << (31 + c)) + d - 1) / d), 31 + c};
+}
+
+// A paged cache with the page table of a call.
+struct Cache {
+    __half *k, *v;
+    int64_t page_stride, head_stride, token_stride;
+    const int* table;
+    int64_t ld_table;
+    int table_pages, pages, page_size, kv, d, seqs;
+    Divider by_page;
+    int tokens() const { const int64_t n = (int64_t)table_pages * page_size; return n < QEFT_MAX_DIM ? (int)n : QEFT_MAX_DIM; }   // a sequence's most
+};
+
+struct Append {
+    const __half *q, *k, *v;
+    __half* q_out;
+    int64_t ldq, ldq_out, ldk, ldv;
+    const int *seq, *index, *pos;
+    const float* rot;
+    int64_t ld_rot;
+    int positions, rot_dim, heads, tokens;
+};
+hipError_t cache_append(const Cache& c, const Append& a, hipStream_t s);   // (append.hip)
+
+struct Attention {
+    const int* lens;
+    int bound;               // the caller's longest: what the work and its workspace are planned by
+    int longest;             // that, at most c.tokens()
+    const __half* q;
+    __half* out;
+    int64_t ldq, ldo;
+    int heads;
+    float scale;
+    float* score;
+    int64_t ld_score;
+    int accumulate;
+    unsigned char* ws;
+};
+size_t attn_workspace(int kv, int d, int64_t seqs, int heads, int bound, bool weights);   // (attn.hip)
+hipError_t attn_decode(const Cache& c, const Attention& a, hipStream_t s);
+
+struct Evict {
+    const int *lens, *seen;
+    int longest, budget;     // longest at most c.tokens(), budget at most longest
+    const float* score;
+    const int* pos;
+    int64_t ld;
+    int keep_first, keep_last;
+    float* score_out;
+    int* pos_out;
+    int64_t ld_out;
+    int* lens_out;
+    unsigned char* ws;
+};
+size_t evict_workspace(int kv, int64_t seqs, int longest, int budget);   // (evict.hip)
+hipError_t cache_evict(const Cache& c, const Evict& a, hipStream_t s);
+
+struct Norm {                // either direction: what a call does not have is NULL
+    const __half *y, *gate, *w_pre, *w_post, *dx;
+    const void *r, *dh;      // residual dtype; r is the stored h for the gradient
+    void *h, *dr;
+    __half *x, *dy;
+    void* dgate;
+    float *dw_pre, *dw_post;
+    int64_t ldr, ldy, ldg, ldh, ldx, lddx, lddh, lddr, lddy, lddg;
+    int n, f32, gate_kind, accumulate;
+    int64_t m;
+    float scale, eps;
+    unsigned char* ws;
+};
+hipError_t norm_fwd(const Norm& a, hipStream_t s);   // (norm.hip)
+size_t norm_workspace(int n, int64_t m);
+hipError_t norm_bwd(const Norm& a, hipStream_t s);
+
 }  // namespace qeft
