@@ -24,64 +24,95 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 constexpr int FWD_MAX = 32768;    // values of a row that the forward keeps in registers (1024 threads x 4 octets)
 constexpr int BWD_MAX = 16384;    // and the gradient (1024 x 2: beside three column sums)
 
-// Eight values of a row as loaded.  left: how many of them exist (a row's last octet may be partial).
+// A row's address, the same in all lanes: kept from the optimiser, which would otherwise add a lane's offset to every array's base outside the loop over
+// the rows and hold those sums, two registers each (the gradient has eight arrays), instead of adding in the load.
+__device__ __forceinline__ const char* row_of(const void* p, int64_t row, int64_t ld, bool f32) {
+    const char* r = (const char*)p + row * ld * (f32 ? 4 : 2);
+    asm volatile("" : "+s"(r));
+    return r;
+}
+__device__ __forceinline__ char* row_of(void* p, int64_t row, int64_t ld, bool f32) { return const_cast<char*>(row_of((const void*)p, row, ld, f32)); }
+
+// Eight values of a row as loaded.  left: how many of them exist; a row's last octet may be partial, and is read value by value, the last one first.
 template <bool F32> struct Raw;
 template <> struct Raw<false> {
     u4 v;
-    __device__ __forceinline__ void load(const void* row, int64_t at, int left) {
-        const uint16_t* p = (const uint16_t*)row + at;
-        if (left >= 8) v = *reinterpret_cast<const u4*>(p);
-        else
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = (2 * e < left ? p[2 * e] : 0u) | (2 * e + 1 < left ? (uint32_t)p[2 * e + 1] << 16 : 0u);
+    __device__ __forceinline__ void load(const void* row, uint32_t at, int left) {
+        const char* p = (const char*)row + 2 * at;
+        if (left >= 8) {
+            v = *reinterpret_cast<const u4*>(p);
+            return;
+        }
+        v = u4{0, 0, 0, 0};
+#pragma unroll 1
+        for (int e = left - 1; e >= 0; --e) {
+            const uint32_t x = *reinterpret_cast<const uint16_t*>(p + 2 * e);
+            v = u4{v.x << 16 | x, v.y << 16 | v.x >> 16, v.z << 16 | v.y >> 16, v.w << 16 | v.z >> 16};
+        }
     }
     __device__ __forceinline__ float operator[](int e) const { return (float)__builtin_bit_cast(h8, v)[e]; }
     __device__ __forceinline__ void clear() { v = u4{0, 0, 0, 0}; }
+    // Eight values stay four registers: without this the compiler converts once and keeps eight (across a loop for a row of weights).
+    __device__ __forceinline__ void pin() { asm volatile("" : "+v"(v)); }
 };
 template <> struct Raw<true> {
     f4 a, b;
-    __device__ __forceinline__ void load(const void* row, int64_t at, int left) {
-        const float* p = (const float*)row + at;
+    __device__ __forceinline__ void load(const void* row, uint32_t at, int left) {
+        const char* p = (const char*)row + 4 * at;
         if (left >= 8) {
             a = *reinterpret_cast<const f4*>(p);
-            b = *reinterpret_cast<const f4*>(p + 4);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                a[e] = e < left ? p[e] : 0.f;
-                b[e] = 4 + e < left ? p[4 + e] : 0.f;
-            }
+            b = *reinterpret_cast<const f4*>(p + 16);
+            return;
+        }
+        clear();
+#pragma unroll 1
+        for (int e = left - 1; e >= 0; --e) {
+            b = f4{a.w, b.x, b.y, b.z};
+            a = f4{*reinterpret_cast<const float*>(p + 4 * e), a.x, a.y, a.z};
         }
     }
     __device__ __forceinline__ float operator[](int e) const { return e < 4 ? a[e & 3] : b[e & 3]; }
     __device__ __forceinline__ void clear() { a = b = f4{0.f, 0.f, 0.f, 0.f}; }
+    __device__ __forceinline__ void pin() {}
 };
 typedef Raw<false> Half8;
 
-// x rounded to the stored type, in place
+// x goes to the row, rounded to its type (which x then is too)
 template <bool F32>
-__device__ __forceinline__ void store(void* row, int64_t at, int left, float (&x)[8]) {
+__device__ __forceinline__ void store(void* row, uint32_t at, int left, float (&x)[8]) {
     if (F32) {
-        float* p = (float*)row + at;
+        char* p = (char*)row + 4 * at;
+        f4 a = {x[0], x[1], x[2], x[3]}, b = {x[4], x[5], x[6], x[7]};
         if (left >= 8) {
-            *reinterpret_cast<f4*>(p) = f4{x[0], x[1], x[2], x[3]};
-            *reinterpret_cast<f4*>(p + 4) = f4{x[4], x[5], x[6], x[7]};
-        } else
-            for (int e = 0; e < 8; ++e)
-                if (e < left) p[e] = x[e];
+            *reinterpret_cast<f4*>(p) = a;
+            *reinterpret_cast<f4*>(p + 16) = b;
+            return;
+        }
+#pragma unroll 1
+        for (int e = 0; e < left; ++e) {
+            *reinterpret_cast<float*>(p + 4 * e) = a.x;
+            a = f4{a.y, a.z, a.w, b.x};
+            b = f4{b.y, b.z, b.w, b.w};
+        }
         return;
     }
-    h8 v;
+    h8 h;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        v[e] = (_Float16)x[e];
-        x[e] = (float)v[e];
+        h[e] = (_Float16)x[e];
+        x[e] = (float)h[e];
     }
-    _Float16* p = (_Float16*)row + at;
-    if (left >= 8) *reinterpret_cast<u4*>(p) = __builtin_bit_cast(u4, v);
-    else
-        for (int e = 0; e < 8; ++e)
-            if (e < left) p[e] = v[e];
+    u4 v = __builtin_bit_cast(u4, h);
+    char* p = (char*)row + 2 * at;
+    if (left >= 8) {
+        *reinterpret_cast<u4*>(p) = v;
+        return;
+    }
+#pragma unroll 1
+    for (int e = 0; e < left; ++e) {
+        *reinterpret_cast<uint16_t*>(p + 2 * e) = (uint16_t)v.x;
+        v = u4{v.x >> 16 | v.y << 16, v.y >> 16 | v.z << 16, v.z >> 16 | v.w << 16, v.w >> 16};
+    }
 }
 template <bool F32>
 __device__ __forceinline__ void round_to(float (&x)[8]) {
@@ -89,11 +120,6 @@ __device__ __forceinline__ void round_to(float (&x)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = (float)(_Float16)x[e];
 }
-__device__ __forceinline__ const void* row_of(const void* p, int64_t row, int64_t ld, bool f32) {
-    return (const char*)p + row * ld * (f32 ? 4 : 2);
-}
-__device__ __forceinline__ void* row_of(void* p, int64_t row, int64_t ld, bool f32) { return (char*)p + row * ld * (f32 ? 4 : 2); }
-
 __device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) x += __shfl_xor(x, s);
@@ -124,10 +150,10 @@ __device__ __forceinline__ void row_sums(float (&s)[N], float (*buf)[16], int fi
 template <int V, bool F32>
 __global__ __launch_bounds__(1024) void norm_fwd_kernel(Norm a, int waves) {
     __shared__ float buf[2][1][16];
-    const int T = 64 * waves, tid = threadIdx.x % T;
-    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / T) + threadIdx.x / T;
+    const int T = 64 * waves, group = __builtin_amdgcn_readfirstlane(threadIdx.x / T), tid = threadIdx.x - group * T;
+    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / T) + group;
     if (row >= a.m) return;   // (whole waves of one-wave rows only: no barrier follows for them)
-    const int first = (threadIdx.x / T) * waves;
+    const int first = group * waves;
     const float inv = 1.f / (float)a.n;
     const void* r = row_of(a.r, row, a.ldr, F32);
     float h[V][8];
@@ -209,16 +235,16 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(Norm a) {
     float post = 1.f;
     if (a.w_post) {
         float s[1] = {0.f};
-        for (int64_t at = 8 * (int64_t)threadIdx.x; at < a.n; at += 8192) {
+        for (int at = 8 * threadIdx.x; at < a.n; at += 8192) {
             Half8 v;
-            v.load(y, at, (int)min((int64_t)8, a.n - at));
+            v.load(y, at, min(8, a.n - at));
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[0] = fmaf(v[e], v[e], s[0]);
         }
         row_sums(s, buf[0], 0, 16);
         post = 1.f / sqrtf(fmaf(s[0], inv, a.eps));
     }
-    auto make_h = [&](int64_t at, int left, float (&h)[8]) {
+    auto make_h = [&](int at, int left, float (&h)[8]) {
         Raw<F32> rr;
         rr.load(r, at, left);
         if (!y) {
@@ -240,8 +266,8 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(Norm a) {
         round_to<F32>(h);
     };
     float s[1] = {0.f};
-    for (int64_t at = 8 * (int64_t)threadIdx.x; at < a.n; at += 8192) {
-        const int left = (int)min((int64_t)8, a.n - at);
+    for (int at = 8 * threadIdx.x; at < a.n; at += 8192) {
+        const int left = min(8, a.n - at);
         float h[8];
         make_h(at, left, h);
         if (hrow) store<F32>(hrow, at, left, h);
@@ -249,8 +275,8 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(Norm a) {
     }
     row_sums(s, buf[1], 0, 16);
     const float rs = 1.f / sqrtf(fmaf(s[0], inv, a.eps));
-    for (int64_t at = 8 * (int64_t)threadIdx.x; at < a.n; at += 8192) {
-        const int left = (int)min((int64_t)8, a.n - at);
+    for (int at = 8 * threadIdx.x; at < a.n; at += 8192) {
+        const int left = min(8, a.n - at);
         float h[8], x[8];
         if (hrow) {   // (r may be the same row; a thread reads back what it wrote)
             Raw<F32> hh;
@@ -283,12 +309,15 @@ struct RowIn {
 // Workgroup = `groups` rows at a time, `waves` waves a row, V octets a thread.  POST: w_post is given; GATE: 0 none, 1 channel, 2 token.
 template <int V, bool F32, bool POST, int GATE>
 __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int waves, int groups, int rounds) {
-    extern __shared__ __align__(16) float joined[];   // [groups][64 waves][8 V]
+    extern __shared__ __align__(16) float joined[];   // [groups][64 waves][8 V] if groups > 1, then held
     __shared__ float buf[4][3][16];
-    const int T = 64 * waves, group = threadIdx.x / T, tid = threadIdx.x % T;
+    const int T = 64 * waves, group = __builtin_amdgcn_readfirstlane(threadIdx.x / T), tid = threadIdx.x - group * T;   // (rows' addresses are then scalar)
     const int first = group * waves;
     const float inv = 1.f / (float)a.n;
     const bool has_y = a.y != nullptr, has_dh = a.dh != nullptr;
+    // With both norms (and V == 1) the weights and a channel gate, 12 registers a thread, lie in LDS, read again by each step.
+    constexpr bool IN_LDS = POST && V == 1;
+    u4* held = reinterpret_cast<u4*>(joined + (groups > 1 ? blockDim.x * 8 * V : 0));   // [3][64 waves]
     Half8 wpre[V], wpost[V], gch[V];
     float spre[V][8] = {}, spost[V][8] = {}, sgate[V][8] = {};
 #pragma unroll
@@ -303,31 +332,69 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int wave
             if (GATE == QEFT_GATE_CHANNEL) gch[v].load(a.gate, at, left);
         }
     }
+    if (IN_LDS) {
+        if (group == 0) {
+            held[tid] = wpre[0].v;
+            held[T + tid] = wpost[0].v;
+            if (GATE == QEFT_GATE_CHANNEL) held[2 * T + tid] = gch[0].v;
+        }
+        __syncthreads();
+    }
     const int64_t step = (int64_t)gridDim.x * groups;
-    auto load = [&](int64_t row, RowIn<V, F32>& in) {
+    // what a row's first sums need, and the rest: the next row's are loaded apart, as registers fall free
+    auto load_sums = [&](int64_t row, RowIn<V, F32>& in) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int at = 8 * (tid + T * v), left = a.n - at;
             in.dx[v].clear();
             in.y[v].clear();
-            in.g[v].clear();
             in.h[v].clear();
-            in.dh[v].clear();
             if (left > 0 && row < a.m) {
                 in.h[v].load(row_of(a.r, row, a.ldr, F32), at, left);
-                in.dx[v].load(a.dx + row * a.lddx, at, left);
+                in.dx[v].load(row_of(a.dx, row, a.lddx, false), at, left);
+                if (has_y) in.y[v].load(row_of(a.y, row, a.ldy, false), at, left);
+            }
+        }
+    };
+    auto load_rest = [&](int64_t row, RowIn<V, F32>& in) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int at = 8 * (tid + T * v), left = a.n - at;
+            in.g[v].clear();
+            in.dh[v].clear();
+            if (left > 0 && row < a.m) {
                 if (has_dh) in.dh[v].load(row_of(a.dh, row, a.lddh, F32), at, left);
-                if (has_y) in.y[v].load(a.y + row * a.ldy, at, left);
-                if (GATE == QEFT_GATE_TOKEN) in.g[v].load(a.gate + row * a.ldg, at, left);
+                if (GATE == QEFT_GATE_TOKEN) in.g[v].load(row_of(a.gate, row, a.ldg, false), at, left);
             }
         }
     };
     int64_t row = (int64_t)blockIdx.x * groups + group;
     RowIn<V, F32> in;
-    load(row, in);
+    load_sums(row, in);
+    load_rest(row, in);
     for (int round = 0; round < rounds; ++round, row += step) {
         RowIn<V, F32> next;
-        if (V == 1 && round + 1 < rounds) load(row + step, next);
+        if (V == 1 && round + 1 < rounds) load_sums(row + step, next);
+        auto pin = [&] {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (IN_LDS) {
+                    wpre[v].v = held[tid];
+                    wpost[v].v = held[T + tid];
+                    if (GATE == QEFT_GATE_CHANNEL) gch[v].v = held[2 * T + tid];
+                } else {
+                    wpre[v].pin();
+                    if (POST) wpost[v].pin();
+                    if (GATE == QEFT_GATE_CHANNEL) gch[v].pin();
+                }
+                in.dx[v].pin();
+                in.h[v].pin();
+                in.dh[v].pin();
+                in.y[v].pin();
+                if (GATE == QEFT_GATE_TOKEN) in.g[v].pin();
+            }
+        };
+        pin();
         float s[3] = {0.f, 0.f, 0.f};   // h^2, a h, y^2
 #pragma unroll
         for (int v = 0; v < V; ++v)
@@ -346,6 +413,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int wave
         }
         const float rs = 1.f / sqrtf(fmaf(s[0], inv, a.eps)), c = s[1] * inv * rs;   // c = mean(a hh)
         const float rsy = POST ? 1.f / sqrtf(fmaf(s[2], inv, a.eps)) : 1.f;
+        pin();
         float t[V][8], q[1] = {0.f};
 #pragma unroll
         for (int v = 0; v < V; ++v)
@@ -359,7 +427,9 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int wave
                     q[0] = fmaf(a.scale * g * t[v][e] * wpost[v][e], in.y[v][e], q[0]);
                 }
             }
+        if (V == 1 && round + 1 < rounds) load_rest(row + step, next);
         if (POST) row_sums(q, buf[2 * (round & 1) + 1], first, waves);
+        pin();
         const float cy = POST ? q[0] * inv * rsy : 0.f;   // mean(a' yh)
         if (row < a.m) {
 #pragma unroll
@@ -376,7 +446,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int wave
                     const float u = POST ? yh * wpost[v][e] : yh;
                     if (GATE == QEFT_GATE_CHANNEL) sgate[v][e] = fmaf(st, u, sgate[v][e]);
                     if (GATE == QEFT_GATE_TOKEN) dg[e] = st * u;
-                }
+                    }
                 if (a.dr) store<F32>(row_of(a.dr, row, a.lddr, F32), at, left, t[v]);
                 if (a.dy) store<false>(row_of((void*)a.dy, row, a.lddy, false), at, left, dy);
                 if (GATE == QEFT_GATE_TOKEN && a.dgate) store<false>(row_of(a.dgate, row, a.lddg, false), at, left, dg);
@@ -384,7 +454,10 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int wave
         }
         if (round + 1 < rounds) {
             if (V == 1) in = next;
-            else load(row + step, in);
+            else {
+                load_sums(row + step, in);
+                load_rest(row + step, in);
+            }
         }
     }
     // this workgroup's slab: its row groups in order
@@ -453,8 +526,8 @@ __global__ __launch_bounds__(1024) void norm_bwd_stats_kernel(Norm a, RowStat* o
     const int64_t row = blockIdx.x;
     const float inv = 1.f / (float)a.n;
     float s[6] = {};   // h^2, a h, y^2; with k = scale gate w_post: k y dh, k y a, k y h
-    for (int64_t at = 8 * (int64_t)threadIdx.x; at < a.n; at += 8192) {
-        const int left = (int)min((int64_t)8, a.n - at);
+    for (int at = 8 * threadIdx.x; at < a.n; at += 8192) {
+        const int left = min(8, a.n - at);
         Raw<F32> h, dh;
         Half8 dx, w;
         h.load(row_of(a.r, row, a.ldr, F32), at, left);
@@ -494,9 +567,9 @@ __global__ __launch_bounds__(1024) void norm_bwd_stats_kernel(Norm a, RowStat* o
 // ... then gradients and column sums: a workgroup has 2048 columns and the rows blockIdx.y, blockIdx.y + slabs, ...
 template <bool F32>
 __global__ __launch_bounds__(256) void norm_bwd_long_kernel(Norm a, Sums S, const RowStat* stats) {
-    const int64_t at = 2048 * (int64_t)blockIdx.x + 8 * threadIdx.x;
+    const int at = 2048 * blockIdx.x + 8 * threadIdx.x;
     if (at >= a.n) return;
-    const int left = (int)min((int64_t)8, a.n - at);
+    const int left = min(8, a.n - at);
     Half8 w, wp, gc;
     w.load(a.w_pre, at, left);
     if (a.w_post) wp.load(a.w_post, at, left);
@@ -568,7 +641,7 @@ BwdPlan bwd_plan(int n, int64_t m) {
 template <int V, bool F32, bool POST>
 void launch_bwd(const Norm& a, const Sums& S, const BwdPlan& p, hipStream_t s) {
     const int threads = 64 * p.waves * p.groups;
-    const size_t lds = p.groups > 1 ? (size_t)threads * 8 * V * sizeof(float) : 0;
+    const size_t lds = (p.groups > 1 ? (size_t)threads * 8 * V * sizeof(float) : 0) + (POST && V == 1 ? 3 * 64 * (size_t)p.waves * sizeof(u4) : 0);
     if (a.gate_kind == QEFT_GATE_CHANNEL) norm_bwd_kernel<V, F32, POST, QEFT_GATE_CHANNEL><<<p.grid, threads, lds, s>>>(a, S, p.waves, p.groups, p.rounds);
     else if (a.gate_kind == QEFT_GATE_TOKEN) norm_bwd_kernel<V, F32, POST, QEFT_GATE_TOKEN><<<p.grid, threads, lds, s>>>(a, S, p.waves, p.groups, p.rounds);
     else norm_bwd_kernel<V, F32, POST, QEFT_GATE_NONE><<<p.grid, threads, lds, s>>>(a, S, p.waves, p.groups, p.rounds);
