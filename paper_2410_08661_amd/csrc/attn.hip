@@ -29,9 +29,7 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __fp16 hr2 __attribute__((ext_vector_type(2)));   // (what the conversion builtin returns)
 typedef float f4 __attribute__((ext_vector_type(4)));
 
-constexpr int WAVES = 8;
 constexpr int STEP = 32;                // tokens of a wave's step
-constexpr int ROUND = WAVES * STEP;     // tokens a workgroup takes per round of its waves
 constexpr float OFFSET = 7.f;           // log2: exponents are taken against m - OFFSET
 constexpr float SLACK = 8.f;            // log2: growth of a maximum that is let pass without rescaling (2^(OFFSET + SLACK) is below fp16's largest)
 constexpr float NEG_INF = -__builtin_inff();
@@ -56,10 +54,10 @@ template <> struct VReg<64> { typedef u2 type; static constexpr int n = 1; };
 template <> struct VReg<128> { typedef u4 type; static constexpr int n = 1; };
 template <> struct VReg<256> { typedef u4 type; static constexpr int n = 2; };
 
-// DP: head_dim padded to 64, 128 or 256; FULL: head_dim is DP; OCT: page_size is a multiple of 8, one table entry serves an octet of tokens
-template <int DP, bool FULL, bool OCT>
+// DP: head_dim padded to 64, 128 or 256; FULL: head_dim is DP, and a page's rows lie one behind the other; OCT: page_size is a multiple of 8, one table entry serves an octet of tokens
+template <int DP, bool FULL, bool OCT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Attention a, Partials ps, int g, int tiles) {
-    constexpr int KS = DP / 32, NV = DP / 16;
+    constexpr int KS = DP / 32, NV = DP / 16, ROUND = WAVES * STEP;   // (tokens of a round of the waves)
     typedef typename VReg<DP>::type vreg;
     constexpr int VN = VReg<DP>::n, VW = sizeof(vreg) / 4;
     __shared__ float sm[WAVES][16], sl[WAVES][16], sf[WAVES][16], sL[16], sB[16];
@@ -67,12 +65,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
+    // Neighbours in the grid, which run at the same time, take the same tokens of neighbouring heads: what they read lies together in a page.
     int id = blockIdx.x;
+    const int kvh = id % c.kv;
+    id /= c.kv;
     const int tile = id % tiles;
     id /= tiles;
-    const int chunk = id % ps.chunks;
-    id /= ps.chunks;
-    const int kvh = id % c.kv, b = id / c.kv;
+    const int chunk = id % ps.chunks, b = id / ps.chunks;
     const int head0 = kvh * g + 16 * tile, nh = min(16, g - 16 * tile);   // this workgroup's query heads
     const int n = min(a.lens[b], a.longest);
     const int begin = chunk * ps.chunk, end = min(n, begin + ps.chunk);
@@ -97,48 +96,62 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
     const __half* vbase = c.v + head_at;
     const float unit = a.scale * 1.44269504088896340736f;
 
-    // element offset of token t's slot (t is below the length)
-    auto slot_at = [&](int t) -> size_t {
+    // Where an octet's slots begin.  Octets (and everything about them but the choice of a lane's) are the same for the whole wave: scalar work.  Tokens that do
+    // not exist have some page of the pool all the same: what is read there is masked.
+    auto slot_at = [&](int t) -> int64_t {
         const int p = c.by_page.of(t);
-        const int page = min(max(row[p], 0), c.pages - 1);
-        return (size_t)page * c.page_stride + (size_t)(t - p * c.page_size) * c.token_stride;
+        const int page = min(max(row[min(p, c.table_pages - 1)], 0), c.pages - 1);
+        return page * c.page_stride + (t - p * c.page_size) * c.token_stride;
+    };
+    struct Octets {
+        int64_t at[4];
+    };
+    auto octets = [&](int t0) {
+        Octets o;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o.at[x] = OCT ? slot_at(t0 + 8 * x) : 0;
+        return o;
+    };
+    auto chosen = [&](const Octets& o, int x) {
+        const int64_t lo = x & 1 ? o.at[1] : o.at[0], hi = x & 1 ? o.at[3] : o.at[2];
+        return x & 2 ? hi : lo;
     };
     u4 K[2][KS];
     vreg V[8][VN];
-    auto load_k = [&](int t0) {
-        const int oct = t0 + 8 * (col >> 2), r = col & 3;
+    const int64_t krow = (int64_t)(col & 3) * c.token_stride + 8 * grp;
+    auto load_k = [&](int t0, const Octets& o) {
         const __half* p[2];
-        if (OCT) {   // an octet beyond the length: the last one's rows (their scores are masked)
-            p[0] = kbase + slot_at(min(oct, (n - 1) & ~7)) + r * c.token_stride;
-            p[1] = p[0] + 4 * c.token_stride;
+        if (OCT) {
+            p[0] = kbase + (chosen(o, col >> 2) + krow);
+            p[1] = p[0] + 4 * (FULL ? DP : c.token_stride);
         } else {
-            p[0] = kbase + slot_at(min(oct + r, n - 1));
-            p[1] = kbase + slot_at(min(oct + 4 + r, n - 1));
+            const int t = t0 + 8 * (col >> 2) + (col & 3);
+            p[0] = kbase + (slot_at(t) + 8 * grp);
+            p[1] = kbase + (slot_at(t + 4) + 8 * grp);
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                const int dim = 32 * s + 8 * grp;
-                if (FULL) K[u][s] = *reinterpret_cast<const u4*>(p[u] + dim);
+                if (FULL) K[u][s] = *reinterpret_cast<const u4*>(p[u] + 32 * s);
                 else {
                     K[u][s] = u4{0, 0, 0, 0};
-                    if (dim < c.d) K[u][s] = *reinterpret_cast<const u4*>(p[u] + dim);
+                    if (32 * s + 8 * grp < c.d) K[u][s] = *reinterpret_cast<const u4*>(p[u] + 32 * s);
                 }
             }
     };
-    auto load_v = [&](int t0) {
-        const int oct = t0 + 8 * grp, dim = NV * col;
-        const __half* p0 = OCT ? vbase + slot_at(min(oct, (n - 1) & ~7)) : nullptr;
+    auto load_v = [&](int t0, const Octets& o) {
+        const int dim = NV * col;
+        const __half* p0 = OCT ? vbase + (chosen(o, grp) + dim) : nullptr;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const __half* p = OCT ? p0 + i * c.token_stride : vbase + slot_at(min(oct + i, n - 1));
+            const __half* p = OCT ? p0 + i * (FULL ? DP : c.token_stride) : vbase + (slot_at(t0 + 8 * grp + i) + dim);
 #pragma unroll
             for (int x = 0; x < VN; ++x) {
-                if (FULL) V[i][x] = *reinterpret_cast<const vreg*>(p + dim + 8 * x);
+                if (FULL) V[i][x] = *reinterpret_cast<const vreg*>(p + 8 * x);
                 else {
                     V[i][x] = vreg{};
-                    if (dim + 8 * x < c.d) V[i][x] = *reinterpret_cast<const vreg*>(p + dim + 8 * x);
+                    if (dim + 8 * x < c.d) V[i][x] = *reinterpret_cast<const vreg*>(p + 8 * x);
                 }
             }
         }
@@ -150,9 +163,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
     for (int j = 0; j < NV; ++j) acc[j] = f4{0.f, 0.f, 0.f, 0.f};
 
     int t0 = begin + STEP * wave;
+    Octets next;
     if (t0 < end) {
-        load_k(t0);
-        load_v(t0);
+        next = octets(t0);
+        load_k(t0, next);
+        load_v(t0, next);
+        if (t0 + ROUND < end) next = octets(t0 + ROUND);   // (looked up a step ahead of the loads)
     }
     for (; t0 < end; t0 += ROUND) {
         f4 st[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
@@ -161,7 +177,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
 #pragma unroll
             for (int u = 0; u < 2; ++u) st[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, K[u][s]), q[s], st[u], 0, 0, 0);
         const bool more = t0 + ROUND < end;
-        if (more) load_k(t0 + ROUND);   // K's registers are free: the next step's rows fly during the softmax and the second product
+        if (more) load_k(t0 + ROUND, next);   // K's registers are free: the next step's rows fly during the softmax and the second product
 
         float x[8];   // log2 of the weight, unnormalised; token t0 + 8 grp + e
 #pragma unroll
@@ -219,7 +235,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
             acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, __builtin_bit_cast(h8, col8), acc[j], 0, 0, 0);
             acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, __builtin_bit_cast(h8, col8), acc[j], 0, 0, 0);
         }
-        if (more) load_v(t0 + ROUND);
+        if (more) {
+            load_v(t0 + ROUND, next);
+            next = octets(t0 + 2 * ROUND);
+        }
     }
 
     // ---- join the waves ----
@@ -288,53 +307,74 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
 // Base and sum of a query head over its used chunks (a wave's work; the same in every lane).
 __device__ __forceinline__ void join_stats(const Partials& ps, size_t at, int used, float& B, float& L) {
     const int lane = threadIdx.x & 63;
-    B = NEG_INF;
-    for (int i = lane; i < used; i += 64) B = fmaxf(B, ps.l[at + i] == 0.f ? NEG_INF : ps.base[at + i]);
+    // the first 64 chunks' are asked for before `used` is known
+    float l = 0.f, base = NEG_INF;
+    if (lane < ps.chunks) {
+        l = ps.l[at + lane];
+        base = ps.base[at + lane];
+    }
+    if (lane >= used || l == 0.f) base = NEG_INF, l = 0.f;
+    B = base;
+    for (int i = lane + 64; i < used; i += 64) B = fmaxf(B, ps.l[at + i] == 0.f ? NEG_INF : ps.base[at + i]);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) B = fmaxf(B, __shfl_xor(B, x));
-    L = 0.f;
-    for (int i = lane; i < used; i += 64) L += ps.l[at + i] == 0.f ? 0.f : ps.l[at + i] * exp2_fast(ps.base[at + i] - B);
+    L = l == 0.f ? 0.f : l * exp2_fast(base - B);
+    for (int i = lane + 64; i < used; i += 64) L += ps.l[at + i] == 0.f ? 0.f : ps.l[at + i] * exp2_fast(ps.base[at + i] - B);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) L += __shfl_xor(L, x);
 }
 
 constexpr int JOIN_TOKENS = 1024;   // tokens whose weights one workgroup of the second launch makes
 
-// The second launch.  Its first seqs x heads workgroups join the chunks of one query head: 8 lanes of chunks x 32 lanes of dimensions.  The others
+// The second launch.  Its first workgroups join the chunks of one query head, 32 dimensions each: 32 lanes of chunks x 8 of four dimensions.  The others
 // make the weights of one kv head's tokens, JOIN_TOKENS at a time (weight_shares of them divide a kv head's), from the scores in the workspace.  Chunks are taken in order: the sums do not depend on who ran first.
 __global__ __launch_bounds__(256) void attn_join_kernel(Cache c, Attention a, Partials ps, int g, int weight_shares) {
-    const int64_t outs = (int64_t)c.seqs * a.heads;
+    const int slices = (c.d + 31) / 32;
+    const int64_t outs = (int64_t)c.seqs * a.heads * slices;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    __shared__ float red[8][QEFT_MAX_HEAD_DIM];
+    __shared__ __align__(16) float red[32][36];   // (rows four banks apart)
     __shared__ float part[8];
     if ((int64_t)blockIdx.x < outs) {
-        const int b = (int)(blockIdx.x / a.heads), h = (int)(blockIdx.x % a.heads);
-        const int n = min(a.lens[b], a.longest);
-        __half* out = a.out + (size_t)b * a.ldo + (size_t)h * c.d;
-        if (n <= 0) {
-            for (int d = tid; d < c.d; d += 256) out[d] = __float2half_rn(0.f);
-            return;
-        }
-        const int used = (n + ps.chunk - 1) / ps.chunk;
+        const int slice = (int)(blockIdx.x % slices), bh = (int)(blockIdx.x / slices), b = bh / a.heads, h = bh % a.heads;
         const size_t at = ((size_t)b * a.heads + h) * ps.chunks;
+        const int quad = tid & 7, lane_c = tid >> 3, dim = 32 * slice + 4 * quad;
+        const float* po = ps.o + at * c.d + dim;
+        // Everything is asked for at once, before the length says how much of it was written (the rest is not looked at): one latency, not three.
+        constexpr int AHEAD = 4;
+        f4 v[AHEAD];
+        float vl[AHEAD], vb[AHEAD];
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) {
+            const int i = lane_c + 32 * x;
+            v[x] = f4{0.f, 0.f, 0.f, 0.f};
+            vl[x] = vb[x] = 0.f;
+            if (i < ps.chunks) {
+                vl[x] = ps.l[at + i];
+                vb[x] = ps.base[at + i];
+                if (dim < c.d) v[x] = *reinterpret_cast<const f4*>(po + (size_t)i * c.d);
+            }
+        }
+        const int n = min(a.lens[b], a.longest), used = n > 0 ? (n + ps.chunk - 1) / ps.chunk : 0;
+        __half* out = a.out + (size_t)b * a.ldo + (size_t)h * c.d;
         float B, L;
         join_stats(ps, at, used, B, L);
-        const int quads = c.d / 4, ql = tid & 31, cl = tid >> 5;
-        for (int qd = ql; qd < quads; qd += 32) {
-            f4 o = {0.f, 0.f, 0.f, 0.f};
-            for (int i = cl; i < used; i += 8) {
-                const float f = ps.l[at + i] == 0.f ? 0.f : exp2_fast(ps.base[at + i] - B);
-                const f4 v = *reinterpret_cast<const f4*>(ps.o + (at + i) * c.d + 4 * qd);
-                o += v * f;
-            }
-            *reinterpret_cast<f4*>(&red[cl][4 * qd]) = o;
-        }
-        __syncthreads();
-        for (int d = tid; d < c.d; d += 256) {
-            float o = red[0][d];
+        f4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int x = 1; x < 8; ++x) o += red[x][d];
-            out[d] = __float2half_rn(o / L);
+        for (int x = 0; x < AHEAD; ++x)
+            if (lane_c + 32 * x < used && vl[x] != 0.f) o += v[x] * exp2_fast(vb[x] - B);
+        if (dim < c.d)
+            for (int i = lane_c + 32 * AHEAD; i < used; i += 32) {
+                const float l = ps.l[at + i], f = exp2_fast(ps.base[at + i] - B);
+                const f4 w = *reinterpret_cast<const f4*>(po + (size_t)i * c.d);
+                if (l != 0.f) o += w * f;
+            }
+        *reinterpret_cast<f4*>(&red[lane_c][4 * quad]) = o;
+        __syncthreads();
+        if (tid < 32 && 32 * slice + tid < c.d) {
+            float x = 0.f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x += red[i][tid];
+            out[32 * slice + tid] = __float2half_rn(n > 0 ? x / L : 0.f);
         }
         return;
     }
@@ -349,6 +389,14 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Cache c, Attention a, Pa
         float w[JOIN_TOKENS / 256] = {};
         for (int h0 = 0; h0 < g; h0 += 4) {   // a wave for the statistics of each of four heads
             const int h = h0 + wave;
+            float raw[4][JOIN_TOKENS / 256];   // (asked for with the statistics)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+#pragma unroll
+                for (int x = 0; x < JOIN_TOKENS / 256; ++x) {
+                    const int t = begin + 256 * x + tid;
+                    raw[y][x] = h0 + y < g && t < end ? ps.raw[((size_t)b * a.heads + (size_t)kvh * g + h0 + y) * ps.pitch + t] : 0.f;
+                }
             if (h < g) {
                 float B, L;
                 join_stats(ps, ((size_t)b * a.heads + (size_t)kvh * g + h) * ps.chunks, used, B, L);
@@ -358,14 +406,12 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Cache c, Attention a, Pa
                 }
             }
             __syncthreads();
-            for (int y = 0; y < 4 && h0 + y < g; ++y) {
-                const float* rp = ps.raw + ((size_t)b * a.heads + (size_t)kvh * g + h0 + y) * ps.pitch;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                if (h0 + y >= g) break;
                 const float B = part[y], L = part[4 + y];
 #pragma unroll
-                for (int x = 0; x < JOIN_TOKENS / 256; ++x) {
-                    const int t = begin + 256 * x + tid;
-                    if (t < end) w[x] += exp2_fast(rp[t] - B) / L;
-                }
+                for (int x = 0; x < JOIN_TOKENS / 256; ++x) w[x] += exp2_fast(raw[y][x] - B) / L;
             }
             __syncthreads();
         }
@@ -377,8 +423,29 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Cache c, Attention a, Pa
     }
 }
 
+constexpr int SHORT = 512;   // tokens that one workgroup takes rather than two launches: 32 heads of one sequence, 256 / 400 / 800 tokens: 6.2 / 8.5 / 12.3 us against 8.4 / 8.5 / 9.0
+constexpr int CUS = 256;
+
+// Chunks of a row (a sequence's kv head, and 16 of its query heads) of `rounds` 128-token rounds of 64 KiB at head_dim 128.  A CU reads 20 bytes a ns
+// at most, so what counts is that all have the same number of workgroups: one or two each, or, between 128 and 512 rows, what the estimate finds
+// (us: 160 rows of 2049 tokens in 1 / 2 / 3 chunks: 46.4 / 46.3 / 39.4; 256 of 2048: 48.2 / 52.6; 8 of 131001 in 32 / 64 / 128 / 256: 95.6 / 97.3 / 102.6 / 109.9).
+// The second launch is 4 us, and more where many heads have many chunks; one chunk a row leaves the longest of a ragged batch to the end (256 rows of 900 to 3001 tokens:
+// 58.1 us against 56.0), hence its tenth.
+int chunks_of(int64_t rows, int64_t rounds, int d) {
+    if (rounds <= 1 || rows >= 2 * CUS) return 1;
+    if (rows <= CUS / 2) return (int)(2 * CUS / rows < rounds ? 2 * CUS / rows : rounds);
+    int best = 1;
+    float least = 0.f;
+    for (int c = 1; c <= 8 && c <= rounds; ++c) {
+        const float per_cu = (float)((rows * c + CUS - 1) / CUS), us = 3.2f * d / 128.f;   // (a round's time on a CU)
+        const float t = per_cu * ((float)((rounds + c - 1) / c) * us + 0.5f) * (c == 1 ? 1.1f : 1.f) + (c > 1 ? 4.f : 0.f);
+        if (c == 1 || t < least) best = c, least = t;
+    }
+    return best;
+}
+
 struct Plan {
-    int chunk, chunks, tiles;
+    int waves, chunk, chunks, tiles;
     bool direct;
     size_t at_l, at_o, at_raw, bytes;
     int64_t pitch;
@@ -389,12 +456,13 @@ Plan plan_of(int kv, int d, int64_t seqs, int heads, int longest, bool weights) 
     const int g = heads / kv;
     p.tiles = (g + 15) / 16;
     const int64_t rows = seqs * kv * p.tiles;
-    // Chunks of whole rounds.  One chunk, and no second launch, up to 512 tokens; else about 2048 workgroups (4 to a CU's two, so that the last ones to end
-    // leave little idle), as short as one round where there are few rows.
-    const int64_t rounds = ((int64_t)longest + ROUND - 1) / ROUND;
-    int64_t per = longest <= 2 * ROUND ? rounds : rows * rounds / 2048;
-    if (per < 1) per = 1;
-    p.chunk = (int)(per * ROUND);
+    // Eight waves for what is one chunk of few rows (256 rows of 1000 to 2048 tokens, 4 heads each: 41.2 us against 43.1), four else: a round of 128 tokens wastes
+    // less at a row's end (2048 rows of 100 to 300 tokens: 44.9 us against 52.9).
+    int chunks = longest <= SHORT ? 1 : chunks_of(rows, ((int64_t)longest + 4 * STEP - 1) / (4 * STEP), d);
+    p.waves = chunks == 1 && rows < 2 * CUS ? 8 : 4;
+    const int round = p.waves * STEP;
+    const int64_t rounds = ((int64_t)longest + round - 1) / round, per = rounds > 0 ? (rounds + chunks - 1) / chunks : 1;
+    p.chunk = (int)(per * round);
     p.chunks = rounds > 0 ? (int)((rounds + per - 1) / per) : 1;   // (longest 0: the chunk that writes the zeros)
     p.direct = p.chunks == 1 && (p.tiles == 1 || !weights);
     const size_t parts = p.direct ? 0 : (size_t)seqs * heads * p.chunks;
@@ -402,20 +470,21 @@ Plan plan_of(int kv, int d, int64_t seqs, int heads, int longest, bool weights) 
     p.at_l = up(parts * 4);
     p.at_o = 2 * p.at_l;
     p.at_raw = p.at_o + up(parts * d * 4);
-    p.pitch = weights ? rounds * ROUND : 0;
+    p.pitch = weights ? rounds * round : 0;
     p.bytes = p.at_raw + (size_t)seqs * heads * p.pitch * 4;
     return p;
 }
 
 template <int DP, bool FULL, bool OCT>
-void launch(const Cache& c, const Attention& a, const Partials& ps, int g, int tiles, unsigned grid, hipStream_t s) {
-    attn_chunk_kernel<DP, FULL, OCT><<<grid, 64 * WAVES, 0, s>>>(c, a, ps, g, tiles);
+void launch(const Cache& c, const Attention& a, const Partials& ps, int g, const Plan& p, unsigned grid, hipStream_t s) {
+    if (p.waves == 8) attn_chunk_kernel<DP, FULL, OCT, 8><<<grid, 512, 0, s>>>(c, a, ps, g, p.tiles);
+    else attn_chunk_kernel<DP, FULL, OCT, 4><<<grid, 256, 0, s>>>(c, a, ps, g, p.tiles);
 }
 template <int DP>
-void launch_dim(const Cache& c, const Attention& a, const Partials& ps, int g, int tiles, unsigned grid, hipStream_t s) {
-    if (c.page_size % 8 != 0) return launch<DP, false, false>(c, a, ps, g, tiles, grid, s);
-    if (c.d == DP) return launch<DP, true, true>(c, a, ps, g, tiles, grid, s);
-    launch<DP, false, true>(c, a, ps, g, tiles, grid, s);
+void launch_dim(const Cache& c, const Attention& a, const Partials& ps, int g, const Plan& p, unsigned grid, hipStream_t s) {
+    if (c.page_size % 8 != 0) return launch<DP, false, false>(c, a, ps, g, p, grid, s);
+    if (c.d == DP && c.token_stride == DP) return launch<DP, true, true>(c, a, ps, g, p, grid, s);
+    launch<DP, false, true>(c, a, ps, g, p, grid, s);
 }
 
 }  // namespace
@@ -441,13 +510,13 @@ hipError_t attn_decode(const Cache& c, const Attention& a, hipStream_t s) {
         ps.pitch = p.pitch;
     }
     const unsigned grid = (unsigned)((int64_t)c.seqs * c.kv * ps.chunks * p.tiles);
-    if (c.d <= 64) launch_dim<64>(c, a, ps, g, p.tiles, grid, s);
-    else if (c.d <= 128) launch_dim<128>(c, a, ps, g, p.tiles, grid, s);
-    else launch_dim<256>(c, a, ps, g, p.tiles, grid, s);
+    if (c.d <= 64) launch_dim<64>(c, a, ps, g, p, grid, s);
+    else if (c.d <= 128) launch_dim<128>(c, a, ps, g, p, grid, s);
+    else launch_dim<256>(c, a, ps, g, p, grid, s);
     if (!p.direct) {
         const int64_t rows = (int64_t)c.seqs * c.kv, most = rows < 32768 ? 65536 / rows : 1;   // (workgroups enough to fill the GPU, and a grid of bounded size)
         const int tiles = weights ? (a.longest + JOIN_TOKENS - 1) / JOIN_TOKENS : 0, shares = tiles < most ? tiles : (int)most;
-        attn_join_kernel<<<(unsigned)((int64_t)c.seqs * a.heads + rows * shares), 256, 0, s>>>(c, a, ps, g, shares);
+        attn_join_kernel<<<(unsigned)((int64_t)c.seqs * a.heads * ((c.d + 31) / 32) + rows * shares), 256, 0, s>>>(c, a, ps, g, shares);
     }
     return hipGetLastError();
 }
