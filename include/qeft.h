@@ -319,8 +319,8 @@ int qeft_weak_grad_noalloc(const qeft_desc_t* desc, const void* dY, int64_t M, i
  * names: token t in slot t % page_size of page table[b][t / page_size].  page_size is any number from 1; a multiple of 8
  * is fastest (one table entry then serves 8 tokens of a wave). */
 #define QEFT_MAX_HEAD_DIM 256
-/* Most rows (a grid's workgroups) of one of these calls: tokens appended, rows normed, seqs * kv_heads of an eviction (and its possible moves, seqs *
- * kv_heads * longest / 2 / 64, four times that); seqs * heads of an attention an eighth of it.  More is QEFT_ERR_SHAPE. */
+/* Most rows (a grid's workgroups) of one of these calls: tokens appended, rows normed, seqs * kv_heads of an eviction (and, of its second launch, seqs *
+ * kv_heads * (longest / 128 + 1), four times that); seqs * heads of an attention an eighth of it.  More is QEFT_ERR_SHAPE. */
 #define QEFT_MAX_ROWS (1 << 21)
 typedef struct {
     int32_t pages, page_size, kv_heads, head_dim;

@@ -72,7 +72,7 @@ int check_attn(const qeft_cache_desc_t* d, int64_t seqs, int32_t heads, int64_t 
 }
 int check_evict(const qeft_cache_desc_t* d, int64_t seqs, int64_t longest, int64_t budget) {
     if (seqs < 0 || seqs > QEFT_MAX_DIM || longest < 0 || longest > QEFT_MAX_DIM || budget < 0 || budget > QEFT_MAX_DIM) return QEFT_ERR_SHAPE;
-    const int64_t tiles = longest / 64 / 2 + 1;   // (most moves of a row: half of it)
+    const int64_t tiles = longest / 128 + 1;   // (workgroups of the second launch for a row)
     if (seqs * d->kv_heads > QEFT_MAX_ROWS || seqs * d->kv_heads * tiles > 4 * (int64_t)QEFT_MAX_ROWS) return QEFT_ERR_SHAPE;
     return QEFT_OK;
 }

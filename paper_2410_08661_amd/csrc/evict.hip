@@ -2,39 +2,63 @@
 //
 // A row is one kv head of one sequence: n tokens with a weight and a position each, of which `budget` stay.  Order of preference: rank (weight as an ordered
 // 32-bit key, or the key of +infinity for the first and last positions) from high to low, then slot from low to high.  The kept set is everything before
-// one border in that order, (key, slot), which a workgroup finds with its row's keys in LDS:
+// one border in that order, (key, slot), which a workgroup finds with its row's keys in registers, 4 to 32 a thread:
 //   few to go (a sequence one token over its budget): the least preferred token, so many times;
-//   else a selection by digits of 8 bits from the top, each from a histogram of what still agrees with the border's digits; where the border cuts through
-//   equal keys, the same again over the slots.
-// Then kept tokens behind the budget are matched with freed slots before it, both counted off in slot order (a wave per share of the row, ballots).
-// Bytes bound it: 16 a token for weights and positions, and 8 head_dim per token that moves.  Few moves are made by the same workgroup; where there can be many,
-// they go into lists and a second launch spreads them over the GPU.
+//   else three digits from the top, 11, 11 and 10 bits (eight would be a float's exponent, and say little), each from a histogram in LDS of the keys that agree with
+//   the border above it; fewer digits where a bin's keys all stay.  (Bisection over the key, a comparison, a scalar count and an addition a key and step, takes 1 us a
+//   step for 32768 keys, bound by the scalar unit, and some 25 steps.)
+//   Where the border cuts through equal keys, they are counted off in slot order.
+// What changes is a bit a token: freed slots before the budget, kept tokens behind it.  The i-th of the one takes the i-th of the other in, both counted off in
+// slot order.  Where a call has few to move the workgroup does that itself; else the bits go to the workspace and a second launch has a workgroup for every
+// 128 tokens behind the budget, which counts the bits before its own.
+// Bytes bound it: 16 a token for weights and positions, and 8 head_dim per token that moves.
 #include "qeft_internal.h"
+#include "wave.h"
 
 namespace qeft {
 namespace {
 
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef int i4 __attribute__((ext_vector_type(4)));
+typedef float f4 __attribute__((ext_vector_type(4)));
 
-constexpr int BINS = 256, COPIES = 16;          // a digit's histogram: counters of a bin side by side, a lane adds to its own of 16 (equal weights are common:
-                                                // one counter would take a wave's 64 additions one after the other)
 constexpr int FEW = 4;                          // tokens to go that are found one by one
-constexpr int INLINE_MOVES = 32;                // moves that the selecting workgroup makes itself
-constexpr int MAX_KEYS = 35 * 1024;             // keys that fit LDS beside the histogram and the lists
+constexpr int TILE = 128;                       // tokens behind the budget whose moves one workgroup of the second launch makes; also the most that the first does
+constexpr int MAX_IN_REGISTERS = 32 * 1024;     // keys that a workgroup's registers hold, 32 a thread
 constexpr uint32_t KEY_INF = 0xff800000u;
 
-__device__ __forceinline__ uint32_t key_of(float x) {
+// Ordered like the value, or like +infinity for the positions that always stay; never 0.
+__device__ __forceinline__ uint32_t key_of(float x, int pos, int first, int recent) {
     const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.f);   // (-0 becomes +0)
-    if (x != x) return 0xffffffffu;
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    uint32_t k = u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
+    k = x != x ? 0xffffffffu : k;
+    return ((pos < first) | (pos >= recent)) ? KEY_INF : k;
+}
+__device__ __forceinline__ int first_recent(int seen, int keep_last) {
+    const int64_t r = (int64_t)seen - keep_last;
+    return r < INT32_MIN ? INT32_MIN : (int)r;
 }
 
-struct Moves {
-    int* count;   // [rows]
-    int* src;     // [rows][cap]
-    int* dst;
-    int cap;
+// A row's arrays.
+struct Row {
+    int b, h, n, left;
+    const float* score;
+    const int* pos;
+    float* score_out;
+    int* pos_out;
 };
+__device__ __forceinline__ Row row_at(const Cache& c, const Evict& a, int row) {
+    Row r;
+    r.b = row / c.kv;
+    r.h = row % c.kv;
+    r.n = min(max(a.lens[r.b], 0), a.longest);
+    r.left = min(r.n, a.budget);
+    r.score = a.score + (size_t)row * a.ld;
+    r.pos = a.pos + (size_t)row * a.ld;
+    r.score_out = a.score_out + (size_t)row * a.ld_out;
+    r.pos_out = a.pos_out + (size_t)row * a.ld_out;
+    return r;
+}
 
 __device__ __forceinline__ __half* slot_ptr(const Cache& c, __half* pool, int b, int h, int t) {
     const int p = c.by_page.of(t);
@@ -42,13 +66,64 @@ __device__ __forceinline__ __half* slot_ptr(const Cache& c, __half* pool, int b,
     return pool + (size_t)page * c.page_stride + (size_t)h * c.head_stride + (size_t)(t - p * c.page_size) * c.token_stride;
 }
 
-// Moves number first, first + step, ... of a row: `lane` of the 16 that share a move takes pieces lane, lane + 16, ... of both rows.
-__device__ __forceinline__ void move_rows(const Cache& c, int b, int h, const int* src, const int* dst, int count, int first, int step, int lane) {
-    for (int i = first; i < count; i += step) {
-        const int s = src[i], t = dst[i];
-        const __half *ks = slot_ptr(c, c.k, b, h, s), *vs = slot_ptr(c, c.v, b, h, s);
-        __half *kd = slot_ptr(c, c.k, b, h, t), *vd = slot_ptr(c, c.v, b, h, t);
-        for (int x = 8 * lane; x < c.d; x += 128) {
+// What changes in a row: a bit a token, set for freed slots below row.left and for kept tokens behind it, and before every word of 64 the number of bits
+// set in the words below.
+struct Changes {
+    const uint64_t* bits;
+    const int* below;
+};
+
+struct MoveLists {
+    int src[TILE], dst[TILE];
+};
+
+// The moves of the kept tokens in [from, to) (TILE at most).  A workgroup.
+__device__ __forceinline__ void make_moves(const Cache& c, const Row& r, const Changes& ch, int from, int to, MoveLists& l) {
+    const int tid = threadIdx.x, T = blockDim.x, lane = tid & 63, wave = tid >> 6, waves = T >> 6;
+    const uint64_t under = ((uint64_t)1 << lane) - 1;
+    auto low = [](int n) { return ((uint64_t)1 << n) - 1; };   // the n lowest bits, n < 64
+    // set bits below row.left (the freed slots) and below `from`: the first mover's rank is the difference, and so for the end
+    const int cl = r.left / 64, cf = from / 64, ct = (to - 1) / 64;
+    const int holes = ch.below[cl] + __popcll(ch.bits[cl] & low(r.left & 63));
+    const int first = ch.below[cf] + __popcll(ch.bits[cf] & low(from & 63)) - holes;
+    const int last = ch.below[ct] + __popcll(ch.bits[ct] & (low((to - 1) & 63) | (uint64_t)1 << ((to - 1) & 63))) - holes;
+    const int count = last - first;
+    if (count == 0) return;
+    // the movers, three words at most: a wave a word, a lane a token
+    for (int w = cf + wave; w <= ct; w += waves) {
+        const uint64_t x = ch.bits[w];
+        const int t = 64 * w + lane, rank = ch.below[w] + __popcll(x & under) - holes - first;
+        if ((x >> lane & 1) && t >= from && t < to) l.src[rank] = t;
+    }
+    // the freed slots of ranks first .. last - 1: a wave looks through 64 words at a time for those that hold any, then takes these one by one
+    for (int w0 = 64 * wave; w0 <= cl; w0 += 64 * waves) {
+        const int w = w0 + lane;
+        uint64_t x = 0;
+        int at = 0;
+        if (w <= cl) {
+            x = ch.bits[w];
+            at = ch.below[w];
+            if (w == cl) x &= low(r.left & 63);
+        }
+        for (uint64_t hit = __ballot(x != 0 && at < last && at + __popcll(x) > first); hit; hit &= hit - 1) {
+            const int o = __builtin_ctzll(hit);
+            const uint64_t y = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), o) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, o);
+            const int rank = __builtin_amdgcn_readlane(at, o) + __popcll(y & under);
+            if ((y >> lane & 1) && rank >= first && rank < last) l.dst[rank - first] = 64 * (w0 + o) + lane;
+        }
+    }
+    __syncthreads();
+    if (tid < count) {
+        const int s = l.src[tid], t = l.dst[tid];
+        r.score_out[t] = r.score[s];
+        r.pos_out[t] = r.pos[s];
+    }
+    // 16 lanes a move, K and V
+    for (int i = tid >> 4; i < count; i += T >> 4) {
+        const int s = l.src[i], t = l.dst[i];
+        const __half *ks = slot_ptr(c, c.k, r.b, r.h, s), *vs = slot_ptr(c, c.v, r.b, r.h, s);
+        __half *kd = slot_ptr(c, c.k, r.b, r.h, t), *vd = slot_ptr(c, c.v, r.b, r.h, t);
+        for (int x = 8 * (tid & 15); x < c.d; x += 128) {
             const u4 k = *reinterpret_cast<const u4*>(ks + x), v = *reinterpret_cast<const u4*>(vs + x);
             *reinterpret_cast<u4*>(kd + x) = k;
             *reinterpret_cast<u4*>(vd + x) = v;
@@ -56,236 +131,495 @@ __device__ __forceinline__ void move_rows(const Cache& c, int b, int h, const in
     }
 }
 
-// The digit at `shift` of the border, among the values that agree with `prefix` above it: from the top down, the bin in which the `want`-th value lies.
-// `each(f)` calls f(value) for every value of this thread.  Returns prefix with the digit; want becomes the rank within the bin, size its values.
-template <class Each>
-__device__ __forceinline__ uint32_t border_digit(int* hist, int* bins, int* found, uint32_t prefix, int shift, int& want, int& size, const Each& each) {
-    const int tid = threadIdx.x, lane = tid & 63;
-    for (int i = tid; i < BINS * COPIES; i += blockDim.x) hist[i] = 0;
-    __syncthreads();
-    const uint32_t above = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-    each([&](uint32_t v) {
-        if ((v & above) == (prefix & above)) atomicAdd(&hist[((v >> shift) & 255) * COPIES + (lane & (COPIES - 1))], 1);
-    });
-    __syncthreads();
-    for (int i = tid; i < BINS; i += blockDim.x) {
-        int s = 0;
+// The border of a row's keys, 4 J a thread: `left` keys stay, all from lo on if exact, else all above lo and `want` of those equal to it.
+struct Border {
+    uint32_t lo;
+    bool exact;
+    int want;
+};
+constexpr int BINS = 1 << 11;
+// Counters of a bin side by side, a lane adds to its own: equal weights are common, and one counter takes a wave's 64 additions one after the other.  More of
+// them cost more to clear and to read, which a workgroup of few keys notices.
+template <int J> constexpr int COPIES = J == 1 ? 2 : J < 8 ? 4 : 8;
+struct DigitShared {
+    int tally[16], found[3];
+};
+template <int J>
+__device__ __forceinline__ Border find_border(const uint32_t (&key)[J][4], int left, int* hist, DigitShared& sh) {
+    constexpr int C = COPIES<J>;
+    const int tid = threadIdx.x, T = blockDim.x, lane = tid & 63, wave = tid >> 6;
+    Border r{0, false, left};
+#pragma unroll 1
+    for (int shift = 21; !r.exact; shift = shift == 21 ? 10 : 0) {
+        for (int i = 4 * tid; i < BINS * C; i += 4 * T) *reinterpret_cast<i4*>(hist + i) = i4{0, 0, 0, 0};
+        __syncthreads();
+        const uint32_t mask = shift == 0 ? 1023 : 2047, known = shift == 21 ? 0 : ~0u << (shift == 10 ? 21 : 10);
 #pragma unroll
-        for (int x = 0; x < COPIES; ++x) s += hist[i * COPIES + x];
-        bins[i] = s;
-    }
-    __syncthreads();
-    if (tid < 64) {   // lane 0 has the four highest bins
-        int own[4], sum = 0;
+        for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) sum += own[x] = bins[BINS - 1 - (4 * lane + x)];
-        int before = sum;
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t k = key[j][e];
+                if (k != 0 && ((k ^ r.lo) & known) == 0) atomicAdd(&hist[((k >> shift) & mask) * C + (lane & (C - 1))], 1);
+            }
+        __syncthreads();
+        // runs of 4 bins, the highest first: thread x has runs x, x + T, ... of 512; a sum over runs needs them in order, so threads take neighbouring ones
+        const int per = (BINS / 4 + T - 1) / T, first = per * tid;   // runs of this thread: 1 to 4
+        int sum = 0;
+        for (int x = 0; x < per && first + x < BINS / 4; ++x) {
+            const i4* p = reinterpret_cast<const i4*>(hist + (size_t)(BINS - 4 * (first + x + 1)) * C);
 #pragma unroll
-        for (int x = 1; x < 64; x <<= 1) {
-            const int y = __shfl_up(before, x);
-            if (lane >= x) before += y;
+            for (int y = 0; y < C; ++y) sum += p[y].x + p[y].y + p[y].z + p[y].w;
         }
-        before -= sum;
-        if (want > before && want <= before + sum) {
+        const int upto = wave_upto(sum);
+        if (lane == 63) sh.tally[wave] = upto;
+        __syncthreads();
+        int before = upto - sum + waves_reduce(sh.tally, 0, wave, 0, Sum());
+        if (r.want > before && r.want <= before + sum) {   // one thread
+            for (int bin = BINS - 4 * first - 1;; --bin) {
+                int own = 0;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                if (want > before && want <= before + own[x]) {
-                    found[0] = BINS - 1 - (4 * lane + x);
-                    found[1] = want - before;
-                    found[2] = own[x];
+                for (int y = 0; y < C; ++y) own += hist[bin * C + y];
+                if (r.want <= before + own) {
+                    sh.found[0] = bin;
+                    sh.found[1] = r.want - before;
+                    sh.found[2] = own;
+                    break;
                 }
-                before += own[x];
+                before += own;
+            }
+        }
+        __syncthreads();
+        r.lo |= (uint32_t)sh.found[0] << shift;
+        r.want = sh.found[1];
+        r.exact = sh.found[2] == r.want;
+        if (shift == 0) break;
+    }
+    return r;
+}
+
+// The tokens to go are at most FEW: the least preferred one, so many times.  What may move is known beforehand, the last `go` tokens, and was loaded beside
+// the keys: 32 threads a token, 16 of them for K's row and 16 for V's.
+template <int J>
+__device__ __forceinline__ void evict_few(const Cache& c, const Row& r, const uint32_t (&key)[J][4], const u4 (&carried)[2], float carried_score, int carried_pos, uint64_t (*least)[16]) {
+    const int tid = threadIdx.x, T = blockDim.x, waves = T >> 6, go = r.n - r.left;
+    int gone[FEW];
+    uint64_t last = 0;
+#pragma unroll
+    for (int i = 0; i < FEW; ++i) {
+        gone[i] = -1;
+        if (i >= go) continue;
+        uint64_t x = ~0ull;   // (key, slots from the highest down)
+        int t0 = 4 * tid;
+        asm volatile("" : "+v"(t0));   // (or the compiler keeps every slot's number for all rounds)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t k = key[j][e];
+                asm volatile("" : "+v"(k));   // (or it is kept as the upper half of a pair all the time)
+                const uint64_t v = (uint64_t)k << 32 | (uint32_t)~(t0 + 4 * j * T + e);
+                if (k != 0 && v < x && v > last) x = v;
+            }
+        x = wave_reduce(x, Least());
+        if ((tid & 63) == 0) least[i & 1][tid >> 6] = x;
+        __syncthreads();
+        last = waves_reduce(least[i & 1], 0, waves, ~(uint64_t)0, Least());
+        gone[i] = (int)~(uint32_t)last;
+    }
+    const int mine = tid >> 5, token = r.left + mine;
+    if (mine >= go) return;
+    // the mover's rank among the movers; the freed slot of the same rank
+    int rank = 0, to = -1;
+#pragma unroll
+    for (int t = 0; t < FEW; ++t)
+        if (t < mine) {
+            bool stays = true;
+#pragma unroll
+            for (int i = 0; i < FEW; ++i) stays &= gone[i] != r.left + t;
+            rank += stays;
+        }
+#pragma unroll
+    for (int i = 0; i < FEW; ++i) {
+        if (gone[i] == token) return;
+        if (gone[i] < 0 || gone[i] >= r.left) continue;
+        int lower = 0;
+#pragma unroll
+        for (int k = 0; k < FEW; ++k) lower += gone[k] >= 0 && gone[k] < gone[i];
+        if (lower == rank) to = gone[i];
+    }
+    if (to < 0) return;
+    __half* p = slot_ptr(c, tid & 16 ? c.v : c.k, r.b, r.h, to) + 8 * (tid & 15);
+    if (8 * (tid & 15) < c.d) *reinterpret_cast<u4*>(p) = carried[0];
+    if (8 * (tid & 15) + 128 < c.d) *reinterpret_cast<u4*>(p + 128) = carried[1];
+    if ((tid & 31) == 0) {
+        r.score_out[to] = carried_score;
+        r.pos_out[to] = carried_pos;
+    }
+}
+
+// Workgroup = a row of at most 4 J blockDim.x tokens.  VEC: rows start on 16 bytes.  all_bits: where the bits go, [rows][words], or NULL: no row has more than TILE to go.
+template <int J, bool VEC>
+__global__ __launch_bounds__(1024, J == 1 ? 8 : 4) void evict_select_kernel(Cache c, Evict a, uint64_t* all_bits, int* all_below, int words) {
+    constexpr int WORDS = 4 * J * 1024 / 64;
+    __shared__ __align__(16) uint64_t bits[WORDS];
+    __shared__ int below[WORDS];
+    __shared__ uint64_t least[2][16];
+    __shared__ int counts[16 * J];
+    __shared__ int cut_at;
+    __shared__ MoveLists lists;
+    __shared__ DigitShared digit;
+    extern __shared__ __align__(16) int hist[];   // [BINS][COPIES<J>]
+    const int tid = threadIdx.x, T = blockDim.x, lane = tid & 63, wave = tid >> 6, waves = T >> 6;
+    const Row r = row_at(c, a, blockIdx.x);
+    const int n = r.n, left = r.left, go = n - left;
+    if (r.h == 0 && tid == 0) a.lens_out[r.b] = left;
+    const bool copy_score = a.score_out != a.score, copy_pos = a.pos_out != a.pos;
+    const int recent = first_recent(a.seen[r.b], a.keep_last);
+    const bool few = go > 0 && go <= FEW && left > 0;
+    u4 carried[2];
+    float carried_score = 0.f;
+    int carried_pos = 0;
+    if (few && (tid >> 5) < go) {
+        const int token = left + (tid >> 5);
+        const __half* p = slot_ptr(c, tid & 16 ? c.v : c.k, r.b, r.h, token) + 8 * (tid & 15);
+        if (8 * (tid & 15) < c.d) carried[0] = *reinterpret_cast<const u4*>(p);
+        if (8 * (tid & 15) + 128 < c.d) carried[1] = *reinterpret_cast<const u4*>(p + 128);
+        carried_score = r.score[token];
+        carried_pos = r.pos[token];
+    }
+
+    // Vector j of an array: a base that all lanes share and one offset for all of a lane's, or the compiler keeps 64 addresses a thread.
+    const uint32_t offset = 16u * tid;
+    auto vec_of = [&](const void* p, int j) { return (const char*)p + 16 * (size_t)(j * T) + offset; };
+    auto vec_to = [&](void* p, int j) { return (char*)p + 16 * (size_t)(j * T) + offset; };
+    uint32_t key[J][4];   // token 4 (j T + tid) + e; 0: no token
+    constexpr int AT_ONCE = J < 4 ? J : 4;
+#pragma unroll
+    for (int j0 = 0; j0 < J; j0 += AT_ONCE) {
+        f4 s[AT_ONCE];
+        i4 p[AT_ONCE];
+#pragma unroll
+        for (int y = 0; y < AT_ONCE; ++y) {   // loads before the first use
+            const int t = 4 * ((j0 + y) * T + tid);
+            if (VEC && t + 4 <= n) {
+                s[y] = *reinterpret_cast<const f4*>(vec_of(r.score, j0 + y));
+                p[y] = *reinterpret_cast<const i4*>(vec_of(r.pos, j0 + y));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[y][e] = t + e < n ? reinterpret_cast<const float*>(vec_of(r.score, j0 + y))[e] : 0.f;
+                    p[y][e] = t + e < n ? reinterpret_cast<const int*>(vec_of(r.pos, j0 + y))[e] : 0;
+                }
+            }
+        }
+        // weights and positions of the slots that stay go out as they came; what moves into a freed slot is written over them later
+#pragma unroll
+        for (int y = 0; y < AT_ONCE; ++y) {
+            const int t = 4 * ((j0 + y) * T + tid);
+            if (VEC && t + 4 <= left) {
+                if (copy_score) *reinterpret_cast<f4*>(vec_to(r.score_out, j0 + y)) = s[y];
+                if (copy_pos) *reinterpret_cast<i4*>(vec_to(r.pos_out, j0 + y)) = p[y];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (t + e < left) {
+                        if (copy_score) reinterpret_cast<float*>(vec_to(r.score_out, j0 + y))[e] = s[y][e];
+                        if (copy_pos) reinterpret_cast<int*>(vec_to(r.pos_out, j0 + y))[e] = p[y][e];
+                    }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t k = key_of(s[y][e], p[y][e], a.keep_first, recent);
+                key[j0 + y][e] = t + e >= n ? 0u : k;
             }
         }
     }
-    __syncthreads();
-    want = found[1];
-    size = found[2];
-    return prefix | (uint32_t)found[0] << shift;
+    // (rows of one call can be of any kind: those whose moves are made here, or that have none, leave no bits)
+    const bool moves = go > 0 && !few && left > 0;
+    if (moves) {
+        const Border border = find_border<J>(key, left, hist, digit);
+        const uint32_t lo = border.lo;
+        const bool exact = border.exact;
+        // equal keys at the border: those in the lowest slots stay, `want` of them
+        int cut = n;
+        if (!exact) {
+            const int want = border.want;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                int all = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) all += __popcll(__ballot(key[j][e] == lo));
+                if (lane == 0) counts[j * waves + wave] = all;
+            }
+            __syncthreads();
+            // sums over the vectors one after the other and the waves within them, the slots' order; up to four counts a lane
+            constexpr int PER = (16 * J + 63) / 64;
+            int own[PER], sum = 0;
+#pragma unroll
+            for (int x = 0; x < PER; ++x) {
+                const int o = PER * lane + x;
+                sum += own[x] = o < J * waves ? counts[o] : 0;
+            }
+            const int upto = wave_upto(sum), l = __builtin_ctzll(__ballot(upto >= want));   // (there are enough)
+            int before = __shfl(upto - sum, l), o = PER * l;
+#pragma unroll
+            for (int x = 0; x + 1 < PER; ++x) {
+                const int y = __shfl(own[x], l);
+                if (o == PER * l + x && before + y < want) before += y, ++o;
+            }
+            if (o % waves == wave) {
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    if (o / waves != j) continue;
+                    int rank = before;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint64_t x = __ballot(key[j][e] == lo);
+                        rank += __builtin_amdgcn_mbcnt_hi((uint32_t)(x >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)x, 0));
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (key[j][e] == lo && ++rank == want) cut_at = 4 * (j * T + tid) + e + 1;
+                }
+            }
+            __syncthreads();
+            cut = cut_at;
+        }
+        // a bit a token, two threads to a byte
+        int t0 = 4 * tid;
+        asm volatile("" : "+v"(t0));   // (or the compiler keeps every comparison of a slot since the loads, a pair of registers each)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            int f = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int t = t0 + 4 * j * T + e;
+                const bool kept = key[j][e] > lo || (key[j][e] == lo && (exact || t < cut));
+                f |= (int)(key[j][e] != 0 && (t < left) != kept) << e;
+            }
+            f |= (int)rotated<15>((uint32_t)f) << 4;   // (the next lane's)
+            if ((tid & 1) == 0) reinterpret_cast<uint8_t*>(bits)[(j * T + tid) / 2] = (uint8_t)f;
+        }
+        __syncthreads();
+        // the words' bits, summed up to each by the first wave
+        const int used = (n + 63) / 64;
+        if (wave == 0) {
+            int passed = 0;
+            for (int w0 = 0; w0 < used; w0 += 64) {
+                const uint64_t x = w0 + lane < used ? bits[w0 + lane] : 0;
+                const int own = __popcll(x), upto = wave_upto(own);
+                if (w0 + lane < used) {
+                    below[w0 + lane] = passed + upto - own;
+                    if (all_bits) {
+                        all_bits[(size_t)blockIdx.x * words + w0 + lane] = x;
+                        all_below[(size_t)blockIdx.x * words + w0 + lane] = passed + upto - own;
+                    }
+                }
+                passed += __builtin_amdgcn_readlane(upto, 63);
+            }
+        }
+    }
+    if (few) evict_few<J>(c, r, key, carried, carried_score, carried_pos, least);
+    if (all_bits) {
+        if (!moves)
+            for (int w = tid; 64 * w < n; w += T) all_bits[(size_t)blockIdx.x * words + w] = 0, all_below[(size_t)blockIdx.x * words + w] = 0;
+    } else if (moves) {
+        __syncthreads();
+        make_moves(c, r, Changes{bits, below}, left, n, lists);
+    }
 }
 
-// Workgroup = a row.  IN_LDS: the keys stay in LDS, else every pass takes them from the inputs again.
-template <bool IN_LDS>
-__global__ __launch_bounds__(1024) void evict_select_kernel(Cache c, Evict a, Moves mv) {
-    extern __shared__ __align__(16) uint32_t shared[];
-    int* hist = (int*)shared;                                // [BINS * COPIES]
-    uint32_t* keys = shared + BINS * COPIES;                 // [longest] if IN_LDS
-    __shared__ int bins[BINS], found[3], holes[16], movers[16];
-    __shared__ uint64_t least[16];
-    __shared__ int src[INLINE_MOVES], dst[INLINE_MOVES];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
-    const int row = blockIdx.x, b = row / c.kv, h = row % c.kv;
-    const int n = min(max(a.lens[b], 0), a.longest), left = min(n, a.budget);
-    if (h == 0 && tid == 0) a.lens_out[b] = left;
-    const float* score = a.score + (size_t)row * a.ld;
-    const int* pos = a.pos + (size_t)row * a.ld;
-    float* score_out = a.score_out + (size_t)row * a.ld_out;
-    int* pos_out = a.pos_out + (size_t)row * a.ld_out;
-    const bool copy_score = a.score_out != a.score, copy_pos = a.pos_out != a.pos;
-    const bool listed = mv.count != nullptr;
-    if (n == left) {
-        for (int t = tid; t < n; t += blockDim.x) {
-            if (copy_score) score_out[t] = score[t];
-            if (copy_pos) pos_out[t] = pos[t];
-        }
-        if (listed && tid == 0) mv.count[row] = 0;
+// Rows of any length: the keys taken from the inputs again by each step, the border found digit by digit from histograms, 11, 11 and 10 bits.
+constexpr int LONG_COPIES = 4;
+__global__ __launch_bounds__(1024) void evict_select_long_kernel(Cache c, Evict a, uint64_t* all_bits, int* all_below, int words) {
+    __shared__ __align__(16) int hist[BINS * LONG_COPIES];
+    __shared__ int tally[16], found[3], cut_at;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Row r = row_at(c, a, blockIdx.x);
+    const int n = r.n, left = r.left;
+    if (r.h == 0 && tid == 0) a.lens_out[r.b] = left;
+    for (int t = tid; t < left; t += 1024) {
+        if (a.score_out != a.score) r.score_out[t] = r.score[t];
+        if (a.pos_out != a.pos) r.pos_out[t] = r.pos[t];
+    }
+    uint64_t* bits = all_bits + (size_t)blockIdx.x * words;
+    int* below = all_below + (size_t)blockIdx.x * words;
+    if (n == left || left == 0) {   // (always, where there is no workspace for bits)
+        if (all_bits)
+            for (int w = tid; 64 * w < n; w += 1024) bits[w] = 0, below[w] = 0;
         return;
     }
-    const int64_t recent = (int64_t)a.seen[b] - a.keep_last;
-    auto rank = [&](float s, int p) { return p < a.keep_first || p >= recent ? KEY_INF : key_of(s); };
-    // weights and positions of the slots that stay go out as they come; what moves into a freed slot is written over them below
-    for (int t = tid; t < n; t += blockDim.x) {
-        const float s = score[t];
-        const int p = pos[t];
-        if (IN_LDS) keys[t] = rank(s, p);
-        if (t < left) {
-            if (copy_score) score_out[t] = s;
-            if (copy_pos) pos_out[t] = p;
-        }
-    }
-    __syncthreads();
-    auto key_at = [&](int t) -> uint32_t { return IN_LDS ? keys[t] : rank(score[t], pos[t]); };
-
-    uint32_t border = 0;   // kept: key > border, or key == border in a slot < cut
-    int cut = 0;
-    const int go = n - left;
-    if (left == 0) {
-        border = 0xffffffffu;
-    } else if (go <= FEW) {
-        // the least preferred: the smallest (key, slots from the highest down)
-        uint64_t last = 0;
-        for (int i = 0; i < go; ++i) {
-            uint64_t mine = ~0ull;
-            for (int t = tid; t < n; t += blockDim.x) {
-                const uint64_t v = (uint64_t)key_at(t) << 32 | (uint32_t)~t;
-                if (v < mine && (i == 0 || v > last)) mine = v;
+    const int recent = first_recent(a.seen[r.b], a.keep_last);
+    auto key_from = [&](float s, int p) { return key_of(s, p, a.keep_first, recent); };
+    // f(key, slot) for this thread's tokens in [from, to), `step` apart, eight loads at a time
+    auto each = [&](int from, int to, int step, auto&& f) {
+        for (int t0 = from; t0 < to; t0 += 8 * step) {
+            float s[8];
+            int p[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const int t = t0 + x * step;
+                s[x] = t < to ? r.score[t] : 0.f;
+                p[x] = t < to ? r.pos[t] : 0;
             }
 #pragma unroll
-            for (int x = 1; x < 64; x <<= 1) {
-                const uint64_t o = (uint64_t)__shfl_xor((unsigned long long)mine, x);
-                mine = o < mine ? o : mine;
-            }
-            if (lane == 0) least[wave] = mine;
-            __syncthreads();
-            for (int w = 0; w < waves; ++w) mine = least[w] < mine ? least[w] : mine;
-            __syncthreads();
-            last = mine;
+            for (int x = 0; x < 8; ++x)
+                if (t0 + x * step < to) f(key_from(s[x], p[x]), t0 + x * step);
         }
-        border = (uint32_t)(last >> 32);
-        cut = (int)~(uint32_t)last;
-    } else {
-        int want = left, size = n;
-        for (int shift = 24; shift >= 0; shift -= 8)
-            border = border_digit(hist, bins, found, border, shift, want, size, [&](auto&& f) {
-                for (int t = tid; t < n; t += blockDim.x) f(key_at(t));
-            });
-        cut = n;   // all of the border's key, or the `want` lowest slots of it: the highest values of ~slot
-        if (want < size) {
-            uint32_t low = 0;
-            for (int shift = 24; shift >= 0; shift -= 8)
-                low = border_digit(hist, bins, found, low, shift, want, size, [&](auto&& f) {
-                    for (int t = tid; t < n; t += blockDim.x)
-                        if (key_at(t) == border) f(~(uint32_t)t);
-                });
-            cut = (int)~low + 1;
-        }
-    }
-
-    // freed slots below `left`, kept tokens from `left` on: counted per wave, then written in order.  A wave has a share of whole groups of 64.
-    const int share = (n + 64 * waves - 1) / (64 * waves) * 64, from = wave * share, to = min(n, from + share);
-    auto kept = [&](int t) {
-        const uint32_t k = key_at(t);
-        return k > border || (k == border && t < cut);
     };
-    int nh = 0, nm = 0;
-    for (int t0 = from; t0 < to; t0 += 64) {
-        const int t = t0 + lane;
-        const bool in = t < to, k = in && kept(t);
-        nh += __popcll(__ballot(in && !k && t < left));
-        nm += __popcll(__ballot(k && t >= left));
+    uint32_t border = 0;
+    int want = left, size = n;
+    for (int d = 0; d < 3; ++d) {
+        const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, top = d == 0 ? 32 : d == 1 ? 21 : 10;
+        const uint32_t mask = d == 2 ? 1023 : 2047;
+        for (int i = tid; i < BINS * LONG_COPIES; i += 1024) hist[i] = 0;
+        __syncthreads();
+        each(tid, n, 1024, [&](uint32_t k, int) {
+            if (d == 0 || k >> top == border >> top) atomicAdd(&hist[((k >> shift) & mask) * LONG_COPIES + (lane & (LONG_COPIES - 1))], 1);
+        });
+        __syncthreads();
+        // two bins a thread, thread 0 the highest
+        int own[2], sum = 0;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const i4 v = *reinterpret_cast<const i4*>(&hist[(BINS - 1 - (2 * tid + x)) * LONG_COPIES]);
+            sum += own[x] = v.x + v.y + v.z + v.w;
+        }
+        const int upto_wave = wave_upto(sum);
+        if (lane == 63) tally[wave] = upto_wave;
+        __syncthreads();
+        int before = upto_wave - sum;
+        for (int w = 0; w < wave; ++w) before += tally[w];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            if (want > before && want <= before + own[x]) {
+                found[0] = BINS - 1 - (2 * tid + x);
+                found[1] = want - before;
+                found[2] = own[x];
+            }
+            before += own[x];
+        }
+        __syncthreads();
+        border |= (uint32_t)found[0] << shift;
+        want = found[1];
+        size = found[2];
     }
-    if (lane == 0) {
-        holes[wave] = nh;
-        movers[wave] = nm;
+    // a wave has a share of whole words; equal keys at the border are counted by shares first, `want` of them stay
+    const int share = (n + 64 * 16 - 1) / (64 * 16) * 64, from = min(n, wave * share), to = min(n, from + share);
+    int cut = n;
+    if (want < size) {
+        int mine = 0;
+        each(from + lane, to, 64, [&](uint32_t k, int) { mine += k == border; });
+        mine = wave_reduce(mine, Sum());
+        if (lane == 0) tally[wave] = mine;
+        __syncthreads();
+        int before = 0;
+        for (int w = 0; w < wave; ++w) before += tally[w];
+        if (before < want && before + mine >= want) {
+            for (int t0 = from; t0 < to && before < want; t0 += 64) {
+                const int t = t0 + lane;
+                const bool tie = t < to && key_from(r.score[t], r.pos[t]) == border;
+                const uint64_t x = __ballot(tie);
+                if (tie && before + __popcll(x & (((uint64_t)1 << lane) - 1)) + 1 == want) cut_at = t + 1;
+                before += __popcll(x);
+            }
+        }
+        __syncthreads();
+        cut = cut_at;
     }
+    int mine = 0;
+    for (int t0 = from; t0 < to; t0 += 8 * 64) {
+        float s[8];
+        int p[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int t = t0 + 64 * x + lane;
+            s[x] = t < to ? r.score[t] : 0.f;
+            p[x] = t < to ? r.pos[t] : 0;
+        }
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int t = t0 + 64 * x + lane;
+            const uint32_t k = key_from(s[x], p[x]);
+            const uint64_t w = __ballot(t < to && (t < left) != (k > border || (k == border && t < cut)));
+            if (t0 + 64 * x < to && lane == 0) {
+                bits[t0 / 64 + x] = w;
+                below[t0 / 64 + x] = mine;
+            }
+            mine += __popcll(w);
+        }
+    }
+    __syncthreads();   // (tally may still be read)
+    if (lane == 0) tally[wave] = mine;
     __syncthreads();
-    int at_h = 0, at_m = 0, count = 0;
-    for (int w = 0; w < waves; ++w) {
-        if (w < wave) {
-            at_h += holes[w];
-            at_m += movers[w];
-        }
-        count += movers[w];
-    }
-    int* ls = listed ? mv.src + (size_t)row * mv.cap : src;
-    int* ld = listed ? mv.dst + (size_t)row * mv.cap : dst;
-    if (nh | nm) {
-        for (int t0 = from; t0 < to; t0 += 64) {
-            const int t = t0 + lane;
-            const bool in = t < to, k = in && kept(t), hole = in && !k && t < left, mover = k && t >= left;
-            const uint64_t bh = __ballot(hole), bm = __ballot(mover), below = ((uint64_t)1 << lane) - 1;
-            if (hole) ld[at_h + __popcll(bh & below)] = t;
-            if (mover) ls[at_m + __popcll(bm & below)] = t;
-            at_h += __popcll(bh);
-            at_m += __popcll(bm);
-        }
-    }
-    __syncthreads();   // (the lists, and the copies that what follows writes over)
-    for (int i = tid; i < count; i += blockDim.x) {
-        const int s = ls[i], t = ld[i];
-        score_out[t] = score[s];
-        pos_out[t] = pos[s];
-    }
-    if (listed) {
-        if (tid == 0) mv.count[row] = count;
-    } else {
-        move_rows(c, b, h, src, dst, count, tid >> 4, blockDim.x >> 4, tid & 15);
-    }
+    int before = 0;
+    for (int w = 0; w < wave; ++w) before += tally[w];
+    for (int w = from / 64 + lane; 64 * w < to; w += 64) below[w] += before;
 }
 
-constexpr int TILE_MOVES = 64;
-
-// Workgroup = TILE_MOVES moves of a row, 16 lanes a move.
-__global__ __launch_bounds__(256) void evict_move_kernel(Cache c, Moves mv, int tiles) {
+// The second launch: workgroup = TILE tokens behind a row's budget.
+__global__ __launch_bounds__(256) void evict_move_kernel(Cache c, Evict a, const uint64_t* all_bits, const int* all_below, int words, int tiles) {
+    __shared__ MoveLists lists;
     const int row = blockIdx.x / tiles, tile = blockIdx.x % tiles;
-    const int count = min(mv.count[row] - tile * TILE_MOVES, TILE_MOVES);
-    const size_t at = (size_t)row * mv.cap + (size_t)tile * TILE_MOVES;
-    move_rows(c, row / c.kv, row % c.kv, mv.src + at, mv.dst + at, count, threadIdx.x >> 4, 16, threadIdx.x & 15);
+    const Row r = row_at(c, a, row);
+    const int from = r.left + TILE * tile, to = min(r.n, from + TILE);
+    if (from >= to || r.left == 0) return;
+    make_moves(c, r, Changes{all_bits + (size_t)row * words, all_below + (size_t)row * words}, from, to, lists);
 }
 
-int most_moves(int longest, int budget) { return budget < longest - budget ? budget : longest - budget; }
+struct Bits {
+    uint64_t* bits;
+    int* below;
+    int words;
+};
+template <int J, bool VEC>
+hipError_t select_rows(const Cache& c, const Evict& a, const Bits& x, int rows, int threads, hipStream_t s) {
+    constexpr int HISTOGRAM = BINS * COPIES<J> * sizeof(int);
+    const int lds = a.longest - a.budget > FEW ? HISTOGRAM : 0;   // (else no row of this call has more to go)
+    static bool raised = false;
+    if (lds >= 32 * 1024 && !raised) {   // (with what else the kernel holds, 64 KB are too much by default)
+        const hipError_t e = hipFuncSetAttribute((const void*)evict_select_kernel<J, VEC>, hipFuncAttributeMaxDynamicSharedMemorySize, HISTOGRAM);
+        if (e != hipSuccess) return e;
+        raised = true;
+    }
+    evict_select_kernel<J, VEC><<<rows, threads, lds, s>>>(c, a, x.bits, x.below, x.words);
+    return hipSuccess;
+}
+template <int J>
+hipError_t select_with(const Cache& c, const Evict& a, const Bits& x, int rows, int threads, bool vec, hipStream_t s) {
+    return vec ? select_rows<J, true>(c, a, x, rows, threads, s) : select_rows<J, false>(c, a, x, rows, threads, s);
+}
+
+bool second_launch(int longest, int budget) { return longest - budget > TILE || longest > MAX_IN_REGISTERS; }
+int words_of(int longest) { return (longest + 63) / 64; }
 
 }  // namespace
 
 size_t evict_workspace(int kv, int64_t seqs, int longest, int budget) {
-    const int cap = most_moves(longest, budget);
-    if (cap <= INLINE_MOVES) return 0;
-    return (size_t)seqs * kv * (1 + 2 * (size_t)cap) * sizeof(int);
+    if (longest <= budget || !second_launch(longest, budget)) return 0;
+    return (size_t)seqs * kv * words_of(longest) * (sizeof(uint64_t) + sizeof(int));
 }
 
 hipError_t cache_evict(const Cache& c, const Evict& a, hipStream_t s) {
-    const int rows = c.seqs * c.kv, cap = most_moves(a.longest, a.budget);
-    Moves mv{};
-    if (cap > INLINE_MOVES) {
-        mv.cap = cap;
-        mv.src = (int*)a.ws;
-        mv.dst = mv.src + (size_t)rows * cap;
-        mv.count = mv.dst + (size_t)rows * cap;
+    const int rows = c.seqs * c.kv;
+    Bits x{nullptr, nullptr, words_of(a.longest)};
+    if (evict_workspace(c.kv, c.seqs, a.longest, a.budget) > 0) {
+        x.bits = (uint64_t*)a.ws;
+        x.below = (int*)(x.bits + (size_t)rows * x.words);
     }
-    const int threads = a.longest <= 4096 ? 512 : 1024;
-    const bool in_lds = a.longest <= MAX_KEYS;
-    const size_t lds = (size_t)BINS * COPIES * 4 + (in_lds ? (size_t)a.longest * 4 : 0);
-    static bool raised = false;   // (see qeft.h: the one kind of state)
-    if (in_lds && lds > 48 * 1024 && !raised) {
-        const hipError_t e = hipFuncSetAttribute((const void*)evict_select_kernel<true>, hipFuncAttributeMaxDynamicSharedMemorySize, (MAX_KEYS + BINS * COPIES) * 4);
-        if (e != hipSuccess) return e;
-        raised = true;
-    }
-    if (in_lds) evict_select_kernel<true><<<rows, threads, lds, s>>>(c, a, mv);
-    else evict_select_kernel<false><<<rows, threads, lds, s>>>(c, a, mv);
-    if (mv.count) {
-        const int tiles = (cap + TILE_MOVES - 1) / TILE_MOVES;
-        evict_move_kernel<<<(unsigned)((int64_t)rows * tiles), 256, 0, s>>>(c, mv, tiles);
+    const auto on16 = [](const void* p) { return ((uintptr_t)p & 15u) == 0; };
+    const bool vec = on16(a.score) && on16(a.pos) && on16(a.score_out) && on16(a.pos_out) && a.ld % 4 == 0 && a.ld_out % 4 == 0;
+    // 4 tokens a thread up to 4096, then whole workgroups with 8, 16, 32
+    hipError_t e = hipSuccess;
+    if (a.longest <= 4096) e = select_with<1>(c, a, x, rows, a.longest <= 512 ? 128 : (a.longest + 255) / 256 * 64, vec, s);
+    else if (a.longest <= 8192) e = select_with<2>(c, a, x, rows, 1024, vec, s);
+    else if (a.longest <= 16384) e = select_with<4>(c, a, x, rows, 1024, vec, s);
+    else if (a.longest <= MAX_IN_REGISTERS) e = select_with<8>(c, a, x, rows, 1024, vec, s);
+    else evict_select_long_kernel<<<rows, 1024, 0, s>>>(c, a, x.bits, x.below, x.words);
+    if (e != hipSuccess) return e;
+    if (x.bits) {
+        const int tiles = (a.longest - a.budget + TILE - 1) / TILE;
+        evict_move_kernel<<<(unsigned)((int64_t)rows * tiles), 256, 0, s>>>(c, a, x.bits, x.below, x.words, tiles);
     }
     return hipGetLastError();
 }

@@ -13,6 +13,7 @@
 // workgroup goes to the workspace, summed by a second launch in a fixed order.  The next row's loads are issued before the current one's sums: a
 // CU has one or two workgroups and nothing else to hide them.
 #include "qeft_internal.h"
+#include "wave.h"
 
 namespace qeft {
 namespace {
@@ -120,17 +121,12 @@ __device__ __forceinline__ void round_to(float (&x)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = (float)(_Float16)x[e];
 }
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) x += __shfl_xor(x, s);
-    return x;
-}
 // N sums over the `waves` waves from `first` on of a workgroup (a row's), the same for every thread of them.  buf: the LDS slots of this call; the
 // call before it on the same slots must lie behind a barrier.
 template <int N>
 __device__ __forceinline__ void row_sums(float (&s)[N], float (*buf)[16], int first, int waves) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
+    for (int i = 0; i < N; ++i) s[i] = wave_reduce(s[i], Sum());
     if (waves == 1) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (lane == 0)
@@ -138,11 +134,7 @@ __device__ __forceinline__ void row_sums(float (&s)[N], float (*buf)[16], int fi
         for (int i = 0; i < N; ++i) buf[i][wave] = s[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        float x = 0.f;
-        for (int w = 0; w < waves; ++w) x += buf[i][first + w];
-        s[i] = x;
-    }
+    for (int i = 0; i < N; ++i) s[i] = waves_reduce(buf[i], first, waves, 0.f, Sum());
 }
 
 // ---- forward ----------------------------------------------------------------------------------------------------------

@@ -106,7 +106,7 @@ def test_evict_refuses(over, status):
     if over is None:        # more moves than the first launch makes: the lists need a workspace
         d, pools, table = cache_args(cols=100)
         need = B.qeft_evict_workspace(d, 2, 1000, 500)
-        assert need >= 2 * 4 * 2 * 500 * 4 and B.qeft_evict_workspace(d, 2, 1000, 999) == 0 == B.qeft_evict_workspace(d, 2, 1000, 1000)
+        assert need >= 2 * 4 * 1000 / 8 and B.qeft_evict_workspace(d, 2, 1000, 999) == 0 == B.qeft_evict_workspace(d, 2, 1000, 1000)
         a = evict(longest=1000, budget=500, ld=1000, ld_out=1000, ws=P, ws_bytes=need - 1)
         assert call(B.raw.qeft_cache_evict, d, pools, table, a) == status
         return
