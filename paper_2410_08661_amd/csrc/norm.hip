@@ -312,26 +312,6 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int wave
     u4* held = reinterpret_cast<u4*>(joined + (groups > 1 ? blockDim.x * 8 * V : 0));   // [3][64 waves]
     Half8 wpre[V], wpost[V], gch[V];
     float spre[V][8] = {}, spost[V][8] = {}, sgate[V][8] = {};
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int at = 8 * (tid + T * v), left = a.n - at;
-        wpre[v].clear();
-        wpost[v].clear();
-        gch[v].clear();
-        if (left > 0) {
-            wpre[v].load(a.w_pre, at, left);
-            if (POST) wpost[v].load(a.w_post, at, left);
-            if (GATE == QEFT_GATE_CHANNEL) gch[v].load(a.gate, at, left);
-        }
-    }
-    if (IN_LDS) {
-        if (group == 0) {
-            held[tid] = wpre[0].v;
-            held[T + tid] = wpost[0].v;
-            if (GATE == QEFT_GATE_CHANNEL) held[2 * T + tid] = gch[0].v;
-        }
-        __syncthreads();
-    }
     const int64_t step = (int64_t)gridDim.x * groups;
     // what a row's first sums need, and the rest: the next row's are loaded apart, as registers fall free
     auto load_sums = [&](int64_t row, RowIn<V, F32>& in) {
@@ -364,6 +344,26 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int wave
     RowIn<V, F32> in;
     load_sums(row, in);
     load_rest(row, in);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int at = 8 * (tid + T * v), left = a.n - at;
+        wpre[v].clear();
+        wpost[v].clear();
+        gch[v].clear();
+        if (left > 0) {
+            wpre[v].load(a.w_pre, at, left);
+            if (POST) wpost[v].load(a.w_post, at, left);
+            if (GATE == QEFT_GATE_CHANNEL) gch[v].load(a.gate, at, left);
+        }
+    }
+    if (IN_LDS) {
+        if (group == 0) {
+            held[tid] = wpre[0].v;
+            held[T + tid] = wpost[0].v;
+            if (GATE == QEFT_GATE_CHANNEL) held[2 * T + tid] = gch[0].v;
+        }
+        __syncthreads();
+    }
     for (int round = 0; round < rounds; ++round, row += step) {
         RowIn<V, F32> next;
         if (V == 1 && round + 1 < rounds) load_sums(row + step, next);
@@ -496,7 +496,16 @@ __global__ __launch_bounds__(256) void norm_slabs_kernel(Sums S, float* o0, floa
     const int quad = threadIdx.x & 15, share = threadIdx.x >> 4, col = 64 * blockIdx.x + 4 * quad;
     f4 s = {0.f, 0.f, 0.f, 0.f};
     if (col < n)   // (a slab's pitch is a multiple of 8)
-        for (int i = share; i < S.slabs; i += 16) s += *reinterpret_cast<const f4*>(slab + (size_t)i * S.pitch + col);
+        for (int i0 = share; i0 < S.slabs; i0 += 16 * 8) {
+            f4 x[8];   // eight loads before the first sum
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+                const int i = i0 + 16 * y;
+                x[y] = i < S.slabs ? *reinterpret_cast<const f4*>(slab + (size_t)i * S.pitch + col) : f4{0.f, 0.f, 0.f, 0.f};
+            }
+#pragma unroll
+            for (int y = 0; y < 8; ++y) s += x[y];
+        }
     *reinterpret_cast<f4*>(&red[share][4 * quad]) = s;
     __syncthreads();
     if (threadIdx.x < 64) {
