@@ -311,6 +311,18 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int wave
     constexpr bool IN_LDS = POST && V == 1;
     u4* held = reinterpret_cast<u4*>(joined + (groups > 1 ? blockDim.x * 8 * V : 0));   // [3][64 waves]
     Half8 wpre[V], wpost[V], gch[V];
+    // Two octets a thread leave no registers for two of the three sums: they lie in LDS, where every thread adds to its own columns.
+    constexpr bool SUMS_IN_LDS = V > 1;
+    f4* sums_at = reinterpret_cast<f4*>(joined) + threadIdx.x;   // [w_pre, w_post][octet][half][threads]
+    auto add_to = [&](int which, int v, const float (&x)[8]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f4& s = sums_at[(size_t)((which * V + v) * 2 + h) * blockDim.x];
+            s += f4{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+        }
+    };
+    if (SUMS_IN_LDS)
+        for (int i = 0; i < (POST ? 2 : 1) * V * 2; ++i) sums_at[(size_t)i * blockDim.x] = f4{0.f, 0.f, 0.f, 0.f};
     float spre[V][8] = {}, spost[V][8] = {}, sgate[V][8] = {};
     const int64_t step = (int64_t)gridDim.x * groups;
     // what a row's first sums need, and the rest: the next row's are loaded apart, as registers fall free
@@ -408,17 +420,21 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int wave
         pin();
         float t[V][8], q[1] = {0.f};
 #pragma unroll
-        for (int v = 0; v < V; ++v)
+        for (int v = 0; v < V; ++v) {
+            float pre[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float hh = in.h[v][e] * rs, dx = in.dx[v][e];
                 t[v][e] = fmaf(rs, fmaf(-hh, c, dx * wpre[v][e]), in.dh[v][e]);
-                spre[v][e] = fmaf(dx, hh, spre[v][e]);
+                if (SUMS_IN_LDS) pre[e] = dx * hh;
+                else spre[v][e] = fmaf(dx, hh, spre[v][e]);
                 if (POST) {
                     const float g = GATE == QEFT_GATE_CHANNEL ? gch[v][e] : GATE == QEFT_GATE_TOKEN ? in.g[v][e] : 1.f;
                     q[0] = fmaf(a.scale * g * t[v][e] * wpost[v][e], in.y[v][e], q[0]);
                 }
             }
+            if (SUMS_IN_LDS) add_to(0, v, pre);
+        }
         if (V == 1 && round + 1 < rounds) load_rest(row + step, next);
         if (POST) row_sums(q, buf[2 * (round & 1) + 1], first, waves);
         pin();
@@ -428,17 +444,19 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int wave
             for (int v = 0; v < V; ++v) {
                 const int at = 8 * (tid + T * v), left = a.n - at;
                 if (left <= 0) continue;
-                float dy[8], dg[8];
+                float dy[8], dg[8], post[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float g = GATE == QEFT_GATE_CHANNEL ? gch[v][e] : GATE == QEFT_GATE_TOKEN ? in.g[v][e] : 1.f;
                     const float st = a.scale * t[v][e], du = st * g, yh = in.y[v][e] * rsy;
                     dy[e] = POST ? rsy * fmaf(-yh, cy, du * wpost[v][e]) : du;
-                    if (POST) spost[v][e] = fmaf(du, yh, spost[v][e]);
+                    if (POST && SUMS_IN_LDS) post[e] = du * yh;
+                    else if (POST) spost[v][e] = fmaf(du, yh, spost[v][e]);
                     const float u = POST ? yh * wpost[v][e] : yh;
                     if (GATE == QEFT_GATE_CHANNEL) sgate[v][e] = fmaf(st, u, sgate[v][e]);
                     if (GATE == QEFT_GATE_TOKEN) dg[e] = st * u;
                     }
+                if (POST && SUMS_IN_LDS) add_to(1, v, post);
                 if (a.dr) store<F32>(row_of(a.dr, row, a.lddr, F32), at, left, t[v]);
                 if (a.dy) store<false>(row_of((void*)a.dy, row, a.lddy, false), at, left, dy);
                 if (GATE == QEFT_GATE_TOKEN && a.dgate) store<false>(row_of(a.dgate, row, a.lddg, false), at, left, dg);
@@ -463,6 +481,13 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int wave
             for (int v = 0; v < V; ++v) {
                 const int at = 8 * (tid + T * v), left = a.n - at;
                 float(&x)[8] = w == 0 ? spre[v] : w == 1 ? spost[v] : sgate[v];
+                if (SUMS_IN_LDS && w < 2) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const f4 s = sums_at[(size_t)((w * V + v) * 2 + h) * blockDim.x];
+                        x[4 * h] = s.x, x[4 * h + 1] = s.y, x[4 * h + 2] = s.z, x[4 * h + 3] = s.w;
+                    }
+                }
                 if (add)
                     for (int e = 0; e < 8; ++e) x[e] = e < left ? out[at + e] + x[e] : 0.f;
                 if (left > 0) store<true>(out, at, left, x);
@@ -639,13 +664,22 @@ BwdPlan bwd_plan(int n, int64_t m) {
     return p;
 }
 
+template <int V, bool F32, bool POST, int GATE>
+void launch_gate(const Norm& a, const Sums& S, const BwdPlan& p, int threads, size_t lds, hipStream_t s) {
+    static bool raised = false;
+    if (lds > 60 * 1024 && !raised) {   // (an error shows at the launch)
+        raised = hipFuncSetAttribute((const void*)norm_bwd_kernel<V, F32, POST, GATE>, hipFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024) == hipSuccess;
+    }
+    norm_bwd_kernel<V, F32, POST, GATE><<<p.grid, threads, lds, s>>>(a, S, p.waves, p.groups, p.rounds);
+}
 template <int V, bool F32, bool POST>
 void launch_bwd(const Norm& a, const Sums& S, const BwdPlan& p, hipStream_t s) {
     const int threads = 64 * p.waves * p.groups;
-    const size_t lds = (p.groups > 1 ? (size_t)threads * 8 * V * sizeof(float) : 0) + (POST && V == 1 ? 3 * 64 * (size_t)p.waves * sizeof(u4) : 0);
-    if (a.gate_kind == QEFT_GATE_CHANNEL) norm_bwd_kernel<V, F32, POST, QEFT_GATE_CHANNEL><<<p.grid, threads, lds, s>>>(a, S, p.waves, p.groups, p.rounds);
-    else if (a.gate_kind == QEFT_GATE_TOKEN) norm_bwd_kernel<V, F32, POST, QEFT_GATE_TOKEN><<<p.grid, threads, lds, s>>>(a, S, p.waves, p.groups, p.rounds);
-    else norm_bwd_kernel<V, F32, POST, QEFT_GATE_NONE><<<p.grid, threads, lds, s>>>(a, S, p.waves, p.groups, p.rounds);
+    const size_t lds = V > 1 ? (size_t)threads * (POST ? 2 : 1) * 8 * V * sizeof(float)
+                             : (p.groups > 1 ? (size_t)threads * 8 * sizeof(float) : 0) + (POST ? 3 * 64 * (size_t)p.waves * sizeof(u4) : 0);
+    if (a.gate_kind == QEFT_GATE_CHANNEL) launch_gate<V, F32, POST, QEFT_GATE_CHANNEL>(a, S, p, threads, lds, s);
+    else if (a.gate_kind == QEFT_GATE_TOKEN) launch_gate<V, F32, POST, QEFT_GATE_TOKEN>(a, S, p, threads, lds, s);
+    else launch_gate<V, F32, POST, QEFT_GATE_NONE>(a, S, p, threads, lds, s);
 }
 template <int V>
 void launch_bwd_of(const Norm& a, const Sums& S, const BwdPlan& p, hipStream_t s) {
