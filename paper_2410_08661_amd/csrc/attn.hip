@@ -19,6 +19,7 @@
 // Work: a workgroup of 8 waves takes a chunk of one sequence's tokens for one kv head (16 query heads at a time; more heads read the chunk again, from L2),
 // joins its waves through LDS and writes out, or, where the sequence is cut in several chunks, m, l and O to the workspace for a second launch.
 #include "qeft_internal.h"
+#include "wave.h"
 
 namespace qeft {
 namespace {
@@ -60,7 +61,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
     constexpr int KS = DP / 32, NV = DP / 16, ROUND = WAVES * STEP;   // (tokens of a round of the waves)
     typedef typename VReg<DP>::type vreg;
     constexpr int VN = VReg<DP>::n, VW = sizeof(vreg) / 4;
-    __shared__ float sm[WAVES][16], sl[WAVES][16], sf[WAVES][16], sL[16], sB[16];
+    __shared__ float sm[WAVES][16], sl[WAVES][16], sL[16], sB[16];
     __shared__ __align__(16) float so[WAVES][4][DP];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -73,9 +74,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
     id /= tiles;
     const int chunk = id % ps.chunks, b = id / ps.chunks;
     const int head0 = kvh * g + 16 * tile, nh = min(16, g - 16 * tile);   // this workgroup's query heads
-    const int n = min(a.lens[b], a.longest);
-    const int begin = chunk * ps.chunk, end = min(n, begin + ps.chunk);
-    if (end <= begin && chunk > 0) return;   // (an empty sequence's first chunk writes the zeros)
+    const int begin = chunk * ps.chunk;
 
     // head slot of a column or row r of the products: r = 4 (h % 4) + h / 4, so that up to 4 heads lie in one register of O
     const int my_head = (col >> 2) + 4 * (col & 3);
@@ -116,6 +115,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
         const int64_t lo = x & 1 ? o.at[1] : o.at[0], hi = x & 1 ? o.at[3] : o.at[2];
         return x & 2 ? hi : lo;
     };
+    // the first lookups are asked for with the length, not after it
+    int t0 = begin + STEP * wave;
+    Octets next{};
+    if (OCT && a.longest > 0) next = octets(t0);
+    const int n = min(a.lens[b], a.longest), end = min(n, begin + ps.chunk);
+    if (end <= begin && chunk > 0) return;   // (an empty sequence's first chunk writes the zeros)
     u4 K[2][KS];
     vreg V[8][VN];
     const int64_t krow = (int64_t)(col & 3) * c.token_stride + 8 * grp;
@@ -162,10 +167,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
 #pragma unroll
     for (int j = 0; j < NV; ++j) acc[j] = f4{0.f, 0.f, 0.f, 0.f};
 
-    int t0 = begin + STEP * wave;
-    Octets next;
     if (t0 < end) {
-        next = octets(t0);
         load_k(t0, next);
         load_v(t0, next);
         if (t0 + ROUND < end) next = octets(t0 + ROUND);   // (looked up a step ahead of the loads)
@@ -201,18 +203,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
 #pragma unroll
         for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
         if (__ballot(mx > m + SLACK)) {   // (m = -inf at first: taken for any score above it)
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            mx = fmaxf(mx, m);
-            const float f = m == NEG_INF ? 0.f : exp2_fast(m - mx);   // (nothing but zeros to scale before the first score)
-            m = mx;
-            l = l == 0.f ? 0.f : l * f;
+            const auto larger = [](float x, float y) { return fmaxf(x, y); };
+            mx = fmaxf(m, across<true>(across<false>(mx, larger), larger));   // over the lanes of this column
+            if (__ballot(m != NEG_INF)) {   // (nothing but zeros to scale before the first score)
+                const float f = m == NEG_INF ? 0.f : exp2_fast(m - mx);
+                l = l == 0.f ? 0.f : l * f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float fr = __shfl(f, 4 * grp + i);
+                for (int i = 0; i < 4; ++i) {
+                    const float fr = __shfl(f, 4 * grp + i);
 #pragma unroll
-                for (int j = 0; j < NV; ++j) acc[j][i] *= fr;
+                    for (int j = 0; j < NV; ++j) acc[j][i] *= fr;
+                }
             }
+            m = mx;
         }
         const float base = base_of(m);
         h8 hi, lo;
@@ -241,49 +244,50 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
         }
     }
 
-    // ---- join the waves ----
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    // ---- join the waves: maxima, sums and outputs as they are, four heads at a time; every thread that sums an output makes the factors itself ----
+    l = across<true>(across<false>(l, Sum()), Sum());
     if (lane < 16) {
         sm[wave][lane] = m;
         sl[wave][lane] = l;
     }
-    __syncthreads();
-    if (threadIdx.x < 16) {
-        float M = NEG_INF, L = 0.f;
-        for (int w = 0; w < WAVES; ++w) M = fmaxf(M, sm[w][threadIdx.x]);
-        for (int w = 0; w < WAVES; ++w) {
-            const float f = sm[w][threadIdx.x] == NEG_INF ? 0.f : exp2_fast(sm[w][threadIdx.x] - M);
-            sf[w][threadIdx.x] = f;
-            L += sl[w][threadIdx.x] * (sl[w][threadIdx.x] == 0.f ? 0.f : f);
-        }
-        sL[threadIdx.x] = L;
-        sB[threadIdx.x] = base_of(M);
-    }
-    __syncthreads();
     const bool direct = ps.chunks == 1 && ps.base == nullptr;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (4 * i >= nh) break;   // heads 4 i .. 4 i + 3
-        const float f = sf[wave][4 * grp + i];
 #pragma unroll
         for (int j = 0; j < NV; j += 4)
-            *reinterpret_cast<f4*>(&so[wave][grp][NV * col + j]) = f4{acc[j][i] * f, acc[j + 1][i] * f, acc[j + 2][i] * f, acc[j + 3][i] * f};
+            *reinterpret_cast<f4*>(&so[wave][grp][NV * col + j]) = f4{acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]};
         __syncthreads();
         for (int e = threadIdx.x; e < 4 * DP; e += 64 * WAVES) {
-            const int hl = e / DP, dim = e % DP, h = hl + 4 * i;
+            const int hl = e / DP, dim = e % DP, h = hl + 4 * i, r = 4 * hl + i;
             if (h < nh && (FULL || dim < c.d)) {
-                float o = 0.f;
+                float wm[WAVES], wl[WAVES], wo[WAVES], M = NEG_INF, L = 0.f, o = 0.f;
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) o += so[w][hl][dim];
+                for (int w = 0; w < WAVES; ++w) {
+                    wm[w] = sm[w][r];
+                    wl[w] = sl[w][r];
+                    wo[w] = so[w][hl][dim];
+                    M = fmaxf(M, wm[w]);
+                }
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    const float f = wm[w] == NEG_INF ? 0.f : exp2_fast(wm[w] - M);
+                    L += wl[w] == 0.f ? 0.f : wl[w] * f;
+                    o = fmaf(wo[w], f, o);
+                }
+                const float base = base_of(M);
                 if (direct) {
-                    a.out[(size_t)b * a.ldo + (size_t)(head0 + h) * c.d + dim] = __float2half_rn(n > 0 ? o / sL[4 * hl + i] : 0.f);
+                    a.out[(size_t)b * a.ldo + (size_t)(head0 + h) * c.d + dim] = __float2half_rn(n > 0 ? o / L : 0.f);
+                    if (dim == 0) {
+                        sB[r] = base;
+                        sL[r] = L;
+                    }
                 } else {
                     const size_t at = ((size_t)b * a.heads + head0 + h) * ps.chunks + chunk;
                     ps.o[at * c.d + dim] = o;
                     if (dim == 0) {
-                        ps.base[at] = sB[4 * hl + i];
-                        ps.l[at] = sL[4 * hl + i];
+                        ps.base[at] = base;
+                        ps.l[at] = L;
                     }
                 }
             }
