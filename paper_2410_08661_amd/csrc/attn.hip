@@ -433,8 +433,7 @@ constexpr int CUS = 256;
 // Chunks of a row (a sequence's kv head, and 16 of its query heads) of `rounds` 128-token rounds of 64 KiB at head_dim 128.  A CU reads 20 bytes a ns
 // at most, so what counts is that all have the same number of workgroups: one or two each, or, between 128 and 512 rows, what the estimate finds
 // (us: 160 rows of 2049 tokens in 1 / 2 / 3 chunks: 46.4 / 46.3 / 39.4; 256 of 2048: 48.2 / 52.6; 8 of 131001 in 32 / 64 / 128 / 256: 95.6 / 97.3 / 102.6 / 109.9).
-// The second launch is 4 us, and more where many heads have many chunks; one chunk a row leaves the longest of a ragged batch to the end (256 rows of 900 to 3001 tokens:
-// 58.1 us against 56.0), hence its tenth.
+// The second launch is 4 us, and more where many heads have many chunks.
 int chunks_of(int64_t rows, int64_t rounds, int d) {
     if (rounds <= 1 || rows >= 2 * CUS) return 1;
     if (rows <= CUS / 2) return (int)(2 * CUS / rows < rounds ? 2 * CUS / rows : rounds);
@@ -442,7 +441,7 @@ int chunks_of(int64_t rows, int64_t rounds, int d) {
     float least = 0.f;
     for (int c = 1; c <= 8 && c <= rounds; ++c) {
         const float per_cu = (float)((rows * c + CUS - 1) / CUS), us = 3.2f * d / 128.f;   // (a round's time on a CU)
-        const float t = per_cu * ((float)((rounds + c - 1) / c) * us + 0.5f) * (c == 1 ? 1.1f : 1.f) + (c > 1 ? 4.f : 0.f);
+        const float t = per_cu * ((float)((rounds + c - 1) / c) * us + 0.5f) + (c > 1 ? 4.f : 0.f);
         if (c == 1 || t < least) best = c, least = t;
     }
     return best;
