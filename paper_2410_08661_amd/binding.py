@@ -479,8 +479,8 @@ def _fail(status: int, where: str, what: str):
     raise e
 
 
-def _take(where, name, t, dtype, shape, optional=False):
-    """Pointer and row pitch of tensor t of this type and shape (entries None: any), whose rows are contiguous and whose leading axes, if there are
+def _take(where, name, t, dtype, shape, optional=False, least=0):
+    """Pointer and row pitch of tensor t of this type and shape (entries None: any; rows of `least` values or more), whose rows are contiguous and whose leading axes, if there are
     three, lie one behind the other."""
     if t is None:
         if not optional:
@@ -490,6 +490,8 @@ def _take(where, name, t, dtype, shape, optional=False):
         _fail(QEFT_ERR_UNSUPPORTED, where, f"{name} is {t.dtype} of {t.dim()} axes, not {dtype} of {len(shape)}")
     if any(want is not None and have != want for have, want in zip(t.shape, shape)):
         _fail(QEFT_ERR_SHAPE, where, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.shape[0] > 0 and t.shape[-1] < least:   # (a view's pitch can be wider than its rows are)
+        _fail(QEFT_ERR_SHAPE, where, f"{name}'s rows hold {t.shape[-1]} tokens, not {least}")
     if not t.is_cuda or t.device.index != torch.cuda.current_device():
         _fail(QEFT_ERR_UNSUPPORTED, where, f"{name} is not on the current GPU")
     if t.numel() == 0:   # (an empty tensor's pitch says nothing)
@@ -609,7 +611,7 @@ def qeft_attn_decode(cache: Cache, table: torch.Tensor, lens: torch.Tensor, long
             _fail(QEFT_ERR_SHAPE, at, "q's rows are not whole heads")
         po, ldo = _take(at, "out", out, torch.float16, (n, q.shape[1]))
         pl, _ = _take(at, "lens", lens, torch.int32, (n,))
-        ps, lds = _take(at, "score", score, torch.float32, (n, d.kv_heads, None), True)
+        ps, lds = _take(at, "score", score, torch.float32, (n, d.kv_heads, None), True, min(longest, table.shape[1] * d.page_size))
         pw, nw = _c_workspace(at, ws)
         a = qeft_attn_t(pl, int(longest), pq, po, ldq, ldo, heads, float(scale), ps, score.shape[2] if ps and lds < score.shape[2] else lds,
                         int(bool(accumulate)), pw, nw)
@@ -640,8 +642,12 @@ def qeft_cache_evict(cache: Cache, table: torch.Tensor, lens: torch.Tensor, long
         pools, tab = cache.c_struct(), _c_table(at, table)
         n = table.shape[0]
         pl, pn, po = (_take(at, name, t, torch.int32, (n,))[0] for name, t in (("lens", lens), ("seen", seen), ("lens_out", lens_out)))
-        (ps, lds), (pso, ldso) = (_take(at, name, t, torch.float32, (n, d.kv_heads, None)) for name, t in (("score", score), ("score_out", score_out)))
-        (pp, ldp), (ppo, ldpo) = (_take(at, name, t, torch.int32, (n, d.kv_heads, None)) for name, t in (("pos", pos), ("pos_out", pos_out)))
+        most = min(longest, table.shape[1] * d.page_size)
+        kept = min(budget, most)
+        (ps, lds), (pso, ldso) = (_take(at, name, t, torch.float32, (n, d.kv_heads, None), False, least)
+                                  for name, t, least in (("score", score, most), ("score_out", score_out, kept)))
+        (pp, ldp), (ppo, ldpo) = (_take(at, name, t, torch.int32, (n, d.kv_heads, None), False, least)
+                                  for name, t, least in (("pos", pos, most), ("pos_out", pos_out, kept)))
         if score.shape != pos.shape or lds != ldp or score_out.shape != pos_out.shape or ldso != ldpo:
             _fail(QEFT_ERR_SHAPE, at, "score and pos differ in shape or pitch")
         one = n * d.kv_heads == 1   # (one row: its width is all there is)

@@ -11,6 +11,7 @@
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
+#include <algorithm>
 #include <cstring>
 
 #include "qeft.h"
@@ -138,14 +139,14 @@ struct Call {
         if (!t || t->scalar_type() != type || t->dim() != 1 || t->size(0) != n || n == 0 || (n > 1 && t->stride(0) != 1)) return no();
         return t->data_ptr();
     }
-    // [seqs][heads][any], rows one pitch apart throughout
-    void* planes(PyObject* o, at::ScalarType type, int64_t seqs, int64_t heads, int64_t& pitch, bool optional = false) {
+    // [seqs][heads][least or more], rows one pitch apart throughout (a single row's pitch: its width)
+    void* planes(PyObject* o, at::ScalarType type, int64_t seqs, int64_t heads, int64_t least, int64_t& pitch, bool optional = false) {
         pitch = 0;
         if (o == Py_None && optional) return nullptr;
         const at::Tensor* t = tensor(o);
-        if (!t || t->scalar_type() != type || t->dim() != 3 || t->numel() == 0 || t->size(0) != seqs || t->size(1) != heads || seqs * heads < 2) return no();
+        if (!t || t->scalar_type() != type || t->dim() != 3 || t->numel() == 0 || t->size(0) != seqs || t->size(1) != heads || t->size(2) < least) return no();
         if (t->size(2) > 1 && t->stride(2) != 1) return no();
-        pitch = heads > 1 ? t->stride(1) : t->stride(0);
+        pitch = heads > 1 ? t->stride(1) : seqs > 1 ? t->stride(0) : t->size(2);
         if (seqs > 1 && t->stride(0) != pitch * heads) return no();
         return t->data_ptr();
     }
@@ -364,6 +365,8 @@ bool cache_args(Call& c, PyObject* const* a, const qeft_cache_desc_t*& d, qeft_c
     table.seqs = (int32_t)seqs;
     return true;
 }
+// tokens that a row of the table can hold
+int64_t slots(const qeft_cache_desc_t* d, const qeft_table_t& table) { return (int64_t)table.table_pages * d->page_size; }
 // (desc, K, V, table, k, v, index, seq, q, q_out, rot, pos)
 PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&](Call& c, int& st) {
@@ -405,7 +408,7 @@ PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
         p.longest = c.whole(a[5]);
         p.q = c.rows(a[6], at::kHalf, seqs, width, p.ldq);
         p.out = c.rows(a[7], at::kHalf, seqs, width, p.ldo);
-        p.score = (float*)c.planes(a[8], at::kFloat, seqs, d->kv_heads, p.ld_score, true);
+        p.score = (float*)c.planes(a[8], at::kFloat, seqs, d->kv_heads, std::min(p.longest, slots(d, table)), p.ld_score, true);
         p.accumulate = PyObject_IsTrue(a[9]) == 1;
         p.scale = (float)c.real(a[10]);
         p.ws = c.bytes(a[11], p.ws_bytes);
@@ -429,12 +432,13 @@ PyObject* cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
         p.lens = (const int32_t*)c.vec(a[4], at::kInt, seqs);
         p.longest = c.whole(a[5]);
         p.budget = c.whole(a[6]);
-        p.score = (const float*)c.planes(a[7], at::kFloat, seqs, d->kv_heads, p.ld);
-        p.pos = (const int32_t*)c.planes(a[8], at::kInt, seqs, d->kv_heads, ld_pos);
+        const int64_t longest = std::min(p.longest, slots(d, table));
+        p.score = (const float*)c.planes(a[7], at::kFloat, seqs, d->kv_heads, longest, p.ld);
+        p.pos = (const int32_t*)c.planes(a[8], at::kInt, seqs, d->kv_heads, longest, ld_pos);
         p.seen = (const int32_t*)c.vec(a[9], at::kInt, seqs);
         const int64_t first = c.whole(a[10]), last = c.whole(a[11]);
-        p.score_out = (float*)c.planes(a[12], at::kFloat, seqs, d->kv_heads, p.ld_out);
-        p.pos_out = (int32_t*)c.planes(a[13], at::kInt, seqs, d->kv_heads, ld_pos_out);
+        p.score_out = (float*)c.planes(a[12], at::kFloat, seqs, d->kv_heads, std::min(p.budget, longest), p.ld_out);
+        p.pos_out = (int32_t*)c.planes(a[13], at::kInt, seqs, d->kv_heads, std::min(p.budget, longest), ld_pos_out);
         p.lens_out = (int32_t*)c.vec(a[14], at::kInt, seqs);
         p.ws = c.bytes(a[15], p.ws_bytes);
         void* s = c.stream();

@@ -183,3 +183,10 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     with pytest.raises(B.QeftError) as e:
         B.qeft_norm_bwd(n, r, r, None, ws=torch.zeros(4096, dtype=torch.uint8))
     assert e.value.status in (B.QEFT_ERR_NULL, B.QEFT_ERR_UNSUPPORTED)
+
+
+def test_rows_of_weights_hold_the_tokens_whatever_their_pitch():
+    for t in (torch.zeros((1, 1, 5)), torch.zeros((2, 2, 16))[:, :, :5], torch.zeros((2, 2, 0))):   # (a single row's pitch counts in eights; a view's is its base's)
+        with pytest.raises(B.QeftError) as e:
+            B._take("f", "score", t, torch.float32, (t.shape[0], t.shape[1], None), True, 6)
+        assert e.value.status == B.QEFT_ERR_SHAPE

@@ -176,3 +176,30 @@ def test_replayed_from_a_graph_on_another_stream():
         want = B.qeft_attn_decode(cache, table, dev_lens, 1000, q, score=s2)
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(score, s2)
+
+
+@pytest.mark.parametrize("kv,seqs", [(1, 1), (2, 1), (2, 2)])
+def test_rows_of_weights_narrower_than_the_tokens_are_refused(kv, seqs):
+    d, page, n = 64, 8, 32
+    gen = torch.Generator(device="cuda").manual_seed(kv + 10 * seqs)
+    K, V = (U.pool_of(4 * seqs, kv, page, d, gen) for _ in range(2))
+    cache = B.Cache(B.make_cache_desc(4 * seqs, page, kv, d), k=K, v=V)
+    table = torch.arange(4 * seqs, dtype=torch.int32, device="cuda").view(seqs, 4)
+    lens = torch.full((seqs,), n, dtype=torch.int32, device="cuda")
+    q = torch.randn((seqs, kv * d), generator=gen, device="cuda").half()
+    base = torch.full((seqs, kv, 64), 7.0, device="cuda")
+    pos = torch.arange(64, dtype=torch.int32, device="cuda").expand(seqs, kv, 64).contiguous()
+    for width in (29, 31):
+        with pytest.raises(B.QeftError) as e:
+            B.qeft_attn_decode(cache, table, lens, n, q, score=base[:, :, :width])
+        assert e.value.status == B.QEFT_ERR_SHAPE
+        with pytest.raises(B.QeftError) as e:
+            B.qeft_cache_evict(cache, table, lens, n, 16, base[:, :, :width], pos[:, :, :width], lens)
+        assert e.value.status == B.QEFT_ERR_SHAPE
+        with pytest.raises(B.QeftError) as e:
+            B.qeft_cache_evict(cache, table, lens, n, 30, base, pos, lens, score_out=base.clone()[:, :, :29], pos_out=pos.clone()[:, :, :29])
+        assert e.value.status == B.QEFT_ERR_SHAPE
+    assert (base == 7.0).all()
+    B.qeft_attn_decode(cache, table, lens, n, q, score=base[:, :, :n])
+    torch.testing.assert_close(base[:, :, :n].sum(2), torch.ones((seqs, kv), device="cuda"), rtol=0, atol=n * 2.0 ** -20)
+    assert (base[:, :, n:] == 7.0).all()
