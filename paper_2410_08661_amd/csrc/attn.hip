@@ -333,15 +333,15 @@ __device__ __forceinline__ void join_stats(const Partials& ps, size_t at, int us
     if (lane >= used || l == 0.f) base = NEG_INF, l = 0.f;
     B = base;
     for (int i = lane + 64; i < used; i += 64) B = fmaxf(B, ps.l[at + i] == 0.f ? NEG_INF : ps.base[at + i]);
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) B = fmaxf(B, __shfl_xor(B, x));
+    B = wave_reduce(B, [](float x, float y) { return fmaxf(x, y); });
     L = l == 0.f ? 0.f : l * exp2_fast(base - B);
     for (int i = lane + 64; i < used; i += 64) L += ps.l[at + i] == 0.f ? 0.f : ps.l[at + i] * exp2_fast(ps.base[at + i] - B);
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) L += __shfl_xor(L, x);
+    L = wave_reduce(L, Sum());
 }
 
-constexpr int JOIN_TOKENS = 1024;   // tokens whose weights one workgroup of the second launch makes
+constexpr int JOIN_TOKENS = 512;   // tokens whose weights one workgroup of the second launch makes (4 x 4096 tokens, 64 heads on 8: 19.4 us with 1024, 18.7 with 256;
+                                   // 16 x 4000, 32 on 8: 57.7 and 59.8, this 58.4)
+constexpr int JOIN_HEADS = 8;      // heads whose scores and statistics are under way at a time (8 x 4000, 32 on 1: 23.8 us with 4, 20.5 with 16, this 20.8)
 
 // The second launch.  Its first workgroups join the chunks of one query head, 32 dimensions each: 32 lanes of chunks x 8 of four dimensions.  The others
 // make the weights of one kv head's tokens, JOIN_TOKENS at a time (weight_shares of them divide a kv head's), from the scores in the workspace.  Chunks are taken in order: the sums do not depend on who ran first.
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Cache c, Attention a, Pa
     const int64_t outs = (int64_t)c.seqs * a.heads * slices;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     __shared__ __align__(16) float red[32][36];   // (rows four banks apart)
-    __shared__ float part[8];
+    __shared__ float part[2 * JOIN_HEADS];
     if ((int64_t)blockIdx.x < outs) {
         const int slice = (int)(blockIdx.x % slices), bh = (int)(blockIdx.x / slices), b = bh / a.heads, h = bh % a.heads;
         const size_t at = ((size_t)b * a.heads + h) * ps.chunks;
@@ -404,31 +404,34 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Cache c, Attention a, Pa
     for (int begin = first * JOIN_TOKENS; begin < n; begin += weight_shares * JOIN_TOKENS) {
         const int end = min(n, begin + JOIN_TOKENS);
         float w[JOIN_TOKENS / 256] = {};
-        for (int h0 = 0; h0 < g; h0 += 4) {   // a wave for the statistics of each of four heads
-            const int h = h0 + wave;
-            float raw[4][JOIN_TOKENS / 256];   // (asked for with the statistics)
+        for (int h0 = 0; h0 < g; h0 += JOIN_HEADS) {   // a wave for the statistics of each fourth head
+            float raw[JOIN_HEADS][JOIN_TOKENS / 256];   // (asked for with the statistics)
 #pragma unroll
-            for (int y = 0; y < 4; ++y)
+            for (int y = 0; y < JOIN_HEADS; ++y)
 #pragma unroll
                 for (int x = 0; x < JOIN_TOKENS / 256; ++x) {
                     const int t = begin + 256 * x + tid;
                     raw[y][x] = h0 + y < g && t < end ? ps.raw[((size_t)b * a.heads + (size_t)kvh * g + h0 + y) * ps.pitch + t] : 0.f;
                 }
-            if (h < g) {
-                float B, L;
-                join_stats(ps, ((size_t)b * a.heads + (size_t)kvh * g + h) * ps.chunks, used, B, L);
-                if (lane == 0) {
-                    part[wave] = B;
-                    part[4 + wave] = L;
+#pragma unroll
+            for (int y = 0; y < JOIN_HEADS; y += 4) {
+                const int h = h0 + y + wave;
+                if (h < g) {
+                    float B, L;
+                    join_stats(ps, ((size_t)b * a.heads + (size_t)kvh * g + h) * ps.chunks, used, B, L);
+                    if (lane == 0) {
+                        part[y + wave] = B;
+                        part[JOIN_HEADS + y + wave] = 1.f / L;
+                    }
                 }
             }
             __syncthreads();
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
+            for (int y = 0; y < JOIN_HEADS; ++y) {
                 if (h0 + y >= g) break;
-                const float B = part[y], L = part[4 + y];
+                const float B = part[y], by = part[JOIN_HEADS + y];
 #pragma unroll
-                for (int x = 0; x < JOIN_TOKENS / 256; ++x) w[x] += exp2_fast(raw[y][x] - B) / L;
+                for (int x = 0; x < JOIN_TOKENS / 256; ++x) w[x] += exp2_fast(raw[y][x] - B) * by;
             }
             __syncthreads();
         }
@@ -444,12 +447,16 @@ constexpr int SHORT = 512;   // tokens that one workgroup takes rather than two 
 constexpr int CUS = 256;
 
 // Chunks of a row (a sequence's kv head, and 16 of its query heads) of `rounds` 128-token rounds of 64 KiB at head_dim 128.  A CU reads 20 bytes a ns
-// at most, so what counts is that all have the same number of workgroups: one or two each, or, between 128 and 512 rows, what the estimate finds
+// at most, so what counts is that all have the same number of workgroups: one each for up to 16 rows (1 of 130000 tokens, 8 heads on 1: 21.1 us against 29.3 with two; 8 of 60000:
+// 48.8 against 49.7), two for up to 128 (32 of 2048, with weights: 11.2 against 12.0; 128 of 2800: 35.8 against 38.0), or, between 128 and 512 rows, what the estimate finds
 // (us: 160 rows of 2049 tokens in 1 / 2 / 3 chunks: 46.4 / 46.3 / 39.4; 256 of 2048: 48.2 / 52.6; 8 of 131001 in 32 / 64 / 128 / 256: 95.6 / 97.3 / 102.6 / 109.9).
 // The second launch is 4 us, and more where many heads have many chunks.
 int chunks_of(int64_t rows, int64_t rounds, int d) {
     if (rounds <= 1 || rows >= 2 * CUS) return 1;
-    if (rows <= CUS / 2) return (int)(2 * CUS / rows < rounds ? 2 * CUS / rows : rounds);
+    if (rows <= CUS / 2) {
+        const int64_t most = (rows <= 16 ? CUS : 2 * CUS) / rows;
+        return (int)(most < rounds ? most : rounds);
+    }
     int best = 1;
     float least = 0.f;
     for (int c = 1; c <= 8 && c <= rounds; ++c) {
