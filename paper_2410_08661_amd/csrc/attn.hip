@@ -443,7 +443,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Cache c, Attention a, Pa
     }
 }
 
-constexpr int SHORT = 512;   // tokens that one workgroup takes rather than two launches: 32 heads of one sequence, 256 / 400 / 800 tokens: 6.2 / 8.5 / 12.3 us against 8.4 / 8.5 / 9.0
+// Tokens that one workgroup takes rather than two launches, 512 at head_dim 128: 32 heads of one sequence, 256 / 400 / 800 tokens: 6.2 / 8.5 / 12.3 us against 8.4 / 8.5 / 9.0; at 64,
+// 4 sequences of 600 / 740 / 880: 7.5 / 8.2 / 8.9 against 10.0 / 10.3 / 10.3 (one sequence: 6.7 / 7.5 / 8.1 against 6.8); at 256, 285 / 400 / 500 of one: 10.1 / 13.2 / 15.3 against 9.9 / 10.2 / 10.5.
+int short_row(int d) { return 128 + 49152 / d; }
 constexpr int CUS = 256;
 
 // Chunks of a row (a sequence's kv head, and 16 of its query heads) of `rounds` 128-token rounds of 64 KiB at head_dim 128.  A CU reads 20 bytes a ns
@@ -479,10 +481,11 @@ Plan plan_of(int kv, int d, int64_t seqs, int heads, int longest, bool weights) 
     const int g = heads / kv;
     p.tiles = (g + 15) / 16;
     const int64_t rows = seqs * kv * p.tiles;
-    // Eight waves for what is one chunk of few rows (256 rows of 1000 to 2048 tokens, 4 heads each: 41.2 us against 43.1), four else: a round of 128 tokens wastes
+    // One wave for what is a step of it, or two steps of rows that fill the GPU several times (2048 rows of 1 / 32 / 64 tokens: 6.6 / 8.5 / 13.2 us against 11.0 / 11.7 / 14.9
+    // with four waves; 512 rows of 64 tokens, 4 heads each: 7.8 against 6.5).  Eight waves for what is one chunk of few rows (256 rows of 1000 to 2048 tokens, 4 heads each: 41.2 us against 43.1), four else: a round of 128 tokens wastes
     // less at a row's end (2048 rows of 100 to 300 tokens: 44.9 us against 52.9).
-    int chunks = longest <= SHORT ? 1 : chunks_of(rows, ((int64_t)longest + 4 * STEP - 1) / (4 * STEP), d);
-    p.waves = chunks == 1 && rows < 2 * CUS ? 8 : 4;
+    int chunks = longest <= short_row(d) ? 1 : chunks_of(rows, ((int64_t)longest + 4 * STEP - 1) / (4 * STEP), d);
+    p.waves = longest <= STEP || (longest <= 2 * STEP && rows >= 4 * CUS) ? 1 : chunks == 1 && rows < 2 * CUS ? 8 : 4;
     const int round = p.waves * STEP;
     const int64_t rounds = ((int64_t)longest + round - 1) / round, per = rounds > 0 ? (rounds + chunks - 1) / chunks : 1;
     p.chunk = (int)(per * round);
@@ -500,7 +503,8 @@ Plan plan_of(int kv, int d, int64_t seqs, int heads, int longest, bool weights) 
 
 template <int DP, bool FULL, bool OCT>
 void launch(const Cache& c, const Attention& a, const Partials& ps, int g, const Plan& p, unsigned grid, hipStream_t s) {
-    if (p.waves == 8) attn_chunk_kernel<DP, FULL, OCT, 8><<<grid, 512, 0, s>>>(c, a, ps, g, p.tiles);
+    if (p.waves == 1) attn_chunk_kernel<DP, FULL, OCT, 1><<<grid, 64, 0, s>>>(c, a, ps, g, p.tiles);
+    else if (p.waves == 8) attn_chunk_kernel<DP, FULL, OCT, 8><<<grid, 512, 0, s>>>(c, a, ps, g, p.tiles);
     else attn_chunk_kernel<DP, FULL, OCT, 4><<<grid, 256, 0, s>>>(c, a, ps, g, p.tiles);
 }
 template <int DP>

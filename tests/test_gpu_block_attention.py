@@ -203,3 +203,17 @@ def test_rows_of_weights_narrower_than_the_tokens_are_refused(kv, seqs):
     B.qeft_attn_decode(cache, table, lens, n, q, score=base[:, :, :n])
     torch.testing.assert_close(base[:, :, :n].sum(2), torch.ones((seqs, kv), device="cuda"), rtol=0, atol=n * 2.0 ** -20)
     assert (base[:, :, n:] == 7.0).all()
+
+
+@pytest.mark.parametrize("heads,kv,d,page,lens", [
+    (4, 4, 128, 16, [1, 31, 32, 0, 17]),
+    (40, 2, 72, 5, [32, 9]),            # two tiles of heads
+    (32, 1, 64, 8, [6, 32, 1]),
+    (12, 2, 256, 8, [20, 0, 32, 3]),
+    (5, 1, 200, 7, [30, 11]),
+    (64, 64, 64, 16, [64, 33, 32, 63] * 4),
+    (32, 32, 256, 32, [50, 1, 64, 40] * 8),
+    (96, 32, 80, 24, [64, 60, 0, 33] * 8),
+])
+def test_short_rows(heads, kv, d, page, lens):
+    test_attention(heads, kv, d, page, lens)
