@@ -13,6 +13,7 @@
 // 128 tokens behind the budget, which counts the bits before its own.
 // Bytes bound it: 16 a token for weights and positions, and 8 head_dim per token that moves.  16 x 32 rows of 2049 tokens, one to go: 5.8 us (latencies of one
 // workgroup a row; the bytes alone 3.4); 8 rows, 32768 -> 4096: 24 us for the selection (loads 4, three digits 13, equal keys 1.6, bits 4: eight CUs), 10 for the moves.
+#include <algorithm>
 #include "qeft_internal.h"
 #include "wave.h"
 
@@ -633,9 +634,11 @@ hipError_t cache_evict(const Cache& c, const Evict& a, hipStream_t s) {
     }
     const auto on16 = [](const void* p) { return ((uintptr_t)p & 15u) == 0; };
     const bool vec = on16(a.score) && on16(a.pos) && on16(a.score_out) && on16(a.pos_out) && a.ld % 4 == 0 && a.ld_out % 4 == 0;
-    // 4 tokens a thread up to 4096, then whole workgroups with 8, 16, 32
+    // 4 tokens a thread up to 4096, then whole workgroups with 8, 16, 32.  Where histograms are taken, 512 threads at least: their bins are what takes the time (32 heads, 300 tokens -> 200:
+    // 13.9 us with 128 threads, 10.0 with 256, 8.7 with 512, 8.9 with 1024; of 32 sequences 100 -> 50: 15.6, 12.5, 12.5, 20.6).
+    const int least = a.longest - a.budget > FEW ? 512 : 128;
     hipError_t e = hipSuccess;
-    if (a.longest <= 4096) e = select_with<1>(c, a, x, rows, a.longest <= 512 ? 128 : (a.longest + 255) / 256 * 64, vec, s);
+    if (a.longest <= 4096) e = select_with<1>(c, a, x, rows, std::max(least, (a.longest + 255) / 256 * 64), vec, s);
     else if (a.longest <= 8192) e = select_with<2>(c, a, x, rows, 1024, vec, s);
     else if (a.longest <= 16384) e = select_with<4>(c, a, x, rows, 1024, vec, s);
     else if (a.longest <= MAX_IN_REGISTERS) e = select_with<8>(c, a, x, rows, 1024, vec, s);
