@@ -481,11 +481,11 @@ Plan plan_of(int kv, int d, int64_t seqs, int heads, int longest, bool weights) 
     const int g = heads / kv;
     p.tiles = (g + 15) / 16;
     const int64_t rows = seqs * kv * p.tiles;
-    // One wave for what is a step of it, or two steps of rows that fill the GPU several times (2048 rows of 1 / 32 / 64 tokens: 6.6 / 8.5 / 13.2 us against 11.0 / 11.7 / 14.9
-    // with four waves; 512 rows of 64 tokens, 4 heads each: 7.8 against 6.5).  Eight waves for what is one chunk of few rows (256 rows of 1000 to 2048 tokens, 4 heads each: 41.2 us against 43.1), four else: a round of 128 tokens wastes
+    // One wave for two steps of rows that fill the GPU several times (2048 rows of 1 / 32 / 64 tokens: 6.6 / 8.5 / 13.2 us against 11.0 / 11.7 / 14.9 with four waves; 512 rows of 20
+    // tokens, 4 heads each: 5.4 against 4.7).  Eight waves for what is one chunk of few rows (256 rows of 1000 to 2048 tokens, 4 heads each: 41.2 us against 43.1), four else: a round of 128 tokens wastes
     // less at a row's end (2048 rows of 100 to 300 tokens: 44.9 us against 52.9).
     int chunks = longest <= short_row(d) ? 1 : chunks_of(rows, ((int64_t)longest + 4 * STEP - 1) / (4 * STEP), d);
-    p.waves = longest <= STEP || (longest <= 2 * STEP && rows >= 4 * CUS) ? 1 : chunks == 1 && rows < 2 * CUS ? 8 : 4;
+    p.waves = longest <= 2 * STEP && rows >= 4 * CUS ? 1 : chunks == 1 && rows < 2 * CUS ? 8 : 4;
     const int round = p.waves * STEP;
     const int64_t rounds = ((int64_t)longest + round - 1) / round, per = rounds > 0 ? (rounds + chunks - 1) / chunks : 1;
     p.chunk = (int)(per * round);
