@@ -14,6 +14,7 @@
 // CU has one or two workgroups and nothing else to hide them.
 // Measured: forward 4096 x 4096, fp32 residual: 39 us, 5.2 TB/s; gradient 4096 x 8192 with both norms and a channel gate: 122 us, 4.9 TB/s, 6 of it the slabs' sum;
 // 333 x 5120, token gate: 15 us, where the bytes take 5.3 (two rows a workgroup and the second launch, latencies).
+#include <algorithm>
 #include "qeft_internal.h"
 #include "wave.h"
 
@@ -653,7 +654,10 @@ BwdPlan bwd_plan(int n, int64_t m) {
     if (p.in_registers) {
         p.v = n <= 8192 ? 1 : 2;
         p.waves = (octets + 64 * p.v - 1) / (64 * p.v);
-        p.groups = 16 / p.waves;
+        // Rows side by side in a workgroup: all that fit where one workgroup then takes the whole call (13 x 488: 5.6 us against 8.8), else no more than fill the CUs (200 x 4096:
+        // 10.5 us with one, 11.2 with two; 101 x 3856 with both norms and a token gate 9.6 and 11.4).
+        const int most = 16 / p.waves;
+        p.groups = m <= most ? most : (int)std::min<int64_t>(most, (m + 255) / 256);
         // One workgroup of up to 1024 threads per CU: a slab costs 24 bytes a column however many rows it sums.
         const int64_t teams = (m + p.groups - 1) / p.groups;
         p.rounds = (int)((teams + 255) / 256);
