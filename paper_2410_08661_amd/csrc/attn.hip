@@ -450,12 +450,15 @@ constexpr int CUS = 256;
 
 // Chunks of a row (a sequence's kv head, and 16 of its query heads) of `rounds` 128-token rounds of 64 KiB at head_dim 128.  A CU reads 20 bytes a ns
 // at most, so what counts is that all have the same number of workgroups: one each for up to 16 rows (1 of 130000 tokens, 8 heads on 1: 21.1 us against 29.3 with two; 8 of 60000:
-// 48.8 against 49.7), two for up to 128 (32 of 2048, with weights: 11.2 against 12.0; 128 of 2800: 35.8 against 38.0), or, between 128 and 512 rows, what the estimate finds
+// 48.8 against 49.7), two for up to 128 if they are long (32 of 2048, with weights: 11.2 against 12.0; 128 of 2800: 35.8 against 38.0), or, between 128 and 512 rows, what the estimate finds
 // (us: 160 rows of 2049 tokens in 1 / 2 / 3 chunks: 46.4 / 46.3 / 39.4; 256 of 2048: 48.2 / 52.6; 8 of 131001 in 32 / 64 / 128 / 256: 95.6 / 97.3 / 102.6 / 109.9).
 // The second launch is 4 us, and more where many heads have many chunks.
-int chunks_of(int64_t rows, int64_t rounds, int d) {
+int chunks_of(int64_t rows, int64_t rounds, int d, int g) {
     if (rounds <= 1 || rows >= 2 * CUS) return 1;
     if (rows <= CUS / 2) {
+        // One chunk where its rounds, 1.7 us each by eight waves, cost no more than the second launch (more with many heads a kv head) and the rounds of two workgroups a CU, 2.75 us for all
+        // rows': 128 rows of 700 / 1000 / 1400 tokens, 8 heads each: 12.8 / 15.8 / 20.6 us against 19.3 / 21.5 / 25.8; one head each: 11.5 / 15.0 / 19.6 against 13.7 / 15.9 / 20.0.
+        if (rows >= CUS / 4 && (float)rounds * (1.7f - 2.75f * (float)rows / CUS) * (float)(d + 64) / 192.f <= 4.f + 0.35f * (float)g) return 1;
         const int64_t most = (rows <= 16 ? CUS : 2 * CUS) / rows;
         return (int)(most < rounds ? most : rounds);
     }
@@ -484,7 +487,7 @@ Plan plan_of(int kv, int d, int64_t seqs, int heads, int longest, bool weights) 
     // One wave for two steps of rows that fill the GPU several times (2048 rows of 1 / 32 / 64 tokens: 6.6 / 8.5 / 13.2 us against 11.0 / 11.7 / 14.9 with four waves; 512 rows of 20
     // tokens, 4 heads each: 5.4 against 4.7).  Eight waves for what is one chunk of few rows (256 rows of 1000 to 2048 tokens, 4 heads each: 41.2 us against 43.1), four else: a round of 128 tokens wastes
     // less at a row's end (2048 rows of 100 to 300 tokens: 44.9 us against 52.9).
-    int chunks = longest <= short_row(d) ? 1 : chunks_of(rows, ((int64_t)longest + 4 * STEP - 1) / (4 * STEP), d);
+    int chunks = longest <= short_row(d) ? 1 : chunks_of(rows, ((int64_t)longest + 4 * STEP - 1) / (4 * STEP), d, g);
     p.waves = longest <= 2 * STEP && rows >= 4 * CUS ? 1 : chunks == 1 && rows < 2 * CUS ? 8 : 4;
     const int round = p.waves * STEP;
     const int64_t rounds = ((int64_t)longest + round - 1) / round, per = rounds > 0 ? (rounds + chunks - 1) / chunks : 1;

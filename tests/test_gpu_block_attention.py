@@ -217,3 +217,14 @@ def test_rows_of_weights_narrower_than_the_tokens_are_refused(kv, seqs):
 ])
 def test_short_rows(heads, kv, d, page, lens):
     test_attention(heads, kv, d, page, lens)
+
+
+@pytest.mark.parametrize("heads,kv,d,page,lens", [
+    (64, 8, 128, 16, [1400, 0, 33, 700, 1, 1399, 640, 128] * 2),       # one chunk of eight waves a row
+    (32, 32, 64, 16, [800, 30, 799]),
+    (96, 32, 96, 8, [1100, 257, 600, 4]),
+    (64, 8, 128, 16, [2900, 100, 513, 1664] + [70] * 9),                # four chunks, three, ...
+    (16, 16, 256, 32, [600, 280, 31, 599, 1, 64, 65, 0]),
+])
+def test_rows_that_half_fill_the_gpu(heads, kv, d, page, lens):
+    test_attention(heads, kv, d, page, lens)
