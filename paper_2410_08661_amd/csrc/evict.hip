@@ -578,7 +578,7 @@ __global__ __launch_bounds__(1024) void evict_select_long_kernel(Cache c, Evict 
     __syncthreads();
     int before = 0;
     for (int w = 0; w < wave; ++w) before += tally[w];
-    for (int w = from / 64 + lane; 64 * w < to; w += 64) below[w] += before;
+    for (int w = (from + 63) / 64 + lane; 64 * w < to; w += 64) below[w] += before;   // (a wave without tokens has none of the last word either)
 }
 
 // The second launch: workgroup = TILE tokens behind a row's budget.

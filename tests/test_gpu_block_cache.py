@@ -164,6 +164,14 @@ def test_evict_rows_longer_than_shared_memory(n, budget):
     check_evict(1, 8, 64, [n], budget, 4, 100)
 
 
+@pytest.mark.parametrize("inplace", [False, True])
+def test_evict_short_rows_beside_one_longer_than_shared_memory(inplace):
+    """More rows than several workgroups a row are for, most of them too short to give every wave a token."""
+    def make(s):
+        s.copy_((torch.arange(s.shape[-1], device="cuda") % 3).float().expand_as(s))
+    check_evict(1, 8, 32, [33000] + [10, 60, 64, 1100] * 51 + [32769], 55, 4, 50, inplace=inplace, make=make)
+
+
 def test_evict_pools_of_other_strides_and_a_count_that_is_far_ahead():
     assert check_evict(3, 72, 7, [100, 90], 40, 0, 20, order="tokens") > 0
     check_evict(2, 64, 16, [100], 60, 0, 2 ** 31 - 1, seen=[2 ** 31 - 1])
