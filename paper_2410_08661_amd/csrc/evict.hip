@@ -581,6 +581,156 @@ __global__ __launch_bounds__(1024) void evict_select_long_kernel(Cache c, Evict 
     for (int w = (from + 63) / 64 + lane; 64 * w < to; w += 64) below[w] += before;   // (a wave without tokens has none of the last word either)
 }
 
+// Few rows longer than a workgroup's registers hold: a row by many workgroups, PART tokens each, in five launches, a digit's histograms in each of the first three, then the bits, then their
+// sums over the parts.  Every workgroup finds the border of the digit before from the sum of the row's histograms.  28 us for 8 rows of 40000 or of 131001, launches and latencies.
+constexpr int PART = 8192;
+struct Parts {
+    int* hist;     // [3][rows * parts][BINS]
+    int2* state;   // [rows][2]: the border after the first and the second digit, and how many of its keys stay
+    int* count;    // [rows * parts]: changed tokens
+    int parts;
+};
+template <int STEP>
+__global__ __launch_bounds__(1024) void evict_part_kernel(Cache c, Evict a, Parts p, uint64_t* all_bits, int* all_below, int words) {
+    __shared__ __align__(16) int hist[STEP < 3 ? BINS * LONG_COPIES : 4];
+    __shared__ int tally[16], changes[16], found[3];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int row = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
+    const Row r = row_at(c, a, row);
+    const int n = r.n, left = r.left, from = PART * part, to = min(n, from + PART);
+    if (STEP == 0) {
+        if (r.h == 0 && part == 0 && tid == 0) a.lens_out[r.b] = left;
+        for (int t = from + tid; t < min(to, left); t += 1024) {
+            if (a.score_out != a.score) r.score_out[t] = r.score[t];
+            if (a.pos_out != a.pos) r.pos_out[t] = r.pos[t];
+        }
+    }
+    uint64_t* bits = all_bits + (size_t)row * words;
+    int* below = all_below + (size_t)row * words;
+    if (n == left || left == 0) {
+        if (STEP == 3) {
+            if (tid == 0) p.count[blockIdx.x] = 0;
+            for (int t = from + 64 * tid; t < to; t += 64 * 1024) bits[t / 64] = 0, below[t / 64] = 0;
+        }
+        return;
+    }
+    const int recent = first_recent(a.seen[r.b], a.keep_last);
+    // a wave's tokens follow each other, 64 at a time
+    constexpr int EACH = PART / 1024;
+    float s[EACH];
+    int ps[EACH];
+    const int first = from + 64 * EACH * wave;
+#pragma unroll
+    for (int x = 0; x < EACH; ++x) {
+        const int t = first + 64 * x + lane;
+        s[x] = t < to ? r.score[t] : 0.f;
+        ps[x] = t < to ? r.pos[t] : 0;
+    }
+    uint32_t border = 0;
+    int want = left;
+    if (STEP > 0) {
+        if (STEP > 1) {
+            const int2 st = p.state[2 * row + STEP - 2];
+            border = (uint32_t)st.x;
+            want = st.y;
+        }
+        // two bins a thread, thread 0 the highest
+        constexpr int shift = STEP == 1 ? 21 : STEP == 2 ? 10 : 0;
+        const int bin = BINS - 2 - 2 * tid;
+        const int* h = p.hist + ((size_t)(STEP - 1) * (gridDim.x / p.parts) + row) * p.parts * BINS + bin;
+        int own[2] = {0, 0};
+        for (int q0 = 0; q0 < p.parts; q0 += 8) {
+            int2 v[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) v[y] = q0 + y < p.parts ? *reinterpret_cast<const int2*>(h + (size_t)(q0 + y) * BINS) : int2{0, 0};
+#pragma unroll
+            for (int y = 0; y < 8; ++y) own[0] += v[y].y, own[1] += v[y].x;
+        }
+        const int sum = own[0] + own[1], upto = wave_upto(sum);
+        if (lane == 63) tally[wave] = upto;
+        __syncthreads();
+        int before = upto - sum;
+        for (int w = 0; w < wave; ++w) before += tally[w];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {   // (one thread finds it: there are `want` keys or more)
+            if (want > before && want <= before + own[x]) {
+                found[0] = bin + 1 - x;
+                found[1] = want - before;
+            }
+            before += own[x];
+        }
+        __syncthreads();
+        border |= (uint32_t)found[0] << shift;
+        want = found[1];
+        if (STEP < 3 && part == 0 && tid == 0) p.state[2 * row + STEP - 1] = int2{(int)border, want};
+    }
+    if constexpr (STEP < 3) {
+        constexpr int shift = STEP == 0 ? 21 : STEP == 1 ? 10 : 0;
+        constexpr uint32_t mask = STEP == 2 ? 1023 : 2047, known = STEP == 0 ? 0u : ~0u << (STEP == 1 ? 21 : 10);
+        for (int i = 4 * tid; i < BINS * LONG_COPIES; i += 4 * 1024) *reinterpret_cast<i4*>(hist + i) = i4{0, 0, 0, 0};
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < EACH; ++x) {
+            const uint32_t k = key_of(s[x], ps[x], a.keep_first, recent);
+            if (first + 64 * x + lane < to && ((k ^ border) & known) == 0) atomicAdd(&hist[((k >> shift) & mask) * LONG_COPIES + (lane & (LONG_COPIES - 1))], 1);
+        }
+        __syncthreads();
+        const i4 lo = *reinterpret_cast<const i4*>(&hist[2 * tid * LONG_COPIES]), hi = *reinterpret_cast<const i4*>(&hist[(2 * tid + 1) * LONG_COPIES]);
+        int* h = p.hist + ((size_t)STEP * gridDim.x + blockIdx.x) * BINS + 2 * tid;
+        *reinterpret_cast<int2*>(h) = int2{lo.x + lo.y + lo.z + lo.w, hi.x + hi.y + hi.z + hi.w};
+    } else {
+        // equal keys at the border, counted off in slot order: those of the parts and waves before
+        const int* h = p.hist + ((size_t)2 * gridDim.x + (size_t)row * p.parts) * BINS + (border & 1023);
+        int rank = 0, mine = 0;
+        for (int q = lane; q < part; q += 64) rank += h[(size_t)q * BINS];
+        rank = wave_reduce(rank, Sum());
+        uint32_t k[EACH];
+#pragma unroll
+        for (int x = 0; x < EACH; ++x) {
+            k[x] = key_of(s[x], ps[x], a.keep_first, recent);
+            mine += __popcll(__ballot(first + 64 * x + lane < to && k[x] == border));
+        }
+        __syncthreads();   // (tally may still be read)
+        if (lane == 0) tally[wave] = mine;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) rank += tally[w];
+        const uint64_t under = ((uint64_t)1 << lane) - 1;
+        uint64_t word[EACH];
+        int changed = 0;
+#pragma unroll
+        for (int x = 0; x < EACH; ++x) {
+            const int t = first + 64 * x + lane;
+            const uint64_t ties = __ballot(t < to && k[x] == border);
+            const bool stays = k[x] > border || (k[x] == border && rank + __popcll(ties & under) < want);
+            rank += __popcll(ties);
+            word[x] = __ballot(t < to && (t < left) != stays);
+            changed += __popcll(word[x]);
+        }
+        if (lane == 0) changes[wave] = changed;
+        __syncthreads();
+        int upto = 0;
+        for (int w = 0; w < wave; ++w) upto += changes[w];
+#pragma unroll
+        for (int x = 0; x < EACH; ++x) {
+            const int t = first + 64 * x;
+            if (lane == 0 && t < to) {
+                bits[t / 64] = word[x];
+                below[t / 64] = upto;   // within the part
+            }
+            upto += __popcll(word[x]);
+        }
+        if (tid == 1023) p.count[blockIdx.x] = upto;
+    }
+}
+__global__ __launch_bounds__(256) void evict_parts_below_kernel(Cache c, Evict a, Parts p, int* all_below, int words) {
+    const int row = blockIdx.x / p.parts, part = blockIdx.x % p.parts, lane = threadIdx.x & 63;
+    const int n = row_at(c, a, row).n, w = PART / 64 * part + threadIdx.x;
+    int before = 0;
+    for (int q = lane; q < part; q += 64) before += p.count[row * p.parts + q];
+    before = wave_reduce(before, Sum());
+    if (threadIdx.x < PART / 64 && 64 * (int64_t)w < n) all_below[(size_t)row * words + w] += before;
+}
+
 // The second launch: workgroup = TILE tokens behind a row's budget.
 __global__ __launch_bounds__(256) void evict_move_kernel(Cache c, Evict a, const uint64_t* all_bits, const int* all_below, int words, int tiles) {
     __shared__ MoveLists lists;
@@ -617,12 +767,21 @@ hipError_t select_with(const Cache& c, const Evict& a, const Bits& x, int rows, 
 
 bool second_launch(int longest, int budget) { return longest - budget > TILE || longest > MAX_IN_REGISTERS; }
 int words_of(int longest) { return (longest + 63) / 64; }
+int parts_of(int longest) { return (longest + PART - 1) / PART; }
+// Workgroups that a call of rows longer than MAX_IN_REGISTERS has at most if several take a row (24 KiB of histograms each); with more rows, one a row keeps the CUs busy.  Several against one: 8 rows of
+// 40000 -> 30000 44 us against 82, of 131001 -> 32768 88 against 213; 64 rows of 40000 -> 20000 192 against 212; 200 of 40000 -> 39000 132 against 138.
+constexpr int MOST_PARTS = 1024;
+size_t bits_bytes(int64_t rows, int longest) { return ((size_t)rows * words_of(longest) * (sizeof(uint64_t) + sizeof(int)) + 255) / 256 * 256; }
 
 }  // namespace
 
 size_t evict_workspace(int kv, int64_t seqs, int longest, int budget) {
     if (longest <= budget || !second_launch(longest, budget)) return 0;
-    return (size_t)seqs * kv * words_of(longest) * (sizeof(uint64_t) + sizeof(int));
+    const int64_t rows = seqs * kv, most = rows > 0 ? MOST_PARTS / rows : 0;
+    size_t parts = 0;
+    // (as much as a shorter bound needs, which a short table can make of a longer one)
+    if (longest > MAX_IN_REGISTERS && most >= parts_of(MAX_IN_REGISTERS + 1)) parts = (size_t)rows * std::min<int64_t>(parts_of(longest), most);
+    return bits_bytes(rows, longest) + parts * (3 * BINS + 1) * sizeof(int) + (parts ? (size_t)rows * 2 * sizeof(int2) : 0);
 }
 
 hipError_t cache_evict(const Cache& c, const Evict& a, hipStream_t s) {
@@ -642,7 +801,18 @@ hipError_t cache_evict(const Cache& c, const Evict& a, hipStream_t s) {
     else if (a.longest <= 8192) e = select_with<2>(c, a, x, rows, 1024, vec, s);
     else if (a.longest <= 16384) e = select_with<4>(c, a, x, rows, 1024, vec, s);
     else if (a.longest <= MAX_IN_REGISTERS) e = select_with<8>(c, a, x, rows, 1024, vec, s);
-    else evict_select_long_kernel<<<rows, 1024, 0, s>>>(c, a, x.bits, x.below, x.words);
+    else if (const int64_t grid = (int64_t)rows * parts_of(a.longest); x.bits && grid <= MOST_PARTS) {
+        Parts p;
+        p.parts = parts_of(a.longest);
+        p.state = (int2*)((char*)a.ws + bits_bytes(rows, a.longest));
+        p.hist = (int*)(p.state + 2 * rows);
+        p.count = p.hist + 3 * grid * BINS;
+        evict_part_kernel<0><<<(unsigned)grid, 1024, 0, s>>>(c, a, p, x.bits, x.below, x.words);
+        evict_part_kernel<1><<<(unsigned)grid, 1024, 0, s>>>(c, a, p, x.bits, x.below, x.words);
+        evict_part_kernel<2><<<(unsigned)grid, 1024, 0, s>>>(c, a, p, x.bits, x.below, x.words);
+        evict_part_kernel<3><<<(unsigned)grid, 1024, 0, s>>>(c, a, p, x.bits, x.below, x.words);
+        evict_parts_below_kernel<<<(unsigned)grid, 256, 0, s>>>(c, a, p, x.below, x.words);
+    } else evict_select_long_kernel<<<rows, 1024, 0, s>>>(c, a, x.bits, x.below, x.words);
     if (e != hipSuccess) return e;
     if (x.bits) {
         const int tiles = (a.longest - a.budget + TILE - 1) / TILE;

@@ -190,3 +190,12 @@ def test_rows_of_weights_hold_the_tokens_whatever_their_pitch():
         with pytest.raises(B.QeftError) as e:
             B._take("f", "score", t, torch.float32, (t.shape[0], t.shape[1], None), True, 6)
         assert e.value.status == B.QEFT_ERR_SHAPE
+
+
+def test_the_workspace_of_an_eviction_does_not_shrink_with_the_bound():
+    for rows in (1, 2, 64, 204, 205, 3000):
+        d = B.make_cache_desc(4, 8, rows, 8)
+        bounds = (0, 100, 128, 229, 1000, 32768, 32769, 40960, 40961, 131072, 1 << 18, 1 << 19)
+        sizes = [B.qeft_evict_workspace(d, 1, n, 100) for n in bounds if rows * (n // 128 + 1) <= 4 << 21]   # (more are refused)
+        assert sizes == sorted(sizes) and sizes[2] == 0 < sizes[4]
+        assert B.qeft_evict_workspace(d, 0, 40000, 100) == 0

@@ -172,6 +172,29 @@ def test_evict_short_rows_beside_one_longer_than_shared_memory(inplace):
     check_evict(1, 8, 32, [33000] + [10, 60, 64, 1100] * 51 + [32769], 55, 4, 50, inplace=inplace, make=make)
 
 
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("kv,lens,budget,kind", [
+    (2, [70001, 50000, 20000, 40000], 40000, "equal"),     # many parts a row; rows at, below and above the budget
+    (1, [33000, 8192, 8193, 0], 8192, "few"),              # the border in few different weights, parts that end at the budget
+    (3, [40961], 5, "distinct"),
+    (1, [32769], 32768, "nan"),
+    (1, [36000, 70], 0, "equal"),                          # nothing stays
+    (1, [33000] + [10, 60, 64] * 68 + [32769], 55, "few"),   # more rows than several workgroups a row are for
+])
+def test_evict_rows_of_many_parts(kv, lens, budget, kind, inplace):
+    def make(s):
+        t = torch.arange(s.shape[-1], device="cuda")
+        if kind == "equal":
+            s.fill_(0.5)
+        elif kind == "few":
+            s.copy_((t % 3).float().expand_as(s))
+        elif kind == "distinct":
+            s.copy_(((t * 7919) % s.shape[-1]).float().expand_as(s))
+        else:
+            s.copy_(torch.where(t % 1000 == 3, float("nan"), -(t % 7).float()).expand_as(s))
+    check_evict(kv, 8, 32, lens, budget, 4, 50, inplace=inplace, make=make)
+
+
 def test_evict_pools_of_other_strides_and_a_count_that_is_far_ahead():
     assert check_evict(3, 72, 7, [100, 90], 40, 0, 20, order="tokens") > 0
     check_evict(2, 64, 16, [100], 60, 0, 2 ** 31 - 1, seen=[2 ** 31 - 1])
