@@ -195,6 +195,16 @@ def test_evict_rows_of_many_parts(kv, lens, budget, kind, inplace):
     check_evict(kv, 8, 32, lens, budget, 4, 50, inplace=inplace, make=make)
 
 
+@pytest.mark.parametrize("budget", [60, 300])
+@pytest.mark.parametrize("longest", [190, 430, 2000, 4097, 9000, 20001, 32768, 33001])
+def test_evict_rows_of_all_lengths_in_one_call(longest, budget):
+    """Threads, waves and whole words of a workgroup without tokens; rows at, just above and far above the budget."""
+    lens = [longest] + [n for n in (0, 1, 10, 60, 61, 63, 64, 65, 130, 257, 299, 300, 301, 304, 305, 511, 1100, 4095, 8200) if n <= longest]
+    def make(s):
+        s.copy_(((torch.arange(s.shape[-1], device="cuda") * 31) % 17).float().expand_as(s))
+    check_evict(2, 8, 16, lens, budget, 4, 20, inplace=longest % 2 == 0, make=make)
+
+
 def test_evict_pools_of_other_strides_and_a_count_that_is_far_ahead():
     assert check_evict(3, 72, 7, [100, 90], 40, 0, 20, order="tokens") > 0
     check_evict(2, 64, 16, [100], 60, 0, 2 ** 31 - 1, seen=[2 ** 31 - 1])
