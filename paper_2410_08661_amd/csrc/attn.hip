@@ -16,10 +16,10 @@
 // P enters as hi + lo, two fp16 values (22 bits): rounding it once would add half of the output's own rounding error again.  Exponents carry
 // an offset of 2^7 so that lo keeps its bits down to p = 2^-21 of the largest; the offset cancels in O / l.
 //
-// Work: a workgroup of 4 or 8 waves takes a chunk of one sequence's tokens for one kv head (16 query heads at a time; more heads read the chunk again, from
+// Work: a workgroup of 4 or 8 waves (one wave for a great many short rows) takes a chunk of one sequence's tokens for one kv head (16 query heads at a time; more heads read the chunk again, from
 // L2), joins its waves through LDS and writes out, or, where the sequence is cut in several chunks, m, l and O to the workspace for a second launch.
 //
-// Measured, head_dim 128: 131001 tokens, 64 / 8 heads: 97 us, 5.5 TB/s (a device copy moves 5.2); 8 x 2048 tokens, 32 heads: 47.8 us, 5.6 TB/s;
+// Measured, head_dim 128: 131001 tokens, 64 / 8 heads: 95 us, 5.6 TB/s (a device copy moves 5.2); 8 x 2048 tokens, 32 heads: 47.8 us, 5.6 TB/s;
 // 203 tokens, 32 heads: 5.3 us, a chain of latencies.
 #include "qeft_internal.h"
 #include "wave.h"

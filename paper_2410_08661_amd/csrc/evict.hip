@@ -2,7 +2,8 @@
 //
 // A row is one kv head of one sequence: n tokens with a weight and a position each, of which `budget` stay.  Order of preference: rank (weight as an ordered
 // 32-bit key, or the key of +infinity for the first and last positions) from high to low, then slot from low to high.  The kept set is everything before
-// one border in that order, (key, slot), which a workgroup finds with its row's keys in registers, 4 to 32 a thread:
+// one border in that order, (key, slot), which a workgroup finds with its row's keys in registers, 4 to 32 a thread (rows beyond 32768
+// tokens: several workgroups a row, a launch a step, or one that reads the row again for each):
 //   few to go (a sequence one token over its budget): the least preferred token, so many times;
 //   else three digits from the top, 11, 11 and 10 bits (eight would be a float's exponent, and say little), each from a histogram in LDS of the keys that agree with
 //   the border above it; fewer digits where a bin's keys all stay.  (Bisection over the key, a comparison, a scalar count and an addition a key and step, takes 1 us a

@@ -12,7 +12,7 @@
 // The gradient's workgroups stay for many rows: the column sums are kept in registers, a workgroup's row groups join theirs in LDS, and one slab per
 // workgroup goes to the workspace, summed by a second launch in a fixed order.  The next row's loads are issued before the current one's sums: a
 // CU has one or two workgroups and nothing else to hide them.
-// Measured: forward 4096 x 4096, fp32 residual: 39 us, 5.2 TB/s; gradient 4096 x 8192 with both norms and a channel gate: 122 us, 4.9 TB/s, 6 of it the slabs' sum;
+// Measured: forward 4096 x 4096, fp32 residual: 39 us, 5.2 TB/s; gradient 4096 x 8192 with both norms and a channel gate: 122 - 125 us, 5 TB/s, 6 of it the slabs' sum;
 // 333 x 5120, token gate: 15 us, where the bytes take 5.3 (two rows a workgroup and the second launch, latencies).
 #include <algorithm>
 #include "qeft_internal.h"
