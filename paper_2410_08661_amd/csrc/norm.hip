@@ -418,7 +418,8 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(Norm a, Sums S, int wave
             row_sums(two, buf[2 * (round & 1)], first, waves);
             s[0] = two[0], s[1] = two[1];
         }
-        const float rs = 1.f / sqrtf(fmaf(s[0], inv, a.eps)), c = s[1] * inv * rs;   // c = mean(a hh)
+        // (a row beyond the last has no norm: with eps == 0 its hh would be 0 / 0, and dw_pre's sums take it)
+        const float rs = row < a.m ? 1.f / sqrtf(fmaf(s[0], inv, a.eps)) : 0.f, c = s[1] * inv * rs;   // c = mean(a hh)
         const float rsy = POST ? 1.f / sqrtf(fmaf(s[2], inv, a.eps)) : 1.f;
         pin();
         float t[V][8], q[1] = {0.f};

@@ -174,3 +174,21 @@ def test_gradients_from_a_graph_and_without_the_native_module(monkeypatch):
             assert torch.equal(a, b)
         for a, k in zip(outs, got):
             assert torch.equal(a, got[k])
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("post,gate", [(False, "none"), (True, "channel"), (True, "token")])
+@pytest.mark.parametrize("m,n", [(1, 4096), (3, 7), (3, 512), (301, 8192), (301, 16384), (3, 16400)])
+def test_backward_with_no_eps(m, n, f32, post, gate):
+    """Workgroups have room for more rows than there are: a row that does not exist has no norm, and no part in the sums over rows."""
+    i = inputs(m, n, f32, post, gate)
+    desc = B.make_norm_desc(n, i["r"].dtype, GATES[gate], 0.7, 0.0)
+    got = dict(zip(("dr", "dy", "dw_pre", "dw_post", "dgate"),
+                   B.qeft_norm_bwd(desc, i["dx"], i["r"], i["w_pre"], dh=i["dh"], y=i["y"], w_post=i["w_post"], gate=i["gate"])))
+    want = U.norm_backward(i["dx"], i["dh"], i["r"], i["y"], i["w_pre"], i["w_post"], i["gate"], 0.7, 0.0, gate == "channel")
+    assert {k for k, v in got.items() if v is not None} == set(want)
+    for k, (w, bound) in want.items():
+        U.close(k, got[k], w, bound, U.ROUNDING[got[k].dtype])
+    h, x = B.qeft_norm_fwd(desc, i["r"], i["w_pre"], y=i["y"], w_post=i["w_post"], gate=i["gate"])
+    _, want = U.norm_forward(h, None, i["w_pre"], None, None, 1.0, 0.0)
+    U.close("x", x, want, 2 * U.sums_rounding(n) * want.abs(), U.HALF)
