@@ -544,7 +544,7 @@ class Cache:
 
 def _c_table(where, table):
     p, ld = _take(where, "table", table, torch.int32, (None, None))
-    return qeft_table_t(p, max(ld, table.shape[1]), table.shape[1], table.shape[0])
+    return qeft_table_t(p, ld, table.shape[1], table.shape[0])   # (an expanded view's pitch is 0, which the host's checks refuse)
 
 
 def _c_workspace(where, ws):
@@ -576,7 +576,7 @@ def qeft_cache_append(cache: Cache, table: torch.Tensor, k: torch.Tensor, v: tor
         po, ldo = _take(at, "q_out", q_out if q is not None else None, torch.float16, (n, heads * d.head_dim), q is None)
         pi, ps, pp = (_take(at, name, t, torch.int32, (n,), t is not index)[0] for name, t in (("index", index), ("seq", seq), ("pos", pos)))
         pr, ldr = _take(at, "rot", rot, torch.float32, (None, None), True)
-        a = qeft_append_t(pq, pk, pv, po, ldq, ldo, ldk, ldv, ps, pi, pp, pr, max(ldr, rot.shape[1]) if rot is not None else 0,
+        a = qeft_append_t(pq, pk, pv, po, ldq, ldo, ldk, ldv, ps, pi, pp, pr, ldr,
                           rot.shape[0] if rot is not None else 0, rot.shape[1] if rot is not None else 0, heads, n)
         st = raw.qeft_cache_append(C.byref(d), C.byref(pools), C.byref(tab), C.byref(a), _stream())
     _check(st, "qeft_cache_append")
@@ -613,8 +613,7 @@ def qeft_attn_decode(cache: Cache, table: torch.Tensor, lens: torch.Tensor, long
         pl, _ = _take(at, "lens", lens, torch.int32, (n,))
         ps, lds = _take(at, "score", score, torch.float32, (n, d.kv_heads, None), True, min(longest, table.shape[1] * d.page_size))
         pw, nw = _c_workspace(at, ws)
-        a = qeft_attn_t(pl, int(longest), pq, po, ldq, ldo, heads, float(scale), ps, score.shape[2] if ps and lds < score.shape[2] else lds,
-                        int(bool(accumulate)), pw, nw)
+        a = qeft_attn_t(pl, int(longest), pq, po, ldq, ldo, heads, float(scale), ps, lds, int(bool(accumulate)), pw, nw)
         st = raw.qeft_attn_decode(C.byref(d), C.byref(pools), C.byref(tab), C.byref(a), _stream())
     _check(st, "qeft_attn_decode")
     return out
