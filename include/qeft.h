@@ -363,7 +363,8 @@ int qeft_cache_append(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, 
  * lens int32 [seqs] on the device; `longest` is the host's upper bound of it (a longer sequence is cut there and at
  * table_pages * page_size; at most QEFT_MAX_DIM).  lens[b] <= 0: zeros.  Slots at or behind the length are never used, whatever they hold.
  * Table entries of used tokens are clamped to the pool.  Products of fp16 values, sums and the softmax are fp32; a probability enters the
- * product with V as the sum of two fp16 values (22 bits), the result is rounded once.  Not-a-number or infinite keys and
+ * product with V as the sum of two fp16 values: 22 bits from 2^-16 of the head's largest on, off by at most 2^-39 of the largest below that.  The
+ * result is rounded once.  Not-a-number or infinite keys and
  * values among a sequence's own tokens give non-finite results in the channels they reach.
  * score (optional, fp32 [seqs][kv_heads][ld_score], ld_score >= min(longest, table_pages * page_size)): the weight of every
  * token, sum of p[t] over the query heads of the kv head, is written there, or added if accumulate != 0; entries behind the

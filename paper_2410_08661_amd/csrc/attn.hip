@@ -4,7 +4,7 @@
 //
 // What bounds it: every cached byte is read once and used for 2 flops per query head of its kv head, so HBM for up to about a hundred heads per kv
 // head.  One pass: a wave takes 32 tokens at a time, keeps the running maximum m and sum l of its softmax and the unnormalised output, and rescales
-// those when a maximum grows by more than 8 in log2 (between, exponents are taken against the older maximum: p then is at most 2^8 too large,
+// those when a maximum grows by more than 1 in log2 (between, exponents are taken against the older maximum: p then is at most twice too large,
 // in numerator and denominator alike).
 //
 // Both products run on the matrix units for any number of heads (a single head uses one of 16 columns, which costs nothing a bandwidth-bound
@@ -13,8 +13,9 @@
 //                   the scores of head column c for the 8 consecutive tokens t0 + 8 grp ..: tile u's row r is token t0 + 8 (r >> 2) + 4 u + (r & 3).
 //   O = P V         those 8 probabilities are then the lane's piece of the left operand as they stand, without a shuffle.  V is read by rows (4 rows
 //                   of 256 bytes per load at head_dim 128) so that a lane holds 8 tokens x NV dimensions; one v_perm per register makes the columns.
-// P enters as hi + lo, two fp16 values (22 bits): rounding it once would add half of the output's own rounding error again.  Exponents carry
-// an offset of 2^7 so that lo keeps its bits down to p = 2^-21 of the largest; the offset cancels in O / l.
+// P enters as hi + lo, two fp16 values rounded to nearest (22 bits): rounding it once would add half of the output's own rounding error again.  Exponents carry
+// an offset of 2^14, as large as fp16 holds beside the maximum's growth: the pair has its 22 bits down to p = 2^-16 of the largest, and is off by 2^-39 of the largest
+// at most below that (many tokens of little weight beside one of much must not vanish from O while l counts them).  The offset cancels in O / l.
 //
 // Work: a workgroup of 4 or 8 waves (one wave for a great many short rows) takes a chunk of one sequence's tokens for one kv head (16 query heads at a time; more heads read the chunk again, from
 // L2), joins its waves through LDS and writes out, or, where the sequence is cut in several chunks, m, l and O to the workspace for a second launch.
@@ -30,12 +31,13 @@ namespace {
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-typedef __fp16 hr2 __attribute__((ext_vector_type(2)));   // (what the conversion builtin returns)
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 
 constexpr int STEP = 32;                // tokens of a wave's step
-constexpr float OFFSET = 7.f;           // log2: exponents are taken against m - OFFSET
-constexpr float SLACK = 8.f;            // log2: growth of a maximum that is let pass without rescaling (2^(OFFSET + SLACK) is below fp16's largest)
+constexpr float OFFSET = 14.f;          // log2: exponents are taken against m - OFFSET
+constexpr float SLACK = 1.f;            // log2: growth of a maximum that is let pass without rescaling (2^(OFFSET + SLACK) is below fp16's largest)
 constexpr float NEG_INF = -__builtin_inff();
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -237,10 +239,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
             const float p0 = exp2_fast(x[e] - base), p1 = exp2_fast(x[e + 1] - base);
             l += p0;
             l += p1;
-            const hr2 h = __builtin_amdgcn_cvt_pkrtz(p0, p1);   // (rounded towards zero: lo takes what is cut off)
-            const hr2 r = __builtin_amdgcn_cvt_pkrtz(p0 - (float)h.x, p1 - (float)h.y);
-            hi[e] = (_Float16)h.x, hi[e + 1] = (_Float16)h.y;
-            lo[e] = (_Float16)r.x, lo[e + 1] = (_Float16)r.y;
+            const h2 h = __builtin_convertvector((f2{p0, p1}), h2), r = __builtin_convertvector((f2{p0 - (float)h.x, p1 - (float)h.y}), h2);
+            hi[e] = h.x, hi[e + 1] = h.y;
+            lo[e] = r.x, lo[e + 1] = r.y;
         }
 #pragma unroll
         for (int j = 0; j < NV; ++j) {

@@ -1,5 +1,7 @@
 """qeft_attn_decode against the definition in 64 bits: head layouts, head and page sizes, lengths from none to many chunks, pools of other strides, slots
 that were never written."""
+import math
+
 import pytest
 import torch
 
@@ -228,3 +230,26 @@ def test_short_rows(heads, kv, d, page, lens):
 ])
 def test_rows_that_half_fill_the_gpu(heads, kv, d, page, lens):
     test_attention(heads, kv, d, page, lens)
+
+
+@pytest.mark.parametrize("kv,lens", [(64, [2048] * 7 + [1500]), (1, [20001])])
+@pytest.mark.parametrize("below", [31.01, 30.2, 25.3, 20.5])
+def test_many_tokens_of_little_weight_beside_one_of_much(below, kv, lens):
+    """The first token has nearly all the weight and nothing in half of its value's channels; the others, 2^-below of its weight each, are what those channels hold."""
+    d, page = 8, 16
+    cache, table, dev_lens, q = setup(kv, kv, d, page, lens)
+    q.fill_(1.0)
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    cache.k.masked_fill_(cache.k == cache.k, 0.0)                                    # (slots that were never written stay not-a-number)
+    cache.v.copy_(torch.where(cache.v == cache.v, (torch.rand(cache.v.shape, generator=gen, device="cuda") * 4096 + 4096).half(), cache.v))
+    for b in range(len(lens)):
+        cache.k[int(table[b, 0]), :, 0] = 1.0
+        cache.v[int(table[b, 0]), :, 0] = torch.tensor([0.0] * 4 + [1.0] * 4, device="cuda").half()
+    scale = below * math.log(2.0) / d
+    want, weights, eo, ew = U.attention(cache.k, cache.v, table, lens, q, kv, scale)
+    score = torch.zeros((len(lens), kv, max(lens)), device="cuda")
+    got = B.qeft_attn_decode(cache, table, dev_lens, max(lens), q, scale=scale, score=score)
+    # beside the bound of ordinary rows: half a step of fp16's smallest numbers for each token, against a largest of 2^14 or more
+    U.close("out", got, want, eo + max(lens) * 2.0 ** -39 * 8192)
+    for b, n in enumerate(lens):
+        U.close("weights", score[b, :, :n], weights[b, :, :n], ew[b, :, :n])
