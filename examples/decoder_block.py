@@ -3,7 +3,7 @@
 
     python examples/decoder_block.py [--steps 24] [--budget 16]
 
-Random weights, quantized to 4 bits with weak columns.  Decode: a few sequences of different lengths take one token at a time through a stack of blocks - norm,
+Random weights, quantized to 4 bits with weak columns.  Decode: a few sequences take one token at a time through a stack of blocks - norm,
 query / key / value projections in one launch, rotation and append to the paged cache, attention over it with its weights accumulated, output projection,
 norm with the residual addition, gate / up, down - and caches that have grown over the budget drop the tokens of least accumulated weight.  Fine-tuning:
 forward and backward of a block's second half, with the gradients of its norms and weak columns.  PyTorch does what is not the library's: memory, SiLU,
@@ -48,7 +48,10 @@ class Block:
         self.pos = torch.zeros((seqs, kv_heads, tokens), dtype=torch.int32, device="cuda")
 
     def decode(self, norm, h, x, table, lens, longest, seen, rot, w_next):
-        """One token of every sequence: residual stream h, its norm x; returns both for the next block.  lens: the tokens in the cache before this one."""
+        """One token of every sequence: residual stream h, its norm x; returns both for the next block.  lens: the tokens in the cache before this one, fewer than
+        `longest`, which is what the caller knows of them."""
+        if longest > self.score.shape[2]:
+            raise ValueError(f"a sequence of {longest} tokens in a table for {self.score.shape[2]}")
         q, k, v = B.qeft_linear_fwd_group([l.desc for l in (self.q, self.k, self.v)], [l.weight for l in (self.q, self.k, self.v)], x)
         B.qeft_cache_append(self.cache, table, k, v, lens, q=q, q_out=q, rot=rot, pos=seen)
         at = lens.long()[:, None, None].expand(-1, self.kv, 1)      # the new token's weight starts at zero
@@ -99,12 +102,15 @@ def main():
     ap.add_argument("--steps", type=int, default=24)
     ap.add_argument("--budget", type=int, default=16)
     args = ap.parse_args()
+    if args.steps < 1 or args.budget < 1:
+        ap.error("--steps and --budget are 1 or more")
     gen = torch.Generator(device="cuda").manual_seed(0)
-    hidden, heads, kv, ffn, page, seqs, cols = 512, 8, 2, 1408, 8, 3, 8
+    hidden, heads, kv, ffn, page, seqs = 512, 8, 2, 1408, 8, 3
+    cols = -(-min(args.steps, args.budget + 1) // page)   # pages for the most tokens that a sequence has before an eviction
     blocks = [Block(hidden, heads, kv, ffn, 8, gen, seqs * cols, page, seqs, cols) for _ in range(2)]
     w_last = torch.ones(hidden, dtype=torch.float16, device="cuda")
     table = torch.randperm(seqs * cols, generator=gen, device="cuda").int().view(seqs, cols)
-    rot = rotation(4096, hidden // heads)
+    rot = rotation(args.steps, hidden // heads)
     lens, seen = torch.zeros(seqs, dtype=torch.int32, device="cuda"), torch.zeros(seqs, dtype=torch.int32, device="cuda")
     longest = 0
     for step in range(args.steps):
