@@ -398,7 +398,8 @@ int qeft_attn_decode(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, c
  * (each the same array as score / pos, or one that does not overlap it; pitch ld_out) receive the entries of slots < min(lens, budget), lens_out
  * (int32 [seqs], may be lens) that number; entries behind it keep their values.  Sequences within the budget keep everything.
  * lens is clamped to 0 .. min(longest, table_pages * page_size); ld >= that bound, ld_out >= min(that, budget).
- * Rows are seqs * kv_heads; table entries of moved tokens are clamped to the pool; pages must not be shared between sequences.
+ * Rows are seqs * kv_heads; pages must not be shared between sequences.  Table entries of tokens that move are clamped to the pool; a freed slot
+ * whose entry is out of range gets its token's score and position, and keys and values are stored nowhere.
  * ws: qeft_evict_workspace bytes, 16-byte aligned. */
 size_t qeft_evict_workspace(const qeft_cache_desc_t* desc, int64_t seqs, int64_t longest, int64_t budget);
 typedef struct {

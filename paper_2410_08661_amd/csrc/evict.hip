@@ -63,11 +63,12 @@ __device__ __forceinline__ Row row_at(const Cache& c, const Evict& a, int row) {
     return r;
 }
 
-// Where token t's row begins, in either pool
+// Where token t's row begins, in either pool.  A page out of range is clamped to be read from, and nothing is written to it: OUT gives a place below 0.
+template <bool OUT>
 __device__ __forceinline__ int64_t slot_at(const Cache& c, int b, int h, int t) {
-    const int p = c.by_page.of(t);
-    const int page = min(max(c.table[(size_t)b * c.ld_table + p], 0), c.pages - 1);
-    return (int64_t)page * c.page_stride + h * c.head_stride + (t - p * c.page_size) * c.token_stride;
+    const int p = c.by_page.of(t), named = c.table[(size_t)b * c.ld_table + p], page = min(max(named, 0), c.pages - 1);
+    const int64_t at = (int64_t)page * c.page_stride + h * c.head_stride + (t - p * c.page_size) * c.token_stride;
+    return OUT && named != page ? -1 : at;
 }
 
 // What changes in a row: a bit a token, set for freed slots below row.left and for kept tokens behind it, and before every word of 64 the number of bits
@@ -130,8 +131,8 @@ __device__ __forceinline__ void make_moves(const Cache& c, const Row& r, const C
 #pragma unroll
         for (int y = 0; y < AT_ONCE; ++y) {
             const int i = min(i0 + y * groups, count - 1);
-            from_at[y] = slot_at(c, r.b, r.h, l.src[i]);
-            to_at[y] = slot_at(c, r.b, r.h, l.dst[i]);
+            from_at[y] = slot_at<false>(c, r.b, r.h, l.src[i]);
+            to_at[y] = slot_at<true>(c, r.b, r.h, l.dst[i]);
         }
         for (int x = 8 * (tid & 15); x < c.d; x += 128) {
             u4 k[AT_ONCE], v[AT_ONCE];
@@ -143,7 +144,7 @@ __device__ __forceinline__ void make_moves(const Cache& c, const Row& r, const C
             }
 #pragma unroll
             for (int y = 0; y < AT_ONCE; ++y) {
-                if (i0 + y * groups >= count) continue;
+                if (i0 + y * groups >= count || to_at[y] < 0) continue;
                 *reinterpret_cast<u4*>(c.k + to_at[y] + x) = k[y];
                 *reinterpret_cast<u4*>(c.v + to_at[y] + x) = v[y];
             }
@@ -268,13 +269,15 @@ __device__ __forceinline__ void evict_few(const Cache& c, const Row& r, const ui
         if (lower == rank) to = gone[i];
     }
     if (to < 0) return;
-    __half* p = (tid & 16 ? c.v : c.k) + slot_at(c, r.b, r.h, to) + 8 * (tid & 15);
-    if (8 * (tid & 15) < c.d) *reinterpret_cast<u4*>(p) = carried[0];
-    if (8 * (tid & 15) + 128 < c.d) *reinterpret_cast<u4*>(p + 128) = carried[1];
     if ((tid & 31) == 0) {
         r.score_out[to] = carried_score;
         r.pos_out[to] = carried_pos;
     }
+    const int64_t at = slot_at<true>(c, r.b, r.h, to);
+    if (at < 0) return;
+    __half* p = (tid & 16 ? c.v : c.k) + at + 8 * (tid & 15);
+    if (8 * (tid & 15) < c.d) *reinterpret_cast<u4*>(p) = carried[0];
+    if (8 * (tid & 15) + 128 < c.d) *reinterpret_cast<u4*>(p + 128) = carried[1];
 }
 
 // Workgroup = a row of at most 4 J blockDim.x tokens.  VEC: rows start on 16 bytes.  all_bits: where the bits go, [rows][words], or NULL: no row has more than TILE to go.
@@ -301,7 +304,7 @@ __global__ __launch_bounds__(1024, J == 1 ? 8 : 4) void evict_select_kernel(Cach
     int carried_pos = 0;
     if (few && (tid >> 5) < go) {
         const int token = left + (tid >> 5);
-        const __half* p = (tid & 16 ? c.v : c.k) + slot_at(c, r.b, r.h, token) + 8 * (tid & 15);
+        const __half* p = (tid & 16 ? c.v : c.k) + slot_at<false>(c, r.b, r.h, token) + 8 * (tid & 15);
         if (8 * (tid & 15) < c.d) carried[0] = *reinterpret_cast<const u4*>(p);
         if (8 * (tid & 15) + 128 < c.d) carried[1] = *reinterpret_cast<const u4*>(p + 128);
         carried_score = r.score[token];

@@ -243,3 +243,38 @@ def test_calls_without_the_native_module_give_the_same(monkeypatch):
         plain = all_of_it()
     for a, b in zip(native, plain):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("seqs,n,budget", [(3, 70, 67), (3, 150, 60), (3, 900, 500), (2, 33000, 20000), (700, 33000, 40)])
+def test_evict_stores_nothing_in_pages_that_are_out_of_range(seqs, n, budget):
+    """Few to go, moves by the workgroup itself, by a second launch, of rows by many workgroups and of long rows by one: slots freed in pages that are not the pool's."""
+    kv, d, page = 1, 8, 10
+    cols = -(-n // page)
+    own, lens = min(seqs, 3), [n] * 3 + [5] * seqs
+    lens, pages = lens[:seqs], own * cols + 2                     # (the first page and the last are no sequence's; short sequences, within the budget, name any)
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    K, V = (torch.randn((pages, kv, page, d), generator=gen, device="cuda").half() for _ in range(2))
+    table = torch.ones((seqs, cols), dtype=torch.int32, device="cuda")
+    table[:own] = (1 + torch.randperm(own * cols, generator=gen, device="cuda")).int().view(own, cols)
+    bad = torch.tensor([-1, pages, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda")
+    table[0, 0], table[1, 1:5] = bad[0], bad
+    table[0, -1] = bad[0] if own > 1 else table[0, -1]            # and a source, which is read from the first page
+    score = torch.rand((seqs, kv, n), generator=gen, device="cuda")
+    score[:, :, : budget // 2] *= 0.1                             # most that go are in the first slots
+    pos = torch.arange(n, device="cuda").int().expand(seqs, kv, n).contiguous()
+    cache = B.Cache(B.make_cache_desc(pages, page, kv, d), k=K.clone(), v=V.clone())
+    dev_lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    so, po = score.clone(), pos.clone()
+    _, _, left = B.qeft_cache_evict(cache, table, dev_lens, n, budget, so, po, dev_lens)
+    skipped = 0
+    for b in range(own):
+        at = torch.tensor(U.evicted(score[b, 0].tolist(), pos[b, 0].tolist(), n, n, budget, 0, 0), device="cuda")
+        dst = torch.arange(budget, device="cuda")
+        assert torch.equal(so[b, 0, :budget], score[b, 0, at]) and torch.equal(po[b, 0, :budget], pos[b, 0, at])
+        to, src = table[b].long()[dst // page], table[b].long().clamp(0, pages - 1)[at // page]
+        stored = (at != dst) & (to >= 0) & (to < pages)
+        skipped += int(((at != dst) & ~stored).sum())
+        for pool in (K, V):
+            pool[to[stored], 0, dst[stored] % page] = pool[src[stored], 0, at[stored] % page]
+    assert skipped > 0 and left.tolist() == [min(x, budget) for x in lens]
+    assert torch.equal(cache.k, K) and torch.equal(cache.v, V)
