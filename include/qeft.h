@@ -344,7 +344,7 @@ typedef struct {
  * values of a head (rot_dim even, at most head_dim) are pairs rot_dim / 2 apart: (a, b) -> (a c - b s, b c + a s), in fp32, rounded
  * once.  Position of token t: pos[t], or index[t] where pos is NULL, clamped to 0 .. positions - 1.  rot_dim == 0: no rotation.
  * A token whose sequence, index or page is out of range is not stored (its q is rotated all the same).  Two tokens of one
- * call for the same slot: either may end up there. */
+ * call for the same slot: each of the slot's values is one of theirs. */
 typedef struct {
     const void *q, *k, *v;
     void* q_out;
@@ -369,8 +369,8 @@ int qeft_cache_append(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, 
  * score (optional, fp32 [seqs][kv_heads][ld_score], ld_score >= min(longest, table_pages * page_size)): the weight of every
  * token, sum of p[t] over the query heads of the kv head, is written there, or added if accumulate != 0; entries behind the
  * length keep their values.
- * ws: qeft_attn_workspace bytes, 16-byte aligned (QEFT_ERR_WORKSPACE otherwise; 0 bytes: NULL).  The results do not depend on the
- * order in which workgroups run. */
+ * ws: qeft_attn_workspace bytes (fewer: QEFT_ERR_WORKSPACE; 0 bytes: NULL will do), 16-byte aligned (QEFT_ERR_ALIGN).  The results do not
+ * depend on the order in which workgroups run. */
 size_t qeft_attn_workspace(const qeft_cache_desc_t* desc, int64_t seqs, int32_t heads, int64_t longest, int weights);
 typedef struct {
     const int32_t* lens;
@@ -396,7 +396,8 @@ int qeft_attn_decode(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, c
  * stays; -0 equals +0; not-a-number ranks above infinity.  Kept tokens in slots < budget stay where they are; the i-th kept token of
  * the others (in slot order) moves, keys, values, score and position, into the i-th freed slot.  score_out and pos_out
  * (each the same array as score / pos, or one that does not overlap it; pitch ld_out) receive the entries of slots < min(lens, budget), lens_out
- * (int32 [seqs], may be lens) that number; entries behind it keep their values.  Sequences within the budget keep everything.
+ * (int32 [seqs]) that number; entries behind it keep their values.  lens_out may not overlap lens or seen (QEFT_ERR_UNSUPPORTED): every head of a sequence
+ * reads those.  Sequences within the budget keep everything.
  * lens is clamped to 0 .. min(longest, table_pages * page_size); ld >= that bound, ld_out >= min(that, budget).
  * Rows are seqs * kv_heads; pages must not be shared between sequences.  Table entries of tokens that move are clamped to the pool; a freed slot
  * whose entry is out of range gets its token's score and position, and keys and values are stored nowhere.
@@ -432,7 +433,7 @@ int qeft_cache_evict(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, c
  * dr of residual dtype (may be dh), dy fp16 (may be dx), dw_pre, dw_post fp32 [n]; dgate fp32 [n] (CHANNEL) or fp16 [m][ldg] (TOKEN).
  * Every gradient may be NULL (not computed).  accumulate != 0 adds dw_pre, dw_post and a CHANNEL gate's dgate to what is there.  Sums over rows are
  * taken in a fixed order.  m == 0: a no-op, but for the sums, which are set to zero unless accumulated.
- * ws: qeft_norm_workspace bytes, 16-byte aligned, needed where one of those sums is asked for. */
+ * ws: qeft_norm_workspace bytes, 16-byte aligned, needed where one of those sums is asked for, and for rows of more than 16384 values in any case. */
 enum { QEFT_GATE_NONE = 0, QEFT_GATE_CHANNEL = 1, QEFT_GATE_TOKEN = 2 };
 typedef struct {
     int32_t n, residual_dtype, gate;
