@@ -288,17 +288,13 @@ inline int dxp_tiles(const Layer& L, int c) { return ceil_div(L.kq, c) + ceil_di
 
 template <int NI, int J, bool ONCE>
 hipError_t launch(const Layer& L, const __half* dY, int64_t M, int64_t lddy, __half* dX, int64_t lddx, hipStream_t s, WeakGrad* g) {
-    static bool attr = false;
     constexpr int KS = 8, LDS_BYTES = KS * dxp_piece(NI, J) > WG_LDS ? KS * dxp_piece(NI, J) : WG_LDS;
-    if (!attr) {
-        hipError_t e = hipFuncSetAttribute((const void*)dx_panel_kernel<NI, J, ONCE>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);
-        if (e != hipSuccess) return e;
-        attr = true;
-    }
+    hipError_t e = allow_lds((const void*)dx_panel_kernel<NI, J, ONCE>, LDS_BYTES, LDS_BYTES);
+    if (e != hipSuccess) return e;
     const int tn = dxp_tiles(L, 32 * NI), tm = ceil_div(M, 32 * J);
     const Strips D = make_strips(g, dY, M, lddy, g ? g->used : 0);
     dx_panel_kernel<NI, J, ONCE><<<8 * ceil_div((int64_t)tn * tm, 8) + D.n, 64 * KS, LDS_BYTES, s>>>(L, dY, (int)M, lddy, dX, lddx, tn, tm, D);
-    const hipError_t e = hipGetLastError();
+    e = hipGetLastError();
     return e == hipSuccess ? finish_strips(g, D, s) : e;
 }
 

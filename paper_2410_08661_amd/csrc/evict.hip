@@ -755,14 +755,9 @@ template <int J, bool VEC>
 hipError_t select_rows(const Cache& c, const Evict& a, const Bits& x, int rows, int threads, hipStream_t s) {
     constexpr int HISTOGRAM = BINS * COPIES<J> * sizeof(int);
     const int lds = a.longest - a.budget > FEW ? HISTOGRAM : 0;   // (else no row of this call has more to go)
-    static bool raised = false;
-    if (lds >= 32 * 1024 && !raised) {   // (with what else the kernel holds, 64 KB are too much by default)
-        const hipError_t e = hipFuncSetAttribute((const void*)evict_select_kernel<J, VEC>, hipFuncAttributeMaxDynamicSharedMemorySize, HISTOGRAM);
-        if (e != hipSuccess) return e;
-        raised = true;
-    }
-    evict_select_kernel<J, VEC><<<rows, threads, lds, s>>>(c, a, x.bits, x.below, x.words);
-    return hipSuccess;
+    const hipError_t e = allow_lds((const void*)evict_select_kernel<J, VEC>, lds, HISTOGRAM);
+    if (e == hipSuccess) evict_select_kernel<J, VEC><<<rows, threads, lds, s>>>(c, a, x.bits, x.below, x.words);
+    return e;
 }
 template <int J>
 hipError_t select_with(const Cache& c, const Evict& a, const Bits& x, int rows, int threads, bool vec, hipStream_t s) {

@@ -1237,13 +1237,6 @@ __global__ __launch_bounds__(256) void weak_grad_reduce_kernel(const float* __re
     }
 }
 
-hipError_t raise_lds_limit(const void* fn, bool& done) {
-    if (done) return hipSuccess;
-    hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, GEMM_LDS);
-    if (e == hipSuccess) done = true;
-    return e;
-}
-
 }  // namespace
 
 // The tiled kernels round every dequantized weight once to fp16 (relative 2^-11).  Over a long contraction these
@@ -1384,14 +1377,10 @@ hipError_t gemm_fwd(const Layer& L, const __half* X, int64_t M, int64_t ldx, __h
                          gemm_fwd_rega_kernel<7, ONCE>, gemm_fwd_rega_kernel<8, ONCE>}
         static const Kern table[2][5] = {QEFT_REGA(false), QEFT_REGA(true)};
 #undef QEFT_REGA
-        static bool attr[2][5] = {};
         const int rows = ceil_div(M, tiles_m), j = rows <= 128 ? 4 : ceil_div(rows, 32);
         const Kern kern = table[L.once][j - 4];
-        if (!attr[L.once][j - 4]) {
-            e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, REGA_LDS);
-            if (e != hipSuccess) return e;
-            attr[L.once][j - 4] = true;
-        }
+        e = allow_lds((const void*)kern, REGA_LDS, REGA_LDS);
+        if (e != hipSuccess) return e;
         const int tiles = tiles_oc * tiles_m;
         const int wide = (ldy % 8 == 0) && (reinterpret_cast<uintptr_t>(Y) % 16 == 0);
         const SplitPlan p = ws ? gemm_fwd_plan(L, M) : SplitPlan();
@@ -1405,8 +1394,7 @@ hipError_t gemm_fwd(const Layer& L, const __half* X, int64_t M, int64_t ldx, __h
         }
         kern<<<xcd_grid(tiles), 256, REGA_LDS, s>>>(L, X, (int)M, ldx, Y, ldy, tiles_oc, wide, 1, 0, 0, nullptr);
     } else {
-        static bool attr = false;
-        e = raise_lds_limit((const void*)gemm_fwd_kernel, attr);
+        e = allow_lds((const void*)gemm_fwd_kernel, GEMM_LDS, GEMM_LDS);
         if (e != hipSuccess) return e;
         gemm_fwd_kernel<<<xcd_grid(tiles_oc * tiles_m), 256, GEMM_LDS, s>>>(L, X, (int)M, ldx, Y, ldy, tiles_oc);
     }
@@ -1442,13 +1430,9 @@ hipError_t gemm_dx(const Layer& L, const __half* dY, int64_t M, int64_t lddy, __
     const int tiles_m = ceil_div(M, BT), tiles_ic = ceil_div(in_registers ? dx_columns(L) : L.ic, BT);
     hipError_t e;
     if (in_registers) {
-        static bool attr[2] = {};
         const auto kern = L.once ? gemm_dx_rega_kernel<true> : gemm_dx_rega_kernel<false>;
-        if (!attr[L.once]) {
-            e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, DX_LDS);
-            if (e != hipSuccess) return e;
-            attr[L.once] = true;
-        }
+        e = allow_lds((const void*)kern, DX_LDS, DX_LDS);
+        if (e != hipSuccess) return e;
         const int tiles = tiles_ic * tiles_m;
         const SplitPlan p = ws ? gemm_dx_plan(L, M) : SplitPlan();
         if (p.splits > 1) {
@@ -1458,12 +1442,8 @@ hipError_t gemm_dx(const Layer& L, const __half* dY, int64_t M, int64_t lddy, __
             const int n_sum = 32 * split_tail_tiles(tiles, p.tail_first);
             const Strips S = make_strips(g, dY, M, lddy, g ? (size_t)((unsigned char*)ws - g->ws) + split_workspace(tiles, p) : 0);
             if (S.n > 0) {
-                static bool dw_attr = false;
-                if (!dw_attr) {
-                    e = hipFuncSetAttribute((const void*)splitk_reduce_dw_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, WG_LDS);
-                    if (e != hipSuccess) return e;
-                    dw_attr = true;
-                }
+                e = allow_lds((const void*)splitk_reduce_dw_kernel, wg_lds(S.kw), WG_LDS);
+                if (e != hipSuccess) return e;
                 splitk_reduce_dw_kernel<<<S.n + n_sum, 256, wg_lds(S.kw), s>>>(part, p.splits, tiles, tiles_ic, p.tail_first, (int)M, L.ic, dX, lddx, S);
                 e = hipGetLastError();
                 return e == hipSuccess ? finish_strips(g, S, s) : e;
@@ -1478,8 +1458,7 @@ hipError_t gemm_dx(const Layer& L, const __half* dY, int64_t M, int64_t lddy, __
         }
         kern<<<xcd_grid(tiles), 256, DX_LDS, s>>>(L, dY, (int)M, lddy, dX, lddx, tiles_ic, 1, 0, 0, nullptr);
     } else {
-        static bool attr = false;
-        e = raise_lds_limit((const void*)gemm_dx_kernel, attr);
+        e = allow_lds((const void*)gemm_dx_kernel, GEMM_LDS, GEMM_LDS);
         if (e != hipSuccess) return e;
         gemm_dx_kernel<<<xcd_grid(tiles_ic * tiles_m), 256, GEMM_LDS, s>>>(L, dY, (int)M, lddy, dX, lddx, tiles_ic, 0);
     }
@@ -1500,14 +1479,10 @@ hipError_t weak_grad_mfma(int oc, int k, const __half* dY, int64_t M, int64_t ld
     if (!strip_offsets_fit(lddy) || !strip_offsets_fit(ldxw)) return weak_grad_generic(oc, k, dY, M, lddy, Xw, ldxw, dW, out_f32, accumulate, s);
     const StripPlan p = weak_grad_strip_split(oc, k, M);
     const auto kern = p.kw == 128 ? weak_grad_strip_kernel<128> : weak_grad_strip_kernel<64>;
-    static bool strip_attr[2] = {};
-    if (!strip_attr[p.kw == 128]) {
-        hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, wg_lds(p.kw));
-        if (e != hipSuccess) return e;
-        strip_attr[p.kw == 128] = true;
-    }
+    hipError_t e = allow_lds((const void*)kern, wg_lds(p.kw), wg_lds(p.kw));
+    if (e != hipSuccess) return e;
     kern<<<p.workgroups(oc, k), 256, wg_lds(p.kw), s>>>(oc, k, dY, (int)M, lddy, Xw, ldxw, (float*)ws, p.splits, p.chunk, dW, out_f32, accumulate);
-    hipError_t e = hipGetLastError();
+    e = hipGetLastError();
     return e == hipSuccess && p.splits > 1 ? weak_grad_reduce((const float*)ws, p.splits, (int64_t)oc * k, dW, out_f32, accumulate, s) : e;
 }
 hipError_t weak_grad_reduce(const float* part, int splits, int64_t n, void* dW, int out_f32, int accumulate, hipStream_t s) {
@@ -1529,14 +1504,10 @@ static bool gemm_dx_dw_preferred(const Strips& S) { return S.k <= 128; }
 
 static hipError_t gemm_dx_dw(const Layer& L, const __half* dY, int64_t M, int64_t lddy, __half* dX, int64_t lddx, const Strips& S, hipStream_t s) {
     const int tiles_ic = ceil_div(dx_columns(L), BT), n_dx = xcd_grid(tiles_ic * ceil_div(M, BT));
-    static bool attr[2] = {};
     constexpr int LDS_BYTES = DX_LDS > WG_LDS ? DX_LDS : WG_LDS;
     const auto kern = L.once ? gemm_dx_dw_kernel<true> : gemm_dx_dw_kernel<false>;
-    if (!attr[L.once]) {
-        hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);
-        if (e != hipSuccess) return e;
-        attr[L.once] = true;
-    }
+    const hipError_t e = allow_lds((const void*)kern, LDS_BYTES, LDS_BYTES);
+    if (e != hipSuccess) return e;
     kern<<<n_dx + S.n, 256, LDS_BYTES, s>>>(L, dY, (int)M, lddy, dX, lddx, tiles_ic, n_dx, S);
     return hipGetLastError();
 }

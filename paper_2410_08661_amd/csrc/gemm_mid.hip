@@ -506,14 +506,10 @@ __global__ __launch_bounds__(64 * mid_waves(MT, NT)) void fwd_mid_kernel(MidArgs
 
 template <int MT, int NT, Fmt F, int XR>
 hipError_t launch_mid(const MidArgs& A, int KS, hipStream_t s) {
-    static bool attr = false;
     const size_t lds_bytes = (size_t)KS * (mid_piece(MT, NT, F == W4) + NT * 128);
     if (lds_bytes > 160 * 1024) return hipErrorInvalidValue;
-    if (!attr) {
-        hipError_t e = hipFuncSetAttribute((const void*)fwd_mid_kernel<MT, NT, F, XR>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        if (e != hipSuccess) return e;
-        attr = true;
-    }
+    const hipError_t e = allow_lds((const void*)fwd_mid_kernel<MT, NT, F, XR>, lds_bytes, 160 * 1024);
+    if (e != hipSuccess) return e;
     fwd_mid_kernel<MT, NT, F, XR><<<8 * ceil_div((int64_t)A.n_tiles * A.tiles_m, 8), 64 * KS, lds_bytes, s>>>(A);
     return hipGetLastError();
 }

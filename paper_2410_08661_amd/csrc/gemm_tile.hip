@@ -699,13 +699,9 @@ constexpr int finish_lds() { return 2 * (KW - 1) * 2 * J * 4096; }
 
 template <int J, int KW, int MINW, bool ONCE>
 hipError_t launch_fwd(const Layer& L, const __half* X, int64_t M, int64_t ldx, __half* Y, int64_t ldy, hipStream_t s) {
-    static bool attr = false;
     constexpr int XL = KW * 2 * 32 * J * 128, LDS_BYTES = XL > finish_lds<J, KW>() ? XL : finish_lds<J, KW>();
-    if (!attr) {
-        hipError_t e = hipFuncSetAttribute((const void*)fwd_tile_kernel<J, KW, MINW, ONCE>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);
-        if (e != hipSuccess) return e;
-        attr = true;
-    }
+    const hipError_t e = allow_lds((const void*)fwd_tile_kernel<J, KW, MINW, ONCE>, LDS_BYTES, LDS_BYTES);
+    if (e != hipSuccess) return e;
     const int tn = ceil_div(L.oc, 128), tm = ceil_div(M, 32 * J);
     Layer A = L;
     if (A.k == 0) A.weak = reinterpret_cast<const __half*>(A.qweight);   // requests whose result is not used
@@ -715,19 +711,15 @@ hipError_t launch_fwd(const Layer& L, const __half* X, int64_t M, int64_t ldx, _
 
 template <int J, int KW, int MINW, bool ONCE, bool RAGGED>
 hipError_t launch_dx(const Layer& L, const __half* dY, int64_t M, int64_t lddy, __half* dX, int64_t lddx, hipStream_t s, WeakGrad* g) {
-    static bool attr = false;
     constexpr int XT = 32 * J * 128, QL = KW * (2 * XT + 2 * 4096 + 2 * (ONCE ? 384 : 256)), WL = KW * 2 * (XT / 2 + 32 * 272);
     constexpr int A = QL > WL ? QL : WL, LDS_BYTES = A > finish_lds<J, KW>() ? A : finish_lds<J, KW>();
     static_assert(LDS_BYTES <= 160 * 1024 && LDS_BYTES >= WG_LDS, "");
-    if (!attr) {
-        hipError_t e = hipFuncSetAttribute((const void*)dx_tile_kernel<J, KW, MINW, ONCE, RAGGED>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);
-        if (e != hipSuccess) return e;
-        attr = true;
-    }
+    hipError_t e = allow_lds((const void*)dx_tile_kernel<J, KW, MINW, ONCE, RAGGED>, LDS_BYTES, LDS_BYTES);
+    if (e != hipSuccess) return e;
     const int tn = dx_tiles(L), tm = ceil_div(M, 32 * J);
     const Strips D = make_strips(g, dY, M, lddy, g ? g->used : 0);
     dx_tile_kernel<J, KW, MINW, ONCE, RAGGED><<<xcd_grid(tn * tm) + D.n, 128 * KW, LDS_BYTES, s>>>(L, dY, (int)M, lddy, dX, lddx, tn, tm, D);
-    const hipError_t e = hipGetLastError();
+    e = hipGetLastError();
     return e == hipSuccess ? finish_strips(g, D, s) : e;
 }
 

@@ -933,17 +933,13 @@ bool launch_small(const Layer& L, int tiles, const GroupTail& tail, const int* p
         {QEFT_SMALL_ROW(true, 4, 1, false), QEFT_SMALL_ROW(true, 8, 1, false), QEFT_SMALL_ROW(true, 8, 2, false), QEFT_SMALL_ROW(true, 4, 4, false)},
         {QEFT_SMALL_ROW(false, 4, 1, true), QEFT_SMALL_ROW(false, 8, 1, true), QEFT_SMALL_ROW(false, 8, 2, true), QEFT_SMALL_ROW(false, 4, 4, true)}};
 #undef QEFT_SMALL_ROW
-    static bool attr_set[3][4][3] = {};
     const int nj_max = 4 * ceil_div(units, ks);
     const int wi = wmax <= 1 ? (nj_max <= 4 ? 0 : 1) : (wmax <= 2 ? 2 : 3), si = nsz - 1;
     if (L.dense && perm) return false;   // no gathering variant for 3-bit codes
     const int pi = L.dense ? 2 : (perm ? 1 : 0);
     const Kern kern = table[pi][wi][si];
-    if (!attr_set[pi][wi][si]) {
-        *err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, SMALL_LDS_LIMIT);
-        if (*err != hipSuccess) return true;
-        attr_set[pi][wi][si] = true;
-    }
+    *err = allow_lds((const void*)kern, ld.total, SMALL_LDS_LIMIT);
+    if (*err != hipSuccess) return true;
     kern<<<ceil_div(tiles, tw), 64 * ks * tw, ld.total, s>>>(L, X, M, ldx, Y, ldy, ld, ks, ceil_div(65536, ks), tail, perm);
     *err = hipGetLastError();
     return true;
@@ -1009,13 +1005,9 @@ bool launch_regs(const Layer* Ls, int n, const __half* X, int M, int64_t ldx, __
                                gemv_w4_regs_kernel<S, 2, 4, XM, 8, MU>, gemv_w4_regs_kernel<S, 2, 6, XM, 8, MU>, gemv_w4_regs_kernel<S, 2, 8, XM, 8, MU>}
     static const Kern table[2][2][6] = {{QEFT_REGS_ROW(8, false), QEFT_REGS_ROW(16, false)}, {QEFT_REGS_ROW(8, true), QEFT_REGS_ROW(16, true)}};
 #undef QEFT_REGS_ROW
-    static bool attr_set[2][2][6] = {};
     const Kern kern = table[passes > 1 ? 1 : 0][xi][ti];
-    if (lds_bytes > 64 * 1024 && !attr_set[passes > 1 ? 1 : 0][xi][ti]) {
-        *err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024);
-        if (*err != hipSuccess) return true;
-        attr_set[passes > 1 ? 1 : 0][xi][ti] = true;
-    }
+    *err = allow_lds((const void*)kern, lds_bytes, 128 * 1024);
+    if (*err != hipSuccess) return true;
     kern<<<grid, 64 * ks, lds_bytes, s>>>(A, passes);
     *err = hipGetLastError();
     return true;

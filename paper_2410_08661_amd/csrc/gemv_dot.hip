@@ -765,10 +765,8 @@ hipError_t gemv_dot_fwd(const Layer* Ls, int n, const int* perm, const __half* X
     const int blocks = ceil_div(sets, DOT_WAVES >> p.ks_log2);
     if (L.dense && perm) return hipSuccess;   // no gathering variant for 3-bit codes
     const DotKern kern = L.dense ? dot_kernel<false, true>(p.nscw, p.nkw) : (perm ? dot_kernel<true, false>(p.nscw, p.nkw) : dot_kernel<false, false>(p.nscw, p.nkw));
-    if (p.lds > 64 * 1024) {   // (rows of more than 24 K columns; idempotent, so set on every such launch)
-        hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024);
-        if (e != hipSuccess) return e;
-    }
+    const hipError_t e = allow_lds((const void*)kern, p.lds, 80 * 1024);   // (rows of more than 24 K columns)
+    if (e != hipSuccess) return e;
     kern<<<blocks, DOT_THREADS, p.lds, s>>>(R, L.kq, L.k, 4 * L.stride, L.gs, X, perm, L.ic, p.B, p.ks_log2);
     *handled = true;
     return hipGetLastError();

@@ -672,26 +672,24 @@ BwdPlan bwd_plan(int n, int64_t m) {
 }
 
 template <int V, bool F32, bool POST, int GATE>
-void launch_gate(const Norm& a, const Sums& S, const BwdPlan& p, int threads, size_t lds, hipStream_t s) {
-    static bool raised = false;
-    if (lds > 60 * 1024 && !raised) {   // (an error shows at the launch)
-        raised = hipFuncSetAttribute((const void*)norm_bwd_kernel<V, F32, POST, GATE>, hipFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024) == hipSuccess;
-    }
-    norm_bwd_kernel<V, F32, POST, GATE><<<p.grid, threads, lds, s>>>(a, S, p.waves, p.groups, p.rounds);
+hipError_t launch_gate(const Norm& a, const Sums& S, const BwdPlan& p, int threads, size_t lds, hipStream_t s) {
+    const hipError_t e = allow_lds((const void*)norm_bwd_kernel<V, F32, POST, GATE>, lds, 128 * 1024);
+    if (e == hipSuccess) norm_bwd_kernel<V, F32, POST, GATE><<<p.grid, threads, lds, s>>>(a, S, p.waves, p.groups, p.rounds);
+    return e;
 }
 template <int V, bool F32, bool POST>
-void launch_bwd(const Norm& a, const Sums& S, const BwdPlan& p, hipStream_t s) {
+hipError_t launch_bwd(const Norm& a, const Sums& S, const BwdPlan& p, hipStream_t s) {
     const int threads = 64 * p.waves * p.groups;
     const size_t lds = V > 1 ? (size_t)threads * (POST ? 2 : 1) * 8 * V * sizeof(float)
                              : (p.groups > 1 ? (size_t)threads * 8 * sizeof(float) : 0) + (POST ? 3 * 64 * (size_t)p.waves * sizeof(u4) : 0);
-    if (a.gate_kind == QEFT_GATE_CHANNEL) launch_gate<V, F32, POST, QEFT_GATE_CHANNEL>(a, S, p, threads, lds, s);
-    else if (a.gate_kind == QEFT_GATE_TOKEN) launch_gate<V, F32, POST, QEFT_GATE_TOKEN>(a, S, p, threads, lds, s);
-    else launch_gate<V, F32, POST, QEFT_GATE_NONE>(a, S, p, threads, lds, s);
+    if (a.gate_kind == QEFT_GATE_CHANNEL) return launch_gate<V, F32, POST, QEFT_GATE_CHANNEL>(a, S, p, threads, lds, s);
+    if (a.gate_kind == QEFT_GATE_TOKEN) return launch_gate<V, F32, POST, QEFT_GATE_TOKEN>(a, S, p, threads, lds, s);
+    return launch_gate<V, F32, POST, QEFT_GATE_NONE>(a, S, p, threads, lds, s);
 }
 template <int V>
-void launch_bwd_of(const Norm& a, const Sums& S, const BwdPlan& p, hipStream_t s) {
-    if (a.f32) a.w_post ? launch_bwd<V, true, true>(a, S, p, s) : launch_bwd<V, true, false>(a, S, p, s);
-    else a.w_post ? launch_bwd<V, false, true>(a, S, p, s) : launch_bwd<V, false, false>(a, S, p, s);
+hipError_t launch_bwd_of(const Norm& a, const Sums& S, const BwdPlan& p, hipStream_t s) {
+    if (a.f32) return a.w_post ? launch_bwd<V, true, true>(a, S, p, s) : launch_bwd<V, true, false>(a, S, p, s);
+    return a.w_post ? launch_bwd<V, false, true>(a, S, p, s) : launch_bwd<V, false, false>(a, S, p, s);
 }
 
 template <int V>
@@ -742,8 +740,8 @@ hipError_t norm_bwd(const Norm& a, hipStream_t s) {
     for (int i = 0; i < 3; ++i)
         if (outs[i]) S.slab[i] = one ? outs[i] : (float*)(a.ws + p.at_slabs + i * p.slab_bytes);
     if (p.in_registers) {
-        if (p.v == 1) launch_bwd_of<1>(a, S, p, s);
-        else launch_bwd_of<2>(a, S, p, s);
+        const hipError_t e = p.v == 1 ? launch_bwd_of<1>(a, S, p, s) : launch_bwd_of<2>(a, S, p, s);
+        if (e != hipSuccess) return e;
     } else {
         RowStat* stats = (RowStat*)a.ws;
         const dim3 grid((a.n + 2047) / 2048, p.grid);

@@ -27,6 +27,12 @@ struct Layer {
 
 inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
+// Before a launch with `used` bytes of dynamic LDS: beyond the 64 KB that a launch gets by default, a kernel's own arrays included, they have to be allowed, `most`
+// for every launch of that kernel.  The allowance is the current device's, so it is given each time: 70 ns, as asking which device that is would take.
+inline hipError_t allow_lds(const void* kernel, size_t used, int most) {
+    return used > 32 * 1024 ? hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, most) : hipSuccess;
+}
+
 // Code of column j of a row of packed words, either layout (the plain definition: conversion and fallback kernels).
 __device__ __forceinline__ uint32_t code_at(const Layer& L, const uint32_t* __restrict__ row, int j) {
     if (L.dense) {
