@@ -289,9 +289,7 @@ int qeft_norm_bwd(const qeft_norm_desc_t* desc, const qeft_norm_bwd_t* a, void* 
         CHECK(check_norm_weights(desc, a->w_pre, a->w_post, a->gate, a->y, a->ldg, a->m));
         if ((a->dy && !a->y) || (a->dw_post && !a->w_post) || (a->dgate && !a->gate)) return QEFT_ERR_NULL;
         if (desc->gate == QEFT_GATE_TOKEN) CHECK(check_optional(a->dgate, a->m, a->lddg, desc->n));
-        // only rows too long for registers need the workspace for anything but the sums
-        const size_t need = sums || desc->n > 16384 ? norm_workspace(desc->n, a->m) : 0;
-        CHECK(check_workspace(a->ws, a->ws_bytes, need));
+        CHECK(check_workspace(a->ws, a->ws_bytes, norm_bwd_workspace(desc->n, a->m, sums)));
     }
     if (!aligned16(a->dw_pre) || !aligned16(a->dw_post) || !aligned16(a->dgate)) return QEFT_ERR_ALIGN;
     Norm p{};

@@ -724,6 +724,7 @@ size_t norm_workspace(int n, int64_t m) {
     const BwdPlan p = bwd_plan(n, m);
     return p.at_slabs + 3 * p.slab_bytes;
 }
+size_t norm_bwd_workspace(int n, int64_t m, bool sums) { return sums || n > BWD_MAX ? norm_workspace(n, m) : 0; }   // (rows too long for registers leave their statistics there)
 
 hipError_t norm_bwd(const Norm& a, hipStream_t s) {
     float* gate = a.gate_kind == QEFT_GATE_CHANNEL ? (float*)a.dgate : nullptr;

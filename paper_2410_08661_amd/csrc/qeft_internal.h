@@ -264,6 +264,7 @@ struct Norm {                // either direction: what a call does not have is N
 };
 hipError_t norm_fwd(const Norm& a, hipStream_t s);   // (norm.hip)
 size_t norm_workspace(int n, int64_t m);
+size_t norm_bwd_workspace(int n, int64_t m, bool sums);   // that, or 0 where a call without sums over rows uses none of it
 hipError_t norm_bwd(const Norm& a, hipStream_t s);
 
 }  // namespace qeft

@@ -192,3 +192,19 @@ def test_backward_with_no_eps(m, n, f32, post, gate):
     h, x = B.qeft_norm_fwd(desc, i["r"], i["w_pre"], y=i["y"], w_post=i["w_post"], gate=i["gate"])
     _, want = U.norm_forward(h, None, i["w_pre"], None, None, 1.0, 0.0)
     U.close("x", x, want, 2 * U.sums_rounding(n) * want.abs(), U.HALF)
+
+
+@pytest.mark.parametrize("n", [16384, 16385])
+def test_backward_without_sums_and_without_a_workspace(n):
+    """Rows that fit the registers need none; longer ones are refused without it."""
+    i = inputs(3, n, False, False, "none")
+    desc = B.make_norm_desc(n, torch.float16, eps=EPS)
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    if n > 16384:
+        with pytest.raises(B.QeftError) as e:
+            B.qeft_norm_bwd(desc, i["dx"], i["r"], i["w_pre"], dw_pre=False, ws=none)
+        assert e.value.status == B.QEFT_ERR_WORKSPACE
+        none = torch.empty(B.qeft_norm_workspace(desc, 3), dtype=torch.uint8, device="cuda")
+    got = B.qeft_norm_bwd(desc, i["dx"], i["r"], i["w_pre"], dw_pre=False, ws=none)
+    want, bound = U.norm_backward(i["dx"], None, i["r"], None, i["w_pre"], None, None, 1.0, EPS, False)["dr"]
+    U.close("dr", got[0], want, bound, U.HALF)
