@@ -7,8 +7,8 @@
 //   dw_pre = sum dx hh     dw_post = sum du yh     dgate = scale u t
 //
 // Bytes bound both: a row stays in registers from its one load to its one store.  Rows of up to 512 values are a wave's (sums by shuffles); longer ones up to
-// 8192 have a thread per 8 values, so that a load is 16 or 32 bytes a lane; longer still two and four times 8 values a thread, and beyond REG_MAX
-// values the row is read again for each step.
+// 8192 have a thread per 8 values, so that a load is 16 or 32 bytes a lane; longer still two and (forward) four times 8 values a thread, and beyond FWD_MAX
+// or BWD_MAX values the row is read again for each step.
 // The gradient's workgroups stay for many rows: the column sums are kept in registers, a workgroup's row groups join theirs in LDS, and one slab per
 // workgroup goes to the workspace, summed by a second launch in a fixed order.  The next row's loads are issued before the current one's sums: a
 // CU has one or two workgroups and nothing else to hide them.

@@ -53,9 +53,6 @@ struct Sum {
 struct Least {
     template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return b < a ? b : a; }
 };
-struct Most {
-    template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return b > a ? b : a; }
-};
 
 // Over waves first .. first + waves - 1 of a workgroup (16 at most) from the values they left in slots[]; none: what an absent wave counts for.  The caller has a
 // barrier between the writes and this, and one between this and the next writes.
