@@ -12,7 +12,7 @@
 // What changes is a bit a token: freed slots before the budget, kept tokens behind it.  The i-th of the one takes the i-th of the other in, both counted off in
 // slot order.  Where a call has few to move the workgroup does that itself; else the bits go to the workspace and a second launch has a workgroup for every
 // 128 tokens behind the budget, which counts the bits before its own.
-// Bytes bound it: 16 a token for weights and positions, and 8 head_dim per token that moves.  16 x 32 rows of 2049 tokens, one to go: 5.8 us (latencies of one
+// Bytes bound it: 16 a token for weights and positions, and 8 head_dim per token that moves.  16 x 32 rows of 2049 tokens, one to go: 5.9 us (latencies of one
 // workgroup a row; the bytes alone 3.4); 8 rows, 32768 -> 4096: 24 us for the selection (loads 4, three digits 13, equal keys 1.6, bits 4: eight CUs), 10 for the moves.
 #include <algorithm>
 #include "qeft_internal.h"
