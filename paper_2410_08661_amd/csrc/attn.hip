@@ -4,8 +4,8 @@
 //
 // What bounds it: every cached byte is read once and used for 2 flops per query head of its kv head, so HBM for up to about a hundred heads per kv
 // head.  One pass: a wave takes 32 tokens at a time, keeps the running maximum m and sum l of its softmax and the unnormalised output, and rescales
-// those when a maximum grows by more than 1 in log2 (between, exponents are taken against the older maximum: p then is at most twice too large,
-// in numerator and denominator alike).
+// those when a maximum grows by more than 1 in log2 (between, p = 2^(x - m) is taken against the older maximum: it then is at most twice too large, in numerator and
+// denominator alike).
 //
 // Both products run on the matrix units for any number of heads (a single head uses one of 16 columns, which costs nothing a bandwidth-bound
 // kernel misses), on fragments that come straight from global memory:
@@ -13,9 +13,10 @@
 //                   the scores of head column c for the 8 consecutive tokens t0 + 8 grp ..: tile u's row r is token t0 + 8 (r >> 2) + 4 u + (r & 3).
 //   O = P V         those 8 probabilities are then the lane's piece of the left operand as they stand, without a shuffle.  V is read by rows (4 rows
 //                   of 256 bytes per load at head_dim 128) so that a lane holds 8 tokens x NV dimensions; one v_perm per register makes the columns.
-// P enters as hi + lo, two fp16 values rounded to nearest (22 bits): rounding it once would add half of the output's own rounding error again.  Exponents carry
-// an offset of 2^14, as large as fp16 holds beside the maximum's growth: the pair has its 22 bits down to p = 2^-16 of the largest, and is off by 2^-39 of the largest
-// at most below that (many tokens of little weight beside one of much must not vanish from O while l counts them).  The offset cancels in O / l.
+// P enters as hi + lo, two fp16 values rounded to nearest (22 bits): rounding it once would add half of the output's own rounding error again.  The pair is
+// of 2^14 p, as large as fp16 holds beside the maximum's growth: it has its 22 bits down to p = 2^-16 of the largest, and is off by 2^-39 of the largest
+// at most below that (many tokens of little weight beside one of much must not vanish from O while l counts them).  O's factor is taken out with l's.  (By a product, not in the
+// exponent: beside a maximum of 2^25 a difference of 14 is rounded, up to 16, which fp16 does not hold.)
 //
 // Work: a workgroup of 4 or 8 waves (one wave for a great many short rows) takes a chunk of one sequence's tokens for one kv head (16 query heads at a time; more heads read the chunk again, from
 // L2), joins its waves through LDS and writes out, or, where the sequence is cut in several chunks, m, l and O to the workspace for a second launch.
@@ -36,19 +37,17 @@ typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 
 constexpr int STEP = 32;                // tokens of a wave's step
-constexpr float OFFSET = 14.f;          // log2: exponents are taken against m - OFFSET
-constexpr float SLACK = 1.f;            // log2: growth of a maximum that is let pass without rescaling (2^(OFFSET + SLACK) is below fp16's largest)
+constexpr float FACTOR = 16384.f;       // of O, and of p in the product that makes it
+constexpr float SLACK = 1.f;            // log2: growth of a maximum that is let pass without rescaling (FACTOR 2^SLACK is below fp16's largest)
 constexpr float NEG_INF = -__builtin_inff();
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-// what exponents are taken against for a maximum of m (a maximum of -inf: every score so far was -inf, their weight is 0)
-__device__ __forceinline__ float base_of(float m) { return m == NEG_INF ? 0.f : m - OFFSET; }
 
-// Partial results of one (sequence, query head, chunk): base, l, and O[d], in arrays of their own.
+// Partial results of one (sequence, query head, chunk): m, l, and O[d], in arrays of their own.
 struct Partials {
-    float* base;   // [seqs][heads][chunks]
+    float* m;      // [seqs][heads][chunks]
     float* l;
-    float* o;      // [seqs][heads][chunks][d]
+    float* o;      // [seqs][heads][chunks][d], FACTOR times what it stands for
     float* raw;    // scores in log2 units, [seqs][heads][pitch] (only where weights are asked for)
     int64_t pitch;
     int chunks, chunk;
@@ -70,7 +69,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
     // (8 x 2000 tokens, 32 heads: 90 us against 125).
     constexpr bool Q_IN_LDS = DP == 256;
     __shared__ u4 sq[Q_IN_LDS ? KS : 1][64];
-    __shared__ float sm[WAVES][16], sl[WAVES][16], sL[16], sB[16];
+    __shared__ float sm[WAVES][16], sl[WAVES][16], sL[16], sM[16];
     __shared__ __align__(16) float so[WAVES][4][DP];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -232,14 +231,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
             }
             m = mx;
         }
-        const float base = base_of(m);
+        const float base = m == NEG_INF ? 0.f : m;   // (every score so far was -inf: their weight is 0)
         h8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
             const float p0 = exp2_fast(x[e] - base), p1 = exp2_fast(x[e + 1] - base);
             l += p0;
             l += p1;
-            const h2 h = __builtin_convertvector((f2{p0, p1}), h2), r = __builtin_convertvector((f2{p0 - (float)h.x, p1 - (float)h.y}), h2);
+            const h2 h = __builtin_convertvector((f2{p0 * FACTOR, p1 * FACTOR}), h2);
+            const h2 r = __builtin_convertvector((f2{fmaf(p0, FACTOR, -(float)h.x), fmaf(p1, FACTOR, -(float)h.y)}), h2);
             hi[e] = h.x, hi[e + 1] = h.y;
             lo[e] = r.x, lo[e + 1] = r.y;
         }
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
         sm[wave][lane] = m;
         sl[wave][lane] = l;
     }
-    const bool direct = ps.chunks == 1 && ps.base == nullptr;
+    const bool direct = ps.chunks == 1 && ps.m == nullptr;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (4 * i >= nh) break;   // heads 4 i .. 4 i + 3
@@ -289,18 +289,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
                     L += wl[w] == 0.f ? 0.f : wl[w] * f;
                     o = fmaf(wo[w], f, o);
                 }
-                const float base = base_of(M);
                 if (direct) {
-                    a.out[(size_t)b * a.ldo + (size_t)(head0 + h) * c.d + dim] = __float2half_rn(n > 0 ? o / L : 0.f);
+                    a.out[(size_t)b * a.ldo + (size_t)(head0 + h) * c.d + dim] = __float2half_rn(n > 0 ? o / (L * FACTOR) : 0.f);
                     if (dim == 0) {
-                        sB[r] = base;
+                        sM[r] = M;
                         sL[r] = L;
                     }
                 } else {
                     const size_t at = ((size_t)b * a.heads + head0 + h) * ps.chunks + chunk;
                     ps.o[at * c.d + dim] = o;
                     if (dim == 0) {
-                        ps.base[at] = base;
+                        ps.m[at] = M;
                         ps.l[at] = L;
                     }
                 }
@@ -315,28 +314,28 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_chunk_kernel(Cache c, Atte
             float w = 0.f;
             for (int h = 0; h < nh; ++h) {
                 const int at = 4 * (h & 3) + (h >> 2);
-                w += exp2_fast(rp[(size_t)h * ps.pitch + t] - sB[at]) / sL[at];
+                w += exp2_fast(rp[(size_t)h * ps.pitch + t] - sM[at]) / sL[at];
             }
             out[t] = a.accumulate ? out[t] + w : w;
         }
     }
 }
 
-// Base and sum of a query head over its used chunks (a wave's work; the same in every lane).
-__device__ __forceinline__ void join_stats(const Partials& ps, size_t at, int used, float& B, float& L) {
+// Maximum and sum of a query head over its used chunks (a wave's work; the same in every lane).
+__device__ __forceinline__ void join_stats(const Partials& ps, size_t at, int used, float& M, float& L) {
     const int lane = threadIdx.x & 63;
     // the first 64 chunks' are asked for before `used` is known
-    float l = 0.f, base = NEG_INF;
+    float l = 0.f, m = NEG_INF;
     if (lane < ps.chunks) {
         l = ps.l[at + lane];
-        base = ps.base[at + lane];
+        m = ps.m[at + lane];
     }
-    if (lane >= used || l == 0.f) base = NEG_INF, l = 0.f;
-    B = base;
-    for (int i = lane + 64; i < used; i += 64) B = fmaxf(B, ps.l[at + i] == 0.f ? NEG_INF : ps.base[at + i]);
-    B = wave_reduce(B, [](float x, float y) { return fmaxf(x, y); });
-    L = l == 0.f ? 0.f : l * exp2_fast(base - B);
-    for (int i = lane + 64; i < used; i += 64) L += ps.l[at + i] == 0.f ? 0.f : ps.l[at + i] * exp2_fast(ps.base[at + i] - B);
+    if (lane >= used || l == 0.f) m = NEG_INF, l = 0.f;
+    M = m;
+    for (int i = lane + 64; i < used; i += 64) M = fmaxf(M, ps.l[at + i] == 0.f ? NEG_INF : ps.m[at + i]);
+    M = wave_reduce(M, [](float x, float y) { return fmaxf(x, y); });
+    L = l == 0.f ? 0.f : l * exp2_fast(m - M);
+    for (int i = lane + 64; i < used; i += 64) L += ps.l[at + i] == 0.f ? 0.f : ps.l[at + i] * exp2_fast(ps.m[at + i] - M);
     L = wave_reduce(L, Sum());
 }
 
@@ -360,29 +359,29 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Cache c, Attention a, Pa
         // Everything is asked for at once, before the length says how much of it was written (the rest is not looked at): one latency, not three.
         constexpr int AHEAD = 4;
         f4 v[AHEAD];
-        float vl[AHEAD], vb[AHEAD];
+        float vl[AHEAD], vm[AHEAD];
 #pragma unroll
         for (int x = 0; x < AHEAD; ++x) {
             const int i = lane_c + 32 * x;
             v[x] = f4{0.f, 0.f, 0.f, 0.f};
-            vl[x] = vb[x] = 0.f;
+            vl[x] = vm[x] = 0.f;
             if (i < ps.chunks) {
                 vl[x] = ps.l[at + i];
-                vb[x] = ps.base[at + i];
+                vm[x] = ps.m[at + i];
                 if (dim < c.d) v[x] = *reinterpret_cast<const f4*>(po + (size_t)i * c.d);
             }
         }
         const int n = min(a.lens[b], a.longest), used = n > 0 ? (n + ps.chunk - 1) / ps.chunk : 0;
         __half* out = a.out + (size_t)b * a.ldo + (size_t)h * c.d;
-        float B, L;
-        join_stats(ps, at, used, B, L);
+        float M, L;
+        join_stats(ps, at, used, M, L);
         f4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int x = 0; x < AHEAD; ++x)
-            if (lane_c + 32 * x < used && vl[x] != 0.f) o += v[x] * exp2_fast(vb[x] - B);
+            if (lane_c + 32 * x < used && vl[x] != 0.f) o += v[x] * exp2_fast(vm[x] - M);
         if (dim < c.d)
             for (int i = lane_c + 32 * AHEAD; i < used; i += 32) {
-                const float l = ps.l[at + i], f = exp2_fast(ps.base[at + i] - B);
+                const float l = ps.l[at + i], f = exp2_fast(ps.m[at + i] - M);
                 const f4 w = *reinterpret_cast<const f4*>(po + (size_t)i * c.d);
                 if (l != 0.f) o += w * f;
             }
@@ -392,7 +391,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Cache c, Attention a, Pa
             float x = 0.f;
 #pragma unroll
             for (int i = 0; i < 32; ++i) x += red[i][tid];
-            out[32 * slice + tid] = __float2half_rn(n > 0 ? x / L : 0.f);
+            out[32 * slice + tid] = __float2half_rn(n > 0 ? x / (L * FACTOR) : 0.f);
         }
         return;
     }
@@ -418,10 +417,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Cache c, Attention a, Pa
             for (int y = 0; y < JOIN_HEADS; y += 4) {
                 const int h = h0 + y + wave;
                 if (h < g) {
-                    float B, L;
-                    join_stats(ps, ((size_t)b * a.heads + (size_t)kvh * g + h) * ps.chunks, used, B, L);
+                    float M, L;
+                    join_stats(ps, ((size_t)b * a.heads + (size_t)kvh * g + h) * ps.chunks, used, M, L);
                     if (lane == 0) {
-                        part[y + wave] = B;
+                        part[y + wave] = M;
                         part[JOIN_HEADS + y + wave] = 1.f / L;
                     }
                 }
@@ -430,9 +429,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Cache c, Attention a, Pa
 #pragma unroll
             for (int y = 0; y < JOIN_HEADS; ++y) {
                 if (h0 + y >= g) break;
-                const float B = part[y], by = part[JOIN_HEADS + y];
+                const float M = part[y], by = part[JOIN_HEADS + y];
 #pragma unroll
-                for (int x = 0; x < JOIN_TOKENS / 256; ++x) w[x] += exp2_fast(raw[y][x] - B) * by;
+                for (int x = 0; x < JOIN_TOKENS / 256; ++x) w[x] += exp2_fast(raw[y][x] - M) * by;
             }
             __syncthreads();
         }
@@ -532,7 +531,7 @@ hipError_t attn_decode(const Cache& c, const Attention& a, hipStream_t s) {
     ps.chunk = p.chunk;
     ps.chunks = p.chunks;
     if (!p.direct) {
-        ps.base = (float*)a.ws;
+        ps.m = (float*)a.ws;
         ps.l = (float*)(a.ws + p.at_l);
         ps.o = (float*)(a.ws + p.at_o);
     }

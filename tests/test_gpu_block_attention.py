@@ -253,3 +253,33 @@ def test_many_tokens_of_little_weight_beside_one_of_much(below, kv, lens):
     U.close("out", got, want, eo + max(lens) * 2.0 ** -39 * 8192)
     for b, n in enumerate(lens):
         U.close("weights", score[b, :, :n], weights[b, :, :n], ew[b, :, :n])
+
+
+@pytest.mark.parametrize("heads,kv,lens", [(4, 4, [300, 33]), (16, 2, [5000, 64])])
+@pytest.mark.parametrize("power", [24, 25, 26, 27, 28, 30])
+def test_scores_far_beyond_the_exponents_reach(power, heads, kv, lens):
+    """Scores of 2^power in log2, where fp32 has steps of 2 to 128: equal ones share the weight, of distant ones the largest has it all."""
+    d = 64
+    cache, table, dev_lens, q = setup(heads, kv, d, 16, lens)
+    longest = max(lens)
+    for odd in (1.0, 1.25, 1.75):
+        q.fill_(odd)
+        scale = math.log(2.0) * 2.0 ** power / d
+        score = torch.zeros((len(lens), kv, longest), device="cuda")
+        cache.k.copy_(torch.where(cache.k == cache.k, 1.0, cache.k))
+        got = B.qeft_attn_decode(cache, table, dev_lens, longest, q, scale=scale, score=score)
+        for b, n in enumerate(lens):
+            for h in range(heads):
+                v = U.rows_of(cache.v, table, b, h * kv // heads, n)
+                bound = U.HALF * v.mean(0).abs() + U.TINY + (n / 32 + 64 + d) * U.U * v.abs().mean(0) + 2.0 ** -20 * v.abs().mean(0)
+                U.close("mean", got[b, h * d: (h + 1) * d], v.mean(0), bound)
+            U.close("weights", score[b, :, :n], torch.full((kv, n), heads / kv / n, dtype=torch.float64, device="cuda"), (n / 32 + 64) * U.U * heads / kv / n)
+        # every 7th token's keys half as large again as its neighbours', the last of all twice
+        cache.k.copy_(torch.where(cache.k == cache.k, 1.0 + 0.5 * (torch.arange(16, device="cuda")[:, None] % 7 == 3), cache.k))
+        for b, n in enumerate(lens):
+            cache.k[int(table[b, (n - 1) // 16]), :, (n - 1) % 16] = 2.0
+        got = B.qeft_attn_decode(cache, table, dev_lens, longest, q, scale=scale, score=score)
+        for b, n in enumerate(lens):
+            last = torch.stack([cache.v[int(table[b, (n - 1) // 16]), h * kv // heads, (n - 1) % 16] for h in range(heads)])
+            assert torch.equal(got[b].view(heads, d), last)
+            assert bool((score[b, :, n - 1] == heads / kv).all()) and not bool(score[b, :, : n - 1].any())
