@@ -459,6 +459,158 @@ int qeft_norm_fwd(const qeft_norm_desc_t* desc, const qeft_norm_fwd_t* a, void* 
 size_t qeft_norm_workspace(const qeft_norm_desc_t* desc, int64_t m);
 int qeft_norm_bwd(const qeft_norm_desc_t* desc, const qeft_norm_bwd_t* a, void* stream);
 
+/* ==== the ends of a step: log probabilities with the gradient of the logits, norms of the heads of queries and keys with their rotation, and the
+ * optimizer of what is trained ====
+ *
+ * The conventions above hold; tokens, positions, step counts and factors that lie in device memory are clamped or make a row or a step be left out as
+ * stated, so that no value leads to an access outside the buffers described. */
+
+/* Log probabilities.  With x = scale * z for logits z [m][ldz] of n entries (fp16 or fp32 by dtype; scale > 0, one over the temperature),
+ *     lse = log sum_j exp x_j     logp = x_token - lse     entropy = lse - sum_j p_j x_j, p = exp(x - lse)
+ * and the `top` likeliest entries, in order of z, equal ones by index: top_index and their log probabilities top_logp, both [m][ld_top].
+ * token int32 [m]; NULL: no logp.  A row whose token is not in 0 .. n - 1 is left out: its logp, lse and entropy are 0, it has no alternatives, and it is
+ * not read.  An entry of -infinity has no probability and is no alternative; where there are fewer than `top` others, top_index is -1 and top_logp
+ * -infinity.  A row of nothing else: lse and logp -infinity, entropy 0, gradient 0.  Not-a-number and +infinity make their row's lse, logp, entropy, top_logp and
+ * gradient not-a-number; top_index counts not-a-number above +infinity.  Sums and exponentials are fp32.  logp, lse, entropy (fp32 [m]) and both top arrays may be
+ * NULL (top = 0: both must be, and the other way round).
+ * qeft_logprob_bwd: with the gradients dlogp, dlse, dentropy (fp32 [m], NULL: 0) of those three, and lse and entropy (needed with dentropy) as the forward gave them,
+ *     dz_j = scale * (dlogp ([j = token] - p_j) + dlse p_j - dentropy p_j (log p_j + entropy))
+ * of dtype, [m][lddz], which may be z itself; a row that is left out gets zeros.  dlogp needs token.
+ * qeft_logprob_fwd_bwd: both in one call, where the gradients are known before: fwd's lse, logp and entropy if asked for (no alternatives: top = 0), and dz; lse
+ * and entropy of the bwd struct, and its z and token, are not looked at.  Each row is read once if its n values fit a workgroup's registers (131072 fp16 or 65536 fp32).
+ * ws: qeft_logprob_workspace bytes, 16-byte aligned, for fwd and fwd_bwd (0 bytes: NULL will do).  n at most QEFT_MAX_DIM, top at most QEFT_MAX_TOP and n, m at most QEFT_MAX_ROWS.
+ * Rows of logits and gradients are 16-byte aligned, pitches multiples of 8; those of the alternatives any from `top`. */
+#define QEFT_MAX_TOP 64
+typedef struct {
+    int32_t n, dtype;
+    float scale;
+} qeft_logprob_desc_t;
+typedef struct {
+    const void* z;
+    const int32_t* token;
+    float *logp, *lse, *entropy, *top_logp;
+    int32_t* top_index;
+    int64_t ldz, ld_top, m;
+    int32_t top;
+    void* ws;
+    size_t ws_bytes;
+} qeft_logprob_fwd_t;
+typedef struct {
+    const void* z;
+    const int32_t* token;
+    const float *lse, *entropy, *dlogp, *dlse, *dentropy;
+    void* dz;
+    int64_t ldz, lddz, m;
+} qeft_logprob_bwd_t;
+size_t qeft_logprob_workspace(const qeft_logprob_desc_t* desc, int64_t m, int32_t top);
+int qeft_logprob_fwd(const qeft_logprob_desc_t* desc, const qeft_logprob_fwd_t* a, void* stream);
+int qeft_logprob_bwd(const qeft_logprob_desc_t* desc, const qeft_logprob_bwd_t* a, void* stream);
+int qeft_logprob_fwd_bwd(const qeft_logprob_desc_t* desc, const qeft_logprob_fwd_t* a, const qeft_logprob_bwd_t* b, void* stream);
+
+/* Norms of heads with rotation.  Every head x (head_dim values: a multiple of 8, at most QEFT_MAX_HEAD_DIM) of q, fp16 [m][ldq] with `heads` heads a row, and
+ * of k, [m][ldk] with kv_heads, becomes
+ *     R(pos) (unit(x) * w),   unit(x) = x / sqrt(mean(x^2) + eps) over the head
+ * with w_q or w_k, fp16 [head_dim] (NULL: those heads are rotated only), and the rotation R of qeft_cache_append: rot fp32 [positions][ld_rot], rot_dim values of a
+ * head in pairs half of them apart, pos int32 [m] (NULL: row t has position t) clamped to the table; rot_dim == 0: no rotation.  q or k may be left out (NULL).
+ * q_out, k_out may be q, k.  fp32 arithmetic, one rounding per output.
+ * qeft_qk_norm_bwd: from the gradients gq, gk of q_out, k_out, and q, k as the forward took them (needed where w is),
+ *     g = R^T gq     a = g w_q     dq = rs (a - unit(q) mean(a unit(q))), rs = 1 / sqrt(mean(q^2) + eps)     dw_q = sum over rows and heads of g unit(q)
+ * and the same for k; without w, dq = g.  dq may be gq, dk gk; dw_q, dw_k fp32 [head_dim], 16-byte aligned like w_q and w_k.  Every gradient may be NULL; accumulate
+ * != 0 adds to dw_q and dw_k.  Sums are taken in a fixed order.  m == 0: a no-op, but for dw, which is set to zero unless accumulated.
+ * ws: qeft_qk_norm_workspace bytes, 16-byte aligned, needed where dw_q or dw_k is asked for.
+ * qeft_cache_append_norm: qeft_cache_append with these norms ahead of the rotation of q and k. */
+typedef struct {
+    int32_t head_dim, heads, kv_heads, rot_dim;
+    float eps;
+} qeft_qk_desc_t;
+typedef struct {
+    const void *q, *k, *w_q, *w_k;
+    void *q_out, *k_out;
+    const int32_t* pos;
+    const float* rot;
+    int64_t ldq, ldk, ldq_out, ldk_out, ld_rot, m;
+    int32_t positions;
+} qeft_qk_fwd_t;
+typedef struct {
+    const void *gq, *gk, *q, *k, *w_q, *w_k;
+    void *dq, *dk;
+    float *dw_q, *dw_k;
+    const int32_t* pos;
+    const float* rot;
+    int64_t ldgq, ldgk, ldq, ldk, lddq, lddk, ld_rot, m;
+    int32_t positions, accumulate;
+    void* ws;
+    size_t ws_bytes;
+} qeft_qk_bwd_t;
+typedef struct {
+    const void *w_q, *w_k;
+    float eps;
+} qeft_append_norm_t;
+int qeft_qk_norm_fwd(const qeft_qk_desc_t* desc, const qeft_qk_fwd_t* a, void* stream);
+size_t qeft_qk_norm_workspace(const qeft_qk_desc_t* desc, int64_t m);
+int qeft_qk_norm_bwd(const qeft_qk_desc_t* desc, const qeft_qk_bwd_t* a, void* stream);
+int qeft_cache_append_norm(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, const qeft_table_t* table, const qeft_append_t* a,
+                           const qeft_append_norm_t* norm, void* stream);
+
+/* The optimizer: one step of AdamW (Loshchilov and Hutter) over a list of tensors in one launch.  For each value, with gradient g = factor * grad and in step t
+ *     m = beta1 m + (1 - beta1) g     v = beta2 v + (1 - beta2) g^2     w = w - lr decay w - lr (m / c1) / (sqrt(v / c2) + eps),  c = 1 - beta^t
+ * in fp32.  A tensor is n contiguous values: grad (fp16 or fp32, grad_dtype), the weight fp16 and / or its fp32 copy `master` (at least one; where there are both, master is
+ * what is updated and weight its rounding), and the states m, v: fp32, or 8 bits.  All arrays but the scales are 16-byte aligned and none of those that are written may overlap another; all
+ * tensors of a list have the same arrays (all a master or none ...).  decay: a tensor's own weight decay.
+ * 8-bit states (state_bits == 8): m is n bytes of e4m3 (OCP, finite), v n bytes of e5m2, and m_scale, v_scale one byte e8m0 (2^(byte - 127)) for every QEFT_STATE_BLOCK values, the last
+ * block of a tensor may be partial: a state is its code times its block's power of two.  Zero bytes are zero states.  The largest value of a block is brought to [2^7, 2^8) for m and
+ * [2^14, 2^15) for v, by exponents of -110 at least.  States are rounded stochastically, up with the probability that makes the mean right: a second moment that moves by a thousandth
+ * a step would never leave a code to the nearest.  A second moment that is not zero does not become zero.  The random number belongs to seed, step, and the value's place in the
+ * list (tensors counted in whole blocks), so that a step can be repeated.  stochastic != 0 rounds fp16 weights without a master in the same way, otherwise to nearest.
+ * Infinities and not-a-number in the gradient go through the formulas; an 8-bit block whose moments are not all finite becomes not-a-number.
+ *
+ * qeft_tensors_plan writes the plan of a list to host memory (qeft_tensors_plan_bytes bytes); the caller copies it to the device, 16-byte aligned, and gives its address
+ * together with the numbers in `list` to the calls below.  It refuses what they cannot do, so that they read the plan as it is: it must be the unchanged copy, on the device of the call.
+ * A list without m, v, weight and master (all NULL) serves qeft_grad_norm alone.  n from 0 (skipped) to 2^40, count at most QEFT_MAX_TENSORS, 2^30 blocks of work.
+ * qeft_adamw_step: lr, step (1 for the first, at most 2^30) by value, or read from the device where lr_at / step_at are given (a captured graph's); beta1, beta2 in [0, 1), eps > 0.
+ * factor (device, NULL: 1): where it is not a finite number, the call leaves everything as it was.  A step on the device that is below 1 counts as 1.
+ * qeft_grad_norm: out[0] = scale * sqrt(sum of all grad^2), summed in fp64, and out[1] = scale * min(1, max_norm / out[0]), the factor for a step: the gradients of a loss that was
+ * multiplied by 1 / scale are brought back and clipped.  Where the norm is not finite, out[1] is not-a-number, and the step is left out.  max_norm = infinity: no clipping.
+ * steps (int32, device, optional) is counted up by one where the norm is finite: with step_at, a step that is left out does not count.  ws: qeft_grad_norm_workspace
+ * bytes, 16-byte aligned. */
+#define QEFT_STATE_BLOCK 128
+#define QEFT_MAX_TENSORS (1 << 20)
+typedef struct {
+    void* weight;
+    float* master;
+    const void* grad;
+    void *m, *v;
+    uint8_t *m_scale, *v_scale;
+    int64_t n;
+    float decay;
+} qeft_tensor_t;
+typedef struct {
+    const void* plan;      /* device */
+    int64_t work;          /* pieces of work in it */
+    int32_t count, grad_dtype, state_bits, has_weight, has_master;
+} qeft_tensors_t;
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t step;
+    uint64_t seed;
+    const float* lr_at;
+    const int32_t* step_at;
+    const float* factor;
+    int32_t stochastic;
+} qeft_adamw_t;
+typedef struct {
+    float scale, max_norm;
+    float* out;
+    int32_t* steps;
+    void* ws;
+    size_t ws_bytes;
+} qeft_grad_norm_t;
+size_t qeft_tensors_plan_bytes(const qeft_tensor_t* tensors, int32_t count);
+int qeft_tensors_plan(const qeft_tensor_t* tensors, int32_t count, int32_t grad_dtype, int32_t state_bits, void* plan, size_t bytes, qeft_tensors_t* list);
+int qeft_adamw_step(const qeft_tensors_t* list, const qeft_adamw_t* a, void* stream);
+size_t qeft_grad_norm_workspace(const qeft_tensors_t* list);
+int qeft_grad_norm(const qeft_tensors_t* list, const qeft_grad_norm_t* a, void* stream);
+
 /* Static, never NULL. */
 const char* qeft_status_string(int status);
 

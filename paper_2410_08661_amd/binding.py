@@ -25,6 +25,7 @@ QEFT_OP_FWD, QEFT_OP_BWD_DX, QEFT_OP_WEAK_GRAD, QEFT_OP_FWD_IRREGULAR, QEFT_OP_B
 QEFT_DTYPE_F16, QEFT_DTYPE_F32 = 0, 1
 QEFT_LAYOUT_CANONICAL, QEFT_LAYOUT_DENSE3 = 0, 1
 QEFT_GATE_NONE, QEFT_GATE_CHANNEL, QEFT_GATE_TOKEN = 0, 1, 2
+QEFT_MAX_TOP, QEFT_STATE_BLOCK = 64, 128
 _DTYPES = {torch.float16: QEFT_DTYPE_F16, torch.float32: QEFT_DTYPE_F32}
 
 
@@ -90,6 +91,57 @@ class qeft_norm_bwd_t(C.Structure):
                [("accumulate", C.c_int32), ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
 
 
+class qeft_logprob_desc_t(C.Structure):
+    _fields_ = [("n", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
+
+
+class qeft_logprob_fwd_t(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("z", "token", "logp", "lse", "entropy", "top_logp", "top_index")] + \
+               [("ldz", C.c_int64), ("ld_top", C.c_int64), ("m", C.c_int64), ("top", C.c_int32), ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
+class qeft_logprob_bwd_t(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("z", "token", "lse", "entropy", "dlogp", "dlse", "dentropy", "dz")] + \
+               [(f, C.c_int64) for f in ("ldz", "lddz", "m")]
+
+
+class qeft_qk_desc_t(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("rot_dim", C.c_int32), ("eps", C.c_float)]
+
+
+class qeft_qk_fwd_t(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("q", "k", "w_q", "w_k", "q_out", "k_out", "pos", "rot")] + \
+               [(f, C.c_int64) for f in ("ldq", "ldk", "ldq_out", "ldk_out", "ld_rot", "m")] + [("positions", C.c_int32)]
+
+
+class qeft_qk_bwd_t(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("gq", "gk", "q", "k", "w_q", "w_k", "dq", "dk", "dw_q", "dw_k", "pos", "rot")] + \
+               [(f, C.c_int64) for f in ("ldgq", "ldgk", "ldq", "ldk", "lddq", "lddk", "ld_rot", "m")] + \
+               [("positions", C.c_int32), ("accumulate", C.c_int32), ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
+class qeft_append_norm_t(C.Structure):
+    _fields_ = [("w_q", C.c_void_p), ("w_k", C.c_void_p), ("eps", C.c_float)]
+
+
+class qeft_tensor_t(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("weight", "master", "grad", "m", "v", "m_scale", "v_scale")] + [("n", C.c_int64), ("decay", C.c_float)]
+
+
+class qeft_tensors_t(C.Structure):
+    _fields_ = [("plan", C.c_void_p), ("work", C.c_int64), ("count", C.c_int32), ("grad_dtype", C.c_int32), ("state_bits", C.c_int32), ("has_weight", C.c_int32),
+                ("has_master", C.c_int32)]
+
+
+class qeft_adamw_t(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64), ("seed", C.c_uint64),
+                ("lr_at", C.c_void_p), ("step_at", C.c_void_p), ("factor", C.c_void_p), ("stochastic", C.c_int32)]
+
+
+class qeft_grad_norm_t(C.Structure):
+    _fields_ = [("scale", C.c_float), ("max_norm", C.c_float), ("out", C.c_void_p), ("steps", C.c_void_p), ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
 EXPORTS = {
     "qeft_layout": (C.c_int, [C.POINTER(qeft_desc_t), C.POINTER(qeft_layout_t)]),
     "qeft_pack": (C.c_int, [C.POINTER(qeft_desc_t), C.c_void_p, C.c_int64, C.POINTER(qeft_weight_t), C.c_void_p]),
@@ -136,6 +188,20 @@ EXPORTS = {
     "qeft_norm_fwd": (C.c_int, [C.POINTER(qeft_norm_desc_t), C.POINTER(qeft_norm_fwd_t), C.c_void_p]),
     "qeft_norm_workspace": (C.c_size_t, [C.POINTER(qeft_norm_desc_t), C.c_int64]),
     "qeft_norm_bwd": (C.c_int, [C.POINTER(qeft_norm_desc_t), C.POINTER(qeft_norm_bwd_t), C.c_void_p]),
+    "qeft_logprob_workspace": (C.c_size_t, [C.POINTER(qeft_logprob_desc_t), C.c_int64, C.c_int32]),
+    "qeft_logprob_fwd": (C.c_int, [C.POINTER(qeft_logprob_desc_t), C.POINTER(qeft_logprob_fwd_t), C.c_void_p]),
+    "qeft_logprob_bwd": (C.c_int, [C.POINTER(qeft_logprob_desc_t), C.POINTER(qeft_logprob_bwd_t), C.c_void_p]),
+    "qeft_logprob_fwd_bwd": (C.c_int, [C.POINTER(qeft_logprob_desc_t), C.POINTER(qeft_logprob_fwd_t), C.POINTER(qeft_logprob_bwd_t), C.c_void_p]),
+    "qeft_qk_norm_fwd": (C.c_int, [C.POINTER(qeft_qk_desc_t), C.POINTER(qeft_qk_fwd_t), C.c_void_p]),
+    "qeft_qk_norm_workspace": (C.c_size_t, [C.POINTER(qeft_qk_desc_t), C.c_int64]),
+    "qeft_qk_norm_bwd": (C.c_int, [C.POINTER(qeft_qk_desc_t), C.POINTER(qeft_qk_bwd_t), C.c_void_p]),
+    "qeft_cache_append_norm": (C.c_int, [C.POINTER(qeft_cache_desc_t), C.POINTER(qeft_cache_t), C.POINTER(qeft_table_t), C.POINTER(qeft_append_t),
+                                         C.POINTER(qeft_append_norm_t), C.c_void_p]),
+    "qeft_tensors_plan_bytes": (C.c_size_t, [C.POINTER(qeft_tensor_t), C.c_int32]),
+    "qeft_tensors_plan": (C.c_int, [C.POINTER(qeft_tensor_t), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.POINTER(qeft_tensors_t)]),
+    "qeft_adamw_step": (C.c_int, [C.POINTER(qeft_tensors_t), C.POINTER(qeft_adamw_t), C.c_void_p]),
+    "qeft_grad_norm_workspace": (C.c_size_t, [C.POINTER(qeft_tensors_t)]),
+    "qeft_grad_norm": (C.c_int, [C.POINTER(qeft_tensors_t), C.POINTER(qeft_grad_norm_t), C.c_void_p]),
     "qeft_status_string": (C.c_char_p, [C.c_int]),
 }
 
@@ -207,7 +273,7 @@ class Weight:
 
 _MARSHALLED = ("qeft_linear_fwd", "qeft_linear_fwd_group", "qeft_linear_bwd_dx", "qeft_linear_bwd", "qeft_linear_fwd_irregular",
                "qeft_linear_bwd_dx_irregular", "qeft_weak_grad", "qeft_cache_append", "qeft_attn_decode", "qeft_cache_evict", "qeft_norm_fwd",
-               "qeft_norm_bwd")
+               "qeft_norm_bwd", "qeft_logprob_fwd", "qeft_logprob_bwd", "qeft_logprob_fwd_bwd", "qeft_qk_norm_fwd", "qeft_qk_norm_bwd", "qeft_cache_append_norm")
 
 
 def _load_marshal():
@@ -215,7 +281,8 @@ def _load_marshal():
         from . import _marshal as m
     except ImportError:   # not built, or not for this torch: every call is ctypes'
         return types.SimpleNamespace(**{n.removeprefix("qeft_"): lambda *args: None for n in _MARSHALLED})
-    m.init(tuple(C.cast(getattr(raw, n), C.c_void_p).value for n in _MARSHALLED), qeft_desc_t, Weight, qeft_cache_desc_t, qeft_norm_desc_t)
+    m.init(tuple(C.cast(getattr(raw, n), C.c_void_p).value for n in _MARSHALLED), qeft_desc_t, Weight, qeft_cache_desc_t, qeft_norm_desc_t,
+           qeft_logprob_desc_t, qeft_qk_desc_t)
     return m
 
 
@@ -554,6 +621,26 @@ def _c_workspace(where, ws):
     return p, ws.numel()
 
 
+def _c_append(at, cache, table, k, v, index, seq, q, q_out, rot, pos):
+    """The structs of an append."""
+    d = cache.desc
+    pools, tab = cache.c_struct(), _c_table(at, table)
+    n = k.shape[0] if k is not None and k.dim() == 2 else None
+    width = d.kv_heads * d.head_dim
+    pk, ldk = _take(at, "k", k, torch.float16, (n, width))
+    pv, ldv = _take(at, "v", v, torch.float16, (n, width))
+    pq, ldq = _take(at, "q", q, torch.float16, (n, None), True)
+    heads = 0 if q is None else q.shape[1] // d.head_dim
+    if q is not None and heads * d.head_dim != q.shape[1]:
+        _fail(QEFT_ERR_SHAPE, at, "q's rows are not whole heads")
+    po, ldo = _take(at, "q_out", q_out if q is not None else None, torch.float16, (n, heads * d.head_dim), q is None)
+    pi, ps, pp = (_take(at, name, t, torch.int32, (n,), t is not index)[0] for name, t in (("index", index), ("seq", seq), ("pos", pos)))
+    pr, ldr = _take(at, "rot", rot, torch.float32, (None, None), True)
+    a = qeft_append_t(pq, pk, pv, po, ldq, ldo, ldk, ldv, ps, pi, pp, pr, ldr,
+                      rot.shape[0] if rot is not None else 0, rot.shape[1] if rot is not None else 0, heads, n)
+    return pools, tab, a
+
+
 def qeft_cache_append(cache: Cache, table: torch.Tensor, k: torch.Tensor, v: torch.Tensor, index: torch.Tensor, seq: torch.Tensor | None = None,
                       q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, rot: torch.Tensor | None = None,
                       pos: torch.Tensor | None = None) -> torch.Tensor | None:
@@ -563,21 +650,8 @@ def qeft_cache_append(cache: Cache, table: torch.Tensor, k: torch.Tensor, v: tor
         q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
     st = _native.cache_append(cache.desc, cache.k, cache.v, table, k, v, index, seq, q, q_out, rot, pos)
     if st is None:
-        at, d = "qeft_cache_append", cache.desc
-        pools, tab = cache.c_struct(), _c_table(at, table)
-        n = k.shape[0] if k is not None and k.dim() == 2 else None
-        width = d.kv_heads * d.head_dim
-        pk, ldk = _take(at, "k", k, torch.float16, (n, width))
-        pv, ldv = _take(at, "v", v, torch.float16, (n, width))
-        pq, ldq = _take(at, "q", q, torch.float16, (n, None), True)
-        heads = 0 if q is None else q.shape[1] // d.head_dim
-        if q is not None and heads * d.head_dim != q.shape[1]:
-            _fail(QEFT_ERR_SHAPE, at, "q's rows are not whole heads")
-        po, ldo = _take(at, "q_out", q_out if q is not None else None, torch.float16, (n, heads * d.head_dim), q is None)
-        pi, ps, pp = (_take(at, name, t, torch.int32, (n,), t is not index)[0] for name, t in (("index", index), ("seq", seq), ("pos", pos)))
-        pr, ldr = _take(at, "rot", rot, torch.float32, (None, None), True)
-        a = qeft_append_t(pq, pk, pv, po, ldq, ldo, ldk, ldv, ps, pi, pp, pr, ldr,
-                          rot.shape[0] if rot is not None else 0, rot.shape[1] if rot is not None else 0, heads, n)
+        d = cache.desc
+        pools, tab, a = _c_append("qeft_cache_append", cache, table, k, v, index, seq, q, q_out, rot, pos)
         st = raw.qeft_cache_append(C.byref(d), C.byref(pools), C.byref(tab), C.byref(a), _stream())
     _check(st, "qeft_cache_append")
     return q_out
@@ -734,3 +808,284 @@ def qeft_norm_bwd(desc: qeft_norm_desc_t, dx: torch.Tensor, h: torch.Tensor, w_p
         st = raw.qeft_norm_bwd(C.byref(desc), C.byref(a), _stream())
     _check(st, "qeft_norm_bwd")
     return dr, dy, dw_pre, dw_post, dgate
+
+
+# ---- the ends of a step: log probabilities, norms of heads with rotation, the optimizer ----------------------------------------------------------
+
+def make_logprob_desc(n, dtype=torch.float16, scale=1.0) -> qeft_logprob_desc_t:
+    """n logits of dtype (float16 or float32) a row, scaled by `scale` (one over the temperature)."""
+    return qeft_logprob_desc_t(n, _DTYPES[dtype], scale)
+
+
+def _logits(desc):
+    return torch.float32 if desc.dtype == QEFT_DTYPE_F32 else torch.float16
+
+
+def qeft_logprob_workspace(desc: qeft_logprob_desc_t, m: int, top: int = 0) -> int:
+    return int(raw.qeft_logprob_workspace(C.byref(desc), m, top))
+
+
+def _logprob_outputs(desc, z, token, logp, lse, entropy, top, ws):
+    m, dev = z.shape[0], z.device
+    new = lambda t, has: None if t is False or not has else torch.empty(m, dtype=torch.float32, device=dev) if t is None else t  # noqa: E731
+    logp, lse, entropy = new(logp, token is not None), new(lse, True), new(entropy, True)
+    if ws is None:
+        n = qeft_logprob_workspace(desc, m, top)
+        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    return logp, lse, entropy, ws
+
+
+def _c_logprob_fwd(at, desc, z, token, logp, lse, entropy, top, top_logp, top_index, ws):
+    m = z.shape[0]
+    pz, ldz = _take(at, "z", z, _logits(desc), (m, desc.n))
+    pt = _take(at, "token", token, torch.int32, (m,), True)[0]
+    pl, ps, pe = (_take(at, name, t, torch.float32, (m,), True)[0] for name, t in (("logp", logp), ("lse", lse), ("entropy", entropy)))
+    (pv, ldv), (pi, ldi) = _take(at, "top_logp", top_logp, torch.float32, (m, top), True), _take(at, "top_index", top_index, torch.int32, (m, top), True)
+    if m > 1 and top_logp is not None and top_index is not None and ldv != ldi:
+        _fail(QEFT_ERR_SHAPE, at, "top_logp and top_index differ in pitch")
+    pw, nw = _c_workspace(at, ws)
+    return qeft_logprob_fwd_t(pz, pt, pl, ps, pe, pv, pi, ldz, ldv if m > 1 else top, m, top, pw, nw)
+
+
+def qeft_logprob_fwd(desc: qeft_logprob_desc_t, z: torch.Tensor, token: torch.Tensor | None = None, top: int = 0, logp: torch.Tensor | None = None,
+                     lse: torch.Tensor | None = None, entropy: torch.Tensor | None = None, top_logp: torch.Tensor | None = None,
+                     top_index: torch.Tensor | None = None, ws: torch.Tensor | None = None):
+    """(logp, lse, entropy, top_logp, top_index) of rows of logits z [m][n] and tokens int32 [m]; rows whose token is not in 0 .. n - 1 are left out.  Outputs that are
+    not given are allocated, False leaves one out; without tokens logp is None, with top = 0 the alternatives are."""
+    logp, lse, entropy, ws = _logprob_outputs(desc, z, token, logp, lse, entropy, top, ws)
+    if top > 0:
+        top_logp = torch.empty((z.shape[0], top), dtype=torch.float32, device=z.device) if top_logp is None else top_logp
+        top_index = torch.empty((z.shape[0], top), dtype=torch.int32, device=z.device) if top_index is None else top_index
+    st = _native.logprob_fwd(desc, z, token, logp, lse, entropy, top, top_logp, top_index, ws)
+    if st is None:
+        a = _c_logprob_fwd("qeft_logprob_fwd", desc, z, token, logp, lse, entropy, top, top_logp, top_index, ws)
+        st = raw.qeft_logprob_fwd(C.byref(desc), C.byref(a), _stream())
+    _check(st, "qeft_logprob_fwd")
+    return logp, lse, entropy, top_logp, top_index
+
+
+def _c_logprob_bwd(at, desc, z, lse, token, dlogp, dlse, entropy, dentropy, dz):
+    m = z.shape[0]
+    pz, ldz = _take(at, "z", z, _logits(desc), (m, desc.n))
+    pdz, lddz = _take(at, "dz", dz, _logits(desc), (m, desc.n))
+    pt = _take(at, "token", token, torch.int32, (m,), True)[0]
+    pl, pe, pdl, pds, pde = (_take(at, name, t, torch.float32, (m,), True)[0]
+                             for name, t in (("lse", lse), ("entropy", entropy), ("dlogp", dlogp), ("dlse", dlse), ("dentropy", dentropy)))
+    return qeft_logprob_bwd_t(pz, pt, pl, pe, pdl, pds, pde, pdz, ldz, lddz, m)
+
+
+def qeft_logprob_bwd(desc: qeft_logprob_desc_t, z: torch.Tensor, lse: torch.Tensor, token: torch.Tensor | None = None, dlogp: torch.Tensor | None = None,
+                     dlse: torch.Tensor | None = None, entropy: torch.Tensor | None = None, dentropy: torch.Tensor | None = None,
+                     dz: torch.Tensor | None = None) -> torch.Tensor:
+    """The logits' gradient (of their dtype; dz may be z) from those of logp, lse and entropy, fp32 [m]; lse, and with dentropy entropy, as the forward gave them."""
+    if dz is None:
+        dz = _empty_rows(z.shape[0], desc.n, z.dtype, z.device)
+    st = _native.logprob_bwd(desc, z, lse, token, dlogp, dlse, entropy, dentropy, dz)
+    if st is None:
+        a = _c_logprob_bwd("qeft_logprob_bwd", desc, z, lse, token, dlogp, dlse, entropy, dentropy, dz)
+        st = raw.qeft_logprob_bwd(C.byref(desc), C.byref(a), _stream())
+    _check(st, "qeft_logprob_bwd")
+    return dz
+
+
+def qeft_logprob_fwd_bwd(desc: qeft_logprob_desc_t, z: torch.Tensor, token: torch.Tensor | None = None, dlogp: torch.Tensor | None = None,
+                         dlse: torch.Tensor | None = None, dentropy: torch.Tensor | None = None, dz: torch.Tensor | None = None,
+                         logp: torch.Tensor | None = None, lse: torch.Tensor | None = None, entropy: torch.Tensor | None = None,
+                         ws: torch.Tensor | None = None):
+    """(dz, logp, lse, entropy): qeft_logprob_fwd and qeft_logprob_bwd in one call, where the gradients are known before, as those of a mean loss are."""
+    logp, lse, entropy, ws = _logprob_outputs(desc, z, token, logp, lse, entropy, 0, ws)
+    if dz is None:
+        dz = _empty_rows(z.shape[0], desc.n, z.dtype, z.device)
+    st = _native.logprob_fwd_bwd(desc, z, token, dlogp, dlse, dentropy, dz, logp, lse, entropy, ws)
+    if st is None:
+        at = "qeft_logprob_fwd_bwd"
+        a = _c_logprob_fwd(at, desc, z, token, logp, lse, entropy, 0, None, None, ws)
+        b = _c_logprob_bwd(at, desc, z, None, token, dlogp, dlse, None, dentropy, dz)
+        st = raw.qeft_logprob_fwd_bwd(C.byref(desc), C.byref(a), C.byref(b), _stream())
+    _check(st, "qeft_logprob_fwd_bwd")
+    return dz, logp, lse, entropy
+
+
+def make_qk_desc(head_dim, heads, kv_heads, rot_dim=0, eps=1e-6) -> qeft_qk_desc_t:
+    return qeft_qk_desc_t(head_dim, heads, kv_heads, rot_dim, eps)
+
+
+def _c_turn(at, desc, m, rot, pos):
+    """Pointers of positions and rotations, the table's pitch and length."""
+    pr, ldr = _take(at, "rot", rot, torch.float32, (None, desc.rot_dim), True)
+    return _take(at, "pos", pos, torch.int32, (m,), True)[0], pr, ldr, rot.shape[0] if rot is not None else 0
+
+
+def qeft_qk_norm_fwd(desc: qeft_qk_desc_t, q: torch.Tensor | None, k: torch.Tensor | None, w_q: torch.Tensor | None = None, w_k: torch.Tensor | None = None,
+                     rot: torch.Tensor | None = None, pos: torch.Tensor | None = None, q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None):
+    """(q_out, k_out): every head of q fp16 [m][heads * head_dim] and k [m][kv_heads * head_dim] normed (with w_q, w_k fp16 [head_dim]; None: not normed), then rotated by
+    rot fp32 [positions][rot_dim] at pos int32 [m] (None: the row's number).  q or k may be None."""
+    q_out, k_out = (None if x is None else torch.empty_like(x, memory_format=torch.contiguous_format) if y is None else y for x, y in ((q, q_out), (k, k_out)))
+    st = _native.qk_norm_fwd(desc, q, k, w_q, w_k, rot, pos, q_out, k_out)
+    if st is None:
+        at, half, d = "qeft_qk_norm_fwd", torch.float16, desc.head_dim
+        m = (k if q is None else q).shape[0] if q is not None or k is not None else 0
+        (pq, ldq), (pqo, ldqo) = (_take(at, name, t, half, (m, desc.heads * d), q is None) for name, t in (("q", q), ("q_out", q_out)))
+        (pk, ldk), (pko, ldko) = (_take(at, name, t, half, (m, desc.kv_heads * d), k is None) for name, t in (("k", k), ("k_out", k_out)))
+        pwq, pwk = (_take(at, name, t, half, (d,), True)[0] for name, t in (("w_q", w_q), ("w_k", w_k)))
+        pp, pr, ldr, positions = _c_turn(at, desc, m, rot, pos)
+        a = qeft_qk_fwd_t(pq, pk, pwq, pwk, pqo, pko, pp, pr, ldq, ldk, ldqo, ldko, ldr, m, positions)
+        st = raw.qeft_qk_norm_fwd(C.byref(desc), C.byref(a), _stream())
+    _check(st, "qeft_qk_norm_fwd")
+    return q_out, k_out
+
+
+def qeft_qk_norm_workspace(desc: qeft_qk_desc_t, m: int) -> int:
+    return int(raw.qeft_qk_norm_workspace(C.byref(desc), m))
+
+
+def qeft_qk_norm_bwd(desc: qeft_qk_desc_t, gq: torch.Tensor | None, gk: torch.Tensor | None, q: torch.Tensor | None = None, k: torch.Tensor | None = None,
+                     w_q: torch.Tensor | None = None, w_k: torch.Tensor | None = None, rot: torch.Tensor | None = None, pos: torch.Tensor | None = None,
+                     dq: torch.Tensor | None = None, dk: torch.Tensor | None = None, dw_q: torch.Tensor | None = None, dw_k: torch.Tensor | None = None,
+                     accumulate=False, ws: torch.Tensor | None = None):
+    """(dq, dk, dw_q, dw_k) of qeft_qk_norm_fwd's q, k, w_q and w_k, from the gradients gq, gk of its outputs and q, k as it took them (needed where the heads are normed).
+    Gradients of what the call does not have are None; those not given are allocated, False leaves one out.  accumulate: added to what dw_q, dw_k hold."""
+    some = gk if gq is None else gq
+    m, d = (some.shape[0] if some is not None else 0), desc.head_dim
+    sums = torch.zeros if accumulate else torch.empty
+
+    def out(t, has, make):
+        return None if t is False or not has else make() if t is None else t
+
+    dq = out(dq, gq is not None, lambda: torch.empty_like(gq, memory_format=torch.contiguous_format))
+    dk = out(dk, gk is not None, lambda: torch.empty_like(gk, memory_format=torch.contiguous_format))
+    dw_q = out(dw_q, gq is not None and w_q is not None, lambda: sums(d, dtype=torch.float32, device=gq.device))
+    dw_k = out(dw_k, gk is not None and w_k is not None, lambda: sums(d, dtype=torch.float32, device=gk.device))
+    if ws is None and (dw_q is not None or dw_k is not None):
+        n = qeft_qk_norm_workspace(desc, m)
+        ws = torch.empty(n, dtype=torch.uint8, device=some.device) if n else None
+    st = _native.qk_norm_bwd(desc, gq, gk, q, k, w_q, w_k, rot, pos, dq, dk, dw_q, dw_k, accumulate, ws)
+    if st is None:
+        at, half, f32 = "qeft_qk_norm_bwd", torch.float16, torch.float32
+        (pgq, ldgq), (pq, ldq), (pdq, lddq) = (_take(at, name, t, half, (m, desc.heads * d), True) for name, t in (("gq", gq), ("q", q), ("dq", dq)))
+        (pgk, ldgk), (pk, ldk), (pdk, lddk) = (_take(at, name, t, half, (m, desc.kv_heads * d), True) for name, t in (("gk", gk), ("k", k), ("dk", dk)))
+        pwq, pwk = (_take(at, name, t, half, (d,), True)[0] for name, t in (("w_q", w_q), ("w_k", w_k)))
+        pdwq, pdwk = (_take(at, name, t, f32, (d,), True)[0] for name, t in (("dw_q", dw_q), ("dw_k", dw_k)))
+        pp, pr, ldr, positions = _c_turn(at, desc, m, rot, pos)
+        pws, nws = _c_workspace(at, ws)
+        a = qeft_qk_bwd_t(pgq, pgk, pq, pk, pwq, pwk, pdq, pdk, pdwq, pdwk, pp, pr, ldgq, ldgk, ldq, ldk, lddq, lddk, ldr, m, positions, int(bool(accumulate)), pws, nws)
+        st = raw.qeft_qk_norm_bwd(C.byref(desc), C.byref(a), _stream())
+    _check(st, "qeft_qk_norm_bwd")
+    return dq, dk, dw_q, dw_k
+
+
+def qeft_cache_append_norm(cache: Cache, table: torch.Tensor, k: torch.Tensor, v: torch.Tensor, index: torch.Tensor, seq: torch.Tensor | None = None,
+                           q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, rot: torch.Tensor | None = None, pos: torch.Tensor | None = None,
+                           w_q: torch.Tensor | None = None, w_k: torch.Tensor | None = None, eps: float = 1e-6) -> torch.Tensor | None:
+    """qeft_cache_append with every head of q and k normed before its rotation (w_q, w_k fp16 [head_dim]; None: those heads are not)."""
+    if q is not None and q_out is None:
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    st = _native.cache_append_norm(cache.desc, cache.k, cache.v, table, k, v, index, seq, q, q_out, rot, pos, w_q, w_k, eps)
+    if st is None:
+        at, d = "qeft_cache_append_norm", cache.desc
+        pools, tab, a = _c_append(at, cache, table, k, v, index, seq, q, q_out, rot, pos)
+        pwq, pwk = (_take(at, name, t, torch.float16, (d.head_dim,), True)[0] for name, t in (("w_q", w_q), ("w_k", w_k)))
+        norm = qeft_append_norm_t(pwq, pwk, float(eps))
+        st = raw.qeft_cache_append_norm(C.byref(d), C.byref(pools), C.byref(tab), C.byref(a), C.byref(norm), _stream())
+    _check(st, "qeft_cache_append_norm")
+    return q_out
+
+
+def make_adamw_states(weights, bits=32) -> dict:
+    """Zero states of an optimizer for these weights, as TensorList takes them: m, v and, with bits = 8, m_scales, v_scales."""
+    if bits not in (8, 32):
+        _fail(QEFT_ERR_UNSUPPORTED, "make_adamw_states", f"states of {bits} bits")
+    blocks = lambda w: -(-w.numel() // QEFT_STATE_BLOCK)  # noqa: E731
+    out = {name: [torch.zeros(w.shape, dtype=torch.uint8 if bits == 8 else torch.float32, device=w.device) for w in weights] for name in ("m", "v")}
+    if bits == 8:
+        out.update({name: [torch.zeros(blocks(w), dtype=torch.uint8, device=w.device) for w in weights] for name in ("m_scales", "v_scales")})
+    return out
+
+
+class TensorList:
+    """What an optimizer's step goes over, and the plan of it on the GPU: lists of contiguous tensors, one entry for each trained tensor.  grads fp16 or fp32; weights
+    fp16 and / or masters fp32; m, v fp32, or uint8 with m_scales, v_scales; decay a number or one for each.  Without weights and masters the list serves
+    qeft_grad_norm alone.  The list keeps the tensors; their contents may change between calls, their addresses may not."""
+
+    def __init__(self, grads, weights=None, masters=None, m=None, v=None, m_scales=None, v_scales=None, decay=0.0):
+        at, n = "TensorList", len(grads)
+        parts = dict(weight=weights, master=masters, grad=grads, m=m, v=v, m_scale=m_scales, v_scale=v_scales)
+        self.tensors = {name: None if ts is None else list(ts) for name, ts in parts.items()}
+        decays = [float(decay)] * n if not hasattr(decay, "__len__") else [float(x) for x in decay]
+        grad = grads[0].dtype if n else torch.float32
+        state = m[0].dtype if m is not None and n else torch.float32
+        if grad not in _DTYPES or state not in (torch.uint8, torch.float32):
+            _fail(QEFT_ERR_UNSUPPORTED, at, f"gradients of {grad}, states of {state}")
+        types = dict(weight=torch.float16, master=torch.float32, grad=grad, m=state, v=state, m_scale=torch.uint8, v_scale=torch.uint8)
+        self.device = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        if len(decays) != n or any(ts is not None and len(ts) != n for ts in self.tensors.values()):
+            _fail(QEFT_ERR_SHAPE, at, "lists of different lengths")
+        rows = (qeft_tensor_t * max(n, 1))()
+        for i in range(n):
+            rows[i].n, rows[i].decay = grads[i].numel(), decays[i]
+            for name, ts in self.tensors.items():
+                if ts is None:
+                    continue
+                t, size = ts[i], -(-rows[i].n // QEFT_STATE_BLOCK) if name.endswith("scale") else rows[i].n
+                if t.dtype != types[name]:
+                    _fail(QEFT_ERR_UNSUPPORTED, at, f"{name} {i} is {t.dtype}, not {types[name]}")
+                if t.numel() != size:
+                    _fail(QEFT_ERR_SHAPE, at, f"{name} {i} has {t.numel()} values, not {size}")
+                if not t.is_contiguous() or not t.is_cuda or t.device != self.device or t.device.index != torch.cuda.current_device():
+                    _fail(QEFT_ERR_UNSUPPORTED, at, f"{name} {i} is not contiguous on the current GPU")
+                setattr(rows[i], name, t.data_ptr())
+        size = int(raw.qeft_tensors_plan_bytes(rows, n))
+        plan = torch.zeros(max(size, 16), dtype=torch.uint8)
+        self.c = qeft_tensors_t()
+        _check(raw.qeft_tensors_plan(rows, n, _DTYPES[grad], 8 if state == torch.uint8 else 32, plan.data_ptr(), size, C.byref(self.c)), "qeft_tensors_plan")
+        self.plan = plan.to(self.device)
+        self.c.plan = self.plan.data_ptr()
+
+    def here(self, at):
+        if self.device.index != torch.cuda.current_device():
+            _fail(QEFT_ERR_UNSUPPORTED, at, "the list's tensors are not on the current GPU")
+        return C.byref(self.c)
+
+
+def _number_at(at, name, t, dtype):
+    """Pointer of a number on the device, the first entry of t."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or t.numel() < 1:
+        _fail(QEFT_ERR_UNSUPPORTED, at, f"{name} is {t.dtype} of {t.numel()} values, not {dtype}")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        _fail(QEFT_ERR_UNSUPPORTED, at, f"{name} is not on the current GPU")
+    return t.data_ptr()
+
+
+def qeft_adamw_step(tensors: TensorList, lr: float | torch.Tensor, step: int | torch.Tensor, beta1=0.9, beta2=0.999, eps=1e-8, factor: torch.Tensor | None = None,
+                    stochastic=False, seed=0) -> None:
+    """One step of AdamW over the list, in place.  lr and step (1 for the first) are numbers, or tensors on the GPU (fp32, int32) that hold one; factor: fp32 on the
+    GPU, multiplies the gradients, and the step is left out where it is not finite.  stochastic: fp16 weights without a master are rounded so, as 8-bit states always are, by
+    seed, step and place."""
+    at = "qeft_adamw_step"
+    lr_at, step_at = (_number_at(at, name, t, kind) if isinstance(t, torch.Tensor) else 0 for name, t, kind in (("lr", lr, torch.float32), ("step", step, torch.int32)))
+    a = qeft_adamw_t(0.0 if lr_at else lr, beta1, beta2, eps, 0 if step_at else step, seed & 0xFFFFFFFFFFFFFFFF, lr_at, step_at,
+                     _number_at(at, "factor", factor, torch.float32), int(bool(stochastic)))
+    _check(raw.qeft_adamw_step(tensors.here(at), C.byref(a), _stream()), at)
+
+
+def qeft_grad_norm_workspace(tensors: TensorList) -> int:
+    return int(raw.qeft_grad_norm_workspace(C.byref(tensors.c)))
+
+
+def qeft_grad_norm(tensors: TensorList, max_norm=float("inf"), scale=1.0, out: torch.Tensor | None = None, steps: torch.Tensor | None = None,
+                   ws: torch.Tensor | None = None) -> torch.Tensor:
+    """fp32 [2]: the norm of all gradients times scale, and the factor that brings them back by scale and to a norm of max_norm at most (not-a-number where the norm is
+    not finite).  steps: int32 on the GPU, counted up by one where it is finite."""
+    at = "qeft_grad_norm"
+    if out is None:
+        out = torch.empty(2, dtype=torch.float32, device=tensors.device)
+    if ws is None:
+        n = qeft_grad_norm_workspace(tensors)
+        ws = torch.empty(n, dtype=torch.uint8, device=tensors.device) if n else None
+    po, ps = _take(at, "out", out, torch.float32, (2,))[0], _number_at(at, "steps", steps, torch.int32)
+    pw, nw = _c_workspace(at, ws)
+    a = qeft_grad_norm_t(float(scale), float(max_norm), po, ps, pw, nw)
+    _check(raw.qeft_grad_norm(tensors.here(at), C.byref(a), _stream()), at)
+    return out

@@ -105,17 +105,15 @@ int check_norm_weights(const qeft_norm_desc_t* d, const void* w_pre, const void*
         if (st_ != QEFT_OK) return st_;  \
     } while (0)
 
-}  // namespace
-
-extern "C" {
-
-int qeft_cache_append(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, const qeft_table_t* table, const qeft_append_t* a, void* stream) {
-    Cache c;
-    CHECK(make_cache(desc, cache, table, &c));
+int make_append(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, const qeft_table_t* table, const qeft_append_t* a, Cache* cp, Append* ap) {
+    CHECK(make_cache(desc, cache, table, cp));
+    const Cache& c = *cp;
     if (!a) return QEFT_ERR_NULL;
     if (a->tokens < 0 || a->tokens > QEFT_MAX_ROWS || a->rot_dim < 0 || a->rot_dim > c.d) return QEFT_ERR_SHAPE;
     if (a->rot_dim % 2 != 0) return QEFT_ERR_UNSUPPORTED;
     if (a->q && (a->heads <= 0 || a->heads > QEFT_MAX_DIM)) return QEFT_ERR_SHAPE;
+    Append& p = *ap;
+    p.tokens = (int)a->tokens;
     if (a->tokens == 0) return QEFT_OK;
     CHECK(check_rows(a->k, a->tokens, a->ldk, (int64_t)c.kv * c.d));
     CHECK(check_rows(a->v, a->tokens, a->ldv, (int64_t)c.kv * c.d));
@@ -130,7 +128,6 @@ int qeft_cache_append(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, 
         if (!a->rot) return QEFT_ERR_NULL;
         if (a->positions <= 0 || a->ld_rot < a->rot_dim) return QEFT_ERR_SHAPE;
     }
-    Append p;
     p.q = (const __half*)a->q;
     p.k = (const __half*)a->k;
     p.v = (const __half*)a->v;
@@ -147,8 +144,30 @@ int qeft_cache_append(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, 
     p.positions = a->positions;
     p.rot_dim = a->rot_dim;
     p.heads = a->q ? a->heads : 0;
-    p.tokens = (int)a->tokens;
-    return hip_status(cache_append(c, p, (hipStream_t)stream));
+    return QEFT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qeft_cache_append(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, const qeft_table_t* table, const qeft_append_t* a, void* stream) {
+    Cache c;
+    Append p;
+    CHECK(make_append(desc, cache, table, a, &c, &p));
+    return p.tokens == 0 ? QEFT_OK : hip_status(cache_append(c, p, (hipStream_t)stream));
+}
+
+int qeft_cache_append_norm(const qeft_cache_desc_t* desc, const qeft_cache_t* cache, const qeft_table_t* table, const qeft_append_t* a,
+                           const qeft_append_norm_t* norm, void* stream) {
+    Cache c;
+    Append p;
+    CHECK(make_append(desc, cache, table, a, &c, &p));
+    if (!norm) return QEFT_ERR_NULL;
+    if (!(norm->eps >= 0.f)) return QEFT_ERR_SHAPE;
+    if (!aligned16(norm->w_q) || !aligned16(norm->w_k)) return QEFT_ERR_ALIGN;
+    if (p.tokens > 0 && !norm->w_q && !norm->w_k) return hip_status(cache_append(c, p, (hipStream_t)stream));
+    return p.tokens == 0 ? QEFT_OK : hip_status(heads_append(c, p, (const __half*)norm->w_q, (const __half*)norm->w_k, norm->eps, (hipStream_t)stream));
 }
 
 size_t qeft_attn_workspace(const qeft_cache_desc_t* desc, int64_t seqs, int32_t heads, int64_t longest, int weights) {

@@ -31,9 +31,15 @@ struct Fns {
     decltype(&qeft_cache_evict) cache_evict;
     decltype(&qeft_norm_fwd) norm_fwd;
     decltype(&qeft_norm_bwd) norm_bwd;
+    decltype(&qeft_logprob_fwd) logprob_fwd;
+    decltype(&qeft_logprob_bwd) logprob_bwd;
+    decltype(&qeft_logprob_fwd_bwd) logprob_fwd_bwd;
+    decltype(&qeft_qk_norm_fwd) qk_norm_fwd;
+    decltype(&qeft_qk_norm_bwd) qk_norm_bwd;
+    decltype(&qeft_cache_append_norm) cache_append_norm;
 } fns;
 constexpr int N_FNS = sizeof(Fns) / sizeof(void*);
-PyTypeObject *desc_type, *weight_type, *cache_desc_type, *norm_desc_type;
+PyTypeObject *desc_type, *weight_type, *cache_desc_type, *norm_desc_type, *logprob_desc_type, *qk_desc_type;
 PyObject *n_desc, *n_qweight, *n_scales, *n_zeros, *n_weak;
 
 // the bytes of a ctypes object (which owns them for its lifetime)
@@ -367,31 +373,54 @@ bool cache_args(Call& c, PyObject* const* a, const qeft_cache_desc_t*& d, qeft_c
 }
 // tokens that a row of the table can hold
 int64_t slots(const qeft_cache_desc_t* d, const qeft_table_t& table) { return (int64_t)table.table_pages * d->page_size; }
-// (desc, K, V, table, k, v, index, seq, q, q_out, rot, pos)
+// an append's arguments: (desc, K, V, table, k, v, index, seq, q, q_out, rot, pos, ...)
+bool append_args(Call& c, PyObject* const* a, const qeft_cache_desc_t*& d, qeft_cache_t& pools, qeft_table_t& table, qeft_append_t& p) {
+    if (!cache_args(c, a, d, pools, table)) return false;
+    int64_t tokens = -1, width = (int64_t)d->kv_heads * d->head_dim, qw = -1, positions = -1, rot = -1;
+    p.k = c.rows(a[4], at::kHalf, tokens, width, p.ldk);
+    p.v = c.rows(a[5], at::kHalf, tokens, width, p.ldv);
+    p.index = (const int32_t*)c.vec(a[6], at::kInt, tokens);
+    p.seq = (const int32_t*)c.vec(a[7], at::kInt, tokens, true);
+    p.q = c.rows(a[8], at::kHalf, tokens, qw, p.ldq, true);
+    p.q_out = nullptr, p.ldq_out = 0;
+    if (p.q) p.q_out = c.rows(a[9], at::kHalf, tokens, qw, p.ldq_out);
+    p.rot = (const float*)c.rows(a[10], at::kFloat, positions, rot, p.ld_rot, true);
+    p.pos = (const int32_t*)c.vec(a[11], at::kInt, tokens, true);
+    if (!c.ok || (p.q && (qw % d->head_dim != 0 || qw / d->head_dim > INT32_MAX)) || positions > INT32_MAX || rot > INT32_MAX) return false;
+    p.heads = p.q ? (int32_t)(qw / d->head_dim) : 0;
+    p.positions = p.rot ? (int32_t)positions : 0;
+    p.rot_dim = p.rot ? (int32_t)rot : 0;
+    p.tokens = tokens;
+    return true;
+}
 PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&](Call& c, int& st) {
         const qeft_cache_desc_t* d;
         qeft_cache_t pools;
         qeft_table_t table;
-        if (n != 12 || !cache_args(c, a, d, pools, table)) return false;
         qeft_append_t p;
-        int64_t tokens = -1, width = (int64_t)d->kv_heads * d->head_dim, qw = -1, positions = -1, rot = -1;
-        p.k = c.rows(a[4], at::kHalf, tokens, width, p.ldk);
-        p.v = c.rows(a[5], at::kHalf, tokens, width, p.ldv);
-        p.index = (const int32_t*)c.vec(a[6], at::kInt, tokens);
-        p.seq = (const int32_t*)c.vec(a[7], at::kInt, tokens, true);
-        p.q = c.rows(a[8], at::kHalf, tokens, qw, p.ldq, true);
-        p.q_out = nullptr, p.ldq_out = 0;
-        if (p.q) p.q_out = c.rows(a[9], at::kHalf, tokens, qw, p.ldq_out);
-        p.rot = (const float*)c.rows(a[10], at::kFloat, positions, rot, p.ld_rot, true);
-        p.pos = (const int32_t*)c.vec(a[11], at::kInt, tokens, true);
+        if (n != 12 || !append_args(c, a, d, pools, table, p)) return false;
         void* s = c.stream();
-        if (!c.ok || (p.q && (qw % d->head_dim != 0 || qw / d->head_dim > INT32_MAX)) || positions > INT32_MAX || rot > INT32_MAX) return false;
-        p.heads = p.q ? (int32_t)(qw / d->head_dim) : 0;
-        p.positions = p.rot ? (int32_t)positions : 0;
-        p.rot_dim = p.rot ? (int32_t)rot : 0;
-        p.tokens = tokens;
+        if (!c.ok) return false;
         st = unlocked([&] { return fns.cache_append(d, &pools, &table, &p, s); });
+        return true;
+    });
+}
+// (..., w_q, w_k, eps)
+PyObject* cache_append_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&](Call& c, int& st) {
+        const qeft_cache_desc_t* d;
+        qeft_cache_t pools;
+        qeft_table_t table;
+        qeft_append_t p;
+        if (n != 15 || !append_args(c, a, d, pools, table, p)) return false;
+        qeft_append_norm_t w;
+        w.w_q = c.vec(a[12], at::kHalf, d->head_dim, true);
+        w.w_k = c.vec(a[13], at::kHalf, d->head_dim, true);
+        w.eps = (float)c.real(a[14]);
+        void* s = c.stream();
+        if (!c.ok) return false;
+        st = unlocked([&] { return fns.cache_append_norm(d, &pools, &table, &p, &w, s); });
         return true;
     });
 }
@@ -507,10 +536,144 @@ PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t argc) {
         return true;
     });
 }
-// (addresses of the C functions in the order of Fns, qeft_desc_t, Weight, qeft_cache_desc_t, qeft_norm_desc_t)
+at::ScalarType logits(const qeft_logprob_desc_t* d) { return d->dtype == QEFT_DTYPE_F32 ? at::kFloat : at::kHalf; }
+// (z, token, logp, lse, entropy, top, top_logp, top_index, ws) of a forward
+bool logprob_args(Call& c, const qeft_logprob_desc_t* d, qeft_logprob_fwd_t& p, PyObject* z, PyObject* token, PyObject* logp, PyObject* lse, PyObject* entropy, PyObject* ws) {
+    int64_t m = -1, n = d->n;
+    p.z = c.rows(z, logits(d), m, n, p.ldz);
+    p.token = (const int32_t*)c.vec(token, at::kInt, m, true);
+    p.logp = (float*)c.vec(logp, at::kFloat, m, true);
+    p.lse = (float*)c.vec(lse, at::kFloat, m, true);
+    p.entropy = (float*)c.vec(entropy, at::kFloat, m, true);
+    p.ws = c.bytes(ws, p.ws_bytes);
+    p.top_logp = nullptr, p.top_index = nullptr, p.ld_top = 0, p.top = 0;
+    p.m = m;
+    return c.ok;
+}
+// (desc, z, token, logp, lse, entropy, top, top_logp, top_index, ws)
+PyObject* logprob_fwd(PyObject*, PyObject* const* a, Py_ssize_t argc) {
+    return guarded([&](Call& c, int& st) {
+        if (argc != 10) return false;
+        const qeft_logprob_desc_t* d = c.described<qeft_logprob_desc_t>(a[0], logprob_desc_type);
+        qeft_logprob_fwd_t p;
+        if (!d || !logprob_args(c, d, p, a[1], a[2], a[3], a[4], a[5], a[9])) return false;
+        int64_t top = c.whole(a[6]), ld_index = 0;
+        if (top > 0) {
+            p.top_logp = (float*)c.rows(a[7], at::kFloat, p.m, top, p.ld_top);
+            p.top_index = (int32_t*)c.rows(a[8], at::kInt, p.m, top, ld_index);
+        } else if (a[7] != Py_None || a[8] != Py_None) return false;
+        void* s = c.stream();
+        if (!c.ok || top < 0 || top > QEFT_MAX_TOP || p.ld_top != ld_index) return false;
+        p.top = (int32_t)top;
+        st = unlocked([&] { return fns.logprob_fwd(d, &p, s); });
+        return true;
+    });
+}
+// (desc, z, lse, token, dlogp, dlse, entropy, dentropy, dz)
+PyObject* logprob_bwd(PyObject*, PyObject* const* a, Py_ssize_t argc) {
+    return guarded([&](Call& c, int& st) {
+        if (argc != 9) return false;
+        const qeft_logprob_desc_t* d = c.described<qeft_logprob_desc_t>(a[0], logprob_desc_type);
+        if (!d) return false;
+        qeft_logprob_bwd_t p;
+        int64_t m = -1, n = d->n;
+        p.z = c.rows(a[1], logits(d), m, n, p.ldz);
+        p.lse = (const float*)c.vec(a[2], at::kFloat, m);
+        p.token = (const int32_t*)c.vec(a[3], at::kInt, m, true);
+        p.dlogp = (const float*)c.vec(a[4], at::kFloat, m, true);
+        p.dlse = (const float*)c.vec(a[5], at::kFloat, m, true);
+        p.entropy = (const float*)c.vec(a[6], at::kFloat, m, true);
+        p.dentropy = (const float*)c.vec(a[7], at::kFloat, m, true);
+        p.dz = c.rows(a[8], logits(d), m, n, p.lddz);
+        p.m = m;
+        void* s = c.stream();
+        if (!c.ok) return false;
+        st = unlocked([&] { return fns.logprob_bwd(d, &p, s); });
+        return true;
+    });
+}
+// (desc, z, token, dlogp, dlse, dentropy, dz, logp, lse, entropy, ws)
+PyObject* logprob_fwd_bwd(PyObject*, PyObject* const* a, Py_ssize_t argc) {
+    return guarded([&](Call& c, int& st) {
+        if (argc != 11) return false;
+        const qeft_logprob_desc_t* d = c.described<qeft_logprob_desc_t>(a[0], logprob_desc_type);
+        qeft_logprob_fwd_t p;
+        if (!d || !logprob_args(c, d, p, a[1], a[2], a[7], a[8], a[9], a[10])) return false;
+        qeft_logprob_bwd_t b{};
+        int64_t m = p.m, n = d->n;
+        b.dlogp = (const float*)c.vec(a[3], at::kFloat, m, true);
+        b.dlse = (const float*)c.vec(a[4], at::kFloat, m, true);
+        b.dentropy = (const float*)c.vec(a[5], at::kFloat, m, true);
+        b.dz = c.rows(a[6], logits(d), m, n, b.lddz);
+        b.m = m;
+        void* s = c.stream();
+        if (!c.ok) return false;
+        st = unlocked([&] { return fns.logprob_fwd_bwd(d, &p, &b, s); });
+        return true;
+    });
+}
+// (desc, q, k, w_q, w_k, rot, pos, q_out, k_out)
+PyObject* qk_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t argc) {
+    return guarded([&](Call& c, int& st) {
+        if (argc != 9) return false;
+        const qeft_qk_desc_t* d = c.described<qeft_qk_desc_t>(a[0], qk_desc_type);
+        if (!d) return false;
+        qeft_qk_fwd_t p;
+        int64_t m = -1, qw = (int64_t)d->heads * d->head_dim, kw = (int64_t)d->kv_heads * d->head_dim, positions = -1, rot = d->rot_dim;
+        p.q = c.rows(a[1], at::kHalf, m, qw, p.ldq, true);
+        p.k = c.rows(a[2], at::kHalf, m, kw, p.ldk, true);
+        if (m < 0) return false;      // (neither)
+        p.w_q = c.vec(a[3], at::kHalf, d->head_dim, true);
+        p.w_k = c.vec(a[4], at::kHalf, d->head_dim, true);
+        p.rot = (const float*)c.rows(a[5], at::kFloat, positions, rot, p.ld_rot, true);
+        p.pos = (const int32_t*)c.vec(a[6], at::kInt, m, true);
+        p.q_out = c.rows(a[7], at::kHalf, m, qw, p.ldq_out, !p.q);
+        p.k_out = c.rows(a[8], at::kHalf, m, kw, p.ldk_out, !p.k);
+        void* s = c.stream();
+        if (!c.ok || positions > INT32_MAX) return false;
+        p.positions = p.rot ? (int32_t)positions : 0;
+        p.m = m;
+        st = unlocked([&] { return fns.qk_norm_fwd(d, &p, s); });
+        return true;
+    });
+}
+// (desc, gq, gk, q, k, w_q, w_k, rot, pos, dq, dk, dw_q, dw_k, accumulate, ws)
+PyObject* qk_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t argc) {
+    return guarded([&](Call& c, int& st) {
+        if (argc != 15) return false;
+        const qeft_qk_desc_t* d = c.described<qeft_qk_desc_t>(a[0], qk_desc_type);
+        if (!d) return false;
+        qeft_qk_bwd_t p;
+        int64_t m = -1, qw = (int64_t)d->heads * d->head_dim, kw = (int64_t)d->kv_heads * d->head_dim, positions = -1, rot = d->rot_dim;
+        p.gq = c.rows(a[1], at::kHalf, m, qw, p.ldgq, true);
+        p.gk = c.rows(a[2], at::kHalf, m, kw, p.ldgk, true);
+        if (m < 0) return false;
+        p.q = c.rows(a[3], at::kHalf, m, qw, p.ldq, true);
+        p.k = c.rows(a[4], at::kHalf, m, kw, p.ldk, true);
+        p.w_q = c.vec(a[5], at::kHalf, d->head_dim, true);
+        p.w_k = c.vec(a[6], at::kHalf, d->head_dim, true);
+        p.rot = (const float*)c.rows(a[7], at::kFloat, positions, rot, p.ld_rot, true);
+        p.pos = (const int32_t*)c.vec(a[8], at::kInt, m, true);
+        p.dq = c.rows(a[9], at::kHalf, m, qw, p.lddq, true);
+        p.dk = c.rows(a[10], at::kHalf, m, kw, p.lddk, true);
+        p.dw_q = (float*)c.vec(a[11], at::kFloat, d->head_dim, true);
+        p.dw_k = (float*)c.vec(a[12], at::kFloat, d->head_dim, true);
+        p.accumulate = PyObject_IsTrue(a[13]) == 1;
+        p.ws = c.bytes(a[14], p.ws_bytes);
+        void* s = c.stream();
+        if (!c.ok || positions > INT32_MAX) return false;
+        p.positions = p.rot ? (int32_t)positions : 0;
+        p.m = m;
+        st = unlocked([&] { return fns.qk_norm_bwd(d, &p, s); });
+        return true;
+    });
+}
+// (addresses of the C functions in the order of Fns, qeft_desc_t, Weight, qeft_cache_desc_t, qeft_norm_desc_t, qeft_logprob_desc_t, qeft_qk_desc_t)
 PyObject* init(PyObject*, PyObject* args) {
-    PyObject *f, *d, *w, *cd, *nd;
-    if (!PyArg_ParseTuple(args, "O!O!O!O!O!", &PyTuple_Type, &f, &PyType_Type, &d, &PyType_Type, &w, &PyType_Type, &cd, &PyType_Type, &nd)) return nullptr;
+    PyObject *f, *d, *w, *cd, *nd, *ld, *qd;
+    if (!PyArg_ParseTuple(args, "O!O!O!O!O!O!O!", &PyTuple_Type, &f, &PyType_Type, &d, &PyType_Type, &w, &PyType_Type, &cd, &PyType_Type, &nd, &PyType_Type, &ld,
+                          &PyType_Type, &qd))
+        return nullptr;
     if (PyTuple_GET_SIZE(f) != N_FNS) return PyErr_Format(PyExc_ValueError, "%d functions expected", N_FNS);
     void* at[N_FNS];
     for (int i = 0; i < N_FNS; ++i) {
@@ -518,11 +681,13 @@ PyObject* init(PyObject*, PyObject* args) {
         if (PyErr_Occurred()) return nullptr;
     }
     memcpy(&fns, at, sizeof fns);
-    for (PyObject* o : {d, w, cd, nd}) Py_INCREF(o);
+    for (PyObject* o : {d, w, cd, nd, ld, qd}) Py_INCREF(o);
     desc_type = (PyTypeObject*)d;
     weight_type = (PyTypeObject*)w;
     cache_desc_type = (PyTypeObject*)cd;
     norm_desc_type = (PyTypeObject*)nd;
+    logprob_desc_type = (PyTypeObject*)ld;
+    qk_desc_type = (PyTypeObject*)qd;
     Py_RETURN_NONE;
 }
 
@@ -540,6 +705,12 @@ PyMethodDef methods[] = {
     {"cache_evict", (PyCFunction)(void (*)())cache_evict, METH_FASTCALL, nullptr},
     {"norm_fwd", (PyCFunction)(void (*)())norm_fwd, METH_FASTCALL, nullptr},
     {"norm_bwd", (PyCFunction)(void (*)())norm_bwd, METH_FASTCALL, nullptr},
+    {"logprob_fwd", (PyCFunction)(void (*)())logprob_fwd, METH_FASTCALL, nullptr},
+    {"logprob_bwd", (PyCFunction)(void (*)())logprob_bwd, METH_FASTCALL, nullptr},
+    {"logprob_fwd_bwd", (PyCFunction)(void (*)())logprob_fwd_bwd, METH_FASTCALL, nullptr},
+    {"qk_norm_fwd", (PyCFunction)(void (*)())qk_norm_fwd, METH_FASTCALL, nullptr},
+    {"qk_norm_bwd", (PyCFunction)(void (*)())qk_norm_bwd, METH_FASTCALL, nullptr},
+    {"cache_append_norm", (PyCFunction)(void (*)())cache_append_norm, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -15,109 +15,16 @@
 // Measured: forward 4096 x 4096, fp32 residual: 39 us, 5.2 TB/s; gradient 4096 x 8192 with both norms and a channel gate: 122 - 125 us, 5 TB/s, 6 of it the slabs' sum;
 // 333 x 5120, token gate: 15 us, where the bytes take 5.3 (two rows a workgroup and the second launch, latencies).
 #include <algorithm>
+#include "octets.h"
 #include "qeft_internal.h"
 #include "wave.h"
 
 namespace qeft {
 namespace {
 
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-typedef float f4 __attribute__((ext_vector_type(4)));
-
 constexpr int FWD_MAX = 32768;    // values of a row that the forward keeps in registers (1024 threads x 4 octets)
 constexpr int BWD_MAX = 16384;    // and the gradient (1024 x 2: beside three column sums)
 
-// A row's address, the same in all lanes: kept from the optimiser, which would otherwise add a lane's offset to every array's base outside the loop over
-// the rows and hold those sums, two registers each (the gradient has eight arrays), instead of adding in the load.
-__device__ __forceinline__ const char* row_of(const void* p, int64_t row, int64_t ld, bool f32) {
-    const char* r = (const char*)p + row * ld * (f32 ? 4 : 2);
-    asm volatile("" : "+s"(r));
-    return r;
-}
-__device__ __forceinline__ char* row_of(void* p, int64_t row, int64_t ld, bool f32) { return const_cast<char*>(row_of((const void*)p, row, ld, f32)); }
-
-// Eight values of a row as loaded.  left: how many of them exist; a row's last octet may be partial, and is read value by value, the last one first.
-template <bool F32> struct Raw;
-template <> struct Raw<false> {
-    u4 v;
-    __device__ __forceinline__ void load(const void* row, uint32_t at, int left) {
-        const char* p = (const char*)row + 2 * at;
-        if (left >= 8) {
-            v = *reinterpret_cast<const u4*>(p);
-            return;
-        }
-        v = u4{0, 0, 0, 0};
-#pragma unroll 1
-        for (int e = left - 1; e >= 0; --e) {
-            const uint32_t x = *reinterpret_cast<const uint16_t*>(p + 2 * e);
-            v = u4{v.x << 16 | x, v.y << 16 | v.x >> 16, v.z << 16 | v.y >> 16, v.w << 16 | v.z >> 16};
-        }
-    }
-    __device__ __forceinline__ float operator[](int e) const { return (float)__builtin_bit_cast(h8, v)[e]; }
-    __device__ __forceinline__ void clear() { v = u4{0, 0, 0, 0}; }
-    // Eight values stay four registers: without this the compiler converts once and keeps eight (across a loop for a row of weights).
-    __device__ __forceinline__ void pin() { asm volatile("" : "+v"(v)); }
-};
-template <> struct Raw<true> {
-    f4 a, b;
-    __device__ __forceinline__ void load(const void* row, uint32_t at, int left) {
-        const char* p = (const char*)row + 4 * at;
-        if (left >= 8) {
-            a = *reinterpret_cast<const f4*>(p);
-            b = *reinterpret_cast<const f4*>(p + 16);
-            return;
-        }
-        clear();
-#pragma unroll 1
-        for (int e = left - 1; e >= 0; --e) {
-            b = f4{a.w, b.x, b.y, b.z};
-            a = f4{*reinterpret_cast<const float*>(p + 4 * e), a.x, a.y, a.z};
-        }
-    }
-    __device__ __forceinline__ float operator[](int e) const { return e < 4 ? a[e & 3] : b[e & 3]; }
-    __device__ __forceinline__ void clear() { a = b = f4{0.f, 0.f, 0.f, 0.f}; }
-    __device__ __forceinline__ void pin() {}
-};
-typedef Raw<false> Half8;
-
-// x goes to the row, rounded to its type (which x then is too)
-template <bool F32>
-__device__ __forceinline__ void store(void* row, uint32_t at, int left, float (&x)[8]) {
-    if (F32) {
-        char* p = (char*)row + 4 * at;
-        f4 a = {x[0], x[1], x[2], x[3]}, b = {x[4], x[5], x[6], x[7]};
-        if (left >= 8) {
-            *reinterpret_cast<f4*>(p) = a;
-            *reinterpret_cast<f4*>(p + 16) = b;
-            return;
-        }
-#pragma unroll 1
-        for (int e = 0; e < left; ++e) {
-            *reinterpret_cast<float*>(p + 4 * e) = a.x;
-            a = f4{a.y, a.z, a.w, b.x};
-            b = f4{b.y, b.z, b.w, b.w};
-        }
-        return;
-    }
-    h8 h;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        h[e] = (_Float16)x[e];
-        x[e] = (float)h[e];
-    }
-    u4 v = __builtin_bit_cast(u4, h);
-    char* p = (char*)row + 2 * at;
-    if (left >= 8) {
-        *reinterpret_cast<u4*>(p) = v;
-        return;
-    }
-#pragma unroll 1
-    for (int e = 0; e < left; ++e) {
-        *reinterpret_cast<uint16_t*>(p + 2 * e) = (uint16_t)v.x;
-        v = u4{v.x >> 16 | v.y << 16, v.y >> 16 | v.z << 16, v.z >> 16 | v.w << 16, v.w >> 16};
-    }
-}
 template <bool F32>
 __device__ __forceinline__ void round_to(float (&x)[8]) {
     if (F32) return;

@@ -267,4 +267,72 @@ size_t norm_workspace(int n, int64_t m);
 size_t norm_bwd_workspace(int n, int64_t m, bool sums);   // that, or 0 where a call without sums over rows uses none of it
 hipError_t norm_bwd(const Norm& a, hipStream_t s);
 
+// ---- the ends of a step: log probabilities, norms of heads with rotation, the optimizer (ends_api.hip checks the arguments) ----
+struct Logprob {             // either direction: what a call does not have is NULL
+    const void* z;
+    const int* token;
+    float *logp, *lse, *entropy, *top_logp;
+    int* top_index;
+    const float *lse_in, *entropy_in, *dlogp, *dlse, *dentropy;
+    void* dz;
+    int64_t ldz, ld_top, lddz, m;
+    int n, f32, top;
+    float scale;
+    unsigned char* ws;
+};
+size_t logprob_workspace(int n, bool f32, int64_t m, int top);   // (logprob.hip)
+hipError_t logprob_fwd(const Logprob& a, hipStream_t s);         // with dz: the gradient too, from dlogp, dlse, dentropy
+hipError_t logprob_bwd(const Logprob& a, hipStream_t s);
+
+struct HeadPart {            // the heads of q or of k: what a call does not have is NULL
+    const __half *x, *w, *g;
+    __half *out, *dx;        // forward, gradient
+    float* dw;
+    int64_t ldx, ldg, ldout, lddx;
+    int heads;
+};
+struct Heads {
+    HeadPart q, k;
+    const int* pos;
+    const float* rot;
+    int64_t ld_rot, m;
+    int d, rot_dim, positions, accumulate;
+    float eps;
+    unsigned char* ws;
+};
+size_t heads_workspace(int d, int heads, int kv, int rot_dim, int64_t m);   // (heads.hip)
+hipError_t heads_fwd(const Heads& a, hipStream_t s);
+hipError_t heads_bwd(const Heads& a, hipStream_t s);
+hipError_t heads_append(const Cache& c, const Append& p, const __half* w_q, const __half* w_k, float eps, hipStream_t s);
+
+// A list of tensors as the device has it: records, then for every piece of work the tensor and the piece's number in it.
+struct TensorRecord {
+    void* weight;
+    float* master;
+    const void* grad;
+    void *m, *v;
+    uint8_t *m_scale, *v_scale;
+    int64_t n;
+    int64_t first_block;     // blocks of the tensors before it
+    float decay;
+    int32_t first_piece;     // pieces of work before it
+};
+constexpr int PIECE = 8192;  // values of a piece of work, whole blocks
+struct Tensors {
+    const TensorRecord* records;
+    const int* piece_of;     // [work] the tensor of a piece
+    int work, grad_f32, bits, has_weight, has_master;
+};
+inline size_t tensors_map_at(int count) { return (size_t)count * sizeof(TensorRecord); }
+struct Adamw {
+    float lr, beta1, beta2, one_minus_beta1, one_minus_beta2, eps, log_beta1, log_beta2, c1, c2;
+    int step, stochastic;
+    uint32_t seed_low, seed_high;
+    const float *lr_at, *factor;
+    const int* step_at;
+};
+hipError_t adamw_step(const Tensors& t, const Adamw& a, hipStream_t s);   // (adamw.hip)
+size_t grad_norm_workspace(int work);
+hipError_t grad_norm(const Tensors& t, float scale, float max_norm, float* out, int* steps, unsigned char* ws, hipStream_t s);
+
 }  // namespace qeft

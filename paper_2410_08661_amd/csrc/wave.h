@@ -50,6 +50,9 @@ __device__ __forceinline__ T wave_reduce(T x, const Op& op) { return across<true
 struct Sum {
     template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a + b; }
 };
+struct Most {
+    template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a < b ? b : a; }
+};
 struct Least {
     template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return b < a ? b : a; }
 };

@@ -1,0 +1,239 @@
+"""qeft_qk_norm_fwd, qeft_qk_norm_bwd and qeft_cache_append_norm against the formulas in 64 bits, and against differences of the forward."""
+import pytest
+import torch
+
+import block_util as BU
+import ends_util as V
+from paper_2410_08661_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-6
+LAYOUTS = [(8, 8, 1, 1), (8, 2, 3, 3), (16, 6, 2, 1), (40, 20, 5, 1), (64, 64, 8, 2), (64, 32, 3, 3), (80, 80, 12, 2), (96, 48, 4, 4), (128, 128, 32, 32), (128, 64, 64, 8), (128, 0, 4, 2),
+           (136, 134, 3, 2), (192, 192, 4, 1), (256, 256, 16, 4), (256, 2, 2, 1), (248, 62, 33, 1)]
+
+
+def padded(m, n, gen, std=1.0, pad=8):
+    return (torch.randn((m, n + pad), generator=gen, device="cuda") * std).half()[:, :n]
+
+
+def inputs(m, d, rot_dim, heads, kv, norm=True, seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed + m + 31 * d + heads)
+    i = dict(q=padded(m, heads * d, gen, 2.0), k=padded(m, kv * d, gen, 1.0, 16), gq=padded(m, heads * d, gen, 0.2, 0), gk=padded(m, kv * d, gen, 0.2, 24),
+             w_q=None, w_k=None, rot=None, pos=torch.randint(-2, m + 20, (m,), generator=gen, device="cuda").int())
+    if norm:
+        i.update(w_q=(1 + 0.2 * torch.randn(d, generator=gen, device="cuda")).half(), w_k=(1 + 0.2 * torch.randn(d, generator=gen, device="cuda")).half())
+    if rot_dim:
+        angle = torch.rand((m + 15, rot_dim // 2), generator=gen, device="cuda", dtype=torch.float64) * 6.3
+        i["rot"] = torch.cat([angle.cos(), angle.sin(), angle[:, :3] * 0 + 9], 1).float()[:, :rot_dim]      # (a pitch of its own)
+    return i
+
+
+def check_fwd(m, d, rot_dim, heads, kv, norm):
+    i = inputs(m, d, rot_dim, heads, kv, norm)
+    desc = B.make_qk_desc(d, heads, kv, rot_dim, EPS)
+    kw = dict(w_q=i["w_q"], w_k=i["w_k"], rot=i["rot"], pos=i["pos"])
+    q, k = B.qeft_qk_norm_fwd(desc, i["q"], i["k"], **kw)
+    for name, got, n, w in (("q", q, heads, i["w_q"]), ("k", k, kv, i["w_k"])):
+        V.close(name, got, *V.heads_forward(i[name], n, w, EPS, i["rot"], i["pos"], rot_dim), V.HALF)
+    # in place; one of the two alone; positions by row
+    q2, k2 = i["q"].clone(), i["k"].clone()
+    q2, k2 = padded(m, heads * d, torch.Generator(device="cuda")).copy_(i["q"]), padded(m, kv * d, torch.Generator(device="cuda")).copy_(i["k"])
+    a, b = B.qeft_qk_norm_fwd(desc, q2, k2, q_out=q2, k_out=k2, **kw)
+    assert a is q2 and b is k2 and torch.equal(a, q) and torch.equal(b, k)
+    a, b = B.qeft_qk_norm_fwd(desc, i["q"], None, **kw)
+    assert b is None and torch.equal(a, q)
+    a, b = B.qeft_qk_norm_fwd(desc, None, i["k"], **{**kw, "w_q": None})
+    assert a is None and torch.equal(b, k)
+    rows = torch.arange(m, device="cuda").int()
+    for x, y in zip(B.qeft_qk_norm_fwd(desc, i["q"], i["k"], **{**kw, "pos": None}), B.qeft_qk_norm_fwd(desc, i["q"], i["k"], **{**kw, "pos": rows})):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("m", [1, 7, 300])
+@pytest.mark.parametrize("d,rot_dim,heads,kv", LAYOUTS)
+def test_forward(d, rot_dim, heads, kv, m, norm):
+    check_fwd(m, d, rot_dim, heads, kv, norm)
+
+
+def check_bwd(m, d, rot_dim, heads, kv, norm=True):
+    i = inputs(m, d, rot_dim, heads, kv, norm)
+    desc = B.make_qk_desc(d, heads, kv, rot_dim, EPS)
+    kw = dict(q=i["q"] if norm else None, k=i["k"] if norm else None, w_q=i["w_q"], w_k=i["w_k"], rot=i["rot"], pos=i["pos"])
+    got = dict(zip(("q", "k", "w_q", "w_k"), B.qeft_qk_norm_bwd(desc, i["gq"], i["gk"], **kw)))
+    for name, n in (("q", heads), ("k", kv)):
+        dx, dw = V.heads_backward(i["g" + name], i[name], n, i["w_" + name], EPS, i["rot"], i["pos"], rot_dim)
+        V.close("d" + name, got[name], *dx, V.HALF)
+        assert (dw is None) == (got["w_" + name] is None)
+        if dw:
+            V.close("dw_" + name, got["w_" + name], *dw, V.U)
+    for a, b in zip(B.qeft_qk_norm_bwd(desc, i["gq"], i["gk"], **kw), got.values()):
+        assert a is b is None or torch.equal(a, b)                   # the order of the sums is fixed
+    return i, desc, kw, got
+
+
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("m", [1, 7, 300])
+@pytest.mark.parametrize("d,rot_dim,heads,kv", LAYOUTS)
+def test_backward(d, rot_dim, heads, kv, m, norm):
+    check_bwd(m, d, rot_dim, heads, kv, norm)
+
+
+@pytest.mark.parametrize("m,d,heads,kv", [(2000, 128, 32, 32), (4001, 64, 12, 2), (20001, 32, 1, 1)])
+def test_backward_of_many_tokens(m, d, heads, kv):
+    check_bwd(m, d, d, heads, kv)
+
+
+@pytest.mark.parametrize("d,rot_dim,heads,kv", [(128, 128, 8, 2), (80, 40, 3, 3), (24, 2, 1, 2)])
+def test_backward_in_place_in_parts_and_accumulated(d, rot_dim, heads, kv):
+    i, desc, kw, got = check_bwd(50, d, rot_dim, heads, kv)
+    gq, gk = (padded(50, n * d, torch.Generator(device="cuda")).copy_(i[name]) for name, n in (("gq", heads), ("gk", kv)))
+    dq, dk, dw_q, dw_k = B.qeft_qk_norm_bwd(desc, gq, gk, dq=gq, dk=gk, **kw)
+    assert dq is gq and dk is gk
+    for a, b in zip((dq, dk, dw_q, dw_k), got.values()):
+        assert torch.equal(a, b)
+    sums = [got["w_q"].clone(), got["w_k"].clone()]
+    B.qeft_qk_norm_bwd(desc, i["gq"], i["gk"], dw_q=sums[0], dw_k=sums[1], accumulate=True, **kw)
+    assert torch.equal(sums[0], 2 * got["w_q"]) and torch.equal(sums[1], 2 * got["w_k"])
+    some = B.qeft_qk_norm_bwd(desc, i["gq"], i["gk"], dq=False, dw_k=False, **kw)
+    assert some[0] is None and some[3] is None and torch.equal(some[1], got["k"]) and torch.equal(some[2], got["w_q"])
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    some = B.qeft_qk_norm_bwd(desc, i["gq"], i["gk"], dw_q=False, dw_k=False, ws=none, **kw)
+    assert torch.equal(some[0], got["q"]) and torch.equal(some[1], got["k"])
+    alone = B.qeft_qk_norm_bwd(desc, None, i["gk"], **{**kw, "q": None, "w_q": None})
+    assert alone[0] is None and alone[2] is None and torch.equal(alone[1], got["k"]) and torch.equal(alone[3], got["w_k"])
+    with pytest.raises(B.QeftError) as e:
+        B.qeft_qk_norm_bwd(desc, i["gq"], i["gk"], ws=none, **kw)
+    assert e.value.status == B.QEFT_ERR_WORKSPACE
+
+
+def test_backward_against_differences():
+    m, d, rot_dim, heads, kv = 5, 24, 16, 3, 2
+    i = inputs(m, d, rot_dim, heads, kv)
+    desc = B.make_qk_desc(d, heads, kv, rot_dim, EPS)
+    got = dict(zip(("q", "k", "w_q", "w_k"), B.qeft_qk_norm_bwd(desc, i["gq"], i["gk"], q=i["q"], k=i["k"], w_q=i["w_q"], w_k=i["w_k"], rot=i["rot"], pos=i["pos"])))
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    for name, grad in got.items():
+        way = torch.randn(i[name].shape, generator=gen, device="cuda", dtype=torch.float64)
+        ends = []
+        for e in (1e-5, -1e-5):
+            x = {k: (v.double() + e * way if k == name else v) for k, v in i.items()}
+            ends.append(sum((V.heads_forward(x[n], h, x["w_" + n], EPS, i["rot"], i["pos"], rot_dim)[0] * i["g" + n].double()).sum() for n, h in (("q", heads), ("k", kv))))
+        slope, along = (ends[0] - ends[1]) / 2e-5, (grad.double() * way).sum()
+        # fp16 gradients of unit directions: half a step of each, in quadrature with room
+        assert abs(float(slope - along)) <= 8 * V.HALF * float((grad.double() * way).norm()) + 1e-6, name
+
+
+def test_no_rows():
+    desc = B.make_qk_desc(64, 2, 1, 64, EPS)
+    e, f, w, rot = (torch.empty((0, n), dtype=torch.float16, device="cuda") for n in (128, 64)).__iter__(), None, torch.ones(64, dtype=torch.float16, device="cuda"), torch.ones((3, 64), device="cuda")
+    e, f = e
+    q, k = B.qeft_qk_norm_fwd(desc, e, f, w_q=w, w_k=w, rot=rot)
+    assert q.shape == (0, 128) and k.shape == (0, 64)
+    dw = [torch.full((64,), 3.0, device="cuda") for _ in range(2)]
+    B.qeft_qk_norm_bwd(desc, e, f, q=e, k=f, w_q=w, w_k=w, rot=rot, dw_q=dw[0], dw_k=dw[1], accumulate=True)
+    assert all(bool((t == 3).all()) for t in dw)
+    B.qeft_qk_norm_bwd(desc, e, f, q=e, k=f, w_q=w, w_k=w, rot=rot, dw_q=dw[0], dw_k=dw[1])
+    assert not any(bool(t.any()) for t in dw)
+
+
+def test_zeros_and_no_eps():
+    """A head of zeros has no direction: with an eps it stays zero."""
+    i = inputs(6, 64, 64, 2, 2)
+    i["q"][2, :64] = 0
+    desc = B.make_qk_desc(64, 2, 2, 64, EPS)
+    q, _ = B.qeft_qk_norm_fwd(desc, i["q"], i["k"], w_q=i["w_q"], w_k=i["w_k"], rot=i["rot"], pos=i["pos"])
+    assert not bool(q[2, :64].any()) and bool(q.isfinite().all())
+    desc = B.make_qk_desc(64, 2, 2, 64, 0.0)
+    _, k = B.qeft_qk_norm_fwd(desc, i["q"], i["k"], w_q=i["w_q"], w_k=i["w_k"], rot=i["rot"], pos=i["pos"])
+    V.close("k", k, *V.heads_forward(i["k"], 2, i["w_k"], 0.0, i["rot"], i["pos"], 64), V.HALF)
+    dw = B.qeft_qk_norm_bwd(desc, None, i["gk"], k=i["k"], w_k=i["w_k"], rot=i["rot"], pos=i["pos"])[3]
+    V.close("dw", dw, *V.heads_backward(i["gk"], i["k"], 2, i["w_k"], 0.0, i["rot"], i["pos"], 64)[1], V.U)
+
+
+@pytest.mark.parametrize("order", ["pages", "tokens", "heads"])
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("d,rot_dim,heads,kv", [(128, 128, 32, 32), (64, 32, 8, 2), (80, 80, 6, 1), (24, 0, 2, 2), (256, 256, 16, 1), (40, 2, 3, 3)])
+def test_append(d, rot_dim, heads, kv, norm, order):
+    m, page, seqs, cols = 21, 8, 3, 4
+    gen = torch.Generator(device="cuda").manual_seed(d + heads)
+    i = inputs(m, d, rot_dim, heads, kv, norm)
+    v = padded(m, kv * d, gen)
+    pools = [BU.pool_of(seqs * cols, kv, page, d, gen, order) for _ in range(2)]
+    cache = B.Cache(B.make_cache_desc(seqs * cols, page, kv, d, *pools[0].stride()[:1], *pools[0].stride()[1:3]), k=pools[0], v=pools[1])
+    table = torch.randperm(seqs * cols, generator=gen, device="cuda").int().view(seqs, cols)
+    seq = (torch.arange(m, device="cuda") // 7).int()
+    index = (torch.arange(m, device="cuda") % 7 + 3).int()
+    index[4], index[5], seq[9], seq[16] = -1, page * cols, -1, seqs                # tokens without a slot
+    table[1, 0] = 77                                                             # a page that does not exist
+    before = [p.clone() for p in pools]
+    q = B.qeft_cache_append_norm(cache, table, i["k"], v, index, seq=seq, q=i["q"], rot=i["rot"], pos=i["pos"], w_q=i["w_q"], w_k=i["w_k"], eps=EPS)
+    V.close("q", q, *V.heads_forward(i["q"], heads, i["w_q"], EPS, i["rot"], i["pos"], rot_dim), V.HALF)
+    want, bound = V.heads_forward(i["k"], kv, i["w_k"], EPS, i["rot"], i["pos"], rot_dim)
+    stored = torch.zeros(pools[0].shape[:3], dtype=torch.bool, device="cuda")
+    for t in range(m):
+        b, n = int(seq[t]), int(index[t])
+        if not (0 <= b < seqs and 0 <= n < page * cols) or int(table[b, n // page]) >= seqs * cols:
+            continue
+        at = (int(table[b, n // page]), slice(None), n % page)
+        V.close("k", pools[0][at].reshape(1, -1), want[t:t + 1], bound[t:t + 1], V.HALF)
+        assert torch.equal(pools[1][at].reshape(-1), v[t])
+        stored[at] = True
+    for a, b in zip(pools, before):
+        assert torch.equal(a[~stored], b[~stored])
+    if not norm:                                                                 # the same as without norms
+        p2 = [b.clone(memory_format=torch.preserve_format) for b in before]
+        c2 = B.Cache(B.make_cache_desc(seqs * cols, page, kv, d, *p2[0].stride()[:1], *p2[0].stride()[1:3]), k=p2[0], v=p2[1])
+        assert torch.equal(B.qeft_cache_append(c2, table, i["k"], v, index, seq=seq, q=i["q"], rot=i["rot"], pos=i["pos"]), q)
+        assert torch.equal(p2[0], pools[0]) and torch.equal(p2[1], pools[1])
+
+
+def test_append_without_queries_sequences_and_positions():
+    m, d, kv, page = 4, 64, 2, 8
+    i = inputs(m, d, d, 1, kv)
+    cache = B.Cache(B.make_cache_desc(8, page, kv, d))
+    table = torch.arange(8, device="cuda").int().view(4, 2)
+    index = torch.tensor([0, 5, 9, 15], device="cuda").int()
+    assert B.qeft_cache_append_norm(cache, table, i["k"], i["k"], index, rot=i["rot"], w_k=i["w_k"], eps=EPS) is None
+    want, bound = V.heads_forward(i["k"], kv, i["w_k"], EPS, i["rot"], index, d)
+    got = torch.stack([cache.k[2 * t + int(n) // page, :, int(n) % page].reshape(-1) for t, n in enumerate(index)])
+    V.close("k", got, want, bound, V.HALF)
+
+
+@pytest.mark.parametrize("m", [2, 700])
+def test_graphs_streams_and_calls_without_the_native_module(monkeypatch, m):
+    d, heads, kv, page = 128, 8, 2, 16
+    i = inputs(m, d, d, heads, kv)
+    desc = B.make_qk_desc(d, heads, kv, d, EPS)
+    kw = dict(w_q=i["w_q"], w_k=i["w_k"], rot=i["rot"], pos=i["pos"])
+    outs = [torch.empty((m, n * d), dtype=torch.float16, device="cuda") for n in (heads, kv, heads, kv, heads)]
+    sums = [torch.empty(d, device="cuda") for _ in range(2)]
+    ws = torch.empty(B.qeft_qk_norm_workspace(desc, m), dtype=torch.uint8, device="cuda")
+    cache = B.Cache(B.make_cache_desc(m, page, kv, d))
+    table, index = torch.arange(m, device="cuda").int().view(m, 1), torch.full((m,), 3, dtype=torch.int32, device="cuda")
+
+    def calls():
+        B.qeft_qk_norm_fwd(desc, i["q"], i["k"], q_out=outs[0], k_out=outs[1], **kw)
+        B.qeft_qk_norm_bwd(desc, i["gq"], i["gk"], q=i["q"], k=i["k"], dq=outs[2], dk=outs[3], dw_q=sums[0], dw_k=sums[1], ws=ws, **kw)
+        B.qeft_cache_append_norm(cache, table, i["k"], i["k"], index, q=i["q"], q_out=outs[4], rot=i["rot"], w_q=i["w_q"], w_k=i["w_k"], eps=EPS)
+
+    calls()
+    torch.cuda.synchronize()
+    everything = (*outs, *sums, cache.k, cache.v)
+    want = [t.clone() for t in everything]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        calls()
+    for _ in range(3):
+        for t in everything:
+            t.zero_()
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(everything, want):
+            assert torch.equal(a, b)
+    with monkeypatch.context() as mp:
+        mp.setattr(B, "_native", V.NONE)
+        calls()
+    for a, b in zip(everything, want):
+        assert torch.equal(a, b)

@@ -1,0 +1,234 @@
+"""qeft_logprob_fwd, _bwd and _fwd_bwd against the formulas in 64 bits, and against differences of the forward."""
+import math
+import zlib
+
+import pytest
+import torch
+
+import ends_util as V
+from paper_2410_08661_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+SIZES = [(1, 1), (3, 7), (2, 8), (5, 64), (70, 100), (9, 513), (300, 1000), (4, 4099), (1, 32000), (33, 32000), (600, 8200), (2, 65537), (3, 131072), (2, 131080), (1, 262147)]
+
+
+def gen_of(*key):
+    g = torch.Generator(device="cuda")
+    return g.manual_seed(zlib.crc32(repr(key).encode()))
+
+
+def some_tokens(m, n, gen, out=0.2):
+    t = torch.randint(0, n, (m,), generator=gen, device="cuda").int()
+    left = torch.rand(m, generator=gen, device="cuda") < out
+    t[left] = torch.where(torch.arange(m, device="cuda") % 2 == 0, -100, n)[left].int()
+    t[0] = n - 1
+    return t
+
+
+def check(m, n, f32, top, scale=1.0, banned=0.0, tokens=True):
+    gen = gen_of(m, n, f32, top)
+    z = V.logits(m, n, f32, gen, banned)
+    if banned and m > 2:
+        z[1] = -math.inf
+    token = some_tokens(m, n, gen) if tokens else None
+    desc = B.make_logprob_desc(n, z.dtype, scale)
+    got = dict(zip(("logp", "lse", "entropy", "top_logp", "top_index"), B.qeft_logprob_fwd(desc, z, token, top=top)))
+    want, r = V.log_probabilities(z, token, scale)
+    V.check_values(got, want)
+    assert (got["logp"] is None) == (token is None) and (got["top_index"] is None) == (top == 0)
+    if top:
+        index = V.alternatives(z, token, top)
+        assert torch.equal(got["top_index"], index)
+        at = index.long().clamp(min=0)
+        lp = torch.where(index >= 0, r["logs"].gather(1, at), -math.inf)
+        there = index >= 0
+        assert torch.equal(got["top_logp"][~there], torch.full_like(got["top_logp"][~there], -math.inf))
+        x = r["x"].gather(1, at)
+        bound = 5 * V.U * torch.where(there, (x - r["x"].amax(1, keepdim=True)).abs(), 0.0) + (r["E"] + 5 * V.U * 13)[:, None]
+        V.close("top_logp", got["top_logp"][there], lp[there], bound[there], V.U)
+    return z, token, desc, got
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("m,n", SIZES)
+def test_forward(m, n, f32):
+    check(m, n, f32, 0)
+    check(m, n, f32, min(n, 5), 1.3, 0.3)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("top", [1, 2, 20, 64])
+@pytest.mark.parametrize("m,n", [(1, 64), (5, 100), (3, 4099), (2, 32000), (130, 32000), (1, 140001), (20, 70003)])
+def test_alternatives(m, n, top, f32):
+    check(m, n, f32, top, tokens=m != 5)
+
+
+def test_alternatives_of_equal_logits_and_few():
+    for n in (64, 1000, 32000, 70003, 140001):
+        for f32 in (False, True):
+            z = torch.zeros((6, (n + 7) // 8 * 8), device="cuda").to(torch.float32 if f32 else torch.float16)[:, :n]
+            z[1] = -5.0
+            z[1, n // 2:] = 3.0                                      # many equal ones beside many smaller
+            z[2] = -math.inf
+            z[2, n - 3:] = torch.tensor([1.0, 2.0, 1.0], device="cuda").to(z.dtype)
+            z[3, ::2] = -0.0                                         # equals +0
+            z[4] = torch.arange(n, device="cuda").remainder(7).to(z.dtype)
+            z[5] = -math.inf
+            for top in (1, 33, 64):
+                got = B.qeft_logprob_fwd(B.make_logprob_desc(n, z.dtype), z, top=top)
+                assert torch.equal(got[4], V.alternatives(z, None, top)), (n, f32, top)
+                assert bool((got[3][got[4] < 0] == -math.inf).all()) and bool((got[4][2, 3:] == -1).all()) and bool((got[4][5] == -1).all())
+                assert got[1][5] == -math.inf and got[2][5] == 0
+
+
+@pytest.mark.parametrize("n", [40, 3000, 32000, 140001])
+def test_infinities_and_not_a_number(n):
+    """They make their own row not-a-number, and no other."""
+    z = V.logits(5, n, True, gen_of(n), 0.1)
+    clean = V.logits(5, n, True, gen_of(n), 0.1)
+    z[1, n // 3], z[2, n - 1], z[3, 0] = math.inf, math.nan, math.nan
+    z[3, 5] = math.inf
+    token = torch.tensor([3, n // 3, 4, 4, 4], device="cuda").int()
+    desc = B.make_logprob_desc(n, torch.float32)
+    dlogp = torch.ones(5, device="cuda")
+    for a, b in ((B.qeft_logprob_fwd(desc, z, token, top=3), B.qeft_logprob_fwd(desc, clean, token, top=3)),
+                 (B.qeft_logprob_fwd_bwd(desc, z, token, dlogp), B.qeft_logprob_fwd_bwd(desc, clean, token, dlogp))):
+        for x, y in zip(a, b):
+            assert torch.equal(x[[0, 4]], y[[0, 4]])
+            if x.is_floating_point():
+                assert bool(x[1:4].isnan().all())
+    index = B.qeft_logprob_fwd(desc, z, token, top=3)[4]
+    assert torch.equal(index, V.alternatives(z, token, 3)) and index[1, 0] == n // 3 and index[3].tolist()[:2] == [0, 5]
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("m,n", SIZES)
+def test_gradient(m, n, f32):
+    for scale, banned, kinds in ((1.0, 0.0, "l"), (0.8, 0.3, "lse"), (1.5, 0.0, "e"), (1.0, 0.2, "s")):
+        gen = gen_of(m, n, f32, kinds)
+        z = V.logits(m, n, f32, gen, banned, 0)
+        if banned and m > 2:
+            z[1] = -math.inf
+        token = some_tokens(m, n, gen) if "l" in kinds else None
+        g = [torch.randn(m, generator=gen, device="cuda") * 20 if k in kinds else None for k in "lse"]
+        desc = B.make_logprob_desc(n, z.dtype, scale)
+        logp, lse, entropy, _, _ = B.qeft_logprob_fwd(desc, z, token)
+        want, bound = V.logit_gradient(z, token, scale, *g)
+        apart = B.qeft_logprob_bwd(desc, z, lse, token=token, dlogp=g[0], dlse=g[1], entropy=entropy if g[2] is not None else None, dentropy=g[2])
+        V.close("dz", apart, want, bound, V.ROUNDING[z.dtype])
+        dz, logp2, lse2, entropy2 = B.qeft_logprob_fwd_bwd(desc, z, token, *g)
+        V.close("dz in one call", dz, want, bound, V.ROUNDING[z.dtype])
+        values, _ = V.log_probabilities(z, token, scale)
+        V.check_values(dict(logp=logp2, lse=lse2, entropy=entropy2), values)
+        # in place, and without the other outputs
+        same = z.clone(memory_format=torch.preserve_format) if n % 8 == 0 else V.logits(m, n, f32, gen).copy_(z)
+        assert B.qeft_logprob_bwd(desc, same, lse, token=token, dlogp=g[0], dlse=g[1], entropy=entropy, dentropy=g[2], dz=same) is same
+        assert torch.equal(same, apart)
+        same.copy_(z)
+        out = B.qeft_logprob_fwd_bwd(desc, same, token, *g, dz=same, logp=False, lse=False, entropy=False)
+        assert out[0] is same and out[1] is out[2] is out[3] is None and torch.equal(same, dz)
+
+
+def test_gradient_against_differences():
+    """Along a random direction of the logits, in 64 bits."""
+    m, n, scale = 5, 60, 0.9
+    gen = gen_of(1)
+    z = V.logits(m, n, True, gen, 0.2)
+    token = torch.randint(0, n, (m,), generator=gen, device="cuda").int()
+    z[torch.arange(m), token.long()] = 0.5
+    g = [torch.randn(m, generator=gen, device="cuda") for _ in range(3)]
+    dz = B.qeft_logprob_fwd_bwd(B.make_logprob_desc(n, torch.float32, scale), z, token, *g)[0]
+    way = torch.randn((m, n), generator=gen, device="cuda", dtype=torch.float64)
+
+    def value(x):
+        x = x * scale
+        lse = torch.logsumexp(x, 1)
+        lp = x - lse[:, None]
+        H = -(torch.where(lp > -math.inf, lp.exp() * lp, 0.0)).sum(1)
+        return (g[0].double() * lp.gather(1, token.long()[:, None])[:, 0] + g[1].double() * lse + g[2].double() * H).sum()
+
+    slope = (value(z.double() + 1e-5 * way) - value(z.double() - 1e-5 * way)) / 2e-5
+    along = (dz.double() * way).sum()
+    # fp32 gradients: 30 roundings' worth each, in quadrature with room; the difference's own error is of the order of the step's square
+    assert abs(float(slope - along)) <= 64 * V.U * float((dz.double() * way).norm()) + 1e-8
+
+
+def test_no_rows_and_one_entry():
+    desc = B.make_logprob_desc(64, torch.float16)
+    e, t = torch.empty((0, 64), dtype=torch.float16, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    out = B.qeft_logprob_fwd(desc, e, t, top=3)
+    assert [x.shape[0] for x in out] == [0] * 5
+    assert B.qeft_logprob_fwd_bwd(desc, e, t, torch.empty(0, device="cuda"))[0].shape == (0, 64)
+    assert B.qeft_logprob_bwd(desc, e, torch.empty(0, device="cuda")).shape == (0, 64)
+
+
+def test_pitches_of_alternatives_and_what_lies_behind():
+    z = V.logits(7, 500, False, gen_of(3))
+    desc = B.make_logprob_desc(500)
+    want = B.qeft_logprob_fwd(desc, z, top=5)
+    lp, ix = torch.full((7, 9), 3.0, device="cuda"), torch.full((7, 9), 3, dtype=torch.int32, device="cuda")
+    B.qeft_logprob_fwd(desc, z, top=5, top_logp=lp[:, 2:7], top_index=ix[:, 2:7])
+    assert torch.equal(lp[:, 2:7], want[3]) and torch.equal(ix[:, 2:7], want[4])
+    for t in (lp, ix):
+        assert bool((t[:, :2] == 3).all()) and bool((t[:, 7:] == 3).all())
+    dz = torch.full((7, 520), 9.0, dtype=torch.float16, device="cuda")
+    B.qeft_logprob_bwd(desc, z, want[1], dlse=torch.ones(7, device="cuda"), dz=dz[:, :500])
+    assert bool((dz[:, 500:] == 9).all())
+
+
+@pytest.mark.parametrize("m,n", [(3, 1000), (2, 140001), (200, 32000)])
+def test_graphs_streams_and_calls_without_the_native_module(monkeypatch, m, n):
+    gen = gen_of(m, n)
+    z, token, g = V.logits(m, n, False, gen), some_tokens(m, n, gen), torch.randn(m, generator=gen, device="cuda")
+    desc = B.make_logprob_desc(n)
+    outs = [torch.empty(m, device="cuda") for _ in range(3)]
+    tops = [torch.empty((m, 7), device="cuda"), torch.empty((m, 7), dtype=torch.int32, device="cuda")]
+    dz, dz2 = (V.logits(m, n, False, gen) for _ in range(2))
+    ws = torch.empty(max(16, B.qeft_logprob_workspace(desc, m, 7)), dtype=torch.uint8, device="cuda")
+
+    def calls():
+        B.qeft_logprob_fwd(desc, z, token, 7, *outs, *tops, ws=ws)
+        B.qeft_logprob_bwd(desc, z, outs[1], token=token, dlogp=g, dz=dz)
+        B.qeft_logprob_fwd_bwd(desc, z, token, g, dz=dz2, logp=False, lse=False, entropy=False, ws=ws)
+
+    calls()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (*outs, *tops, dz, dz2)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        calls()
+    for _ in range(3):
+        for t in (*outs, *tops, dz, dz2):
+            t.fill_(9)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((*outs, *tops, dz, dz2), want):
+            assert torch.equal(a, b)
+    with monkeypatch.context() as mp:
+        mp.setattr(B, "_native", V.NONE)
+        calls()
+    for a, b in zip((*outs, *tops, dz, dz2), want):
+        assert torch.equal(a, b)
+
+
+def test_rows_beyond_32_bit_offsets():
+    m, n = 70001, 32000                       # 2.24e9 logits
+    z = torch.empty((m, n), dtype=torch.float16, device="cuda")
+    z[: m - 5].zero_()
+    last = z[m - 5:]
+    last.copy_(V.logits(5, n, False, gen_of(5)))
+    token = torch.full((m,), -1, dtype=torch.int32, device="cuda")
+    token[m - 5:] = 17
+    g = torch.ones(m, device="cuda")
+    desc = B.make_logprob_desc(n)
+    logp, lse, entropy, lp, ix = B.qeft_logprob_fwd(desc, z, token, top=3)
+    want, _ = V.log_probabilities(last, token[m - 5:], 1.0)
+    V.check_values(dict(logp=logp[m - 5:], lse=lse[m - 5:], entropy=entropy[m - 5:]), want)
+    assert torch.equal(ix[m - 5:], V.alternatives(last, None, 3)) and bool((ix[: m - 5] == -1).all())
+    dwant, bound = V.logit_gradient(last, token[m - 5:], 1.0, g[m - 5:], None, None)
+    dz = B.qeft_logprob_bwd(desc, z, lse, token=token, dlogp=g)
+    V.close("dz", dz[m - 5:], dwant, bound, V.HALF)
+    assert not bool(dz[m - 6].any())
+    B.qeft_logprob_fwd_bwd(desc, z, token, g, dz=dz)
+    V.close("dz", dz[m - 5:], dwant, bound, V.HALF)
