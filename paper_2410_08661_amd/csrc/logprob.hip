@@ -3,6 +3,7 @@
 //   c = scale log2(e)    K = max z c    s = sum 2^(z c - K)    lse = K ln 2 + ln s    logp = (z_t c - K) ln 2 - ln s    entropy = ln s - ln 2 sum 2^u u / s, u = z c - K
 //   dz_j = scale (p_j (dlse - dlogp - dentropy (log p_j + entropy)) + [j = t] dlogp),   p_j = 2^u / s
 //
+// Bytes bound it: a row is read once into registers, by a workgroup or, the longest, by several whose statistics a second launch joins.
 // z c - K is one multiply-add, K as it was rounded: what rounding K costs is in lse alone.  K is finite where the row is empty, so that -infinity minus it stays what it is.
 #include <math.h>
 #include "octets.h"
@@ -43,24 +44,36 @@ struct MostFloat {
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }   // (passes over not-a-number)
 };
 
-// What a row's gradient needs
+// What a row's gradient needs: u = z c - k2, p = 2^u, log p = u ln 2, dz = p (a - dh u), and at_token more at the token
 struct Slope {
-    float c, k2, scale, a, dh, at_token;      // u = z c - k2, p = 2^u, log p = u ln 2
+    float c, k2, a, dh, at_token;
     int token;
-    bool empty;
 };
-__device__ __forceinline__ float slope_of(const Slope& g, float z, int j) {
-    if (g.empty) return 0.f;
-    const float u = fmaf(z, g.c, -g.k2), p = __builtin_amdgcn_exp2f(u);
-    float d = g.a;
-    if (g.dh != 0.f) d = fmaf(-g.dh * LN2, fmaxf(u, FAR), d);      // (p is not-a-number where u is)
-    d *= p;
-    if (j == g.token) d += g.at_token;
-    return g.scale * d;
-}
-__device__ __forceinline__ Slope make_slope(const Logprob& a, int64_t row, int token, float k2, float entropy, bool empty) {
+__device__ __forceinline__ Slope make_slope(const Logprob& a, int64_t row, int token, float k2, float entropy) {
     const float dl = a.dlogp ? a.dlogp[row] : 0.f, ds = a.dlse ? a.dlse[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
-    return Slope{a.scale * LOG2E, k2, a.scale, ds - dl - (dh != 0.f ? dh * entropy : 0.f), dh, dl, token, empty};
+    return Slope{a.scale * LOG2E, k2, a.scale * (ds - dl - (dh != 0.f ? dh * entropy : 0.f)), a.scale * dh * LN2, a.scale * dl, a.token ? token : -1};
+}
+__device__ __forceinline__ float slope_of(const Slope& g, float z) {
+    const float u = fmaf(z, g.c, -g.k2);
+    return __builtin_amdgcn_exp2f(u) * fmaf(-g.dh, fmaxf(u, FAR), g.a);      // (p is 0 where u is far, not-a-number where u is)
+}
+template <bool F32>
+__device__ __forceinline__ void put_slopes(const Slope& g, const Raw<F32>& v, char* dz, int at, int left) {
+    if (left <= 0) return;
+    float x[8];
+    if (g.dh != 0.f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = slope_of(g, v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(v[e], g.c, -g.k2)) * g.a;
+    }
+    if ((uint32_t)(g.token - at) < 8u) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (at + e == g.token) x[e] += g.at_token;
+    }
+    store<F32>(dz, at, left, x);
 }
 template <bool F32>
 __device__ __forceinline__ void zero_row(void* row, int n) {
@@ -82,132 +95,417 @@ __device__ __forceinline__ void left_out(const Logprob& a, int64_t row) {
     }
 }
 
-// Rows of any length, read again for each step: the maximum, the sums, each alternative, the gradient.
-template <bool F32, bool GRAD>
-__global__ __launch_bounds__(1024) void logprob_long_kernel(Logprob a) {
+// ---- rows in registers ------------------------------------------------------------------------------------------------
+struct Stats {       // of a part of a row, relative to its own k
+    float k, s, t;
+};
+__device__ __forceinline__ float shrink(float from, float to) { return fmaxf(from - to, FAR); }      // (2^FAR is 0: what is further away adds nothing)
+
+// A term of a sum over lanes: rounded for itself.  Joined with the sum's first addition it would be rounded otherwise in the lane that adds it than in the lane it is added
+// to, and the lanes' sums would differ.
+__device__ __forceinline__ float term(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+
+// Where a workgroup's part of a row goes: to the call's outputs, or, one of several parts, to the workspace
+struct Part {
+    int parts, len;        // parts of a row, values of one
+    Stats* stats;          // [m][parts]
+    uint64_t* keys;        // [m][parts][top], largest first
+    float *lse, *entropy;  // [m], for a gradient that follows
+};
+constexpr int CANDIDATES = 1024;
+
+// A row's numbers from its joined statistics, by one thread
+__device__ __forceinline__ void put_row(const Logprob& a, const Part& p, int64_t row, const void* z, int token, const Stats& x, float ln_s, float entropy) {
+    const bool empty = x.s == 0.f;
+    const float lse = empty ? -INFINITY : fmaf(x.k, LN2, ln_s);
+    if (a.lse) a.lse[row] = lse;
+    if (a.entropy) a.entropy[row] = entropy;
+    if (p.lse) {
+        p.lse[row] = lse;
+        p.entropy[row] = entropy;
+    }
+    if (a.logp) {
+        const float zt = a.f32 ? ((const float*)z)[token] : (float)((const _Float16*)z)[token];
+        a.logp[row] = empty ? -INFINITY : fmaf(fmaf(zt, a.scale * LOG2E, -x.k), LN2, -ln_s);
+    }
+}
+__device__ __forceinline__ void put_top(const Logprob& a, int64_t row, int i, uint64_t key, float k, float ln_s) {
+    const bool there = (uint32_t)(key >> 32) > RANK_NEG_INF;
+    a.top_index[row * a.ld_top + i] = there ? (int)~(uint32_t)key : -1;
+    a.top_logp[row * a.ld_top + i] = there ? fmaf(fmaf(value_of(key >> 32), a.scale * LOG2E, -k), LN2, -ln_s) : -INFINITY;
+}
+
+// The largest `top` keys of a workgroup, by rounds: each() calls its argument with every key of the thread.  For what the list of candidates does not hold.
+template <class Each, class Put>
+__device__ __forceinline__ void top_by_rounds(int top, uint64_t* slots, const Each& each, const Put& put) {
+    uint64_t last = ~0ull;
+    for (int i = 0; i < top; ++i) {
+        uint64_t best = 0;
+        each([&](uint64_t x) {
+            if (x < last && x > best) best = x;
+        });
+        best = group_reduce(best, slots, (uint64_t)0, Most());
+        if ((uint32_t)(best >> 32) <= RANK_NEG_INF) best = 0;
+        last = best;
+        if (threadIdx.x == 0) put(i, best);
+    }
+}
+// The largest `top` of the `count` keys in a list: each key's place is the number of larger ones.
+template <class Put>
+__device__ __forceinline__ void top_of_list(int top, const uint64_t* list, int count, const Put& put) {
+    for (int i = threadIdx.x; i < count; i += blockDim.x) {
+        const uint64_t mine = list[i];
+        int place = 0;
+        for (int j = 0; j < count; ++j) place += list[j] > mine;
+        if (place < top) put(place, mine);
+    }
+    for (int i = count + threadIdx.x; i < top; i += blockDim.x) put(i, 0);
+}
+
+// Workgroup = a row, or a part of one: V octets a thread.
+template <int V, bool F32, bool GRAD>
+__global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     __shared__ float buf[3][16];
-    __shared__ uint64_t best_buf[16];
-    const int64_t row = blockIdx.x;
-    const char* z = row_of(a.z, row, a.ldz, F32);
-    void* dz = GRAD ? row_of(a.dz, row, a.lddz, F32) : nullptr;
+    const int64_t row = p.parts == 1 ? blockIdx.x : blockIdx.x / p.parts;
+    const int part = p.parts == 1 ? 0 : (int)(blockIdx.x - row * p.parts), from = part * p.len, n = min(p.len, a.n - from), T = blockDim.x;
+    const char* row_at = row_of(a.z, row, a.ldz, F32);
+    const char* z = row_at + (size_t)from * (F32 ? 4 : 2);
     const int token = a.token ? a.token[row] : -1;
     if (a.token && (token < 0 || token >= a.n)) {
+        if (p.parts > 1) return;      // (the join leaves it out)
         left_out(a, row);
-        if (GRAD) zero_row<F32>(dz, a.n);
+        if (GRAD) zero_row<F32>(row_of(a.dz, row, a.lddz, F32), a.n);
         return;
     }
+    // Whole octets by one load each; a partial one is some thread's v[i] (the code for it once, not V times).
+    const int whole = n / 8, last = threadIdx.x == (whole & (T - 1)) && (n & 7) ? whole / T : -1;
+    Raw<F32> v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        v[i].fill(Raw<F32>::NEG_INF);
+        if ((int)threadIdx.x + T * i < whole) v[i].load(z, 8 * (threadIdx.x + T * i), 8);
+    }
+    if (last >= 0) {
+        Raw<F32> x;
+        x.load(z, 8 * whole, n & 7, Raw<F32>::NEG_INF);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i == last) v[i] = x;
+    }
     const float c = a.scale * LOG2E;
-    float most = -INFINITY;
-    for (int at = 8 * threadIdx.x; at < a.n; at += 8 * blockDim.x) {
-        const int left = a.n - at;
-        Raw<F32> v;
-        v.load(z, at, left);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = T >> 6;
+    float mine = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) most = e < left ? fmaxf(most, v[e]) : most;
-    }
-    most = group_reduce(most, buf[0], -INFINITY, MostFloat());
-    const float k = fmaxf(most * c, LEAST);
-    float s = 0.f, t = 0.f;
-    for (int at = 8 * threadIdx.x; at < a.n; at += 8 * blockDim.x) {
-        const int left = a.n - at;
-        Raw<F32> v;
-        v.load(z, at, left);
+    for (int i = 0; i < V; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (e >= left) continue;
-            const float u = fmaf(v[e], c, -k), x = __builtin_amdgcn_exp2f(u);
-            s += x;
-            t = fmaf(x, fmaxf(u, FAR), t);
-        }
-    }
-    s = group_reduce(s, buf[1], 0.f, Sum());
-    t = group_reduce(t, buf[2], 0.f, Sum());
-    const bool empty = s == 0.f;
-    const float ln_s = logf(s), entropy = empty ? 0.f : ln_s - LN2 * (t / s);
-    if (threadIdx.x == 0) {
-        if (a.lse) a.lse[row] = empty ? -INFINITY : fmaf(k, LN2, ln_s);
-        if (a.entropy) a.entropy[row] = entropy;
-        if (a.logp) {
-            const float zt = F32 ? ((const float*)z)[token] : (float)((const _Float16*)z)[token];
-            a.logp[row] = empty ? -INFINITY : fmaf(fmaf(zt, c, -k), LN2, -ln_s);
-        }
-    }
-    uint64_t last = ~0ull;
-    for (int i = 0; i < a.top; ++i) {
-        uint64_t best = 0;
-        for (int at = 8 * threadIdx.x; at < a.n; at += 8 * blockDim.x) {
-            const int left = a.n - at;
-            Raw<F32> v;
-            v.load(z, at, left);
+        for (int e = 0; e < 8; ++e) mine = fmaxf(mine, v[i][e]);
+    Stats x{fmaxf(wave_reduce(mine, MostFloat()) * c, LEAST), 0.f, 0.f};
+    // (kept as loaded between the steps, not as twice the registers of converted values)
+    auto pin = [&] {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (e >= left) continue;
-                const uint64_t x = (uint64_t)rank_of(v[e]) << 32 | (uint32_t)~(at + e);
-                if (x < last && x > best) best = x;
+        for (int i = 0; i < V; ++i) v[i].hold();
+    };
+    pin();
+    const bool wants_t = a.entropy || p.lse || (GRAD && a.dentropy);
+    {
+        float s[4] = {}, t[4] = {};
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if (wants_t) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float u = fmaf(v[i][e], c, -x.k), y = __builtin_amdgcn_exp2f(u);
+                    s[e & 3] += y;
+                    t[e & 3] = fmaf(y, fmaxf(u, FAR), t[e & 3]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[e & 3] += __builtin_amdgcn_exp2f(fmaf(v[i][e], c, -x.k));
             }
         }
-        best = group_reduce(best, best_buf, (uint64_t)0, Most());
-        const bool there = (uint32_t)(best >> 32) > RANK_NEG_INF;
-        last = there ? best : 0;
-        if (threadIdx.x == 0) {
-            a.top_index[row * a.ld_top + i] = there ? (int)~(uint32_t)best : -1;
-            a.top_logp[row * a.ld_top + i] = there ? fmaf(fmaf(value_of(best >> 32), c, -k), LN2, -ln_s) : -INFINITY;
-        }
+        x.s = wave_reduce((s[0] + s[1]) + (s[2] + s[3]), Sum());
+        if (wants_t) x.t = wave_reduce((t[0] + t[1]) + (t[2] + t[3]), Sum());
     }
-    if (GRAD) {
-        const Slope g = make_slope(a, row, token, k + log2f(s), entropy, empty);
-        for (int at = 8 * threadIdx.x; at < a.n; at += 8 * blockDim.x) {
-            const int left = a.n - at;
-            Raw<F32> v;
-            v.load(z, at, left);
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = slope_of(g, v[e], at + e);
-            store<F32>(dz, at, left, x);
+    if (waves > 1) {      // the waves' statistics joined, a lane per wave
+        if (lane == 0) {
+            buf[0][wave] = x.k;
+            buf[1][wave] = x.s;
+            buf[2][wave] = x.t;
         }
+        __syncthreads();
+        const int w = lane & 15;
+        const bool there = w < waves;
+        const Stats y{there ? buf[0][w] : LEAST, there ? buf[1][w] : 0.f, there ? buf[2][w] : 0.f};
+        x.k = row_reduce(y.k, MostFloat());
+        const float d = shrink(y.k, x.k), f = __builtin_amdgcn_exp2f(d);
+        x.s = row_reduce(term(y.s, f), Sum());
+        x.t = row_reduce(term(f, fmaf(d, y.s, y.t)), Sum());
+    }
+    pin();
+    const bool empty = x.s == 0.f;
+    const float ln_s = logf(x.s), entropy = empty ? 0.f : ln_s - LN2 * (x.t / x.s);
+    if (p.parts == 1) {
+        if (threadIdx.x == 0) put_row(a, p, row, row_at, token, x, ln_s, entropy);
+    } else if (threadIdx.x == 0) p.stats[blockIdx.x] = x;
+    if constexpr (!GRAD) {
+        if (a.top == 0) return;
+        // Candidates: whatever reaches the top-th largest of the maxima of groups of threads, 256 groups at most, cut to 16 bits.  Few do, so they are ordered by
+        // comparing each with each.  Rows where many do (equal logits) or with not-a-number, which no maximum shows, go by rounds.
+        __shared__ uint32_t maxima[256];
+        __shared__ uint64_t list[CANDIDATES], slots[16];
+        __shared__ int used;
+        auto put = [&](int i, uint64_t key) {
+            if (p.parts == 1) put_top(a, row, i, key, x.k, ln_s);
+            else p.keys[(size_t)blockIdx.x * a.top + i] = key;
+        };
+        const uint32_t rank = rank_of(mine);
+        uint32_t group = rank;
+        const int side = T > 256 ? 4 : 1;      // threads of a group: neighbours
+        if (side == 4) {
+            group = max(group, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)group, 0xb1, 0xf, 0xf, false));      // quad_perm 1 0 3 2
+            group = max(group, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)group, 0x4e, 0xf, 0xf, false));      // quad_perm 2 3 0 1
+        }
+        if (threadIdx.x % side == 0) maxima[threadIdx.x / side] = group;
+        if (threadIdx.x == 0) used = 0;
+        for (int i = T / side + threadIdx.x; i < 256; i += T) maxima[i] = 0;
+        __syncthreads();
+        uint32_t bound = 0;
+        {
+            uint32_t g[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) g[i] = maxima[lane + 64 * i];
+#pragma unroll 1
+            for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+                int count = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) count += __popcll(__ballot(g[i] >= (bound | bit)));
+                if (count >= a.top) bound |= bit;
+            }
+        }
+        bound = max(bound, RANK_NEG_INF + 1);
+        const float least = value_of(bound);
+        if (rank >= bound) {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (v[i][e] >= least) {
+                        const int j = atomicAdd(&used, 1);
+                        if (j < CANDIDATES) list[j] = (uint64_t)rank_of(v[i][e]) << 32 | (uint32_t)~(from + 8 * (int)(threadIdx.x + T * i) + e);
+                    }
+        }
+        __syncthreads();
+        const int count = used;
+        if (count <= CANDIDATES && x.s == x.s) top_of_list(a.top, list, count, put);
+        else {
+            auto each = [&](auto&& f) {      // (from memory: every value's key would stay in registers through the rounds)
+                for (int at = 8 * threadIdx.x; at < n; at += 8 * T) {
+                    Raw<F32> x;
+                    x.load(z, at, n - at, Raw<F32>::NEG_INF);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f((uint64_t)rank_of(x[e]) << 32 | (uint32_t)~(from + at + e));
+                }
+            };
+            top_by_rounds(a.top, slots, each, put);
+        }
+    } else {
+        char* dz = row_of(a.dz, row, a.lddz, F32);
+        if (empty) return zero_row<F32>(dz, a.n);
+        const Slope g = make_slope(a, row, token, x.k + log2f(x.s), entropy);
+        Raw<F32> x = v[0];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int o = threadIdx.x + T * i;
+            if (o < whole) put_slopes(g, v[i], dz, 8 * o, 8);
+            if (i == last) x = v[i];
+        }
+        if (last >= 0) put_slopes(g, x, dz, 8 * whole, n & 7);
     }
 }
 
+// The parts of a row joined: a thread a part (256 at most).
+__global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
+    __shared__ float buf[3][16];
+    __shared__ uint64_t list[CANDIDATES], slots[16];
+    __shared__ int used;
+    const int64_t row = blockIdx.x;
+    const int token = a.token ? a.token[row] : -1, i = threadIdx.x;
+    if (a.token && (token < 0 || token >= a.n)) {
+        left_out(a, row);
+        return;
+    }
+    const Stats y = i < p.parts ? p.stats[row * p.parts + i] : Stats{LEAST, 0.f, 0.f};
+    Stats x;
+    x.k = group_reduce(y.k, buf[0], LEAST, MostFloat());
+    const float d = shrink(y.k, x.k), f = __builtin_amdgcn_exp2f(d);
+    x.s = group_reduce(term(y.s, f), buf[1], 0.f, Sum());
+    x.t = group_reduce(term(f, fmaf(d, y.s, y.t)), buf[2], 0.f, Sum());
+    const float ln_s = logf(x.s), entropy = x.s == 0.f ? 0.f : ln_s - LN2 * (x.t / x.s);
+    if (i == 0) put_row(a, p, row, row_of(a.z, row, a.ldz, a.f32), token, x, ln_s, entropy);
+    if (a.top == 0) return;
+    const uint64_t* keys = p.keys + (size_t)row * p.parts * a.top;
+    const int total = p.parts * a.top;
+    // a part whose last key is this large has enough of them
+    const uint64_t bound = max(group_reduce(i < p.parts ? keys[(size_t)i * a.top + a.top - 1] : 0, slots, (uint64_t)0, Most()), (uint64_t)(RANK_NEG_INF + 1) << 32);
+    if (i == 0) used = 0;
+    __syncthreads();
+    auto each = [&](auto&& f) {
+        for (int j = i; j < total; j += 256) f(keys[j]);
+    };
+    each([&](uint64_t key) {
+        if (key >= bound) {
+            const int at = atomicAdd(&used, 1);
+            if (at < CANDIDATES) list[at] = key;
+        }
+    });
+    __syncthreads();
+    auto put = [&](int at, uint64_t key) { put_top(a, row, at, key, x.k, ln_s); };
+    if (used <= CANDIDATES) top_of_list(a.top, list, used, put);
+    else top_by_rounds(a.top, slots, each, put);
+}
+
+// ---- the gradient alone -------------------------------------------------------------------------------------------------
+constexpr int CHUNK = 8192;      // values of a workgroup
 template <bool F32>
-__global__ __launch_bounds__(1024) void logprob_bwd_kernel(Logprob a) {
+__global__ __launch_bounds__(256) void logprob_bwd_kernel(Logprob a, int chunks) {
+    const int64_t row = blockIdx.x / chunks;
+    const int from = (int)(blockIdx.x - row * chunks) * CHUNK, n = min(CHUNK, a.n - from);
+    const char* z = row_of(a.z, row, a.ldz, F32) + (size_t)from * (F32 ? 4 : 2);
+    char* dz = row_of(a.dz, row, a.lddz, F32) + (size_t)from * (F32 ? 4 : 2);
+    const int token = a.token ? a.token[row] : -1;
+    if (a.token && (token < 0 || token >= a.n)) return zero_row<F32>(dz, n);
+    const float lse = a.lse_in[row];
+    if (lse == -INFINITY) return zero_row<F32>(dz, n);
+    const Slope g = make_slope(a, row, token - from, lse * LOG2E, a.entropy_in ? a.entropy_in[row] : 0.f);
+    Raw<F32> v[CHUNK / 2048];
+#pragma unroll
+    for (int i = 0; i < CHUNK / 2048; ++i) v[i].load(z, 8 * threadIdx.x + 2048 * i, n - (int)(8 * threadIdx.x + 2048 * i));
+#pragma unroll
+    for (int i = 0; i < CHUNK / 2048; ++i) put_slopes(g, v[i], dz, 8 * threadIdx.x + 2048 * i, n - (int)(8 * threadIdx.x + 2048 * i));
+}
+
+// ---- rows longer than registers, too many for parts: read again for the maximum, the sums and each alternative ------------
+template <bool F32>
+__global__ __launch_bounds__(1024) void logprob_long_kernel(Logprob a, Part p) {
+    __shared__ float buf[3][16];
+    __shared__ uint64_t slots[16];
     const int64_t row = blockIdx.x;
     const char* z = row_of(a.z, row, a.ldz, F32);
-    char* dz = row_of(a.dz, row, a.lddz, F32);
     const int token = a.token ? a.token[row] : -1;
-    if (a.token && (token < 0 || token >= a.n)) return zero_row<F32>(dz, a.n);
-    const float lse = a.lse_in[row];
-    const Slope g = make_slope(a, row, token, lse * LOG2E, a.entropy_in ? a.entropy_in[row] : 0.f, lse == -INFINITY);
-    for (int at = 8 * threadIdx.x; at < a.n; at += 8 * blockDim.x) {
-        const int left = a.n - at;
-        Raw<F32> v;
-        v.load(z, at, left);
-        float x[8];
+    if (a.token && (token < 0 || token >= a.n)) return left_out(a, row);
+    auto each = [&](auto&& f) {
+        for (int at = 8 * threadIdx.x; at < a.n; at += 8192) {
+            Raw<F32> v;
+            v.load(z, at, a.n - at, Raw<F32>::NEG_INF);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = slope_of(g, v[e], at + e);
-        store<F32>(dz, at, left, x);
+            for (int e = 0; e < 8; ++e) f(v[e], at + e);
+        }
+    };
+    const float c = a.scale * LOG2E;
+    float most = -INFINITY;
+    each([&](float x, int) { most = fmaxf(most, x); });
+    Stats x{fmaxf(group_reduce(most, buf[0], -INFINITY, MostFloat()) * c, LEAST), 0.f, 0.f};
+    each([&](float y, int) {
+        const float u = fmaf(y, c, -x.k), w = __builtin_amdgcn_exp2f(u);
+        x.s += w;
+        x.t = fmaf(w, fmaxf(u, FAR), x.t);
+    });
+    x.s = group_reduce(x.s, buf[1], 0.f, Sum());
+    x.t = group_reduce(x.t, buf[2], 0.f, Sum());
+    const float ln_s = logf(x.s);
+    if (threadIdx.x == 0) put_row(a, p, row, z, token, x, ln_s, x.s == 0.f ? 0.f : ln_s - LN2 * (x.t / x.s));
+    top_by_rounds(a.top, slots, [&](auto&& f) { each([&](float y, int j) { f((uint64_t)rank_of(y) << 32 | (uint32_t)~j); }); },
+                  [&](int i, uint64_t key) { put_top(a, row, i, key, x.k, ln_s); });
+}
+
+// ---- what goes where ----------------------------------------------------------------------------------------------------
+struct Plan {
+    int threads, octets;     // of a workgroup, a thread
+    int parts, len;          // parts of a row (0: the kernel for long rows)
+    size_t stats_at, keys_at, lse_at, bytes;
+};
+Plan plan_of(int n, bool f32, int64_t m, int top) {
+    const int most = f32 ? 8 : 16;      // octets that a thread of 1024 holds beside its work: 64 registers
+    Plan p{};
+    const int octets = ceil_div(n, 8), fit = 1024 * most;
+    int parts = ceil_div(octets, fit);
+    p.parts = parts;
+    int per = ceil_div(octets, parts);
+    const int threads = per <= 256 ? 64 : per <= 2048 ? 256 : 1024;
+    int v = 1;
+    while (v * threads < per) v *= 2;
+    p.threads = threads;
+    p.octets = v;
+    p.len = parts > 1 ? 8 * threads * v : n;
+    if (parts == 1) return p;
+    p.parts = parts = ceil_div(n, p.len);
+    p.stats_at = 0;
+    p.keys_at = (size_t)m * parts * sizeof(Stats) + 15 & ~(size_t)15;
+    p.lse_at = p.keys_at + (size_t)m * parts * top * sizeof(uint64_t);
+    if (p.lse_at > (size_t)64 << 20) p.parts = 0, p.lse_at = 0;
+    p.bytes = p.lse_at + (size_t)m * 2 * sizeof(float);
+    return p;
+}
+
+template <bool F32, bool GRAD>
+void launch_rows(const Plan& q, const Logprob& a, const Part& p, hipStream_t s) {
+    const unsigned grid = (unsigned)(a.m * p.parts);
+    switch (q.octets) {
+        case 1: logprob_row_kernel<1, F32, GRAD><<<grid, q.threads, 0, s>>>(a, p); break;
+        case 2: logprob_row_kernel<2, F32, GRAD><<<grid, q.threads, 0, s>>>(a, p); break;
+        case 4: logprob_row_kernel<4, F32, GRAD><<<grid, q.threads, 0, s>>>(a, p); break;
+        case 8: logprob_row_kernel<8, F32, GRAD><<<grid, q.threads, 0, s>>>(a, p); break;
+        default:
+            if constexpr (!F32) logprob_row_kernel<16, F32, GRAD><<<grid, q.threads, 0, s>>>(a, p);
     }
+}
+template <bool F32>
+void launch_bwd(const Logprob& a, hipStream_t s) {
+    const int chunks = ceil_div(a.n, CHUNK);
+    logprob_bwd_kernel<F32><<<(unsigned)(a.m * chunks), 256, 0, s>>>(a, chunks);
+}
+template <bool F32>
+void launch_fwd(const Logprob& a, hipStream_t s) {
+    const Plan q = plan_of(a.n, F32, a.m, a.top);
+    Part p{q.parts, q.len, nullptr, nullptr, nullptr, nullptr};
+    if (q.parts == 1) {
+        if (a.dz) launch_rows<F32, true>(q, a, p, s);
+        else launch_rows<F32, false>(q, a, p, s);
+        return;
+    }
+    p.stats = (Stats*)(a.ws + q.stats_at);
+    p.keys = (uint64_t*)(a.ws + q.keys_at);
+    if (a.dz) {
+        p.lse = (float*)(a.ws + q.lse_at);
+        p.entropy = p.lse + a.m;
+    }
+    if (q.parts > 1) {
+        launch_rows<F32, false>(q, a, p, s);
+        logprob_join_kernel<<<(unsigned)a.m, 256, 0, s>>>(a, p);
+    } else logprob_long_kernel<F32><<<(unsigned)a.m, 1024, 0, s>>>(a, p);
+    if (!a.dz) return;
+    Logprob b = a;
+    b.lse_in = p.lse;
+    b.entropy_in = p.entropy;
+    launch_bwd<F32>(b, s);
 }
 
 }  // namespace
 
-size_t logprob_workspace(int n, bool f32, int64_t m, int top) { return 0; }
+size_t logprob_workspace(int n, bool f32, int64_t m, int top) { return plan_of(n, f32, m, top).bytes; }
 
 hipError_t logprob_fwd(const Logprob& a, hipStream_t s) {
-    const dim3 grid((unsigned)a.m), threads(1024);
-    if (a.f32) {
-        if (a.dz) logprob_long_kernel<true, true><<<grid, threads, 0, s>>>(a);
-        else logprob_long_kernel<true, false><<<grid, threads, 0, s>>>(a);
-    } else {
-        if (a.dz) logprob_long_kernel<false, true><<<grid, threads, 0, s>>>(a);
-        else logprob_long_kernel<false, false><<<grid, threads, 0, s>>>(a);
-    }
+    if (a.f32) launch_fwd<true>(a, s);
+    else launch_fwd<false>(a, s);
     return hipGetLastError();
 }
 
 hipError_t logprob_bwd(const Logprob& a, hipStream_t s) {
-    const dim3 grid((unsigned)a.m), threads(1024);
-    if (a.f32) logprob_bwd_kernel<true><<<grid, threads, 0, s>>>(a);
-    else logprob_bwd_kernel<false><<<grid, threads, 0, s>>>(a);
+    if (a.f32) launch_bwd<true>(a, s);
+    else launch_bwd<false>(a, s);
     return hipGetLastError();
 }
 

@@ -19,17 +19,19 @@ __device__ __forceinline__ const char* row_of(const void* p, int64_t row, int64_
 }
 __device__ __forceinline__ char* row_of(void* p, int64_t row, int64_t ld, bool f32) { return const_cast<char*>(row_of((const void*)p, row, ld, f32)); }
 
-// Eight values of a row as loaded.  left: how many of them exist; a row's last octet may be partial, and is read value by value, the last one first.
+// Eight values of a row as loaded.  left: how many of them exist (none from 0 down); a row's last octet may be partial, and is read value by value, the last one
+// first.  What does not exist is 0, or the word `none`.
 template <bool F32> struct Raw;
 template <> struct Raw<false> {
+    static constexpr uint32_t NEG_INF = 0xfc00fc00u;   // (a word of values)
     u4 v;
-    __device__ __forceinline__ void load(const void* row, uint32_t at, int left) {
+    __device__ __forceinline__ void load(const void* row, uint32_t at, int left, uint32_t none = 0) {
         const char* p = (const char*)row + 2 * at;
         if (left >= 8) {
             v = *reinterpret_cast<const u4*>(p);
             return;
         }
-        v = u4{0, 0, 0, 0};
+        fill(none);
 #pragma unroll 1
         for (int e = left - 1; e >= 0; --e) {
             const uint32_t x = *reinterpret_cast<const uint16_t*>(p + 2 * e);
@@ -37,20 +39,23 @@ template <> struct Raw<false> {
         }
     }
     __device__ __forceinline__ float operator[](int e) const { return (float)__builtin_bit_cast(h8, v)[e]; }
-    __device__ __forceinline__ void clear() { v = u4{0, 0, 0, 0}; }
+    __device__ __forceinline__ void fill(uint32_t word) { v = u4{word, word, word, word}; }
+    __device__ __forceinline__ void clear() { fill(0); }
     // Eight values stay four registers: without this the compiler converts once and keeps eight (across a loop for a row of weights).
     __device__ __forceinline__ void pin() { asm volatile("" : "+v"(v)); }
+    __device__ __forceinline__ void hold() { pin(); }   // (the same for fp32, where nothing is converted but what is made of the values could be kept as well)
 };
 template <> struct Raw<true> {
+    static constexpr uint32_t NEG_INF = 0xff800000u;
     f4 a, b;
-    __device__ __forceinline__ void load(const void* row, uint32_t at, int left) {
+    __device__ __forceinline__ void load(const void* row, uint32_t at, int left, uint32_t none = 0) {
         const char* p = (const char*)row + 4 * at;
         if (left >= 8) {
             a = *reinterpret_cast<const f4*>(p);
             b = *reinterpret_cast<const f4*>(p + 16);
             return;
         }
-        clear();
+        fill(none);
 #pragma unroll 1
         for (int e = left - 1; e >= 0; --e) {
             b = f4{a.w, b.x, b.y, b.z};
@@ -58,8 +63,13 @@ template <> struct Raw<true> {
         }
     }
     __device__ __forceinline__ float operator[](int e) const { return e < 4 ? a[e & 3] : b[e & 3]; }
-    __device__ __forceinline__ void clear() { a = b = f4{0.f, 0.f, 0.f, 0.f}; }
+    __device__ __forceinline__ void fill(uint32_t word) {
+        const float x = __builtin_bit_cast(float, word);
+        a = b = f4{x, x, x, x};
+    }
+    __device__ __forceinline__ void clear() { fill(0); }
     __device__ __forceinline__ void pin() {}
+    __device__ __forceinline__ void hold() { asm volatile("" : "+v"(a), "+v"(b)); }
 };
 typedef Raw<false> Half8;
 
