@@ -159,6 +159,7 @@ __device__ __forceinline__ void top_of_list(int top, const uint64_t* list, int c
     for (int i = threadIdx.x; i < count; i += blockDim.x) {
         const uint64_t mine = list[i];
         int place = 0;
+#pragma unroll 8
         for (int j = 0; j < count; ++j) place += list[j] > mine;
         if (place < top) put(place, mine);
     }
@@ -211,23 +212,23 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     pin();
     const bool wants_t = a.entropy || p.lse || (GRAD && a.dentropy);
     {
-        float s[4] = {}, t[4] = {};
+        float s[2] = {}, t[2] = {};
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             if (wants_t) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float u = fmaf(v[i][e], c, -x.k), y = __builtin_amdgcn_exp2f(u);
-                    s[e & 3] += y;
-                    t[e & 3] = fmaf(y, fmaxf(u, FAR), t[e & 3]);
+                    s[e & 1] += y;
+                    t[e & 1] = fmaf(y, fmaxf(u, FAR), t[e & 1]);
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s[e & 3] += __builtin_amdgcn_exp2f(fmaf(v[i][e], c, -x.k));
+                for (int e = 0; e < 8; ++e) s[e & 1] += __builtin_amdgcn_exp2f(fmaf(v[i][e], c, -x.k));
             }
         }
-        x.s = wave_reduce((s[0] + s[1]) + (s[2] + s[3]), Sum());
-        if (wants_t) x.t = wave_reduce((t[0] + t[1]) + (t[2] + t[3]), Sum());
+        x.s = wave_reduce(s[0] + s[1], Sum());
+        if (wants_t) x.t = wave_reduce(t[0] + t[1], Sum());
     }
     if (waves > 1) {      // the waves' statistics joined, a lane per wave
         if (lane == 0) {
@@ -252,7 +253,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     } else if (threadIdx.x == 0) p.stats[blockIdx.x] = x;
     if constexpr (!GRAD) {
         if (a.top == 0) return;
-        // Candidates: whatever reaches the top-th largest of the maxima of groups of threads, 256 groups at most, cut to 16 bits.  Few do, so they are ordered by
+        // Candidates: whatever reaches the top-th largest of the maxima of groups of threads (64 groups for up to 32 alternatives, 256 for more), cut to 16 bits.  Few do, so they are ordered by
         // comparing each with each.  Rows where many do (equal logits) or with not-a-number, which no maximum shows, go by rounds.
         __shared__ uint32_t maxima[256];
         __shared__ uint64_t list[CANDIDATES], slots[16];
@@ -277,25 +278,37 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
             uint32_t g[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) g[i] = maxima[lane + 64 * i];
-#pragma unroll 1
-            for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
-                int count = 0;
+            if (a.top <= 32) {
+                const uint32_t most = max(max(g[0], g[1]), max(g[2], g[3]));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) count += __popcll(__ballot(g[i] >= (bound | bit)));
-                if (count >= a.top) bound |= bit;
+                for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
+                    if (__popcll(__ballot(most >= (bound | bit))) >= a.top) bound |= bit;
+            } else {
+#pragma unroll 1
+                for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+                    int count = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) count += __popcll(__ballot(g[i] >= (bound | bit)));
+                    if (count >= a.top) bound |= bit;
+                }
             }
         }
         bound = max(bound, RANK_NEG_INF + 1);
         const float least = value_of(bound);
         if (rank >= bound) {
 #pragma unroll
-            for (int i = 0; i < V; ++i)
+            for (int i = 0; i < V; ++i) {
+                float most = v[i][0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) most = fmaxf(most, v[i][e]);
+                if (most < least) continue;      // (most octets)
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     if (v[i][e] >= least) {
                         const int j = atomicAdd(&used, 1);
                         if (j < CANDIDATES) list[j] = (uint64_t)rank_of(v[i][e]) << 32 | (uint32_t)~(from + 8 * (int)(threadIdx.x + T * i) + e);
                     }
+            }
         }
         __syncthreads();
         const int count = used;
@@ -326,7 +339,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     }
 }
 
-// The parts of a row joined: a thread a part (256 at most).
+// The parts of a row joined: a thread a part (256 at most).  One wave where it has lanes for them: no barrier between its steps.
 __global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
     __shared__ float buf[3][16];
     __shared__ uint64_t list[CANDIDATES], slots[16];
@@ -338,6 +351,22 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
         return;
     }
     const Stats y = i < p.parts ? p.stats[row * p.parts + i] : Stats{LEAST, 0.f, 0.f};
+    const uint64_t* keys = p.keys + (size_t)row * p.parts * a.top;
+    const int total = p.parts * a.top;
+    // (asked for together with the statistics: a part's last key, and the first keys of this thread)
+    const uint64_t last = a.top > 0 && i < p.parts ? keys[(size_t)i * a.top + a.top - 1] : 0;
+    uint64_t first[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int j = i + e * (int)blockDim.x;
+        first[e] = j < total ? keys[j] : 0;
+    }
+    auto each = [&](auto&& f) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f(first[e]);
+        for (int j = i + 4 * blockDim.x; j < total; j += blockDim.x) f(keys[j]);
+    };
+    if (i == 0) used = 0;
     Stats x;
     x.k = group_reduce(y.k, buf[0], LEAST, MostFloat());
     const float d = shrink(y.k, x.k), f = __builtin_amdgcn_exp2f(d);
@@ -346,15 +375,9 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
     const float ln_s = logf(x.s), entropy = x.s == 0.f ? 0.f : ln_s - LN2 * (x.t / x.s);
     if (i == 0) put_row(a, p, row, row_of(a.z, row, a.ldz, a.f32), token, x, ln_s, entropy);
     if (a.top == 0) return;
-    const uint64_t* keys = p.keys + (size_t)row * p.parts * a.top;
-    const int total = p.parts * a.top;
     // a part whose last key is this large has enough of them
-    const uint64_t bound = max(group_reduce(i < p.parts ? keys[(size_t)i * a.top + a.top - 1] : 0, slots, (uint64_t)0, Most()), (uint64_t)(RANK_NEG_INF + 1) << 32);
-    if (i == 0) used = 0;
+    const uint64_t bound = max(group_reduce(last, slots, (uint64_t)0, Most()), (uint64_t)1);
     __syncthreads();
-    auto each = [&](auto&& f) {
-        for (int j = i; j < total; j += 256) f(keys[j]);
-    };
     each([&](uint64_t key) {
         if (key >= bound) {
             const int at = atomicAdd(&used, 1);
@@ -362,8 +385,9 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
         }
     });
     __syncthreads();
+    const int count = used;
     auto put = [&](int at, uint64_t key) { put_top(a, row, at, key, x.k, ln_s); };
-    if (used <= CANDIDATES) top_of_list(a.top, list, used, put);
+    if (count <= CANDIDATES) top_of_list(a.top, list, count, put);
     else top_by_rounds(a.top, slots, each, put);
 }
 
@@ -432,6 +456,10 @@ Plan plan_of(int n, bool f32, int64_t m, int top) {
     Plan p{};
     const int octets = ceil_div(n, 8), fit = 1024 * most;
     int parts = ceil_div(octets, fit);
+    // A CU takes 9 us for 130000 values (exponentials and sums, 260 KB): where there are CUs for all of them, parts of 32768 values save more than the join's launch
+    // costs.  1 x 130001 with 20 alternatives 15.7 -> 12.5 us, 57 x 130001 16.2 -> 14.4, 16 x 262144 18.7 -> 11.9; 1 x 64000 would go 9.0 -> 11.2.
+    const int finer = ceil_div(n, 32768);
+    if (n > 98304 && finer > parts && m * finer <= 256) parts = finer;
     p.parts = parts;
     int per = ceil_div(octets, parts);
     const int threads = per <= 256 ? 64 : per <= 2048 ? 256 : 1024;
@@ -484,7 +512,7 @@ void launch_fwd(const Logprob& a, hipStream_t s) {
     }
     if (q.parts > 1) {
         launch_rows<F32, false>(q, a, p, s);
-        logprob_join_kernel<<<(unsigned)a.m, 256, 0, s>>>(a, p);
+        logprob_join_kernel<<<(unsigned)a.m, q.parts <= 64 ? 64 : 256, 0, s>>>(a, p);
     } else logprob_long_kernel<F32><<<(unsigned)a.m, 1024, 0, s>>>(a, p);
     if (!a.dz) return;
     Logprob b = a;
