@@ -4,29 +4,11 @@
 //
 // Nothing but bytes: every value is read and written once, so a thread takes whole pieces of VW values of both halves and keeps the cosines and sines of its
 // piece, fp32 and as many bytes as the pieces themselves, for all heads of the token: a workgroup takes one token and runs over its heads.  4001 tokens, 64 / 8 heads of 128: 34.5 us, 4.8 TB/s.
+#include "pieces.h"
 #include "qeft_internal.h"
 
 namespace qeft {
 namespace {
-
-typedef float f4 __attribute__((ext_vector_type(4)));
-
-template <int VW> struct Piece { typedef uint32_t type __attribute__((ext_vector_type(VW / 2))); };
-template <> struct Piece<2> { typedef uint32_t type; };
-template <> struct Piece<1> { typedef uint16_t type; };
-
-// one piece of VW values: read, write
-template <int VW>
-__device__ __forceinline__ void get(const __half* p, _Float16 (&x)[VW]) {
-    const auto v = *reinterpret_cast<const typename Piece<VW>::type*>(p);
-    __builtin_memcpy(x, &v, sizeof x);
-}
-template <int VW>
-__device__ __forceinline__ void put(__half* p, const _Float16 (&x)[VW]) {
-    typename Piece<VW>::type v;
-    __builtin_memcpy(&v, x, sizeof x);
-    *reinterpret_cast<typename Piece<VW>::type*>(p) = v;
-}
 
 // Workgroup = token x one of `parts` shares of its heads.  Threads: `pieces` of a head x as many heads side by side as fit.  The pieces of a head: rot_dim / 2 / VW
 // pairs (half apart), then what is not rotated, d - rot_dim, in pieces of VW.  Heads: those of q, then k's, then v's (whose d is all "not rotated").

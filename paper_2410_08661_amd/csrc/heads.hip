@@ -4,219 +4,435 @@
 //   y = x rs w, rs = 1 / sqrt(mean x^2 + eps)     z = R y:  (a, b) -> (a c - b s, b c + a s),  a = y[j], b = y[j + half], half = rot_dim / 2
 //   g = R^T gz     dx = rs (a - xh mean(a xh)),  a = g w, xh = x rs     dw = sum g xh
 //
-// A wave takes a head, a lane values half apart.
+// Bytes bound all three.  A head is L lanes', each with two pieces of VW values half apart, so that pairs meet in a lane and the head's sums stay within a row of lanes
+// (no LDS); a wave has 64 / L heads side by side.  Heads of all tokens form one sequence that the grid walks through: no lane waits for a token's last heads.  The
+// gradient's workgroups keep their sums for dw in registers and leave one slab each, summed by a second launch in a fixed order.
+#include "pieces.h"
 #include "qeft_internal.h"
 #include "wave.h"
 
 namespace qeft {
 namespace {
 
-constexpr int MOST_PAIRS = QEFT_MAX_HEAD_DIM / 2 / 64;   // pairs of a lane
-constexpr int SLABS = 1024;
+constexpr int THREADS = 256;
+constexpr int FWD_GROUPS = 2048, BWD_GROUPS = 1024;      // workgroups at most
 
-// Lane's i-th pair of the head's d / 2: the rotated ones, then what is behind them two by two
-struct Pair {
-    int first, second;
-    bool there, turned;
+// Lane's r-th two pieces of a head: the rotated ones, half apart, then what is behind them two by two
+template <int VW>
+struct Place {
+    int first, second;      // values
+    bool turned, one, two;  // two pieces that are a pair; there is a first, a second one
 };
-__device__ __forceinline__ Pair pair_of(int i, int d, int half) {
-    const int p = 64 * i + (threadIdx.x & 63);
-    if (p >= d / 2) return Pair{0, 0, false, false};
-    if (p < half) return Pair{p, p + half, true, true};
-    return Pair{2 * p, 2 * p + 1, true, false};
+template <int VW>
+__device__ __forceinline__ Place<VW> place_of(int p, int d, int half) {
+    const int pairs = half / VW, whole = d / VW;
+    if (p < pairs) return Place<VW>{VW * p, half + VW * p, true, true, true};
+    const int at = 2 * pairs + 2 * (p - pairs);
+    return Place<VW>{VW * at, VW * (at + 1), false, at < whole, at + 1 < whole};
 }
+template <int VW>
+struct Two {
+    _Float16 a[VW], b[VW];
+    __device__ __forceinline__ void load(const __half* head, const Place<VW>& p) {
+        if (p.two) {
+            get<VW>(head + p.first, a);
+            get<VW>(head + p.second, b);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VW; ++e) a[e] = b[e] = 0;
+            if (p.one) get<VW>(head + p.first, a);
+        }
+    }
+    __device__ __forceinline__ void store(__half* head, const Place<VW>& p) const {
+        if (p.one) put<VW>(head + p.first, a);
+        if (p.two) put<VW>(head + p.second, b);
+    }
+    // one of two, word by word (a choice between the objects goes through memory)
+    static __device__ __forceinline__ Two choose(bool first, const Two& x, const Two& y) {
+        uint32_t u[VW], v[VW];
+        __builtin_memcpy(u, &x, sizeof u);
+        __builtin_memcpy(v, &y, sizeof v);
+#pragma unroll
+        for (int i = 0; i < VW; ++i) u[i] = first ? u[i] : v[i];
+        Two o;
+        __builtin_memcpy(&o, u, sizeof u);
+        return o;
+    }
+};
+template <int N, int CTRL>
+__device__ __forceinline__ float moved(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, false)); }
+// Sum over L neighbouring lanes, the same in each of them
+template <int L>
+__device__ __forceinline__ float head_sum(float x) {
+    if (L >= 2) x += moved<1, 0xb1>(x);       // quad_perm 1 0 3 2
+    if (L >= 4) x += moved<2, 0x4e>(x);       // quad_perm 2 3 0 1
+    if (L >= 8) x += moved<4, 0x141>(x);      // row_half_mirror
+    if (L >= 16) x += moved<8, 0x140>(x);     // row_mirror
+    if (L >= 32) x = across<false>(x, Sum());
+    if (L >= 64) x = across<true>(x, Sum());
+    return x;
+}
+// Sum over the heads side by side in a wave: lanes L apart
+template <int L>
+__device__ __forceinline__ float side_sum(float x) {
+    if (L <= 4) x += row_rotated<4>(x);
+    if (L <= 8) x += row_rotated<8>(x);
+    if (L <= 16) x = across<false>(x, Sum());
+    if (L <= 32) x = across<true>(x, Sum());
+    return x;
+}
+
+// Where the grid's walk over `heads` heads of every token begins for this lane, and its step
+struct Walk {
+    int t, h, dt, dh, heads;
+    __device__ __forceinline__ Walk(int slot, int slots, int heads_) : heads(heads_) {
+        t = (int)((uint32_t)slot / (uint32_t)heads);
+        h = slot - t * heads;
+        dt = (int)((uint32_t)slots / (uint32_t)heads);
+        dh = slots - dt * heads;
+    }
+    __device__ __forceinline__ void next() {
+        t += dt;
+        h += dh;
+        if (h >= heads) h -= heads, ++t;
+    }
+};
+
+// cosines and sines of a lane's pairs
+template <int VW>
 struct Turn {
-    float c[MOST_PAIRS], s[MOST_PAIRS];
+    float c[VW], s[VW];
+    __device__ __forceinline__ void load(const float* rot, int64_t ld, int positions, int pos, int first, int half) {
+        const float* r = rot + (size_t)min(max(pos, 0), positions - 1) * ld + first;
+#pragma unroll
+        for (int e = 0; e < VW; ++e) {
+            c[e] = r[e];
+            s[e] = r[half + e];
+        }
+    }
 };
-__device__ __forceinline__ Turn turn_of(const float* rot, int64_t ld, int positions, int pos, int d, int half) {
-    Turn t;
+
+// A head's values (x, and the weights w where it is normed) into what goes out
+template <int VW, int R, int L>
+__device__ __forceinline__ void forward(Two<VW> (&x)[R], const Two<VW> (&w)[R], bool normed, const Place<VW> (&place)[R], const Turn<VW> (&turn)[R], int d, float eps) {
+    float rs = 1.f;
+    if (normed) {
+        float ss = 0.f;
 #pragma unroll
-    for (int i = 0; i < MOST_PAIRS; ++i) {
-        const Pair p = pair_of(i, d, half);
-        t.c[i] = 1.f, t.s[i] = 0.f;
-        if (p.turned) {
-            const float* r = rot + (size_t)min(max(pos, 0), positions - 1) * ld + p.first;
-            t.c[i] = r[0];
-            t.s[i] = r[half];
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < VW; ++e) {
+                const float a = x[r].a[e], b = x[r].b[e];
+                ss = fmaf(a, a, ss);
+                ss = fmaf(b, b, ss);
+            }
+        rs = 1.f / sqrtf(head_sum<L>(ss) / (float)d + eps);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < VW; ++e) {
+            float a = x[r].a[e], b = x[r].b[e];
+            if (normed) {
+                a = a * rs * (float)w[r].a[e];
+                b = b * rs * (float)w[r].b[e];
+            }
+            x[r].a[e] = (_Float16)(place[r].turned ? a * turn[r].c[e] - b * turn[r].s[e] : a);
+            x[r].b[e] = (_Float16)(place[r].turned ? b * turn[r].c[e] + a * turn[r].s[e] : b);
+        }
+}
+
+template <int VW, int R, int L>
+struct Lane {
+    Place<VW> place[R];
+    Two<VW> wq[R], wk[R];
+    __device__ __forceinline__ Lane(int d, int half, const __half* w_q, const __half* w_k) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            place[r] = place_of<VW>((int)(threadIdx.x % L) + L * r, d, half);
+            if (w_q) wq[r].load(w_q, place[r]);
+            if (w_k) wk[r].load(w_k, place[r]);
         }
     }
-    return t;
-}
+};
 
-// One head: x (and w, where it is normed) to dst, rotated
-__device__ __forceinline__ void one_head(const __half* x, const __half* w, __half* dst, const Turn& t, int d, int half, float eps) {
-    float a[MOST_PAIRS], b[MOST_PAIRS], ss = 0.f;
+template <int VW, int R, int L>
+__global__ __launch_bounds__(THREADS) void heads_fwd_kernel(Heads a) {
+    const int half = a.rot_dim / 2, hq = a.q.heads;
+    const Lane<VW, R, L> lane(a.d, half, a.q.w, a.k.w);
+    Walk at((blockIdx.x * THREADS + threadIdx.x) / L, gridDim.x * (THREADS / L), hq + a.k.heads);
+    Two<VW> x[R], ahead[R];
+    int pos = 0, pos_ahead = 0;
+    auto fetch = [&](Two<VW>(&to)[R], int& p) {
+        if (at.t >= a.m) return;
+        const bool is_q = at.h < hq;
+        const __half* head = (is_q ? a.q.x + at.t * a.q.ldx : a.k.x + at.t * a.k.ldx) + (size_t)(is_q ? at.h : at.h - hq) * a.d;
 #pragma unroll
-    for (int i = 0; i < MOST_PAIRS; ++i) {
-        const Pair p = pair_of(i, d, half);
-        a[i] = p.there ? __half2float(x[p.first]) : 0.f;
-        b[i] = p.there ? __half2float(x[p.second]) : 0.f;
-        ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
-    }
-    if (w) {
-        ss = wave_reduce(ss, Sum());
-        const float rs = 1.f / sqrtf(ss / (float)d + eps);
+        for (int r = 0; r < R; ++r) to[r].load(head, lane.place[r]);
+        p = a.pos && half ? a.pos[at.t] : at.t;
+    };
+    fetch(ahead, pos_ahead);
+    while (at.t < a.m) {
+        const int t = at.t, h = at.h;
+        pos = pos_ahead;
 #pragma unroll
-        for (int i = 0; i < MOST_PAIRS; ++i) {
-            const Pair p = pair_of(i, d, half);
-            if (!p.there) continue;
-            a[i] *= rs * __half2float(w[p.first]);
-            b[i] *= rs * __half2float(w[p.second]);
-        }
-    }
+        for (int r = 0; r < R; ++r) x[r] = ahead[r];
+        Turn<VW> turn[R];
 #pragma unroll
-    for (int i = 0; i < MOST_PAIRS; ++i) {
-        const Pair p = pair_of(i, d, half);
-        if (!p.there) continue;
-        dst[p.first] = __float2half(p.turned ? a[i] * t.c[i] - b[i] * t.s[i] : a[i]);
-        dst[p.second] = __float2half(p.turned ? b[i] * t.c[i] + a[i] * t.s[i] : b[i]);
-    }
-}
-
-// Workgroup = a token, four waves over its heads
-__global__ __launch_bounds__(256) void heads_fwd_kernel(Heads a) {
-    const int64_t t = blockIdx.x;
-    const int half = a.rot_dim / 2;
-    const Turn turn = turn_of(a.rot, a.ld_rot, a.positions, a.pos ? a.pos[t] : (int)t, a.d, half);
-    for (int h = threadIdx.x >> 6; h < a.q.heads + a.k.heads; h += 4) {
-        const bool is_q = h < a.q.heads;
-        const HeadPart& p = is_q ? a.q : a.k;
-        const int64_t at = (int64_t)(is_q ? h : h - a.q.heads) * a.d;
-        one_head(p.x + t * p.ldx + at, p.w, p.out + t * p.ldout + at, turn, a.d, half, a.eps);
+        for (int r = 0; r < R; ++r)
+            if (lane.place[r].turned) turn[r].load(a.rot, a.ld_rot, a.positions, pos, lane.place[r].first, half);
+        at.next();
+        fetch(ahead, pos_ahead);
+        const bool is_q = h < hq;
+        Two<VW> w[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) w[r] = Two<VW>::choose(is_q, lane.wq[r], lane.wk[r]);
+        forward<VW, R, L>(x, w, is_q ? a.q.w != nullptr : a.k.w != nullptr, lane.place, turn, a.d, a.eps);
+        __half* out = (is_q ? a.q.out + t * a.q.ldout : a.k.out + t * a.k.ldout) + (size_t)(is_q ? h : h - hq) * a.d;
+#pragma unroll
+        for (int r = 0; r < R; ++r) x[r].store(out, lane.place[r]);
     }
 }
 
-__global__ __launch_bounds__(256) void heads_append_kernel(Cache c, Append a, const __half* w_q, const __half* w_k, float eps) {
-    const int t = blockIdx.x;
-    const int index = a.index[t], b = a.seq ? a.seq[t] : t, half = a.rot_dim / 2;
+// The heads of q, k and v of tokens that enter a cache; as qeft_cache_append otherwise.
+template <int VW, int R, int L>
+__global__ __launch_bounds__(THREADS) void heads_append_kernel(Cache c, Append a, const __half* w_q, const __half* w_k, float eps) {
+    const int half = a.rot_dim / 2, hq = a.q ? a.heads : 0;
+    const Lane<VW, R, L> lane(c.d, half, w_q, w_k);
     const int64_t last = (int64_t)c.table_pages * c.page_size;
-    __half *kd = nullptr, *vd = nullptr;
-    if (b >= 0 && b < c.seqs && index >= 0 && index < last) {
-        const int p = c.by_page.of(index);
-        const int page = c.table[(size_t)b * c.ld_table + p];
-        if (page >= 0 && page < c.pages) {
-            const size_t at = (size_t)page * c.page_stride + (size_t)(index - p * c.page_size) * c.token_stride;
-            kd = c.k + at;
-            vd = c.v + at;
+    for (Walk at((blockIdx.x * THREADS + threadIdx.x) / L, gridDim.x * (THREADS / L), hq + 2 * c.kv); at.t < a.tokens; at.next()) {
+        const int t = at.t;
+        const bool is_q = at.h < hq, is_v = at.h >= hq + c.kv;
+        const int h = is_q ? at.h : is_v ? at.h - hq - c.kv : at.h - hq;
+        const __half* head = (is_q ? a.q + t * a.ldq : is_v ? a.v + t * a.ldv : a.k + t * a.ldk) + (size_t)h * c.d;
+        Two<VW> x[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) x[r].load(head, lane.place[r]);
+        const int index = a.index[t], b = a.seq ? a.seq[t] : t;
+        __half* out = is_q ? a.q_out + t * a.ldq_out + (size_t)h * c.d : nullptr;
+        if (!is_q && b >= 0 && b < c.seqs && index >= 0 && index < last) {
+            const int p = c.by_page.of(index);
+            const int page = c.table[(size_t)b * c.ld_table + p];
+            if (page >= 0 && page < c.pages)
+                out = (is_v ? c.v : c.k) + (size_t)page * c.page_stride + (size_t)(index - p * c.page_size) * c.token_stride + (size_t)h * c.head_stride;
         }
-    }
-    const Turn turn = turn_of(a.rot, a.ld_rot, a.positions, a.pos ? a.pos[t] : index, c.d, half);
-    const int hq = a.q ? a.heads : 0;
-    for (int h = threadIdx.x >> 6; h < hq + 2 * c.kv; h += 4) {
-        if (h < hq) {
-            one_head(a.q + (size_t)t * a.ldq + (size_t)h * c.d, w_q, a.q_out + (size_t)t * a.ldq_out + (size_t)h * c.d, turn, c.d, half, eps);
-        } else if (kd) {
-            const int kh = (h - hq) % c.kv;
-            if (h < hq + c.kv) {
-                one_head(a.k + (size_t)t * a.ldk + (size_t)kh * c.d, w_k, kd + (size_t)kh * c.head_stride, turn, c.d, half, eps);
-            } else {
-                for (int j = threadIdx.x & 63; j < c.d; j += 64) vd[(size_t)kh * c.head_stride + j] = a.v[(size_t)t * a.ldv + (size_t)kh * c.d + j];
+        if (!is_v) {
+            Turn<VW> turn[R];
+            Two<VW> w[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (lane.place[r].turned) turn[r].load(a.rot, a.ld_rot, a.positions, a.pos ? a.pos[t] : index, lane.place[r].first, half);
+                w[r] = Two<VW>::choose(is_q, lane.wq[r], lane.wk[r]);
             }
+            forward<VW, R, L>(x, w, is_q ? w_q != nullptr : w_k != nullptr, lane.place, turn, c.d, eps);
         }
+        if (!out) continue;   // (a token without a slot)
+#pragma unroll
+        for (int r = 0; r < R; ++r) x[r].store(out, lane.place[r]);
     }
 }
 
-// Workgroups stay for tokens blockIdx.x, + gridDim.x ...; slab [workgroup][2 (q, k)][d] of dw
-__global__ __launch_bounds__(256) void heads_bwd_kernel(Heads a, float* slab) {
-    __shared__ float joined[2][4][QEFT_MAX_HEAD_DIM];
+// Gradient: first the heads of q, then those of k.  slab [workgroup][q, k][d], or NULL
+template <int VW, int R, int L>
+__global__ __launch_bounds__(THREADS) void heads_bwd_kernel(Heads a, float* slab) {
+    __shared__ float joined[THREADS / 64][QEFT_MAX_HEAD_DIM];
     const int half = a.rot_dim / 2, wave = threadIdx.x >> 6;
-    float sums[2][2][MOST_PAIRS] = {};
-    for (int64_t t = blockIdx.x; t < a.m; t += gridDim.x) {
-        const Turn turn = turn_of(a.rot, a.ld_rot, a.positions, a.pos ? a.pos[t] : (int)t, a.d, half);
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        const HeadPart& p = which ? a.k : a.q;
+        float sa[R][VW] = {}, sb[R][VW] = {};
+        const Lane<VW, R, L> lane(a.d, half, p.w, nullptr);
+        const bool normed = p.w != nullptr;
+        if (p.heads > 0 && (p.dx || p.dw)) {
+            Walk at((blockIdx.x * THREADS + threadIdx.x) / L, gridDim.x * (THREADS / L), p.heads);
+            Two<VW> g[R], x[R], g_ahead[R], x_ahead[R];
+            int pos = 0, pos_ahead = 0;
+            auto fetch = [&] {
+                if (at.t >= a.m) return;
+                const __half* gh = p.g + at.t * p.ldg + (size_t)at.h * a.d;
+                const __half* xh = p.x + at.t * p.ldx + (size_t)at.h * a.d;
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const HeadPart& p = which ? a.k : a.q;
-            for (int h = wave; h < p.heads; h += 4) {
-                const int64_t at = (int64_t)h * a.d;
-                float ga[MOST_PAIRS], gb[MOST_PAIRS], xa[MOST_PAIRS], xb[MOST_PAIRS], s[2] = {};
-#pragma unroll
-                for (int i = 0; i < MOST_PAIRS; ++i) {
-                    const Pair r = pair_of(i, a.d, half);
-                    const __half* g = p.g + t * p.ldg + at;
-                    const float u = r.there ? __half2float(g[r.first]) : 0.f, v = r.there ? __half2float(g[r.second]) : 0.f;
-                    ga[i] = r.turned ? u * turn.c[i] + v * turn.s[i] : u;
-                    gb[i] = r.turned ? v * turn.c[i] - u * turn.s[i] : v;
-                    if (!p.w || !r.there) continue;
-                    const __half* x = p.x + t * p.ldx + at;
-                    xa[i] = __half2float(x[r.first]);
-                    xb[i] = __half2float(x[r.second]);
-                    s[0] = fmaf(xa[i], xa[i], fmaf(xb[i], xb[i], s[0]));
-                    s[1] = fmaf(ga[i] * __half2float(p.w[r.first]), xa[i], fmaf(gb[i] * __half2float(p.w[r.second]), xb[i], s[1]));
+                for (int r = 0; r < R; ++r) {
+                    g_ahead[r].load(gh, lane.place[r]);
+                    if (normed) x_ahead[r].load(xh, lane.place[r]);
                 }
-                float rs = 0.f, mean = 0.f;
-                if (p.w) {
-                    s[0] = wave_reduce(s[0], Sum());
-                    s[1] = wave_reduce(s[1], Sum());
-                    rs = 1.f / sqrtf(s[0] / (float)a.d + a.eps);
-                    mean = s[1] * rs / (float)a.d;
-                }
+                pos_ahead = a.pos && half ? a.pos[at.t] : at.t;
+            };
+            fetch();
+            while (at.t < a.m) {
+                const int t = at.t, h = at.h;
+                pos = pos_ahead;
 #pragma unroll
-                for (int i = 0; i < MOST_PAIRS; ++i) {
-                    const Pair r = pair_of(i, a.d, half);
-                    if (!r.there) continue;
-                    float da = ga[i], db = gb[i];
-                    if (p.w) {
-                        const float ha = xa[i] * rs, hb = xb[i] * rs;
-                        sums[which][0][i] = fmaf(da, ha, sums[which][0][i]);
-                        sums[which][1][i] = fmaf(db, hb, sums[which][1][i]);
-                        da = rs * (da * __half2float(p.w[r.first]) - ha * mean);
-                        db = rs * (db * __half2float(p.w[r.second]) - hb * mean);
+                for (int r = 0; r < R; ++r) {
+                    g[r] = g_ahead[r];
+                    x[r] = x_ahead[r];
+                }
+                Turn<VW> turn[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    if (lane.place[r].turned) turn[r].load(a.rot, a.ld_rot, a.positions, pos, lane.place[r].first, half);
+                at.next();
+                fetch();
+                float ga[R][VW], gb[R][VW], ss = 0.f, dot = 0.f;
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int e = 0; e < VW; ++e) {
+                        const float u = g[r].a[e], v = g[r].b[e];
+                        ga[r][e] = lane.place[r].turned ? u * turn[r].c[e] + v * turn[r].s[e] : u;
+                        gb[r][e] = lane.place[r].turned ? v * turn[r].c[e] - u * turn[r].s[e] : v;
                     }
-                    if (p.dx) {
-                        p.dx[t * p.lddx + at + r.first] = __float2half(da);
-                        p.dx[t * p.lddx + at + r.second] = __float2half(db);
+                if (normed) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) {
+                            const float xa = x[r].a[e], xb = x[r].b[e];
+                            ss = fmaf(xa, xa, ss);
+                            ss = fmaf(xb, xb, ss);
+                            dot = fmaf(ga[r][e] * (float)lane.wq[r].a[e], xa, dot);
+                            dot = fmaf(gb[r][e] * (float)lane.wq[r].b[e], xb, dot);
+                        }
+                    const float rs = 1.f / sqrtf(head_sum<L>(ss) / (float)a.d + a.eps), mean = head_sum<L>(dot) * rs / (float)a.d;
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) {
+                            const float ha = x[r].a[e] * rs, hb = x[r].b[e] * rs;
+                            sa[r][e] = fmaf(ga[r][e], ha, sa[r][e]);
+                            sb[r][e] = fmaf(gb[r][e], hb, sb[r][e]);
+                            ga[r][e] = rs * (ga[r][e] * (float)lane.wq[r].a[e] - ha * mean);
+                            gb[r][e] = rs * (gb[r][e] * (float)lane.wq[r].b[e] - hb * mean);
+                        }
+                }
+                if (!p.dx) continue;
+                __half* out = p.dx + t * p.lddx + (size_t)h * a.d;
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    Two<VW> o;
+#pragma unroll
+                    for (int e = 0; e < VW; ++e) {
+                        o.a[e] = (_Float16)ga[r][e];
+                        o.b[e] = (_Float16)gb[r][e];
                     }
+                    o.store(out, lane.place[r]);
                 }
             }
         }
-    }
-    if (!slab) return;
+        if (!slab) continue;
+        // the heads side by side, then the waves
 #pragma unroll
-    for (int which = 0; which < 2; ++which)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int i = 0; i < MOST_PAIRS; ++i) {
-            const Pair r = pair_of(i, a.d, half);
-            if (!r.there) continue;
-            joined[which][wave][r.first] = sums[which][0][i];
-            joined[which][wave][r.second] = sums[which][1][i];
-        }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * a.d; i += 256) {
-        const int which = i / a.d, j = i % a.d;
-        slab[((size_t)blockIdx.x * 2 + which) * a.d + j] = ((joined[which][0][j] + joined[which][1][j]) + joined[which][2][j]) + joined[which][3][j];
+            for (int e = 0; e < VW; ++e) {
+                const float x = side_sum<L>(sa[r][e]), y = side_sum<L>(sb[r][e]);
+                if ((threadIdx.x & 63) < L) {
+                    if (lane.place[r].one) joined[wave][lane.place[r].first + e] = x;
+                    if (lane.place[r].two) joined[wave][lane.place[r].second + e] = y;
+                }
+            }
+        __syncthreads();
+        for (int j = threadIdx.x; j < a.d; j += THREADS)
+            slab[((size_t)blockIdx.x * 2 + which) * a.d + j] = ((joined[0][j] + joined[1][j]) + joined[2][j]) + joined[3][j];
+        __syncthreads();
     }
 }
 
-// dw[j] = the slabs' sum in their order
-__global__ __launch_bounds__(256) void heads_sum_kernel(Heads a, const float* slab, int slabs) {
-    const int j = blockIdx.x * 256 + threadIdx.x;
-    if (j >= 2 * a.d) return;
+// dw: the slabs' sum in a fixed order, 32 columns a workgroup, 8 threads a column
+__global__ __launch_bounds__(THREADS) void heads_sum_kernel(Heads a, const float* slab, int slabs) {
+    __shared__ float joined[8][33];
+    const int column = threadIdx.x & 31, share = threadIdx.x >> 5, j = blockIdx.x * 32 + column;
+    float s = 0.f;
+    if (j < 2 * a.d) {
+#pragma unroll 8
+        for (int i = share; i < slabs; i += 8) s += slab[(size_t)i * 2 * a.d + j];
+    }
+    joined[share][column] = s;
+    __syncthreads();
+    if (share != 0 || j >= 2 * a.d) return;
     float* out = j < a.d ? a.q.dw : a.k.dw;
     if (!out) return;
-    float s = 0.f;
-    for (int i = 0; i < slabs; ++i) s += slab[(size_t)i * 2 * a.d + j];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += joined[i][column];
     float* at = out + (j < a.d ? j : j - a.d);
     *at = a.accumulate ? *at + s : s;
 }
 
+// The widest pieces that both halves of a pair consist of, and the lanes of a head: f.template operator()<VW, R, L>()
+struct Form {
+    int vw, lanes;
+};
+Form form_of(int d, int rot_dim) {
+    const int half = rot_dim / 2, vw = half % 8 == 0 ? 8 : half % 4 == 0 ? 4 : half % 2 == 0 ? 2 : 1;
+    const int pairs = half / vw, pieces = pairs + (d / vw - 2 * pairs + 1) / 2;
+    if (vw == 8) return Form{8, pieces <= 4 ? 4 : pieces <= 8 ? 8 : 16};
+    if (vw == 4) return Form{4, pieces <= 16 ? 16 : 32};
+    return Form{vw, 64};
+}
+template <class F>
+void with_form(const Form& f, const F& go) {
+    if (f.vw == 8) {
+        if (f.lanes == 4) go.template operator()<8, 1, 4>();
+        else if (f.lanes == 8) go.template operator()<8, 1, 8>();
+        else go.template operator()<8, 1, 16>();
+    } else if (f.vw == 4) {
+        if (f.lanes == 16) go.template operator()<4, 1, 16>();
+        else go.template operator()<4, 1, 32>();
+    } else if (f.vw == 2) go.template operator()<2, 1, 64>();
+    else go.template operator()<1, 2, 64>();
+}
+// workgroups for so many heads of so many lanes
+int groups_for(int64_t heads, int lanes, int most) {
+    const int64_t n = (heads * lanes + THREADS - 1) / THREADS;
+    return (int)(n < most ? n : most);
+}
+struct Fwd {
+    const Heads& a;
+    unsigned grid;
+    hipStream_t s;
+    template <int VW, int R, int L>
+    void operator()() const { heads_fwd_kernel<VW, R, L><<<grid, THREADS, 0, s>>>(a); }
+};
+struct App {
+    const Cache& c;
+    const Append& a;
+    const __half *w_q, *w_k;
+    float eps;
+    unsigned grid;
+    hipStream_t s;
+    template <int VW, int R, int L>
+    void operator()() const { heads_append_kernel<VW, R, L><<<grid, THREADS, 0, s>>>(c, a, w_q, w_k, eps); }
+};
+struct Bwd {
+    const Heads& a;
+    float* slab;
+    unsigned grid;
+    hipStream_t s;
+    template <int VW, int R, int L>
+    void operator()() const { heads_bwd_kernel<VW, R, L><<<grid, THREADS, 0, s>>>(a, slab); }
+};
+int bwd_groups(int d, int heads, int kv, int rot_dim, int64_t m) { return groups_for(m * (heads > kv ? heads : kv), form_of(d, rot_dim).lanes, BWD_GROUPS); }
+
 }  // namespace
 
-size_t heads_workspace(int d, int heads, int kv, int rot_dim, int64_t m) { return (size_t)(m < SLABS ? m : SLABS) * 2 * d * sizeof(float); }
+size_t heads_workspace(int d, int heads, int kv, int rot_dim, int64_t m) { return (size_t)bwd_groups(d, heads, kv, rot_dim, m) * 2 * d * sizeof(float); }
 
 hipError_t heads_fwd(const Heads& a, hipStream_t s) {
-    heads_fwd_kernel<<<(unsigned)a.m, 256, 0, s>>>(a);
+    const Form f = form_of(a.d, a.rot_dim);
+    with_form(f, Fwd{a, (unsigned)groups_for(a.m * (a.q.heads + a.k.heads), f.lanes, FWD_GROUPS), s});
     return hipGetLastError();
 }
 hipError_t heads_append(const Cache& c, const Append& p, const __half* w_q, const __half* w_k, float eps, hipStream_t s) {
-    heads_append_kernel<<<(unsigned)p.tokens, 256, 0, s>>>(c, p, w_q, w_k, eps);
+    const Form f = form_of(c.d, p.rot_dim);
+    with_form(f, App{c, p, w_q, w_k, eps, (unsigned)groups_for((int64_t)p.tokens * (p.heads + 2 * (int64_t)c.kv), f.lanes, FWD_GROUPS), s});
     return hipGetLastError();
 }
 hipError_t heads_bwd(const Heads& a, hipStream_t s) {
     const bool sums = a.q.dw || a.k.dw;
     float* slab = sums ? (float*)a.ws : nullptr;
-    const int slabs = (int)(a.m < SLABS ? a.m : SLABS);
-    if (slabs > 0) heads_bwd_kernel<<<(unsigned)slabs, 256, 0, s>>>(a, slab);
-    if (sums) heads_sum_kernel<<<(unsigned)(2 * a.d + 255) / 256, 256, 0, s>>>(a, slab, slabs);
+    const int slabs = a.m > 0 ? bwd_groups(a.d, a.q.heads, a.k.heads, a.rot_dim, a.m) : 0;
+    if (slabs > 0) with_form(form_of(a.d, a.rot_dim), Bwd{a, slab, (unsigned)slabs, s});
+    if (sums) heads_sum_kernel<<<(unsigned)(2 * a.d + 31) / 32, THREADS, 0, s>>>(a, slab, slabs);
     return hipGetLastError();
 }
 
