@@ -15,7 +15,7 @@ namespace qeft {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int FWD_GROUPS = 2048, BWD_GROUPS = 1024;      // workgroups at most
+constexpr int FWD_GROUPS = 2048, BWD_GROUPS = 512;      // workgroups at most
 
 // Lane's r-th two pieces of a head: the rotated ones, half apart, then what is behind them two by two
 template <int VW>
@@ -366,8 +366,9 @@ Form form_of(int d, int rot_dim) {
     const int half = rot_dim / 2, vw = half % 8 == 0 ? 8 : half % 4 == 0 ? 4 : half % 2 == 0 ? 2 : 1;
     const int pairs = half / vw, pieces = pairs + (d / vw - 2 * pairs + 1) / 2;
     if (vw == 8) return Form{8, pieces <= 4 ? 4 : pieces <= 8 ? 8 : 16};
-    if (vw == 4) return Form{4, pieces <= 16 ? 16 : 32};
-    return Form{vw, 64};
+    if (vw == 4) return Form{4, pieces <= 8 ? 8 : pieces <= 16 ? 16 : 32};
+    if (vw == 2) return Form{2, pieces <= 16 ? 16 : 64};
+    return Form{1, 64};
 }
 template <class F>
 void with_form(const Form& f, const F& go) {
@@ -376,10 +377,13 @@ void with_form(const Form& f, const F& go) {
         else if (f.lanes == 8) go.template operator()<8, 1, 8>();
         else go.template operator()<8, 1, 16>();
     } else if (f.vw == 4) {
-        if (f.lanes == 16) go.template operator()<4, 1, 16>();
+        if (f.lanes == 8) go.template operator()<4, 1, 8>();
+        else if (f.lanes == 16) go.template operator()<4, 1, 16>();
         else go.template operator()<4, 1, 32>();
-    } else if (f.vw == 2) go.template operator()<2, 1, 64>();
-    else go.template operator()<1, 2, 64>();
+    } else if (f.vw == 2) {
+        if (f.lanes == 16) go.template operator()<2, 1, 16>();
+        else go.template operator()<2, 1, 64>();
+    } else go.template operator()<1, 2, 64>();
 }
 // workgroups for so many heads of so many lanes
 int groups_for(int64_t heads, int lanes, int most) {
