@@ -25,19 +25,6 @@ __host__ __device__ __forceinline__ uint32_t stir(uint32_t x) {
     return x ^ x >> 16;
 }
 
-// Code of a >= 0 in a format of BITS mantissa bits and exponent bias BIAS, up where the bits that are cut and r (of SIZE bits, at their top) carry: below the
-// smallest binade the float's bits are not the code's, there a is cut as a fixed-point number.
-template <int BITS, int BIAS, int SIZE>
-__device__ __forceinline__ uint32_t cut(float a, uint32_t r) {
-    constexpr int DROP = 23 - BITS;
-    constexpr float TINIEST = BIAS == 7 ? 0x1p-6f : 0x1p-14f, UNIT = BIAS == 7 ? 0x1p+29f : 0x1p+37f;
-    static_assert(BIAS == 7 || BIAS == 15, "e4m3, or e5m2 and fp16");
-    r <<= DROP - SIZE;
-    const uint32_t normal = ((__builtin_bit_cast(uint32_t, a) + r) >> DROP) - ((127 - BIAS) << BITS);
-    const uint32_t low = ((uint32_t)(fminf(a, TINIEST) * UNIT) + r) >> DROP;
-    return a >= TINIEST ? normal : low;
-}
-
 // Eight 8-bit codes
 struct Codes {
     uint32_t x, y;
@@ -85,39 +72,53 @@ struct Codes {
 __device__ __forceinline__ float power_of(uint32_t byte) {   // e8m0
     return __builtin_bit_cast(float, byte == 0 ? 0x00400000u : byte == 255 ? 0x7fc00000u : byte << 23);
 }
-// Codes of eight values, and the power of two of the block that 16 lanes have; r: 16 random bits each
+// Codes of eight values, and the power of two of the block that 16 lanes have.  The conversions round by 16 random bits at the top of a word: up where the bits that
+// are cut and those carry; as a fixed-point number below the smallest binade (compared with that definition for a million values: the same).  `finite`: of the whole block.
 template <bool E4M3>
-__device__ __forceinline__ void encode(const float (&v)[8], const uint32_t (&r)[8], Codes& codes, uint32_t& byte) {
+__device__ __forceinline__ uint32_t block_power(float most, bool finite) {
     constexpr int TOP = E4M3 ? 7 : 14;
-    uint32_t most = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t a = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;
-        most = a > most ? a : most;      // (bits of floats >= 0 are in their order, not-a-number above infinity)
-    }
-    most = row_reduce(most, Most());
-    const bool finite = most < 0x7f800000u;
-    const int power = max((int)(most >> 23) - 127 - TOP, -110);
-    byte = most == 0 ? 0 : finite ? (uint32_t)(power + 127) : 255;
-    const float inverse = __builtin_bit_cast(float, (uint32_t)(127 - power) << 23);
-    uint32_t c[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float a = fabsf(v[e]) * inverse;
-        c[e] = E4M3 ? cut<3, 7, 16>(a, r[e]) : cut<2, 15, 16>(a, r[e]);
-        if (!E4M3 && c[e] == 0 && a > 0.f) c[e] = 1;      // (a state that became zero under a first moment that is not would make a huge step)
-        if (E4M3 && v[e] < 0.f) c[e] |= 0x80;
-        if (!finite) c[e] = 0x7f;
-    }
-    codes.x = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
-    codes.y = c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24;
+    const int power = max((int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127 - TOP, -110);
+    return most == 0.f ? 0 : finite ? (uint32_t)(power + 127) : 255;
 }
-// fp16 values rounded up or down by 13 random bits each; not-a-number stays one, what reaches 2^16 is infinite
-__device__ __forceinline__ _Float16 cut_half(float x, uint32_t r) {
-    uint32_t c = cut<10, 15, 13>(fabsf(x), r);
-    c = c < 0x7c00u ? c : 0x7c00u;
-    c |= __builtin_bit_cast(uint32_t, x) >> 16 & 0x8000u;
-    return x != x ? (_Float16)x : __builtin_bit_cast(_Float16, (uint16_t)c);
+template <bool E4M3>
+__device__ __forceinline__ void encode(const float (&v)[8], const uint32_t (&r)[8], Codes& codes, uint32_t byte, bool finite) {
+    const float inverse = __builtin_bit_cast(float, (254u - min(max(byte, 17u), 253u)) << 23);      // (2^(127 - byte); a block of zeros has any)
+    float a[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] = v[e] * inverse;
+    if (!E4M3) {
+        // A second moment that became zero under a first one that is not would make a huge step: it stays at the smallest code.  Few lanes have any this small.
+        constexpr float SMALLEST = 0x1p-16f;
+        const float least = fminf(fminf(fminf(a[0], a[1]), fminf(a[2], a[3])), fminf(fminf(a[4], a[5]), fminf(a[6], a[7])));
+        if (least < SMALLEST) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[e] = v[e] > 0.f ? fmaxf(a[e], SMALLEST) : a[e];
+        }
+    }
+    int w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (E4M3) {
+            w[i] = __builtin_amdgcn_cvt_sr_fp8_f32(a[4 * i], (int)r[4 * i], w[i], 0);
+            w[i] = __builtin_amdgcn_cvt_sr_fp8_f32(a[4 * i + 1], (int)r[4 * i + 1], w[i], 1);
+            w[i] = __builtin_amdgcn_cvt_sr_fp8_f32(a[4 * i + 2], (int)r[4 * i + 2], w[i], 2);
+            w[i] = __builtin_amdgcn_cvt_sr_fp8_f32(a[4 * i + 3], (int)r[4 * i + 3], w[i], 3);
+        } else {
+            w[i] = __builtin_amdgcn_cvt_sr_bf8_f32(a[4 * i], (int)r[4 * i], w[i], 0);
+            w[i] = __builtin_amdgcn_cvt_sr_bf8_f32(a[4 * i + 1], (int)r[4 * i + 1], w[i], 1);
+            w[i] = __builtin_amdgcn_cvt_sr_bf8_f32(a[4 * i + 2], (int)r[4 * i + 2], w[i], 2);
+            w[i] = __builtin_amdgcn_cvt_sr_bf8_f32(a[4 * i + 3], (int)r[4 * i + 3], w[i], 3);
+        }
+    }
+    codes.x = finite ? (uint32_t)w[0] : 0x7f7f7f7fu;
+    codes.y = finite ? (uint32_t)w[1] : 0x7f7f7f7fu;
+}
+// x rounded to a value of fp16, up where the bits that are cut and 13 random ones carry: below the smallest binade 2^-14 is added for the time being, so that the same
+// bits are cut everywhere.  Not-a-number stays one.
+__device__ __forceinline__ float cut_half(float x, uint32_t r) {
+    const float a = fabsf(x), base = a < 0x1p-14f ? 0x1p-14f : 0.f;
+    const uint32_t bits = min(__builtin_bit_cast(uint32_t, a + base) + r, 0x7fffe000u) & 0xffffe000u;
+    return copysignf(__builtin_bit_cast(float, bits) - base, x);
 }
 
 struct Now {      // what the step's number makes
@@ -183,8 +184,9 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Tensors t, Adamw a) {
         for (int e = 0; e < 8; ++e) {
             moments(a, factor * grad[e], m[e], v[e]);
             const float x = weight[e];
-            w[e] = fmaf(-decay, x, x) - now.size * (m[e] / (sqrtf(v[e]) + now.eps));
-            if (e >= left) m[e] = v[e] = 0.f;      // (no part of a block's largest)
+            // (8-bit states: issue bounds the kernel, and the hardware's root and reciprocal are good to a unit of fp32's last place; a root below 2^-63 would be 0)
+            const float up = STATE8 ? m[e] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(fmaxf(v[e], 0x1p-126f)) + now.eps) : m[e] / (sqrtf(v[e]) + now.eps);
+            w[e] = fmaf(-now.size, up, fmaf(-decay, x, x));
         }
         uint32_t r[8] = {};
         if (dice) {
@@ -194,12 +196,29 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Tensors t, Adamw a) {
             for (int e = 0; e < 8; ++e) r[e] = stir(base + e);
         }
         if (STATE8) {
-            Codes cm, cv;
-            uint32_t bm, bv, dm[8], dv[8];
+            if (left < 8) {      // what does not exist is no part of a block's largest
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dm[e] = r[e] >> 16, dv[e] = r[e] & 0xffffu;
-            encode<true>(m, dm, cm, bm);
-            encode<false>(v, dv, cv, bv);
+                for (int e = 0; e < 8; ++e)
+                    if (e >= left) m[e] = v[e] = 0.f;
+            }
+            float most_m = 0.f;
+            uint32_t most_v = 0;      // (bits of floats >= 0 are in their order, not-a-number above infinity)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                most_m = fmaxf(most_m, fabsf(m[e]));
+                most_v = max(most_v, __builtin_bit_cast(uint32_t, v[e]));
+            }
+            most_m = __builtin_bit_cast(float, row_reduce(__builtin_bit_cast(uint32_t, most_m), Most()));
+            most_v = row_reduce(most_v, Most());
+            // (a gradient that is not finite makes v so; a first moment that was not finite before has a block of such)
+            const bool finite = most_v < 0x7f800000u && most_m < INFINITY;
+            const uint32_t bm = block_power<true>(most_m, finite), bv = block_power<false>(__builtin_bit_cast(float, most_v), finite);
+            Codes cm, cv;
+            uint32_t dv[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dv[e] = r[e] << 16;
+            encode<true>(m, r, cm, bm, finite);
+            encode<false>(v, dv, cv, bv, finite);
             cm.store((uint8_t*)rec.m + from + at, left);
             cv.store((uint8_t*)rec.v + from + at, left);
             if ((threadIdx.x & 15) == 0) {
@@ -214,7 +233,7 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Tensors t, Adamw a) {
         if (WEIGHT) {
             if (!MASTER && a.stochastic) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = (float)cut_half(w[e], r[e] * 0x5c3c9ccdu >> 19);
+                for (int e = 0; e < 8; ++e) w[e] = cut_half(w[e], r[e] * 0x5c3c9ccdu >> 19);
             }
             store<false>((__half*)rec.weight + from, at, left, w);
         }
