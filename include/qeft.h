@@ -586,8 +586,8 @@ typedef struct {
 } qeft_tensor_t;
 typedef struct {
     const void* plan;      /* device */
-    int64_t work;          /* pieces of work in it */
-    int32_t count, grad_dtype, state_bits, has_weight, has_master;
+    int64_t work;          /* pieces of work in it, of `piece` values */
+    int32_t piece, count, grad_dtype, state_bits, has_weight, has_master;
 } qeft_tensors_t;
 typedef struct {
     double lr, beta1, beta2, eps;

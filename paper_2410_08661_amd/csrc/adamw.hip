@@ -5,6 +5,7 @@
 // Bytes bound it: every value is read and written once.  A workgroup takes a piece of a tensor, a thread eight values at a time; 16 lanes have a block of an
 // 8-bit state, whose largest value they find without LDS.
 #include <math.h>
+#include <type_traits>
 #include "octets.h"
 #include "qeft_internal.h"
 #include "wave.h"
@@ -14,7 +15,7 @@ namespace {
 
 constexpr int THREADS = 256, STEP = 8 * THREADS;
 constexpr int SUM_GROUPS = 1024;     // workgroups of the norm
-static_assert(PIECE % STEP == 0 && PIECE % QEFT_STATE_BLOCK == 0, "whole blocks");
+static_assert(SMALL_PIECE % STEP == 0 && PIECE % STEP == 0 && STEP % QEFT_STATE_BLOCK == 0, "whole blocks");
 
 // 32 bits stirred: two products with odd constants between shifts (every bit of x flips every bit of the result about half the time)
 __host__ __device__ __forceinline__ uint32_t stir(uint32_t x) {
@@ -142,48 +143,83 @@ __device__ __forceinline__ void moments(const Adamw& a, float g, float& m, float
     v = a.beta2 * v + a.one_minus_beta2 * (g * g);
 }
 
+// An address that is the same in all lanes, kept in scalar registers: loads and stores add a lane's 32-bit offset by themselves.
+template <class T>
+__device__ __forceinline__ T* scalar(T* p) {
+    const uint64_t u = (uint64_t)p;
+    return (T*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
+}
+// Where a piece's arrays begin
+struct Base {
+    const char* grad;
+    char *weight, *master, *m, *v;
+    uint8_t *m_scale, *v_scale;
+};
+// Eight values of everything a step reads
+template <bool GRAD32, bool STATE8, bool MASTER>
+struct Read {
+    Raw<GRAD32> grad;
+    Raw<MASTER> weight;
+    typename std::conditional<STATE8, Codes, Raw<true>>::type m, v;
+    uint8_t m_scale, v_scale;
+    __device__ __forceinline__ void load(const Base& b, int at, int left) {
+        grad.load(b.grad, at, left);
+        weight.load(MASTER ? b.master : b.weight, at, left);
+        if constexpr (STATE8) {
+            m.load((const uint8_t*)b.m + (uint32_t)at, left);
+            v.load((const uint8_t*)b.v + (uint32_t)at, left);
+            m_scale = b.m_scale[(uint32_t)at / QEFT_STATE_BLOCK];
+            v_scale = b.v_scale[(uint32_t)at / QEFT_STATE_BLOCK];
+        } else {
+            m.load(b.m, at, left);
+            v.load(b.v, at, left);
+        }
+    }
+};
+
 template <bool GRAD32, bool STATE8, bool WEIGHT, bool MASTER>
 __global__ __launch_bounds__(THREADS) void adamw_kernel(Tensors t, Adamw a) {
     const float factor = a.factor ? *a.factor : 1.f;
     if (!(fabsf(factor) < INFINITY)) return;
     const TensorRecord& rec = t.records[t.piece_of[blockIdx.x]];
-    const int64_t from = (int64_t)((int)blockIdx.x - rec.first_piece) * PIECE;
-    const int n = (int)min((int64_t)PIECE, rec.n - from);
-    const Now now = now_of(a);
-    const float decay = now.lr * rec.decay;
+    const int64_t from = (int64_t)((int)blockIdx.x - rec.first_piece) * t.piece;
+    const int n = (int)min((int64_t)t.piece, rec.n - from);
+    constexpr int STATE = STATE8 ? 1 : 4;
+    const Base base{scalar((const char*)rec.grad + from * (GRAD32 ? 4 : 2)),  scalar((char*)rec.weight + from * 2),
+                    scalar((char*)rec.master + from * 4),                     scalar((char*)rec.m + from * STATE),
+                    scalar((char*)rec.v + from * STATE),                      scalar(rec.m_scale + from / QEFT_STATE_BLOCK),
+                    scalar(rec.v_scale + from / QEFT_STATE_BLOCK)};
     const bool dice = STATE8 || (!MASTER && a.stochastic);
     const int64_t place = rec.first_block * QEFT_STATE_BLOCK + from;
+    int at = 8 * threadIdx.x;
+    auto there = [&](int i) { return (i & -QEFT_STATE_BLOCK) < n; };      // (the 16 lanes of a block stay together)
+    if (!there(at)) return;
+    Read<GRAD32, STATE8, MASTER> in, ahead;
+    ahead.load(base, at, n - at);
+    const Now now = now_of(a);
+    const float decay = now.lr * rec.decay;
     const uint32_t step = (uint32_t)(a.step_at ? max(*a.step_at, 1) : a.step);
     const uint32_t key = stir(step + stir(a.seed_low + stir(a.seed_high)));
-    for (int at = 8 * threadIdx.x; (at & -QEFT_STATE_BLOCK) < n; at += STEP) {      // (the 16 lanes of a block stay together)
+    for (bool more = true; more; at += STEP) {
+        in = ahead;
         const int left = n - at;
-        Raw<GRAD32> grad;
-        grad.load((const char*)rec.grad + from * (GRAD32 ? 4 : 2), at, left);
-        Raw<MASTER> weight;
-        if (MASTER) weight.load(rec.master + from, at, left);
-        else weight.load((const char*)rec.weight + from * 2, at, left);
+        more = there(at + STEP);
+        if (more) ahead.load(base, at + STEP, left - STEP);
         float m[8], v[8], w[8];
-        const int64_t block = (from + at) / QEFT_STATE_BLOCK;
-        if (STATE8) {
-            Codes cm, cv;
-            cm.load((const uint8_t*)rec.m + from + at, left);
-            cv.load((const uint8_t*)rec.v + from + at, left);
-            const float pm = power_of(rec.m_scale[block]), pv = power_of(rec.v_scale[block]);
-            cm.values<true>(m);
-            cv.values<false>(v);
+        if constexpr (STATE8) {
+            const float pm = power_of(in.m_scale), pv = power_of(in.v_scale);
+            in.m.template values<true>(m);
+            in.v.template values<false>(v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) m[e] *= pm, v[e] *= pv;
         } else {
-            Raw<true> rm, rv;
-            rm.load((const float*)rec.m + from, at, left);
-            rv.load((const float*)rec.v + from, at, left);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m[e] = rm[e], v[e] = rv[e];
+            for (int e = 0; e < 8; ++e) m[e] = in.m[e], v[e] = in.v[e];
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            moments(a, factor * grad[e], m[e], v[e]);
-            const float x = weight[e];
+            moments(a, factor * in.grad[e], m[e], v[e]);
+            const float x = in.weight[e];
             // (8-bit states: issue bounds the kernel, and the hardware's root and reciprocal are good to a unit of fp32's last place; a root below 2^-63 would be 0)
             const float up = STATE8 ? m[e] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(fmaxf(v[e], 0x1p-126f)) + now.eps) : m[e] / (sqrtf(v[e]) + now.eps);
             w[e] = fmaf(-now.size, up, fmaf(-decay, x, x));
@@ -191,11 +227,11 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Tensors t, Adamw a) {
         uint32_t r[8] = {};
         if (dice) {
             const int64_t first = place + at;
-            const uint32_t base = (uint32_t)first + stir((uint32_t)(first >> 32) + key);
+            const uint32_t base_r = (uint32_t)first + stir((uint32_t)(first >> 32) + key);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) r[e] = stir(base + e);
+            for (int e = 0; e < 8; ++e) r[e] = stir(base_r + e);
         }
-        if (STATE8) {
+        if constexpr (STATE8) {
             if (left < 8) {      // what does not exist is no part of a block's largest
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -219,23 +255,23 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Tensors t, Adamw a) {
             for (int e = 0; e < 8; ++e) dv[e] = r[e] << 16;
             encode<true>(m, r, cm, bm, finite);
             encode<false>(v, dv, cv, bv, finite);
-            cm.store((uint8_t*)rec.m + from + at, left);
-            cv.store((uint8_t*)rec.v + from + at, left);
+            cm.store((uint8_t*)base.m + (uint32_t)at, left);
+            cv.store((uint8_t*)base.v + (uint32_t)at, left);
             if ((threadIdx.x & 15) == 0) {
-                rec.m_scale[block] = (uint8_t)bm;
-                rec.v_scale[block] = (uint8_t)bv;
+                base.m_scale[(uint32_t)at / QEFT_STATE_BLOCK] = (uint8_t)bm;
+                base.v_scale[(uint32_t)at / QEFT_STATE_BLOCK] = (uint8_t)bv;
             }
         } else {
-            store<true>((float*)rec.m + from, at, left, m);
-            store<true>((float*)rec.v + from, at, left, v);
+            store<true>(base.m, at, left, m);
+            store<true>(base.v, at, left, v);
         }
-        if (MASTER) store<true>(rec.master + from, at, left, w);
+        if (MASTER) store<true>(base.master, at, left, w);
         if (WEIGHT) {
             if (!MASTER && a.stochastic) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[e] = cut_half(w[e], r[e] * 0x5c3c9ccdu >> 19);
             }
-            store<false>((__half*)rec.weight + from, at, left, w);
+            store<false>(base.weight, at, left, w);
         }
     }
 }
@@ -247,8 +283,8 @@ __global__ __launch_bounds__(THREADS) void square_sums_kernel(Tensors t, double*
     double s = 0.;
     for (int p = blockIdx.x; p < t.work; p += gridDim.x) {
         const TensorRecord& rec = t.records[t.piece_of[p]];
-        const int64_t from = (int64_t)(p - rec.first_piece) * PIECE;
-        const int n = (int)min((int64_t)PIECE, rec.n - from);
+        const int64_t from = (int64_t)(p - rec.first_piece) * t.piece;
+        const int n = (int)min((int64_t)t.piece, rec.n - from);
         for (int at = 8 * threadIdx.x; at < n; at += STEP) {
             Raw<GRAD32> g;
             g.load((const char*)rec.grad + from * (GRAD32 ? 4 : 2), at, n - at);
@@ -269,7 +305,7 @@ __global__ __launch_bounds__(SUM_GROUPS) void norm_finish_kernel(const double* p
     __syncthreads();
     if (threadIdx.x != 0) return;
     s = 0.;
-    for (int i = 0; i < SUM_GROUPS / 64; ++i) s += slots[i];
+    for (int i = 0; i < (int)blockDim.x / 64; ++i) s += slots[i];
     const double norm = (double)scale * sqrt(s);
     out[0] = (float)norm;
     const bool finite = fabsf((float)norm) < INFINITY;
@@ -306,7 +342,7 @@ hipError_t grad_norm(const Tensors& t, float scale, float max_norm, float* out, 
         if (t.grad_f32) square_sums_kernel<true><<<(unsigned)parts, THREADS, 0, s>>>(t, (double*)ws);
         else square_sums_kernel<false><<<(unsigned)parts, THREADS, 0, s>>>(t, (double*)ws);
     }
-    norm_finish_kernel<<<1, SUM_GROUPS, 0, s>>>((const double*)ws, parts, scale, max_norm, out, steps);
+    norm_finish_kernel<<<1, parts <= 64 ? 64 : parts <= 256 ? 256 : SUM_GROUPS, 0, s>>>((const double*)ws, parts, scale, max_norm, out, steps);
     return hipGetLastError();
 }
 
