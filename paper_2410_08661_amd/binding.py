@@ -273,7 +273,8 @@ class Weight:
 
 _MARSHALLED = ("qeft_linear_fwd", "qeft_linear_fwd_group", "qeft_linear_bwd_dx", "qeft_linear_bwd", "qeft_linear_fwd_irregular",
                "qeft_linear_bwd_dx_irregular", "qeft_weak_grad", "qeft_cache_append", "qeft_attn_decode", "qeft_cache_evict", "qeft_norm_fwd",
-               "qeft_norm_bwd", "qeft_logprob_fwd", "qeft_logprob_bwd", "qeft_logprob_fwd_bwd", "qeft_qk_norm_fwd", "qeft_qk_norm_bwd", "qeft_cache_append_norm")
+               "qeft_norm_bwd", "qeft_logprob_fwd", "qeft_logprob_bwd", "qeft_logprob_fwd_bwd", "qeft_qk_norm_fwd", "qeft_qk_norm_bwd", "qeft_cache_append_norm", "qeft_adamw_step",
+               "qeft_grad_norm")
 
 
 def _load_marshal():
@@ -282,7 +283,7 @@ def _load_marshal():
     except ImportError:   # not built, or not for this torch: every call is ctypes'
         return types.SimpleNamespace(**{n.removeprefix("qeft_"): lambda *args: None for n in _MARSHALLED})
     m.init(tuple(C.cast(getattr(raw, n), C.c_void_p).value for n in _MARSHALLED), qeft_desc_t, Weight, qeft_cache_desc_t, qeft_norm_desc_t,
-           qeft_logprob_desc_t, qeft_qk_desc_t)
+           qeft_logprob_desc_t, qeft_qk_desc_t, qeft_tensors_t)
     return m
 
 
@@ -1018,6 +1019,7 @@ class TensorList:
             _fail(QEFT_ERR_UNSUPPORTED, at, f"gradients of {grad}, states of {state}")
         types = dict(weight=torch.float16, master=torch.float32, grad=grad, m=state, v=state, m_scale=torch.uint8, v_scale=torch.uint8)
         self.device = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        self.index = -1 if self.device.index is None else self.device.index
         if len(decays) != n or any(ts is not None and len(ts) != n for ts in self.tensors.values()):
             _fail(QEFT_ERR_SHAPE, at, "lists of different lengths")
         rows = (qeft_tensor_t * max(n, 1))()
@@ -1042,7 +1044,7 @@ class TensorList:
         self.c.plan = self.plan.data_ptr()
 
     def here(self, at):
-        if self.device.index != torch.cuda.current_device():
+        if self.index != torch.cuda.current_device():
             _fail(QEFT_ERR_UNSUPPORTED, at, "the list's tensors are not on the current GPU")
         return C.byref(self.c)
 
@@ -1063,11 +1065,14 @@ def qeft_adamw_step(tensors: TensorList, lr: float | torch.Tensor, step: int | t
     """One step of AdamW over the list, in place.  lr and step (1 for the first) are numbers, or tensors on the GPU (fp32, int32) that hold one; factor: fp32 on the
     GPU, multiplies the gradients, and the step is left out where it is not finite.  stochastic: fp16 weights without a master are rounded so, as 8-bit states always are, by
     seed, step and place."""
-    at = "qeft_adamw_step"
-    lr_at, step_at = (_number_at(at, name, t, kind) if isinstance(t, torch.Tensor) else 0 for name, t, kind in (("lr", lr, torch.float32), ("step", step, torch.int32)))
-    a = qeft_adamw_t(0.0 if lr_at else lr, beta1, beta2, eps, 0 if step_at else step, seed & 0xFFFFFFFFFFFFFFFF, lr_at, step_at,
-                     _number_at(at, "factor", factor, torch.float32), int(bool(stochastic)))
-    _check(raw.qeft_adamw_step(tensors.here(at), C.byref(a), _stream()), at)
+    st = _native.adamw_step(tensors.c, tensors.index, lr, step, beta1, beta2, eps, factor, stochastic, seed)
+    if st is None:
+        at = "qeft_adamw_step"
+        lr_at, step_at = (_number_at(at, name, t, kind) if isinstance(t, torch.Tensor) else 0 for name, t, kind in (("lr", lr, torch.float32), ("step", step, torch.int32)))
+        a = qeft_adamw_t(0.0 if lr_at else lr, beta1, beta2, eps, 0 if step_at else step, seed & 0xFFFFFFFFFFFFFFFF, lr_at, step_at,
+                         _number_at(at, "factor", factor, torch.float32), int(bool(stochastic)))
+        st = raw.qeft_adamw_step(tensors.here(at), C.byref(a), _stream())
+    _check(st, "qeft_adamw_step")
 
 
 def qeft_grad_norm_workspace(tensors: TensorList) -> int:
@@ -1078,14 +1083,17 @@ def qeft_grad_norm(tensors: TensorList, max_norm=float("inf"), scale=1.0, out: t
                    ws: torch.Tensor | None = None) -> torch.Tensor:
     """fp32 [2]: the norm of all gradients times scale, and the factor that brings them back by scale and to a norm of max_norm at most (not-a-number where the norm is
     not finite).  steps: int32 on the GPU, counted up by one where it is finite."""
-    at = "qeft_grad_norm"
     if out is None:
         out = torch.empty(2, dtype=torch.float32, device=tensors.device)
     if ws is None:
         n = qeft_grad_norm_workspace(tensors)
         ws = torch.empty(n, dtype=torch.uint8, device=tensors.device) if n else None
-    po, ps = _take(at, "out", out, torch.float32, (2,))[0], _number_at(at, "steps", steps, torch.int32)
-    pw, nw = _c_workspace(at, ws)
-    a = qeft_grad_norm_t(float(scale), float(max_norm), po, ps, pw, nw)
-    _check(raw.qeft_grad_norm(tensors.here(at), C.byref(a), _stream()), at)
+    st = _native.grad_norm(tensors.c, tensors.index, max_norm, scale, out, steps, ws)
+    if st is None:
+        at = "qeft_grad_norm"
+        po, ps = _take(at, "out", out, torch.float32, (2,))[0], _number_at(at, "steps", steps, torch.int32)
+        pw, nw = _c_workspace(at, ws)
+        a = qeft_grad_norm_t(float(scale), float(max_norm), po, ps, pw, nw)
+        st = raw.qeft_grad_norm(tensors.here(at), C.byref(a), _stream())
+    _check(st, "qeft_grad_norm")
     return out

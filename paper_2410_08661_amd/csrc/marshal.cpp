@@ -37,9 +37,11 @@ struct Fns {
     decltype(&qeft_qk_norm_fwd) qk_norm_fwd;
     decltype(&qeft_qk_norm_bwd) qk_norm_bwd;
     decltype(&qeft_cache_append_norm) cache_append_norm;
+    decltype(&qeft_adamw_step) adamw_step;
+    decltype(&qeft_grad_norm) grad_norm;
 } fns;
 constexpr int N_FNS = sizeof(Fns) / sizeof(void*);
-PyTypeObject *desc_type, *weight_type, *cache_desc_type, *norm_desc_type, *logprob_desc_type, *qk_desc_type;
+PyTypeObject *desc_type, *weight_type, *cache_desc_type, *norm_desc_type, *logprob_desc_type, *qk_desc_type, *tensors_type;
 PyObject *n_desc, *n_qweight, *n_scales, *n_zeros, *n_weak;
 
 // the bytes of a ctypes object (which owns them for its lifetime)
@@ -668,11 +670,64 @@ PyObject* qk_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t argc) {
         return true;
     });
 }
-// (addresses of the C functions in the order of Fns, qeft_desc_t, Weight, qeft_cache_desc_t, qeft_norm_desc_t, qeft_logprob_desc_t, qeft_qk_desc_t)
+// A list's struct and the GPU that it is on
+const qeft_tensors_t* list_of(Call& c, PyObject* list, PyObject* device) {
+    c.device = c.number(device);
+    return c.described<qeft_tensors_t>(list, tensors_type);
+}
+// a number on the GPU: the first entry of a tensor
+const void* number_at(Call& c, PyObject* o, at::ScalarType type) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor* t = c.tensor(o);
+    if (!t || t->scalar_type() != type || t->numel() < 1) return c.no();
+    return t->data_ptr();
+}
+// (list, device, lr, step, beta1, beta2, eps, factor, stochastic, seed)
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t argc) {
+    return guarded([&](Call& c, int& st) {
+        if (argc != 10) return false;
+        const qeft_tensors_t* l = list_of(c, a[0], a[1]);
+        if (!l || !c.ok) return false;
+        qeft_adamw_t p{};
+        if (THPVariable_CheckExact(a[2])) p.lr_at = (const float*)number_at(c, a[2], at::kFloat);
+        else p.lr = c.real(a[2]);
+        if (THPVariable_CheckExact(a[3])) p.step_at = (const int32_t*)number_at(c, a[3], at::kInt);
+        else p.step = c.whole(a[3]);
+        p.beta1 = c.real(a[4]);
+        p.beta2 = c.real(a[5]);
+        p.eps = c.real(a[6]);
+        p.factor = (const float*)number_at(c, a[7], at::kFloat);
+        p.stochastic = PyObject_IsTrue(a[8]) == 1;
+        p.seed = (uint64_t)c.whole(a[9]);      // (larger ones are ctypes')
+        void* s = c.stream();
+        if (!c.ok) return false;
+        st = unlocked([&] { return fns.adamw_step(l, &p, s); });
+        return true;
+    });
+}
+// (list, device, max_norm, scale, out, steps, ws)
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t argc) {
+    return guarded([&](Call& c, int& st) {
+        if (argc != 7) return false;
+        const qeft_tensors_t* l = list_of(c, a[0], a[1]);
+        if (!l || !c.ok) return false;
+        qeft_grad_norm_t p{};
+        p.max_norm = (float)c.real(a[2]);
+        p.scale = (float)c.real(a[3]);
+        p.out = (float*)c.vec(a[4], at::kFloat, 2);
+        p.steps = (int32_t*)number_at(c, a[5], at::kInt);
+        p.ws = c.bytes(a[6], p.ws_bytes);
+        void* s = c.stream();
+        if (!c.ok) return false;
+        st = unlocked([&] { return fns.grad_norm(l, &p, s); });
+        return true;
+    });
+}
+// (addresses of the C functions in the order of Fns, qeft_desc_t, Weight, qeft_cache_desc_t, qeft_norm_desc_t, qeft_logprob_desc_t, qeft_qk_desc_t, qeft_tensors_t)
 PyObject* init(PyObject*, PyObject* args) {
-    PyObject *f, *d, *w, *cd, *nd, *ld, *qd;
-    if (!PyArg_ParseTuple(args, "O!O!O!O!O!O!O!", &PyTuple_Type, &f, &PyType_Type, &d, &PyType_Type, &w, &PyType_Type, &cd, &PyType_Type, &nd, &PyType_Type, &ld,
-                          &PyType_Type, &qd))
+    PyObject *f, *d, *w, *cd, *nd, *ld, *qd, *td;
+    if (!PyArg_ParseTuple(args, "O!O!O!O!O!O!O!O!", &PyTuple_Type, &f, &PyType_Type, &d, &PyType_Type, &w, &PyType_Type, &cd, &PyType_Type, &nd, &PyType_Type, &ld,
+                          &PyType_Type, &qd, &PyType_Type, &td))
         return nullptr;
     if (PyTuple_GET_SIZE(f) != N_FNS) return PyErr_Format(PyExc_ValueError, "%d functions expected", N_FNS);
     void* at[N_FNS];
@@ -681,13 +736,14 @@ PyObject* init(PyObject*, PyObject* args) {
         if (PyErr_Occurred()) return nullptr;
     }
     memcpy(&fns, at, sizeof fns);
-    for (PyObject* o : {d, w, cd, nd, ld, qd}) Py_INCREF(o);
+    for (PyObject* o : {d, w, cd, nd, ld, qd, td}) Py_INCREF(o);
     desc_type = (PyTypeObject*)d;
     weight_type = (PyTypeObject*)w;
     cache_desc_type = (PyTypeObject*)cd;
     norm_desc_type = (PyTypeObject*)nd;
     logprob_desc_type = (PyTypeObject*)ld;
     qk_desc_type = (PyTypeObject*)qd;
+    tensors_type = (PyTypeObject*)td;
     Py_RETURN_NONE;
 }
 
@@ -711,6 +767,8 @@ PyMethodDef methods[] = {
     {"qk_norm_fwd", (PyCFunction)(void (*)())qk_norm_fwd, METH_FASTCALL, nullptr},
     {"qk_norm_bwd", (PyCFunction)(void (*)())qk_norm_bwd, METH_FASTCALL, nullptr},
     {"cache_append_norm", (PyCFunction)(void (*)())cache_append_norm, METH_FASTCALL, nullptr},
+    {"adamw_step", (PyCFunction)(void (*)())adamw_step, METH_FASTCALL, nullptr},
+    {"grad_norm", (PyCFunction)(void (*)())grad_norm, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

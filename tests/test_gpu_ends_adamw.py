@@ -292,3 +292,41 @@ def test_offsets_beyond_32_bits():
     norm = B.qeft_grad_norm(B.TensorList([g]))
     want = float(before["grads"][0].double().norm())
     assert abs(float(norm[0]) - want) <= 2 * V.U * want
+
+
+def test_calls_without_the_native_module(monkeypatch):
+    for number, seed in ((lambda x, t: x, 5), (lambda x, t: torch.tensor([x], dtype=t, device="cuda"), 2 ** 64 - 1)):
+        results = []
+        for native in (True, False):
+            p = tensors(SIZES, True, 8, master=False)
+            plan = B.TensorList(decay=0.1, **p)
+            steps = torch.zeros(1, dtype=torch.int32, device="cuda")
+            with monkeypatch.context() as mp:
+                if not native:
+                    mp.setattr(B, "_native", V.NONE)
+                norm = B.qeft_grad_norm(plan, max_norm=0.01, scale=0.5, steps=steps)
+                B.qeft_adamw_step(plan, number(1e-3, torch.float32), number(4, torch.int32), 0.8, 0.99, 1e-7, factor=norm[1:], stochastic=True, seed=seed)
+            results.append([norm, steps, *(t for ts in p.values() for t in ts)])
+        for a, b in zip(*results):
+            assert torch.equal(a, b)
+
+
+def test_arguments_that_are_refused():
+    p = tensors([100, 5])
+    plan = B.TensorList(**p)
+    one = torch.ones(1, device="cuda")
+    for kw in (dict(lr=0.1, step=0), dict(lr=float("nan"), step=1), dict(lr=0.1, step=one), dict(lr=one.half(), step=1), dict(lr=0.1, step=1, factor=one.double()),
+               dict(lr=0.1, step=1, factor=one.cpu()), dict(lr=0.1, step=1, factor=one[:0]), dict(lr=0.1, step=1, beta1=1.0), dict(lr=0.1, step=1, eps=0.0)):
+        before = held(p)
+        with pytest.raises(B.QeftError):
+            B.qeft_adamw_step(plan, **kw)
+        assert all(torch.equal(a, b) for k in p for a, b in zip(p[k], before[k]))
+    for kw in (dict(max_norm=0.0), dict(scale=0.0), dict(out=one), dict(steps=one), dict(ws=torch.empty(0, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(B.QeftError):
+            B.qeft_grad_norm(plan, **kw)
+    for change in (dict(weights=[w.float() for w in p["weights"]]), dict(m=[t[:3] for t in p["m"]]), dict(v=p["m"]), dict(grads=[t.repeat(2)[::2] for t in p["grads"]]),
+                   dict(weights=None, masters=None), dict(m_scales=p["m"]), dict(masters=[p["masters"][0], p["masters"][0][:5]])):
+        with pytest.raises(B.QeftError):
+            B.TensorList(**{**p, **change})
+    with pytest.raises(B.QeftError):
+        B.qeft_adamw_step(B.TensorList(p["grads"]), 0.1, 1)
