@@ -153,14 +153,16 @@ __device__ __forceinline__ void top_by_rounds(int top, uint64_t* slots, const Ea
         if (threadIdx.x == 0) put(i, best);
     }
 }
-// The largest `top` of the `count` keys in a list: each key's place is the number of larger ones.
+// The largest `top` of the `count` keys in a list of CANDIDATES, 0 behind them: each key's place is the number of larger ones.
 template <class Put>
 __device__ __forceinline__ void top_of_list(int top, const uint64_t* list, int count, const Put& put) {
     for (int i = threadIdx.x; i < count; i += blockDim.x) {
         const uint64_t mine = list[i];
         int place = 0;
-#pragma unroll 8
-        for (int j = 0; j < count; ++j) place += list[j] > mine;
+#pragma unroll 1
+        for (int j = 0; j < count; j += 8)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) place += list[j + e] > mine;
         if (place < top) put(place, mine);
     }
     for (int i = count + threadIdx.x; i < top; i += blockDim.x) put(i, 0);
@@ -170,6 +172,9 @@ __device__ __forceinline__ void top_of_list(int top, const uint64_t* list, int c
 template <int V, bool F32, bool GRAD>
 __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     __shared__ float buf[3][16];
+    __shared__ uint32_t maxima[GRAD ? 1 : 256];
+    __shared__ uint64_t list[GRAD ? 1 : CANDIDATES], slots[16];
+    __shared__ int used;
     const int64_t row = p.parts == 1 ? blockIdx.x : blockIdx.x / p.parts;
     const int part = p.parts == 1 ? 0 : (int)(blockIdx.x - row * p.parts), from = part * p.len, n = min(p.len, a.n - from), T = blockDim.x;
     const char* row_at = row_of(a.z, row, a.ldz, F32);
@@ -210,6 +215,22 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
         for (int i = 0; i < V; ++i) v[i].hold();
     };
     pin();
+    uint32_t rank = 0;
+    if constexpr (!GRAD) {      // for the alternatives, see there: shared with the statistics' barrier
+        if (a.top > 0) {
+            rank = rank_of(mine);
+            uint32_t group = rank;
+            const int side = T > 256 ? 4 : 1;      // threads of a group: neighbours
+            if (side == 4) {
+                group = max(group, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)group, 0xb1, 0xf, 0xf, false));      // quad_perm 1 0 3 2
+                group = max(group, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)group, 0x4e, 0xf, 0xf, false));      // quad_perm 2 3 0 1
+            }
+            if (threadIdx.x % side == 0) maxima[threadIdx.x / side] = group;
+            for (int i = T / side + threadIdx.x; i < 256; i += T) maxima[i] = 0;
+            for (int i = threadIdx.x; i < CANDIDATES; i += T) list[i] = 0;
+            if (threadIdx.x == 0) used = 0;
+        }
+    }
     const bool wants_t = a.entropy || p.lse || (GRAD && a.dentropy);
     {
         float s[2] = {}, t[2] = {};
@@ -230,13 +251,13 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
         x.s = wave_reduce(s[0] + s[1], Sum());
         if (wants_t) x.t = wave_reduce(t[0] + t[1], Sum());
     }
+    if (lane == 0) {
+        buf[0][wave] = x.k;
+        buf[1][wave] = x.s;
+        buf[2][wave] = x.t;
+    }
+    __syncthreads();
     if (waves > 1) {      // the waves' statistics joined, a lane per wave
-        if (lane == 0) {
-            buf[0][wave] = x.k;
-            buf[1][wave] = x.s;
-            buf[2][wave] = x.t;
-        }
-        __syncthreads();
         const int w = lane & 15;
         const bool there = w < waves;
         const Stats y{there ? buf[0][w] : LEAST, there ? buf[1][w] : 0.f, there ? buf[2][w] : 0.f};
@@ -255,24 +276,10 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
         if (a.top == 0) return;
         // Candidates: whatever reaches the top-th largest of the maxima of groups of threads (64 groups for up to 32 alternatives, 256 for more), cut to 16 bits.  Few do, so they are ordered by
         // comparing each with each.  Rows where many do (equal logits) or with not-a-number, which no maximum shows, go by rounds.
-        __shared__ uint32_t maxima[256];
-        __shared__ uint64_t list[CANDIDATES], slots[16];
-        __shared__ int used;
         auto put = [&](int i, uint64_t key) {
             if (p.parts == 1) put_top(a, row, i, key, x.k, ln_s);
             else p.keys[(size_t)blockIdx.x * a.top + i] = key;
         };
-        const uint32_t rank = rank_of(mine);
-        uint32_t group = rank;
-        const int side = T > 256 ? 4 : 1;      // threads of a group: neighbours
-        if (side == 4) {
-            group = max(group, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)group, 0xb1, 0xf, 0xf, false));      // quad_perm 1 0 3 2
-            group = max(group, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)group, 0x4e, 0xf, 0xf, false));      // quad_perm 2 3 0 1
-        }
-        if (threadIdx.x % side == 0) maxima[threadIdx.x / side] = group;
-        if (threadIdx.x == 0) used = 0;
-        for (int i = T / side + threadIdx.x; i < 256; i += T) maxima[i] = 0;
-        __syncthreads();
         uint32_t bound = 0;
         {
             uint32_t g[4];
@@ -281,8 +288,11 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
             if (a.top <= 32) {
                 const uint32_t most = max(max(g[0], g[1]), max(g[2], g[3]));
 #pragma unroll
-                for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
-                    if (__popcll(__ballot(most >= (bound | bit))) >= a.top) bound |= bit;
+                for (int bit = 30; bit >= 16; bit -= 2) {      // two bits a step
+                    auto reach = [&](uint32_t b) { return (int)__popcll(__ballot(most >= (bound | b << bit))) >= a.top; };
+                    const bool one = reach(1), two = reach(2), three = reach(3);
+                    bound |= (three ? 3u : two ? 2u : one ? 1u : 0u) << bit;
+                }
             } else {
 #pragma unroll 1
                 for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
@@ -367,6 +377,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
         for (int j = i + 4 * blockDim.x; j < total; j += blockDim.x) f(keys[j]);
     };
     if (i == 0) used = 0;
+    for (int j = i; j < CANDIDATES; j += blockDim.x) list[j] = 0;
     Stats x;
     x.k = group_reduce(y.k, buf[0], LEAST, MostFloat());
     const float d = shrink(y.k, x.k), f = __builtin_amdgcn_exp2f(d);
