@@ -48,10 +48,11 @@ struct MostFloat {
 struct Slope {
     float c, k2, a, dh, at_token;
     int token;
+    bool once;
 };
 __device__ __forceinline__ Slope make_slope(const Logprob& a, int64_t row, int token, float k2, float entropy) {
     const float dl = a.dlogp ? a.dlogp[row] : 0.f, ds = a.dlse ? a.dlse[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
-    return Slope{a.scale * LOG2E, k2, a.scale * (ds - dl - (dh != 0.f ? dh * entropy : 0.f)), a.scale * dh * LN2, a.scale * dl, a.token ? token : -1};
+    return Slope{a.scale * LOG2E, k2, a.scale * (ds - dl - (dh != 0.f ? dh * entropy : 0.f)), a.scale * dh * LN2, a.scale * dl, a.token ? token : -1, a.once != 0};
 }
 __device__ __forceinline__ float slope_of(const Slope& g, float z) {
     const float u = fmaf(z, g.c, -g.k2);
@@ -73,13 +74,13 @@ __device__ __forceinline__ void put_slopes(const Slope& g, const Raw<F32>& v, ch
         for (int e = 0; e < 8; ++e)
             if (at + e == g.token) x[e] += g.at_token;
     }
-    store<F32>(dz, at, left, x);
+    store<F32>(dz, at, left, x, g.once);
 }
 template <bool F32>
-__device__ __forceinline__ void zero_row(void* row, int n) {
+__device__ __forceinline__ void zero_row(void* row, int n, bool once) {
     for (int at = 8 * threadIdx.x; at < n; at += 8 * blockDim.x) {
         float x[8] = {};
-        store<F32>(row, at, min(8, n - at), x);
+        store<F32>(row, at, min(8, n - at), x, once);
     }
 }
 // a row without a token: no probability, no alternatives
@@ -183,7 +184,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     if (a.token && (token < 0 || token >= a.n)) {
         if (p.parts > 1) return;      // (the join leaves it out)
         left_out(a, row);
-        if (GRAD) zero_row<F32>(row_of(a.dz, row, a.lddz, F32), a.n);
+        if (GRAD) zero_row<F32>(row_of(a.dz, row, a.lddz, F32), a.n, a.once);
         return;
     }
     // Whole octets by one load each; a partial one is some thread's v[i] (the code for it once, not V times).
@@ -336,7 +337,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
         }
     } else {
         char* dz = row_of(a.dz, row, a.lddz, F32);
-        if (empty) return zero_row<F32>(dz, a.n);
+        if (empty) return zero_row<F32>(dz, a.n, a.once);
         const Slope g = make_slope(a, row, token, x.k + log2f(x.s), entropy);
         Raw<F32> x = v[0];
 #pragma unroll
@@ -411,9 +412,9 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(Logprob a, int chunks)
     const char* z = row_of(a.z, row, a.ldz, F32) + (size_t)from * (F32 ? 4 : 2);
     char* dz = row_of(a.dz, row, a.lddz, F32) + (size_t)from * (F32 ? 4 : 2);
     const int token = a.token ? a.token[row] : -1;
-    if (a.token && (token < 0 || token >= a.n)) return zero_row<F32>(dz, n);
+    if (a.token && (token < 0 || token >= a.n)) return zero_row<F32>(dz, n, a.once);
     const float lse = a.lse_in[row];
-    if (lse == -INFINITY) return zero_row<F32>(dz, n);
+    if (lse == -INFINITY) return zero_row<F32>(dz, n, a.once);
     const Slope g = make_slope(a, row, token - from, lse * LOG2E, a.entropy_in ? a.entropy_in[row] : 0.f);
     Raw<F32> v[CHUNK / 2048];
 #pragma unroll
@@ -536,13 +537,17 @@ void launch_fwd(const Logprob& a, hipStream_t s) {
 
 size_t logprob_workspace(int n, bool f32, int64_t m, int top) { return plan_of(n, f32, m, top).bytes; }
 
-hipError_t logprob_fwd(const Logprob& a, hipStream_t s) {
+hipError_t logprob_fwd(const Logprob& call, hipStream_t s) {
+    Logprob a = call;
+    a.once = a.m * a.n * (a.f32 ? 4 : 2) > CACHED_BYTES;
     if (a.f32) launch_fwd<true>(a, s);
     else launch_fwd<false>(a, s);
     return hipGetLastError();
 }
 
-hipError_t logprob_bwd(const Logprob& a, hipStream_t s) {
+hipError_t logprob_bwd(const Logprob& call, hipStream_t s) {
+    Logprob a = call;
+    a.once = a.m * a.n * (a.f32 ? 4 : 2) > CACHED_BYTES;
     if (a.f32) launch_bwd<true>(a, s);
     else launch_bwd<false>(a, s);
     return hipGetLastError();

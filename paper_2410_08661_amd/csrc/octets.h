@@ -19,16 +19,30 @@ __device__ __forceinline__ const char* row_of(const void* p, int64_t row, int64_
 }
 __device__ __forceinline__ char* row_of(void* p, int64_t row, int64_t ld, bool f32) { return const_cast<char*>(row_of((const void*)p, row, ld, f32)); }
 
+// What a call writes beyond this (the L2 caches hold 32 MB) goes past the caches: nobody finds it there again, and the writes leave the reads' lines alone.
+constexpr int64_t CACHED_BYTES = 32 << 20;
+// One load or store; `once`: of data that the caches need not keep
+template <class T>
+__device__ __forceinline__ T fetch(const char* p, bool once) { return once ? __builtin_nontemporal_load(reinterpret_cast<const T*>(p)) : *reinterpret_cast<const T*>(p); }
+template <class T>
+__device__ __forceinline__ void place(char* p, T x, bool once) {
+    if (once) {      // (between the two empty statements, or it becomes one with the other store, an ordinary one)
+        asm volatile("");
+        __builtin_nontemporal_store(x, reinterpret_cast<T*>(p));
+        asm volatile("");
+    } else *reinterpret_cast<T*>(p) = x;
+}
+
 // Eight values of a row as loaded.  left: how many of them exist (none from 0 down); a row's last octet may be partial, and is read value by value, the last one
 // first.  What does not exist is 0, or the word `none`.
 template <bool F32> struct Raw;
 template <> struct Raw<false> {
     static constexpr uint32_t NEG_INF = 0xfc00fc00u;   // (a word of values)
     u4 v;
-    __device__ __forceinline__ void load(const void* row, uint32_t at, int left, uint32_t none = 0) {
+    __device__ __forceinline__ void load(const void* row, uint32_t at, int left, uint32_t none = 0, bool once = false) {
         const char* p = (const char*)row + 2 * at;
         if (left >= 8) {
-            v = *reinterpret_cast<const u4*>(p);
+            v = fetch<u4>(p, once);
             return;
         }
         fill(none);
@@ -48,11 +62,11 @@ template <> struct Raw<false> {
 template <> struct Raw<true> {
     static constexpr uint32_t NEG_INF = 0xff800000u;
     f4 a, b;
-    __device__ __forceinline__ void load(const void* row, uint32_t at, int left, uint32_t none = 0) {
+    __device__ __forceinline__ void load(const void* row, uint32_t at, int left, uint32_t none = 0, bool once = false) {
         const char* p = (const char*)row + 4 * at;
         if (left >= 8) {
-            a = *reinterpret_cast<const f4*>(p);
-            b = *reinterpret_cast<const f4*>(p + 16);
+            a = fetch<f4>(p, once);
+            b = fetch<f4>(p + 16, once);
             return;
         }
         fill(none);
@@ -75,13 +89,13 @@ typedef Raw<false> Half8;
 
 // x goes to the row, rounded to its type (which x then is too)
 template <bool F32>
-__device__ __forceinline__ void store(void* row, uint32_t at, int left, float (&x)[8]) {
+__device__ __forceinline__ void store(void* row, uint32_t at, int left, float (&x)[8], bool once = false) {
     if (F32) {
         char* p = (char*)row + 4 * at;
         f4 a = {x[0], x[1], x[2], x[3]}, b = {x[4], x[5], x[6], x[7]};
         if (left >= 8) {
-            *reinterpret_cast<f4*>(p) = a;
-            *reinterpret_cast<f4*>(p + 16) = b;
+            place(p, a, once);
+            place(p + 16, b, once);
             return;
         }
 #pragma unroll 1
@@ -101,7 +115,7 @@ __device__ __forceinline__ void store(void* row, uint32_t at, int left, float (&
     u4 v = __builtin_bit_cast(u4, h);
     char* p = (char*)row + 2 * at;
     if (left >= 8) {
-        *reinterpret_cast<u4*>(p) = v;
+        place(p, v, once);
         return;
     }
 #pragma unroll 1
