@@ -6,6 +6,7 @@
 // Bytes bound it: a row is read once into registers, by a workgroup or, the longest, by several whose statistics a second launch joins.
 // z c - K is one multiply-add, K as it was rounded: what rounding K costs is in lse alone.  K is finite where the row is empty, so that -infinity minus it stays what it is.
 #include <math.h>
+#include <algorithm>
 #include "octets.h"
 #include "qeft_internal.h"
 #include "wave.h"
@@ -18,6 +19,10 @@ constexpr float LEAST = -3e38f;      // a finite bound of K
 constexpr float FAR = -200.f;        // 2^u is 0 from here down: u may stop here, where it is a factor beside 2^u
 
 constexpr uint32_t RANK_NEG_INF = 0x007fffffu, RANK_NAN = 0xff800001u;      // (one above +infinity's)
+// A row's address, the same in all lanes
+__host__ __device__ __forceinline__ const char* row_at(const void* p, int64_t row, int64_t ld, bool f32) { return (const char*)p + row * ld * (f32 ? 4 : 2); }
+__device__ __forceinline__ char* row_at(void* p, int64_t row, int64_t ld, bool f32) { return (char*)p + row * ld * (f32 ? 4 : 2); }
+
 // Order of alternatives: by value (-0 as +0, not-a-number highest), then lower index.  0: none.
 __device__ __forceinline__ uint32_t rank_of(float x) {
     if (x != x) return RANK_NAN;
@@ -118,8 +123,9 @@ struct Part {
 };
 constexpr int CANDIDATES = 1024;
 
-// A row's numbers from its joined statistics, by one thread
-__device__ __forceinline__ void put_row(const Logprob& a, const Part& p, int64_t row, const void* z, int token, const Stats& x, float ln_s, float entropy) {
+__device__ __forceinline__ float logit_at(const Logprob& a, const char* row, int j) { return a.f32 ? ((const float*)row)[j] : (float)((const _Float16*)row)[j]; }
+// A row's numbers from its joined statistics, by one thread; zt: the token's logit
+__device__ __forceinline__ void put_row(const Logprob& a, const Part& p, int64_t row, float zt, const Stats& x, float ln_s, float entropy) {
     const bool empty = x.s == 0.f;
     const float lse = empty ? -INFINITY : fmaf(x.k, LN2, ln_s);
     if (a.lse) a.lse[row] = lse;
@@ -128,10 +134,7 @@ __device__ __forceinline__ void put_row(const Logprob& a, const Part& p, int64_t
         p.lse[row] = lse;
         p.entropy[row] = entropy;
     }
-    if (a.logp) {
-        const float zt = a.f32 ? ((const float*)z)[token] : (float)((const _Float16*)z)[token];
-        a.logp[row] = empty ? -INFINITY : fmaf(fmaf(zt, a.scale * LOG2E, -x.k), LN2, -ln_s);
-    }
+    if (a.logp) a.logp[row] = empty ? -INFINITY : fmaf(fmaf(zt, a.scale * LOG2E, -x.k), LN2, -ln_s);
 }
 __device__ __forceinline__ void put_top(const Logprob& a, int64_t row, int i, uint64_t key, float k, float ln_s) {
     const bool there = (uint32_t)(key >> 32) > RANK_NEG_INF;
@@ -178,15 +181,17 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     __shared__ int used;
     const int64_t row = p.parts == 1 ? blockIdx.x : blockIdx.x / p.parts;
     const int part = p.parts == 1 ? 0 : (int)(blockIdx.x - row * p.parts), from = part * p.len, n = min(p.len, a.n - from), T = blockDim.x;
-    const char* row_at = row_of(a.z, row, a.ldz, F32);
-    const char* z = row_at + (size_t)from * (F32 ? 4 : 2);
+    const char* begin = row_at(a.z, row, a.ldz, F32);
+    const char* z = begin + (size_t)from * (F32 ? 4 : 2);
     const int token = a.token ? a.token[row] : -1;
     if (a.token && (token < 0 || token >= a.n)) {
         if (p.parts > 1) return;      // (the join leaves it out)
         left_out(a, row);
-        if (GRAD) zero_row<F32>(row_of(a.dz, row, a.lddz, F32), a.n, a.once);
+        if (GRAD) zero_row<F32>(row_at(a.dz, row, a.lddz, F32), a.n, a.once);
         return;
     }
+    // (before the gradient's first store, which may go to z itself)
+    const float zt = a.logp && p.parts == 1 && threadIdx.x == 0 ? logit_at(a, begin, token) : 0.f;
     // Whole octets by one load each; a partial one is some thread's v[i] (the code for it once, not V times).
     const int whole = n / 8, last = threadIdx.x == (whole & (T - 1)) && (n & 7) ? whole / T : -1;
     Raw<F32> v[V];
@@ -271,7 +276,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     const bool empty = x.s == 0.f;
     const float ln_s = logf(x.s), entropy = empty ? 0.f : ln_s - LN2 * (x.t / x.s);
     if (p.parts == 1) {
-        if (threadIdx.x == 0) put_row(a, p, row, row_at, token, x, ln_s, entropy);
+        if (threadIdx.x == 0) put_row(a, p, row, zt, x, ln_s, entropy);
     } else if (threadIdx.x == 0) p.stats[blockIdx.x] = x;
     if constexpr (!GRAD) {
         if (a.top == 0) return;
@@ -336,7 +341,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
             top_by_rounds(a.top, slots, each, put);
         }
     } else {
-        char* dz = row_of(a.dz, row, a.lddz, F32);
+        char* dz = row_at(a.dz, row, a.lddz, F32);
         if (empty) return zero_row<F32>(dz, a.n, a.once);
         const Slope g = make_slope(a, row, token, x.k + log2f(x.s), entropy);
         Raw<F32> x = v[0];
@@ -361,6 +366,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
         left_out(a, row);
         return;
     }
+    const float zt = a.logp && i == 0 ? logit_at(a, row_at(a.z, row, a.ldz, a.f32), token) : 0.f;
     const Stats y = i < p.parts ? p.stats[row * p.parts + i] : Stats{LEAST, 0.f, 0.f};
     const uint64_t* keys = p.keys + (size_t)row * p.parts * a.top;
     const int total = p.parts * a.top;
@@ -385,7 +391,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
     x.s = group_reduce(term(y.s, f), buf[1], 0.f, Sum());
     x.t = group_reduce(term(f, fmaf(d, y.s, y.t)), buf[2], 0.f, Sum());
     const float ln_s = logf(x.s), entropy = x.s == 0.f ? 0.f : ln_s - LN2 * (x.t / x.s);
-    if (i == 0) put_row(a, p, row, row_of(a.z, row, a.ldz, a.f32), token, x, ln_s, entropy);
+    if (i == 0) put_row(a, p, row, zt, x, ln_s, entropy);
     if (a.top == 0) return;
     // a part whose last key is this large has enough of them
     const uint64_t bound = max(group_reduce(last, slots, (uint64_t)0, Most()), (uint64_t)1);
@@ -409,8 +415,8 @@ template <bool F32>
 __global__ __launch_bounds__(256) void logprob_bwd_kernel(Logprob a, int chunks) {
     const int64_t row = blockIdx.x / chunks;
     const int from = (int)(blockIdx.x - row * chunks) * CHUNK, n = min(CHUNK, a.n - from);
-    const char* z = row_of(a.z, row, a.ldz, F32) + (size_t)from * (F32 ? 4 : 2);
-    char* dz = row_of(a.dz, row, a.lddz, F32) + (size_t)from * (F32 ? 4 : 2);
+    const char* z = row_at(a.z, row, a.ldz, F32) + (size_t)from * (F32 ? 4 : 2);
+    char* dz = row_at(a.dz, row, a.lddz, F32) + (size_t)from * (F32 ? 4 : 2);
     const int token = a.token ? a.token[row] : -1;
     if (a.token && (token < 0 || token >= a.n)) return zero_row<F32>(dz, n, a.once);
     const float lse = a.lse_in[row];
@@ -423,46 +429,14 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(Logprob a, int chunks)
     for (int i = 0; i < CHUNK / 2048; ++i) put_slopes(g, v[i], dz, 8 * threadIdx.x + 2048 * i, n - (int)(8 * threadIdx.x + 2048 * i));
 }
 
-// ---- rows longer than registers, too many for parts: read again for the maximum, the sums and each alternative ------------
-template <bool F32>
-__global__ __launch_bounds__(1024) void logprob_long_kernel(Logprob a, Part p) {
-    __shared__ float buf[3][16];
-    __shared__ uint64_t slots[16];
-    const int64_t row = blockIdx.x;
-    const char* z = row_of(a.z, row, a.ldz, F32);
-    const int token = a.token ? a.token[row] : -1;
-    if (a.token && (token < 0 || token >= a.n)) return left_out(a, row);
-    auto each = [&](auto&& f) {
-        for (int at = 8 * threadIdx.x; at < a.n; at += 8192) {
-            Raw<F32> v;
-            v.load(z, at, a.n - at, Raw<F32>::NEG_INF);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f(v[e], at + e);
-        }
-    };
-    const float c = a.scale * LOG2E;
-    float most = -INFINITY;
-    each([&](float x, int) { most = fmaxf(most, x); });
-    Stats x{fmaxf(group_reduce(most, buf[0], -INFINITY, MostFloat()) * c, LEAST), 0.f, 0.f};
-    each([&](float y, int) {
-        const float u = fmaf(y, c, -x.k), w = __builtin_amdgcn_exp2f(u);
-        x.s += w;
-        x.t = fmaf(w, fmaxf(u, FAR), x.t);
-    });
-    x.s = group_reduce(x.s, buf[1], 0.f, Sum());
-    x.t = group_reduce(x.t, buf[2], 0.f, Sum());
-    const float ln_s = logf(x.s);
-    if (threadIdx.x == 0) put_row(a, p, row, z, token, x, ln_s, x.s == 0.f ? 0.f : ln_s - LN2 * (x.t / x.s));
-    top_by_rounds(a.top, slots, [&](auto&& f) { each([&](float y, int j) { f((uint64_t)rank_of(y) << 32 | (uint32_t)~j); }); },
-                  [&](int i, uint64_t key) { put_top(a, row, i, key, x.k, ln_s); });
-}
-
 // ---- what goes where ----------------------------------------------------------------------------------------------------
 struct Plan {
     int threads, octets;     // of a workgroup, a thread
-    int parts, len;          // parts of a row (0: the kernel for long rows)
-    size_t stats_at, keys_at, lse_at, bytes;
+    int parts, len;          // parts of a row
+    int64_t rows;            // that the workspace holds the parts of
+    size_t keys_at, lse_at, bytes;
 };
+constexpr size_t PARTS_BYTES = 64 << 20;      // of a workspace at most: more rows go in rounds
 Plan plan_of(int n, bool f32, int64_t m, int top) {
     const int most = f32 ? 8 : 16;      // octets that a thread of 1024 holds beside its work: 64 registers
     Plan p{};
@@ -482,10 +456,10 @@ Plan plan_of(int n, bool f32, int64_t m, int top) {
     p.len = parts > 1 ? 8 * threads * v : n;
     if (parts == 1) return p;
     p.parts = parts = ceil_div(n, p.len);
-    p.stats_at = 0;
-    p.keys_at = (size_t)m * parts * sizeof(Stats) + 15 & ~(size_t)15;
-    p.lse_at = p.keys_at + (size_t)m * parts * top * sizeof(uint64_t);
-    if (p.lse_at > (size_t)64 << 20) p.parts = 0, p.lse_at = 0;
+    const size_t row = (size_t)parts * (sizeof(Stats) + top * sizeof(uint64_t));
+    p.rows = std::min(m, (int64_t)(PARTS_BYTES / row));
+    p.keys_at = (size_t)p.rows * parts * sizeof(Stats) + 15 & ~(size_t)15;
+    p.lse_at = p.keys_at + (size_t)p.rows * parts * top * sizeof(uint64_t);
     p.bytes = p.lse_at + (size_t)m * 2 * sizeof(float);
     return p;
 }
@@ -516,20 +490,27 @@ void launch_fwd(const Logprob& a, hipStream_t s) {
         else launch_rows<F32, false>(q, a, p, s);
         return;
     }
-    p.stats = (Stats*)(a.ws + q.stats_at);
+    p.stats = (Stats*)a.ws;
     p.keys = (uint64_t*)(a.ws + q.keys_at);
-    if (a.dz) {
-        p.lse = (float*)(a.ws + q.lse_at);
-        p.entropy = p.lse + a.m;
+    float* const lse = a.dz ? (float*)(a.ws + q.lse_at) : nullptr;
+    for (int64_t from = 0; from < a.m; from += q.rows) {
+        Logprob b = a;
+        b.m = std::min(q.rows, a.m - from);
+        b.z = row_at(a.z, from, a.ldz, F32);
+        auto later = [&](auto*& at, int64_t by) {
+            if (at) at += by;
+        };
+        later(b.token, from), later(b.logp, from), later(b.lse, from), later(b.entropy, from);
+        later(b.top_logp, from * a.ld_top), later(b.top_index, from * a.ld_top);
+        p.lse = lse ? lse + from : nullptr;
+        p.entropy = lse ? lse + a.m + from : nullptr;
+        launch_rows<F32, false>(q, b, p, s);
+        logprob_join_kernel<<<(unsigned)b.m, q.parts <= 64 ? 64 : 256, 0, s>>>(b, p);
     }
-    if (q.parts > 1) {
-        launch_rows<F32, false>(q, a, p, s);
-        logprob_join_kernel<<<(unsigned)a.m, q.parts <= 64 ? 64 : 256, 0, s>>>(a, p);
-    } else logprob_long_kernel<F32><<<(unsigned)a.m, 1024, 0, s>>>(a, p);
     if (!a.dz) return;
     Logprob b = a;
-    b.lse_in = p.lse;
-    b.entropy_in = p.entropy;
+    b.lse_in = lse;
+    b.entropy_in = lse + a.m;
     launch_bwd<F32>(b, s);
 }
 

@@ -127,6 +127,10 @@ def test_gradient(m, n, f32):
         same.copy_(z)
         out = B.qeft_logprob_fwd_bwd(desc, same, token, *g, dz=same, logp=False, lse=False, entropy=False)
         assert out[0] is same and out[1] is out[2] is out[3] is None and torch.equal(same, dz)
+        # (the token's logit is read before the row is overwritten)
+        same.copy_(z)
+        out = B.qeft_logprob_fwd_bwd(desc, same, token, *g, dz=same)
+        assert torch.equal(same, dz) and torch.equal(out[2], lse2) and torch.equal(out[3], entropy2) and (logp2 is None or torch.equal(out[1], logp2))
 
 
 def test_gradient_against_differences():
@@ -232,3 +236,42 @@ def test_rows_beyond_32_bit_offsets():
     assert not bool(dz[m - 6].any())
     B.qeft_logprob_fwd_bwd(desc, z, token, g, dz=dz)
     V.close("dz", dz[m - 5:], dwant, bound, V.HALF)
+
+
+def test_rows_in_parts_that_go_in_rounds():
+    """More rows than the workspace holds the parts of: 64 MB, a row of two parts with 64 alternatives takes 1048 bytes."""
+    m, n, top = 64200, 131080, 64
+    desc = B.make_logprob_desc(n)
+    assert B.qeft_logprob_workspace(desc, m, top) < 65 << 20
+    z = torch.zeros((m, n), dtype=torch.float16, device="cuda")
+    border = (64 << 20) // 1048
+    rows = [0, 1, border - 1, border, border + 1, m - 1]
+    some = V.logits(len(rows), n, False, gen_of(8), pad=0)
+    token = torch.full((m,), -1, dtype=torch.int32, device="cuda")
+    for i, r in enumerate(rows):
+        z[r], token[r] = some[i], 1000 * i
+    got = B.qeft_logprob_fwd(desc, z, token, top=top)
+    want, _ = V.log_probabilities(some, token[rows], 1.0)
+    V.check_values({k: t[rows] for k, t in zip(("logp", "lse", "entropy"), got)}, want)
+    assert torch.equal(got[4][rows], V.alternatives(some, None, top)) and int((got[4] >= 0).any(1).sum()) == len(rows)
+    dz = B.qeft_logprob_fwd_bwd(desc, z, token, torch.ones(m, device="cuda"), dz=z)[0]
+    want, bound = V.logit_gradient(some, token[rows], 1.0, torch.ones(len(rows), device="cuda"), None, None)
+    V.close("dz", dz[rows], want, bound, V.HALF)
+
+
+def test_two_calls_at_once():
+    """Two streams with a workspace each."""
+    z = [V.logits(m, n, False, gen_of(m)) for m, n in ((40, 140001), (3, 140001))]
+    desc = B.make_logprob_desc(140001)
+    want = [B.qeft_logprob_fwd(desc, x, top=20) for x in z]
+    ws = [torch.empty(B.qeft_logprob_workspace(desc, x.shape[0], 20), dtype=torch.uint8, device="cuda") for x in z]
+    outs = [[torch.zeros_like(t) for t in w[1:]] for w in want]
+    streams = [torch.cuda.Stream() for _ in z]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for x, o, w, s in zip(z, outs, ws, streams):
+            with torch.cuda.stream(s):
+                B.qeft_logprob_fwd(desc, x, top=20, lse=o[0], entropy=o[1], top_logp=o[2], top_index=o[3], ws=w)
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert all(torch.equal(a, b) for a, b in zip(o, w[1:]))
