@@ -157,7 +157,7 @@ struct Base {
     char *weight, *master, *m, *v;
     uint8_t *m_scale, *v_scale;
 };
-// Eight values of everything a step reads.  With 8-bit states loads and stores go past the caches (272 million weights 527 -> 499 us); with 32-bit states that
+// Eight values of everything a step reads.  With 8-bit states loads and stores but the master's go past the caches (272 million weights 527 -> 505 us); with 32-bit states that
 // would cost (174 million 1127 -> 1187).
 template <bool GRAD32, bool STATE8, bool MASTER>
 struct Read {
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Tensors t, Adamw a) {
             store<true>(base.m, at, left, m);
             store<true>(base.v, at, left, v);
         }
-        if (MASTER) store<true>(base.master, at, left, w, STATE8);
+        if (MASTER) store<true>(base.master, at, left, w);
         if (WEIGHT) {
             if (!MASTER && a.stochastic) {
 #pragma unroll

@@ -520,7 +520,7 @@ size_t logprob_workspace(int n, bool f32, int64_t m, int top) { return plan_of(n
 
 hipError_t logprob_fwd(const Logprob& call, hipStream_t s) {
     Logprob a = call;
-    a.once = a.m * a.n * (a.f32 ? 4 : 2) > CACHED_BYTES;
+    a.once = !a.f32 && a.m * a.n * 2 > CACHED_BYTES;
     if (a.f32) launch_fwd<true>(a, s);
     else launch_fwd<false>(a, s);
     return hipGetLastError();
@@ -528,7 +528,7 @@ hipError_t logprob_fwd(const Logprob& call, hipStream_t s) {
 
 hipError_t logprob_bwd(const Logprob& call, hipStream_t s) {
     Logprob a = call;
-    a.once = a.m * a.n * (a.f32 ? 4 : 2) > CACHED_BYTES;
+    a.once = !a.f32 && a.m * a.n * 2 > CACHED_BYTES;
     if (a.f32) launch_bwd<true>(a, s);
     else launch_bwd<false>(a, s);
     return hipGetLastError();

@@ -19,7 +19,8 @@ __device__ __forceinline__ const char* row_of(const void* p, int64_t row, int64_
 }
 __device__ __forceinline__ char* row_of(void* p, int64_t row, int64_t ld, bool f32) { return const_cast<char*>(row_of((const void*)p, row, ld, f32)); }
 
-// What a call writes beyond this (the L2 caches hold 32 MB) goes past the caches: nobody finds it there again, and the writes leave the reads' lines alone.
+// What a call writes beyond this (the L2 caches hold 32 MB) goes past the caches: nobody finds it there again, and the writes leave the reads'
+// lines alone.  Only where a lane writes all of an octet at once: the two halves of an fp32 one would go out as parts of lines.
 constexpr int64_t CACHED_BYTES = 32 << 20;
 // One load or store; `once`: of data that the caches need not keep
 template <class T>
