@@ -471,7 +471,7 @@ int qeft_norm_bwd(const qeft_norm_desc_t* desc, const qeft_norm_bwd_t* a, void* 
  * token int32 [m]; NULL: no logp.  A row whose token is not in 0 .. n - 1 is left out: its logp, lse and entropy are 0, it has no alternatives, and it is
  * not read.  An entry of -infinity has no probability and is no alternative; where there are fewer than `top` others, top_index is -1 and top_logp
  * -infinity.  A row of nothing else: lse and logp -infinity, entropy 0, gradient 0.  Not-a-number and +infinity make their row's lse, logp, entropy, top_logp and
- * gradient not-a-number; top_index counts not-a-number above +infinity.  Sums and exponentials are fp32.  logp, lse, entropy (fp32 [m]) and both top arrays may be
+ * gradient not-a-number; top_index counts not-a-number above +infinity.  Sums and exponentials are fp32; scale * z is taken to be below 2^120 in size.  logp, lse, entropy (fp32 [m]) and both top arrays may be
  * NULL (top = 0: both must be, and the other way round).
  * qeft_logprob_bwd: with the gradients dlogp, dlse, dentropy (fp32 [m], NULL: 0) of those three, and lse and entropy (needed with dentropy) as the forward gave them,
  *     dz_j = scale * (dlogp ([j = token] - p_j) + dlse p_j - dentropy p_j (log p_j + entropy))
