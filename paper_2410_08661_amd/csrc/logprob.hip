@@ -437,6 +437,7 @@ struct Plan {
     size_t keys_at, lse_at, bytes;
 };
 constexpr size_t PARTS_BYTES = 64 << 20;      // of a workspace at most: more rows go in rounds
+constexpr int FINER = 32768, FINER_FROM = 98304, FINER_GROUPS = 256;
 Plan plan_of(int n, bool f32, int64_t m, int top) {
     const int most = f32 ? 8 : 16;      // octets that a thread of 1024 holds beside its work: 64 registers
     Plan p{};
@@ -444,8 +445,8 @@ Plan plan_of(int n, bool f32, int64_t m, int top) {
     int parts = ceil_div(octets, fit);
     // A CU takes 9 us for 130000 values (exponentials and sums, 260 KB): where there are CUs for all of them, parts of 32768 values save more than the join's launch
     // costs.  1 x 130001 with 20 alternatives 15.7 -> 12.5 us, 57 x 130001 16.2 -> 14.4, 16 x 262144 18.7 -> 11.9; 1 x 64000 would go 9.0 -> 11.2.
-    const int finer = ceil_div(n, 32768);
-    if (n > 98304 && finer > parts && m * finer <= 256) parts = finer;
+    const int finer = ceil_div(n, FINER);
+    if (n > FINER_FROM && finer > parts && m * finer <= FINER_GROUPS) parts = finer;
     p.parts = parts;
     int per = ceil_div(octets, parts);
     const int threads = per <= 256 ? 64 : per <= 2048 ? 256 : 1024;
@@ -459,7 +460,7 @@ Plan plan_of(int n, bool f32, int64_t m, int top) {
     const size_t row = (size_t)parts * (sizeof(Stats) + top * sizeof(uint64_t));
     p.rows = std::min(m, (int64_t)(PARTS_BYTES / row));
     p.keys_at = (size_t)p.rows * parts * sizeof(Stats) + 15 & ~(size_t)15;
-    p.lse_at = p.keys_at + (size_t)p.rows * parts * top * sizeof(uint64_t);
+    p.lse_at = p.rows < m ? PARTS_BYTES + 16 : p.keys_at + (size_t)p.rows * parts * top * sizeof(uint64_t);
     p.bytes = p.lse_at + (size_t)m * 2 * sizeof(float);
     return p;
 }
@@ -516,7 +517,11 @@ void launch_fwd(const Logprob& a, hipStream_t s) {
 
 }  // namespace
 
-size_t logprob_workspace(int n, bool f32, int64_t m, int top) { return plan_of(n, f32, m, top).bytes; }
+// What m rows need, or fewer: finer parts are for few rows only, and a workspace for many has to do for them.
+size_t logprob_workspace(int n, bool f32, int64_t m, int top) {
+    const int64_t few = FINER_GROUPS / ceil_div(n, FINER);
+    return std::max(plan_of(n, f32, m, top).bytes, few > 0 && few < m ? plan_of(n, f32, few, top).bytes : 0);
+}
 
 hipError_t logprob_fwd(const Logprob& call, hipStream_t s) {
     Logprob a = call;

@@ -101,6 +101,21 @@ def test_workspaces_of_log_probabilities():
     assert B.qeft_logprob_workspace(LDESC, -1) == B.qeft_logprob_workspace(LDESC, 3, 65) == 0
 
 
+def test_a_workspace_for_more_does_for_less():
+    for n in (100, 65537, 98305, 130001, 140001, 262144, 1 << 20, 1 << 24):
+        for kind in (torch.float16, torch.float32):
+            d = B.make_logprob_desc(n, kind)
+            for top in (0, 1, 20, 64):
+                sizes = [B.qeft_logprob_workspace(d, m, top) for m in (*range(1, 300), 1000, 5000, 30000, 60000, 64000, 64100, 100000, 1 << 21)]
+                assert sizes == sorted(sizes), (n, kind, top)
+            for m in (1, 57, 300, 64100, 1 << 21):
+                sizes = [B.qeft_logprob_workspace(d, m, top) for top in range(65)]
+                assert sizes == sorted(sizes), (n, kind, m)
+    for d in (qdesc(), qdesc(head_dim=128, rot_dim=128), qdesc(head_dim=256, rot_dim=2)):
+        sizes = [B.qeft_qk_norm_workspace(d, m) for m in (*range(1, 300), 4096, 1 << 21)]
+        assert sizes == sorted(sizes)
+
+
 def qdesc(**over):
     return struct_of(B.qeft_qk_desc_t, dict(head_dim=64, heads=4, kv_heads=2, rot_dim=32, eps=1e-6), over)
 
