@@ -339,14 +339,15 @@ __global__ __launch_bounds__(THREADS) void heads_bwd_kernel(Heads a, float* slab
     }
 }
 
-// dw: the slabs' sum in a fixed order, 32 columns a workgroup, 8 threads a column
-__global__ __launch_bounds__(THREADS) void heads_sum_kernel(Heads a, const float* slab, int slabs) {
-    __shared__ float joined[8][33];
+// dw: the slabs' sum in a fixed order, 32 columns a workgroup, 32 threads a column: few loads one after the other
+constexpr int SHARES = 32;
+__global__ __launch_bounds__(32 * SHARES) void heads_sum_kernel(Heads a, const float* slab, int slabs) {
+    __shared__ float joined[SHARES][33];
     const int column = threadIdx.x & 31, share = threadIdx.x >> 5, j = blockIdx.x * 32 + column;
     float s = 0.f;
     if (j < 2 * a.d) {
 #pragma unroll 8
-        for (int i = share; i < slabs; i += 8) s += slab[(size_t)i * 2 * a.d + j];
+        for (int i = share; i < slabs; i += SHARES) s += slab[(size_t)i * 2 * a.d + j];
     }
     joined[share][column] = s;
     __syncthreads();
@@ -354,7 +355,7 @@ __global__ __launch_bounds__(THREADS) void heads_sum_kernel(Heads a, const float
     float* out = j < a.d ? a.q.dw : a.k.dw;
     if (!out) return;
 #pragma unroll
-    for (int i = 1; i < 8; ++i) s += joined[i][column];
+    for (int i = 1; i < SHARES; ++i) s += joined[i][column];
     float* at = out + (j < a.d ? j : j - a.d);
     *at = a.accumulate ? *at + s : s;
 }
@@ -441,7 +442,7 @@ hipError_t heads_bwd(const Heads& call, hipStream_t s) {
     float* slab = sums ? (float*)a.ws : nullptr;
     const int slabs = a.m > 0 ? bwd_groups(a.d, a.q.heads, a.k.heads, a.rot_dim, a.m) : 0;
     if (slabs > 0) with_form(form_of(a.d, a.rot_dim), Bwd{a, slab, (unsigned)slabs, s});
-    if (sums) heads_sum_kernel<<<(unsigned)(2 * a.d + 31) / 32, THREADS, 0, s>>>(a, slab, slabs);
+    if (sums) heads_sum_kernel<<<(unsigned)(2 * a.d + 31) / 32, 32 * SHARES, 0, s>>>(a, slab, slabs);
     return hipGetLastError();
 }
 

@@ -330,3 +330,29 @@ def test_arguments_that_are_refused():
             B.TensorList(**{**p, **change})
     with pytest.raises(B.QeftError):
         B.qeft_adamw_step(B.TensorList(p["grads"]), 0.1, 1)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("half", [False, True])
+def test_nothing_beside_the_tensors_is_touched(bits, half):
+    """Tensors of odd sizes in larger buffers, sentinels all round."""
+    sizes, gap = [1, 5, 127, 130, 8192, 8193, 2049, 4000], 128
+    p = tensors(sizes, half, bits)
+    buffers, views = {}, {}
+    for k, ts in p.items():
+        room = [-(-t.numel() // 16) * 16 + gap for t in ts]
+        buffers[k] = torch.full((sum(room) + gap,), 77, dtype=ts[0].dtype, device="cuda")
+        at, views[k] = gap, []
+        for t, r in zip(ts, room):
+            views[k].append(buffers[k][at: at + t.numel()].copy_(t))
+            at += r
+    held_all = {k: b.clone() for k, b in buffers.items()}
+    B.qeft_adamw_step(B.TensorList(decay=0.1, **p), 1e-3, 3, seed=1)
+    B.qeft_adamw_step(B.TensorList(decay=0.1, **views), 1e-3, 3, seed=1)
+    for k in p:
+        inside = torch.zeros_like(buffers[k], dtype=torch.bool)
+        for t, v in zip(p[k], views[k]):
+            assert torch.equal(t, v), k
+            first = (v.data_ptr() - buffers[k].data_ptr()) // v.element_size()
+            inside[first: first + v.numel()] = True
+        assert torch.equal(buffers[k][~inside], held_all[k][~inside]), k

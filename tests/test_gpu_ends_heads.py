@@ -237,3 +237,32 @@ def test_graphs_streams_and_calls_without_the_native_module(monkeypatch, m):
         calls()
     for a, b in zip(everything, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_views_that_are_refused_and_what_lies_beside_rows(monkeypatch, native):
+    if not native:
+        monkeypatch.setattr(B, "_native", V.NONE)
+    m, d, heads, kv = 5, 64, 3, 1
+    i = inputs(m, d, d, heads, kv)
+    desc = B.make_qk_desc(d, heads, kv, d, EPS)
+    kw = dict(w_q=i["w_q"], w_k=i["w_k"], rot=i["rot"], pos=i["pos"])
+    over = lambda x: x.as_strided(x.shape, (x.shape[1] - 8, 1))  # noqa: E731
+    for name in ("q", "k", "rot"):
+        for bad in (i[name][:1].expand_as(i[name]), over(i[name])):
+            x = {**i, name: bad}
+            for call in (lambda: B.qeft_qk_norm_fwd(desc, x["q"], x["k"], q_out=torch.empty_like(i["q"]), k_out=torch.empty_like(i["k"]), **{**kw, "rot": x["rot"]}),
+                         lambda: B.qeft_qk_norm_bwd(desc, i["gq"], i["gk"], q=x["q"], k=x["k"], **{**kw, "rot": x["rot"]})):
+                with pytest.raises(B.QeftError) as e:
+                    call()
+                assert e.value.status == B.QEFT_ERR_SHAPE
+    outs = [torch.full((m + 1, n * d + 16), 7.0, dtype=torch.float16, device="cuda") for n in (heads, kv)]
+    B.qeft_qk_norm_fwd(desc, i["q"], i["k"], q_out=outs[0][:m, 8:-8], k_out=outs[1][:m, 8:-8], **kw)
+    for o in outs:
+        assert bool((o[:, :8] == 7).all()) and bool((o[:, -8:] == 7).all()) and bool((o[m] == 7).all()) and not bool((o[:m, 8:-8] == 7).all())
+    B.qeft_qk_norm_bwd(desc, i["gq"], i["gk"], q=i["q"], k=i["k"], dq=outs[0][:m, 8:-8], dk=outs[1][:m, 8:-8], **kw)
+    for o in outs:
+        assert bool((o[:, :8] == 7).all()) and bool((o[:, -8:] == 7).all()) and bool((o[m] == 7).all())
+    with pytest.raises(B.QeftError) as e:
+        B.qeft_qk_norm_fwd(desc, i["q"], i["k"], **{**kw, "pos": i["pos"].long()})
+    assert e.value.status == B.QEFT_ERR_UNSUPPORTED

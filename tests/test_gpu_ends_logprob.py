@@ -275,3 +275,43 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for o, w in zip(outs, want):
         assert all(torch.equal(a, b) for a, b in zip(o, w[1:]))
+
+
+@pytest.mark.parametrize("m,n", [(4, 40), (4, 32000), (3, 140001), (40, 140001)])
+def test_rows_that_are_left_out_are_not_read(m, n):
+    z = V.logits(m, n, False, gen_of(m, n))
+    z[1] = math.nan
+    token = torch.full((m,), 5, dtype=torch.int32, device="cuda")
+    token[1] = -1
+    desc, g = B.make_logprob_desc(n), torch.full((m,), math.nan, device="cuda")
+    g[torch.arange(m) != 1] = 1
+    logp, lse, entropy, lp, ix = B.qeft_logprob_fwd(desc, z, token, top=4)
+    assert logp[1] == lse[1] == entropy[1] == 0 and bool((ix[1] == -1).all()) and bool((lp[1] == -math.inf).all())
+    assert all(bool(t.isfinite().all()) for t in (logp, lse, entropy))
+    for dz in (B.qeft_logprob_bwd(desc, z, lse, token=token, dlogp=g), B.qeft_logprob_fwd_bwd(desc, z, token, g)[0]):
+        assert not bool(dz[1].any()) and bool(dz.isfinite().all())
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_views_that_are_refused(monkeypatch, native):
+    if not native:
+        monkeypatch.setattr(B, "_native", V.NONE)
+    m, n, top = 4, 64, 3
+    desc = B.make_logprob_desc(n)
+    z, f, t = V.logits(m, n, False, gen_of(1), pad=0), torch.zeros(m, device="cuda"), torch.zeros(m, dtype=torch.int32, device="cuda")
+    lp, ix = torch.zeros((m, top), device="cuda"), torch.zeros((m, top), dtype=torch.int32, device="cuda")
+    over = lambda x: x.as_strided(x.shape, (x.shape[1] - 8 if x.shape[1] > 8 else x.shape[1] - 1, 1))  # noqa: E731
+    for bad in (z[:1].expand(m, n), over(z)):
+        for call in (lambda: B.qeft_logprob_fwd(desc, bad, t), lambda: B.qeft_logprob_bwd(desc, bad, f, dlse=f, dz=z), lambda: B.qeft_logprob_bwd(desc, z, f, dlse=f, dz=bad),
+                     lambda: B.qeft_logprob_fwd_bwd(desc, bad, t, f, dz=z), lambda: B.qeft_logprob_fwd_bwd(desc, z, t, f, dz=bad)):
+            with pytest.raises(B.QeftError) as e:
+                call()
+            assert e.value.status == B.QEFT_ERR_SHAPE
+    for kw in (dict(top_logp=lp[:1].expand(m, top), top_index=ix[:1].expand(m, top)), dict(top_logp=over(lp), top_index=over(ix)), dict(top_logp=lp, top_index=ix[:, :2])):
+        with pytest.raises(B.QeftError) as e:
+            B.qeft_logprob_fwd(desc, z, t, top=top, **{**dict(top_logp=lp, top_index=ix), **kw})
+        assert e.value.status == B.QEFT_ERR_SHAPE
+    for kw in (dict(token=t.long()), dict(token=t, logp=f.half()), dict(token=t, lse=f[:1].expand(m)), dict(token=t.cpu())):
+        with pytest.raises(B.QeftError) as e:
+            B.qeft_logprob_fwd(desc, z, **kw)
+        assert e.value.status == B.QEFT_ERR_UNSUPPORTED
