@@ -157,28 +157,39 @@ __device__ __forceinline__ void top_by_rounds(int top, uint64_t* slots, const Ea
         if (threadIdx.x == 0) put(i, best);
     }
 }
-// The largest `top` of the `count` keys in a list of CANDIDATES, 0 behind them: each key's place is the number of larger ones.
+// The largest `top` of the `count` keys in a list: each key's place is the number of larger ones, counted by 16 lanes.
 template <class Put>
 __device__ __forceinline__ void top_of_list(int top, const uint64_t* list, int count, const Put& put) {
-    for (int i = threadIdx.x; i < count; i += blockDim.x) {
+    const int share = threadIdx.x & 15;
+    for (int i = threadIdx.x >> 4; i < count; i += blockDim.x >> 4) {      // (a row of lanes together)
         const uint64_t mine = list[i];
         int place = 0;
-#pragma unroll 1
-        for (int j = 0; j < count; j += 8)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) place += list[j + e] > mine;
-        if (place < top) put(place, mine);
+        for (int j = share; j < count; j += 16) place += list[j] > mine;
+        place = row_reduce(place, Sum());
+        if (share == 0 && place < top) put(place, mine);
     }
     for (int i = count + threadIdx.x; i < top; i += blockDim.x) put(i, 0);
+}
+// x of the lanes that want it, behind what `used` counts, one atomic a wave; more than `room` are counted only.  All lanes of the wave call it.
+template <class T>
+__device__ __forceinline__ void append(bool want, T x, T* list, int room, int* used) {
+    const uint64_t who = __ballot(want);
+    if (who == 0) return;
+    const int lane = threadIdx.x & 63, leader = __builtin_ctzll(who);
+    int at = 0;
+    if (lane == leader) at = atomicAdd(used, __popcll(who));
+    at = __builtin_amdgcn_readlane(at, leader) + __popcll(who & ((1ull << lane) - 1));
+    if (want && at < room) list[at] = x;
 }
 
 // Workgroup = a row, or a part of one: V octets a thread.
 template <int V, bool F32, bool GRAD>
 __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     __shared__ float buf[3][16];
-    __shared__ uint32_t maxima[GRAD ? 1 : 256];
+    __shared__ uint32_t maxima[GRAD ? 1 : 256], border;
     __shared__ uint64_t list[GRAD ? 1 : CANDIDATES], slots[16];
-    __shared__ int used;
+    __shared__ uint16_t reached[GRAD ? 1 : 1024];
+    __shared__ int used[2];
     const int64_t row = p.parts == 1 ? blockIdx.x : blockIdx.x / p.parts;
     const int part = p.parts == 1 ? 0 : (int)(blockIdx.x - row * p.parts), from = part * p.len, n = min(p.len, a.n - from), T = blockDim.x;
     const char* begin = row_at(a.z, row, a.ldz, F32);
@@ -233,8 +244,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
             }
             if (threadIdx.x % side == 0) maxima[threadIdx.x / side] = group;
             for (int i = T / side + threadIdx.x; i < 256; i += T) maxima[i] = 0;
-            for (int i = threadIdx.x; i < CANDIDATES; i += T) list[i] = 0;
-            if (threadIdx.x == 0) used = 0;
+            if (threadIdx.x < 2) used[threadIdx.x] = 0;
         }
     }
     const bool wants_t = a.entropy || p.lse || (GRAD && a.dentropy);
@@ -280,8 +290,9 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     } else if (threadIdx.x == 0) p.stats[blockIdx.x] = x;
     if constexpr (!GRAD) {
         if (a.top == 0) return;
-        // Candidates: whatever reaches the top-th largest of the maxima of groups of threads (64 groups for up to 32 alternatives, 256 for more), cut to 16 bits.  Few do, so they are ordered by
-        // comparing each with each.  Rows where many do (equal logits) or with not-a-number, which no maximum shows, go by rounds.
+        // Candidates: whatever reaches the top-th largest of the maxima of groups of threads (64 groups for up to 32 alternatives, 256 for more).  Few threads have any, and few of
+        // their values are: the threads are listed, then all look through the listed ones' values, read again.  The few candidates are ordered by comparing each with each.  Rows where
+        // many are (equal logits) or with not-a-number, which no maximum shows, go by rounds.
         auto put = [&](int i, uint64_t key) {
             if (p.parts == 1) put_top(a, row, i, key, x.k, ln_s);
             else p.keys[(size_t)blockIdx.x * a.top + i] = key;
@@ -291,17 +302,18 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
             uint32_t g[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) g[i] = maxima[lane + 64 * i];
-            if (a.top <= 32) {
+            if (a.top <= 32 && waves >= 4) {
+                // each wave looks at a share of the 64: is it the one with fewer than `top` above it and `top` with it?
                 const uint32_t most = max(max(g[0], g[1]), max(g[2], g[3]));
-#pragma unroll
-                for (int bit = 30; bit >= 16; bit -= 2) {      // two bits a step
-                    auto reach = [&](uint32_t b) { return (int)__popcll(__ballot(most >= (bound | b << bit))) >= a.top; };
-                    const bool one = reach(1), two = reach(2), three = reach(3);
-                    bound |= (three ? 3u : two ? 2u : one ? 1u : 0u) << bit;
+                for (int i = 64 / waves * wave; i < 64 / waves * (wave + 1); ++i) {
+                    const uint32_t x = (uint32_t)__builtin_amdgcn_readlane((int)most, i);
+                    if ((int)__popcll(__ballot(most > x)) < a.top && (int)__popcll(__ballot(most >= x)) >= a.top && lane == 0) border = x;      // (the same, if several)
                 }
+                __syncthreads();
+                bound = border;
             } else {
 #pragma unroll 1
-                for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+                for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {      // cut to 16 bits
                     int count = 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) count += __popcll(__ballot(g[i] >= (bound | bit)));
@@ -310,24 +322,20 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
             }
         }
         bound = max(bound, RANK_NEG_INF + 1);
-        const float least = value_of(bound);
-        if (rank >= bound) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float most = v[i][0];
-#pragma unroll
-                for (int e = 1; e < 8; ++e) most = fmaxf(most, v[i][e]);
-                if (most < least) continue;      // (most octets)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (v[i][e] >= least) {
-                        const int j = atomicAdd(&used, 1);
-                        if (j < CANDIDATES) list[j] = (uint64_t)rank_of(v[i][e]) << 32 | (uint32_t)~(from + 8 * (int)(threadIdx.x + T * i) + e);
-                    }
+        append(rank >= bound, (uint16_t)threadIdx.x, reached, 1024, &used[0]);
+        __syncthreads();
+        const int looked = used[0] * 8 * V;
+        for (int i0 = 0; i0 < looked; i0 += T) {
+            const int i = i0 + threadIdx.x;
+            uint64_t key = 0;
+            if (i < looked) {
+                const int j = 8 * (reached[i / (8 * V)] + T * (i / 8 % V)) + i % 8;
+                if (j < n) key = (uint64_t)rank_of(logit_at(a, z, j)) << 32 | (uint32_t)~(from + j);
             }
+            append((uint32_t)(key >> 32) >= bound, key, list, CANDIDATES, &used[1]);
         }
         __syncthreads();
-        const int count = used;
+        const int count = used[1];
         if (count <= CANDIDATES && x.s == x.s) top_of_list(a.top, list, count, put);
         else {
             auto each = [&](auto&& f) {      // (from memory: every value's key would stay in registers through the rounds)
@@ -355,58 +363,49 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     }
 }
 
-// The parts of a row joined: a thread a part (256 at most).  One wave where it has lanes for them: no barrier between its steps.
+// The parts of a row joined: a lane a part where a wave has lanes for them (each wave for itself, no barrier), else a thread a part (256 at most).
 __global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
     __shared__ float buf[3][16];
     __shared__ uint64_t list[CANDIDATES], slots[16];
     __shared__ int used;
     const int64_t row = blockIdx.x;
-    const int token = a.token ? a.token[row] : -1, i = threadIdx.x;
+    const int token = a.token ? a.token[row] : -1;
     if (a.token && (token < 0 || token >= a.n)) {
         left_out(a, row);
         return;
     }
-    const float zt = a.logp && i == 0 ? logit_at(a, row_at(a.z, row, a.ldz, a.f32), token) : 0.f;
+    const bool alone = p.parts <= 64;
+    const int t = threadIdx.x, i = alone ? t & 63 : t;
+    const float zt = a.logp && t == 0 ? logit_at(a, row_at(a.z, row, a.ldz, a.f32), token) : 0.f;
     const Stats y = i < p.parts ? p.stats[row * p.parts + i] : Stats{LEAST, 0.f, 0.f};
     const uint64_t* keys = p.keys + (size_t)row * p.parts * a.top;
     const int total = p.parts * a.top;
-    // (asked for together with the statistics: a part's last key, and the first keys of this thread)
-    const uint64_t last = a.top > 0 && i < p.parts ? keys[(size_t)i * a.top + a.top - 1] : 0;
-    uint64_t first[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int j = i + e * (int)blockDim.x;
-        first[e] = j < total ? keys[j] : 0;
-    }
-    auto each = [&](auto&& f) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f(first[e]);
-        for (int j = i + 4 * blockDim.x; j < total; j += blockDim.x) f(keys[j]);
-    };
-    if (i == 0) used = 0;
-    for (int j = i; j < CANDIDATES; j += blockDim.x) list[j] = 0;
+    // (asked for together with the statistics: a part's last key, and this thread's first)
+    const uint64_t last = a.top > 0 && i < p.parts ? keys[(size_t)i * a.top + a.top - 1] : 0, first = t < total ? keys[t] : 0;
+    if (t == 0) used = 0;
+    auto joined = [&](auto v, auto* slots, auto none, const auto& op) { return alone ? wave_reduce(v, op) : group_reduce(v, slots, none, op); };
     Stats x;
-    x.k = group_reduce(y.k, buf[0], LEAST, MostFloat());
+    x.k = joined(y.k, buf[0], LEAST, MostFloat());
     const float d = shrink(y.k, x.k), f = __builtin_amdgcn_exp2f(d);
-    x.s = group_reduce(term(y.s, f), buf[1], 0.f, Sum());
-    x.t = group_reduce(term(f, fmaf(d, y.s, y.t)), buf[2], 0.f, Sum());
+    x.s = joined(term(y.s, f), buf[1], 0.f, Sum());
+    x.t = joined(term(f, fmaf(d, y.s, y.t)), buf[2], 0.f, Sum());
     const float ln_s = logf(x.s), entropy = x.s == 0.f ? 0.f : ln_s - LN2 * (x.t / x.s);
-    if (i == 0) put_row(a, p, row, zt, x, ln_s, entropy);
+    if (t == 0) put_row(a, p, row, zt, x, ln_s, entropy);
     if (a.top == 0) return;
     // a part whose last key is this large has enough of them
-    const uint64_t bound = max(group_reduce(last, slots, (uint64_t)0, Most()), (uint64_t)1);
+    const uint64_t bound = max(joined(last, slots, (uint64_t)0, Most()), (uint64_t)1);
     __syncthreads();
-    each([&](uint64_t key) {
-        if (key >= bound) {
-            const int at = atomicAdd(&used, 1);
-            if (at < CANDIDATES) list[at] = key;
-        }
-    });
+    for (int j0 = 0; j0 < total; j0 += blockDim.x) {
+        const uint64_t key = j0 == 0 ? first : j0 + t < total ? keys[j0 + t] : 0;
+        append(key >= bound, key, list, CANDIDATES, &used);
+    }
     __syncthreads();
     const int count = used;
     auto put = [&](int at, uint64_t key) { put_top(a, row, at, key, x.k, ln_s); };
     if (count <= CANDIDATES) top_of_list(a.top, list, count, put);
-    else top_by_rounds(a.top, slots, each, put);
+    else top_by_rounds(a.top, slots, [&](auto&& g) {
+        for (int j = t; j < total; j += blockDim.x) g(keys[j]);
+    }, put);
 }
 
 // ---- the gradient alone -------------------------------------------------------------------------------------------------
@@ -506,7 +505,7 @@ void launch_fwd(const Logprob& a, hipStream_t s) {
         p.lse = lse ? lse + from : nullptr;
         p.entropy = lse ? lse + a.m + from : nullptr;
         launch_rows<F32, false>(q, b, p, s);
-        logprob_join_kernel<<<(unsigned)b.m, q.parts <= 64 ? 64 : 256, 0, s>>>(b, p);
+        logprob_join_kernel<<<(unsigned)b.m, q.parts <= 64 && a.top == 0 ? 64 : 256, 0, s>>>(b, p);
     }
     if (!a.dz) return;
     Logprob b = a;
