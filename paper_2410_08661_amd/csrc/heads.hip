@@ -7,7 +7,6 @@
 // Bytes bound all three.  A head is L lanes', each with two pieces of VW values half apart, so that pairs meet in a lane and the head's sums stay within a row of lanes
 // (no LDS); a wave has 64 / L heads side by side.  Heads of all tokens form one sequence that the grid walks through: no lane waits for a token's last heads.  The
 // gradient's workgroups keep their sums for dw in registers and leave one slab each, summed by a second launch in a fixed order.
-#include "octets.h"
 #include "pieces.h"
 #include "qeft_internal.h"
 #include "wave.h"
@@ -16,7 +15,9 @@ namespace qeft {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int FWD_GROUPS = 2048, BWD_GROUPS = 512;      // workgroups at most
+// Workgroups at most.  Forward: as many as run at a time, five a CU (4096 tokens of 40 + 40 heads 38.8 us; 2048 41.7, 10240 - one head a lane - 38.3, but 4096 tokens of 32 + 1 heads
+// of 40 13.9 -> 16.0).  Gradient: two a CU, each leaves a slab (4001 tokens of 64 + 8 heads with 256 / 512 / 768 / 1024 / 2048: 55 / 45 / 47 / 49 / 59 us).
+constexpr int FWD_GROUPS = 1280, BWD_GROUPS = 512;
 
 // Lane's r-th two pieces of a head: the rotated ones, half apart, then what is behind them two by two
 template <int VW>
@@ -44,9 +45,9 @@ struct Two {
             if (p.one) get<VW>(head + p.first, a);
         }
     }
-    __device__ __forceinline__ void store(__half* head, const Place<VW>& p, bool once = false) const {
-        if (p.one) put<VW>(head + p.first, a, once);
-        if (p.two) put<VW>(head + p.second, b, once);
+    __device__ __forceinline__ void store(__half* head, const Place<VW>& p) const {
+        if (p.one) put<VW>(head + p.first, a);
+        if (p.two) put<VW>(head + p.second, b);
     }
     // one of two, word by word (a choice between the objects goes through memory)
     static __device__ __forceinline__ Two choose(bool first, const Two& x, const Two& y) {
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(THREADS) void heads_fwd_kernel(Heads a) {
         forward<VW, R, L>(x, w, is_q ? a.q.w != nullptr : a.k.w != nullptr, lane.place, turn, a.d, a.eps);
         __half* out = (is_q ? a.q.out + t * a.q.ldout : a.k.out + t * a.k.ldout) + (size_t)(is_q ? h : h - hq) * a.d;
 #pragma unroll
-        for (int r = 0; r < R; ++r) x[r].store(out, lane.place[r], a.once);
+        for (int r = 0; r < R; ++r) x[r].store(out, lane.place[r]);
     }
 }
 
@@ -316,7 +317,7 @@ __global__ __launch_bounds__(THREADS) void heads_bwd_kernel(Heads a, float* slab
                         o.a[e] = (_Float16)ga[r][e];
                         o.b[e] = (_Float16)gb[r][e];
                     }
-                    o.store(out, lane.place[r], a.once);
+                    o.store(out, lane.place[r]);
                 }
             }
         }
@@ -423,9 +424,7 @@ int bwd_groups(int d, int heads, int kv, int rot_dim, int64_t m) { return groups
 
 size_t heads_workspace(int d, int heads, int kv, int rot_dim, int64_t m) { return (size_t)bwd_groups(d, heads, kv, rot_dim, m) * 2 * d * sizeof(float); }
 
-hipError_t heads_fwd(const Heads& call, hipStream_t s) {
-    Heads a = call;
-    a.once = a.m * (a.q.heads + a.k.heads) * a.d * 2 > CACHED_BYTES;
+hipError_t heads_fwd(const Heads& a, hipStream_t s) {
     const Form f = form_of(a.d, a.rot_dim);
     with_form(f, Fwd{a, (unsigned)groups_for(a.m * (a.q.heads + a.k.heads), f.lanes, FWD_GROUPS), s});
     return hipGetLastError();
@@ -435,9 +434,7 @@ hipError_t heads_append(const Cache& c, const Append& p, const __half* w_q, cons
     with_form(f, App{c, p, w_q, w_k, eps, (unsigned)groups_for((int64_t)p.tokens * (p.heads + 2 * (int64_t)c.kv), f.lanes, FWD_GROUPS), s});
     return hipGetLastError();
 }
-hipError_t heads_bwd(const Heads& call, hipStream_t s) {
-    Heads a = call;
-    a.once = a.m * (a.q.heads + a.k.heads) * a.d * 2 > CACHED_BYTES;
+hipError_t heads_bwd(const Heads& a, hipStream_t s) {
     const bool sums = a.q.dw || a.k.dw;
     float* slab = sums ? (float*)a.ws : nullptr;
     const int slabs = a.m > 0 ? bwd_groups(a.d, a.q.heads, a.k.heads, a.rot_dim, a.m) : 0;

@@ -53,11 +53,10 @@ struct MostFloat {
 struct Slope {
     float c, k2, a, dh, at_token;
     int token;
-    bool once;
 };
 __device__ __forceinline__ Slope make_slope(const Logprob& a, int64_t row, int token, float k2, float entropy) {
     const float dl = a.dlogp ? a.dlogp[row] : 0.f, ds = a.dlse ? a.dlse[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
-    return Slope{a.scale * LOG2E, k2, a.scale * (ds - dl - (dh != 0.f ? dh * entropy : 0.f)), a.scale * dh * LN2, a.scale * dl, a.token ? token : -1, a.once != 0};
+    return Slope{a.scale * LOG2E, k2, a.scale * (ds - dl - (dh != 0.f ? dh * entropy : 0.f)), a.scale * dh * LN2, a.scale * dl, a.token ? token : -1};
 }
 __device__ __forceinline__ float slope_of(const Slope& g, float z) {
     const float u = fmaf(z, g.c, -g.k2);
@@ -79,13 +78,13 @@ __device__ __forceinline__ void put_slopes(const Slope& g, const Raw<F32>& v, ch
         for (int e = 0; e < 8; ++e)
             if (at + e == g.token) x[e] += g.at_token;
     }
-    store<F32>(dz, at, left, x, g.once);
+    store<F32>(dz, at, left, x);
 }
 template <bool F32>
-__device__ __forceinline__ void zero_row(void* row, int n, bool once) {
+__device__ __forceinline__ void zero_row(void* row, int n) {
     for (int at = 8 * threadIdx.x; at < n; at += 8 * blockDim.x) {
         float x[8] = {};
-        store<F32>(row, at, min(8, n - at), x, once);
+        store<F32>(row, at, min(8, n - at), x);
     }
 }
 // a row without a token: no probability, no alternatives
@@ -198,7 +197,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     if (a.token && (token < 0 || token >= a.n)) {
         if (p.parts > 1) return;      // (the join leaves it out)
         left_out(a, row);
-        if (GRAD) zero_row<F32>(row_at(a.dz, row, a.lddz, F32), a.n, a.once);
+        if (GRAD) zero_row<F32>(row_at(a.dz, row, a.lddz, F32), a.n);
         return;
     }
     // (before the gradient's first store, which may go to z itself)
@@ -350,7 +349,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
         }
     } else {
         char* dz = row_at(a.dz, row, a.lddz, F32);
-        if (empty) return zero_row<F32>(dz, a.n, a.once);
+        if (empty) return zero_row<F32>(dz, a.n);
         const Slope g = make_slope(a, row, token, x.k + log2f(x.s), entropy);
         Raw<F32> x = v[0];
 #pragma unroll
@@ -417,9 +416,9 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(Logprob a, int chunks)
     const char* z = row_at(a.z, row, a.ldz, F32) + (size_t)from * (F32 ? 4 : 2);
     char* dz = row_at(a.dz, row, a.lddz, F32) + (size_t)from * (F32 ? 4 : 2);
     const int token = a.token ? a.token[row] : -1;
-    if (a.token && (token < 0 || token >= a.n)) return zero_row<F32>(dz, n, a.once);
+    if (a.token && (token < 0 || token >= a.n)) return zero_row<F32>(dz, n);
     const float lse = a.lse_in[row];
-    if (lse == -INFINITY) return zero_row<F32>(dz, n, a.once);
+    if (lse == -INFINITY) return zero_row<F32>(dz, n);
     const Slope g = make_slope(a, row, token - from, lse * LOG2E, a.entropy_in ? a.entropy_in[row] : 0.f);
     Raw<F32> v[CHUNK / 2048];
 #pragma unroll
@@ -522,17 +521,13 @@ size_t logprob_workspace(int n, bool f32, int64_t m, int top) {
     return std::max(plan_of(n, f32, m, top).bytes, few > 0 && few < m ? plan_of(n, f32, few, top).bytes : 0);
 }
 
-hipError_t logprob_fwd(const Logprob& call, hipStream_t s) {
-    Logprob a = call;
-    a.once = !a.f32 && a.m * a.n * 2 > CACHED_BYTES;
+hipError_t logprob_fwd(const Logprob& a, hipStream_t s) {
     if (a.f32) launch_fwd<true>(a, s);
     else launch_fwd<false>(a, s);
     return hipGetLastError();
 }
 
-hipError_t logprob_bwd(const Logprob& call, hipStream_t s) {
-    Logprob a = call;
-    a.once = !a.f32 && a.m * a.n * 2 > CACHED_BYTES;
+hipError_t logprob_bwd(const Logprob& a, hipStream_t s) {
     if (a.f32) launch_bwd<true>(a, s);
     else launch_bwd<false>(a, s);
     return hipGetLastError();

@@ -19,19 +19,13 @@ __device__ __forceinline__ const char* row_of(const void* p, int64_t row, int64_
 }
 __device__ __forceinline__ char* row_of(void* p, int64_t row, int64_t ld, bool f32) { return const_cast<char*>(row_of((const void*)p, row, ld, f32)); }
 
-// What a call writes beyond this (the L2 caches hold 32 MB) goes past the caches: nobody finds it there again, and the writes leave the reads'
-// lines alone.  Only where a lane writes all of an octet at once: the two halves of an fp32 one would go out as parts of lines.
-constexpr int64_t CACHED_BYTES = 32 << 20;
 // One load or store; `once`: of data that the caches need not keep
 template <class T>
 __device__ __forceinline__ T fetch(const char* p, bool once) { return once ? __builtin_nontemporal_load(reinterpret_cast<const T*>(p)) : *reinterpret_cast<const T*>(p); }
 template <class T>
 __device__ __forceinline__ void place(char* p, T x, bool once) {
-    if (once) {      // (between the two empty statements, or it becomes one with the other store, an ordinary one)
-        asm volatile("");
-        __builtin_nontemporal_store(x, reinterpret_cast<T*>(p));
-        asm volatile("");
-    } else *reinterpret_cast<T*>(p) = x;
+    if (once) __builtin_nontemporal_store(x, reinterpret_cast<T*>(p));
+    else *reinterpret_cast<T*>(p) = x;
 }
 
 // Eight values of a row as loaded.  left: how many of them exist (none from 0 down); a row's last octet may be partial, and is read value by value, the last one

@@ -18,14 +18,10 @@ __device__ __forceinline__ void get(const __half* p, _Float16 (&x)[VW]) {
     __builtin_memcpy(x, &v, sizeof x);
 }
 template <int VW>
-__device__ __forceinline__ void put(__half* p, const _Float16 (&x)[VW], bool once = false) {   // once: the caches need not keep it
+__device__ __forceinline__ void put(__half* p, const _Float16 (&x)[VW]) {
     typename Piece<VW>::type v;
     __builtin_memcpy(&v, x, sizeof x);
-    if (once) {      // (between the two empty statements, or it becomes one with the other store, an ordinary one)
-        asm volatile("");
-        __builtin_nontemporal_store(v, reinterpret_cast<typename Piece<VW>::type*>(p));
-        asm volatile("");
-    } else *reinterpret_cast<typename Piece<VW>::type*>(p) = v;
+    *reinterpret_cast<typename Piece<VW>::type*>(p) = v;
 }
 
 }  // namespace qeft

@@ -277,7 +277,6 @@ struct Logprob {             // either direction: what a call does not have is N
     void* dz;
     int64_t ldz, ld_top, lddz, m;
     int n, f32, top;
-    int once;                // the gradient is more than the caches hold (logprob.hip decides)
     float scale;
     unsigned char* ws;
 };
@@ -298,7 +297,6 @@ struct Heads {
     const float* rot;
     int64_t ld_rot, m;
     int d, rot_dim, positions, accumulate;
-    int once;                // what is written is more than the caches hold (heads.hip decides)
     float eps;
     unsigned char* ws;
 };
