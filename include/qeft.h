@@ -566,7 +566,7 @@ int qeft_cache_append_norm(const qeft_cache_desc_t* desc, const qeft_cache_t* ca
  *
  * qeft_tensors_plan writes the plan of a list to host memory (qeft_tensors_plan_bytes bytes); the caller copies it to the device, 16-byte aligned, and gives its address
  * together with the numbers in `list` to the calls below.  It refuses what they cannot do, so that they read the plan as it is: it must be the unchanged copy, on the device of the call.
- * A list without m, v, weight and master (all NULL) serves qeft_grad_norm alone.  n from 0 (skipped) to 2^40, count at most QEFT_MAX_TENSORS, 2^30 blocks of work.
+ * A list without m, v, weight and master (all NULL) serves qeft_grad_norm alone.  n from 0 (skipped) to 2^40, count at most QEFT_MAX_TENSORS, 2^30 pieces of 2048 values, each begun one counted.
  * qeft_adamw_step: lr, step (1 for the first, at most 2^30) by value, or read from the device where lr_at / step_at are given (a captured graph's); beta1, beta2 in [0, 1), eps > 0.
  * factor (device, NULL: 1): where it is not a finite number, the call leaves everything as it was.  A step on the device that is below 1 counts as 1.
  * qeft_grad_norm: out[0] = scale * sqrt(sum of all grad^2), summed in fp64, and out[1] = scale * min(1, max_norm / out[0]), the factor for a step: the gradients of a loss that was
@@ -586,8 +586,8 @@ typedef struct {
 } qeft_tensor_t;
 typedef struct {
     const void* plan;      /* device */
-    int64_t work;          /* pieces of work in it, of `piece` values */
-    int32_t piece, count, grad_dtype, state_bits, has_weight, has_master;
+    int64_t work;          /* pieces of work in it */
+    int32_t count, grad_dtype, state_bits, has_weight, has_master;
 } qeft_tensors_t;
 typedef struct {
     double lr, beta1, beta2, eps;

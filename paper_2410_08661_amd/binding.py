@@ -129,7 +129,7 @@ class qeft_tensor_t(C.Structure):
 
 
 class qeft_tensors_t(C.Structure):
-    _fields_ = [("plan", C.c_void_p), ("work", C.c_int64), ("piece", C.c_int32), ("count", C.c_int32), ("grad_dtype", C.c_int32), ("state_bits", C.c_int32), ("has_weight", C.c_int32),
+    _fields_ = [("plan", C.c_void_p), ("work", C.c_int64), ("count", C.c_int32), ("grad_dtype", C.c_int32), ("state_bits", C.c_int32), ("has_weight", C.c_int32),
                 ("has_master", C.c_int32)]
 
 

@@ -5,6 +5,7 @@
 // Bytes bound it: every value is read and written once.  A workgroup takes a piece of a tensor, a thread eight values at a time; 16 lanes have a block of an
 // 8-bit state, whose largest value they find without LDS.
 #include <math.h>
+#include <algorithm>
 #include <type_traits>
 #include "octets.h"
 #include "qeft_internal.h"
@@ -13,9 +14,9 @@
 namespace qeft {
 namespace {
 
-constexpr int THREADS = 256, STEP = 8 * THREADS;
-constexpr int SUM_GROUPS = 1024;     // workgroups of the norm
-static_assert(SMALL_PIECE % STEP == 0 && PIECE % STEP == 0 && STEP % QEFT_STATE_BLOCK == 0, "whole blocks");
+constexpr int THREADS = PIECE / 8;
+constexpr int SUM_GROUPS = 1024;     // workgroups of the norm (512: 174 million gradients 78 us in place of 59)
+static_assert(PIECE % QEFT_STATE_BLOCK == 0, "whole blocks");
 
 // 32 bits stirred: two products with odd constants between shifts (every bit of x flips every bit of the result about half the time)
 __host__ __device__ __forceinline__ uint32_t stir(uint32_t x) {
@@ -157,8 +158,8 @@ struct Base {
     char *weight, *master, *m, *v;
     uint8_t *m_scale, *v_scale;
 };
-// Eight values of everything a step reads.  With 8-bit states loads and stores but the master's go past the caches (272 million weights 527 -> 505 us); with 32-bit states that
-// would cost (174 million 1127 -> 1187).
+// Eight values of everything a step reads.  With 8-bit states loads and stores but the master's go past the caches (272 million weights with masters 839 -> 786 us, without 509 -> 500);
+// with 32-bit states that gains nothing (895 both ways).
 template <bool GRAD32, bool STATE8, bool MASTER>
 struct Read {
     Raw<GRAD32> grad;
@@ -181,12 +182,13 @@ struct Read {
 };
 
 template <bool GRAD32, bool STATE8, bool WEIGHT, bool MASTER>
-__global__ __launch_bounds__(THREADS) void adamw_kernel(Tensors t, Adamw a) {
+__global__ __launch_bounds__(THREADS) void adamw_kernel(Tensors t, Adamw a, int first) {
     const float factor = a.factor ? *a.factor : 1.f;
     if (!(fabsf(factor) < INFINITY)) return;
-    const TensorRecord& rec = t.records[t.piece_of[blockIdx.x]];
-    const int64_t from = (int64_t)((int)blockIdx.x - rec.first_piece) * t.piece;
-    const int n = (int)min((int64_t)t.piece, rec.n - from);
+    const int piece = first + blockIdx.x;
+    const TensorRecord& rec = t.records[t.piece_of[piece]];
+    const int64_t from = (int64_t)(piece - rec.first_piece) * PIECE;
+    const int n = (int)min((int64_t)PIECE, rec.n - from);
     constexpr int STATE = STATE8 ? 1 : 4;
     const Base base{scalar((const char*)rec.grad + from * (GRAD32 ? 4 : 2)),  scalar((char*)rec.weight + from * 2),
                     scalar((char*)rec.master + from * 4),                     scalar((char*)rec.m + from * STATE),
@@ -194,106 +196,110 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Tensors t, Adamw a) {
                     scalar(rec.v_scale + from / QEFT_STATE_BLOCK)};
     const bool dice = STATE8 || (!MASTER && a.stochastic);
     const int64_t place = rec.first_block * QEFT_STATE_BLOCK + from;
-    int at = 8 * threadIdx.x;
-    auto there = [&](int i) { return (i & -QEFT_STATE_BLOCK) < n; };      // (the 16 lanes of a block stay together)
-    if (!there(at)) return;
-    Read<GRAD32, STATE8, MASTER> in, ahead;
-    ahead.load(base, at, n - at);
+    const int at = 8 * threadIdx.x, left = n - at;
+    if ((at & -QEFT_STATE_BLOCK) >= n) return;      // (the 16 lanes of a block stay together)
+    Read<GRAD32, STATE8, MASTER> in;
+    in.load(base, at, left);
     const Now now = now_of(a);
     const float decay = now.lr * rec.decay;
     const uint32_t step = (uint32_t)(a.step_at ? max(*a.step_at, 1) : a.step);
     const uint32_t key = stir(step + stir(a.seed_low + stir(a.seed_high)));
-    for (bool more = true; more; at += STEP) {
-        in = ahead;
-        const int left = n - at;
-        more = there(at + STEP);
-        if (more) ahead.load(base, at + STEP, left - STEP);
-        float m[8], v[8], w[8];
-        if constexpr (STATE8) {
-            const float pm = power_of(in.m_scale), pv = power_of(in.v_scale);
-            in.m.template values<true>(m);
-            in.v.template values<false>(v);
+    float m[8], v[8], w[8];
+    if constexpr (STATE8) {
+        const float pm = power_of(in.m_scale), pv = power_of(in.v_scale);
+        in.m.template values<true>(m);
+        in.v.template values<false>(v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m[e] *= pm, v[e] *= pv;
-        } else {
+        for (int e = 0; e < 8; ++e) m[e] *= pm, v[e] *= pv;
+    } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m[e] = in.m[e], v[e] = in.v[e];
+        for (int e = 0; e < 8; ++e) m[e] = in.m[e], v[e] = in.v[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        moments(a, factor * in.grad[e], m[e], v[e]);
+        const float x = in.weight[e];
+        // (8-bit states: issue bounds the kernel, and the hardware's root and reciprocal are good to a unit of fp32's last place; a root below 2^-63 would be 0)
+        const float up = STATE8 ? m[e] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(fmaxf(v[e], 0x1p-126f)) + now.eps) : m[e] / (sqrtf(v[e]) + now.eps);
+        w[e] = fmaf(-now.size, up, fmaf(-decay, x, x));
+    }
+    uint32_t r[8] = {};
+    if (dice) {
+        const int64_t spot = place + at;
+        const uint32_t base_r = (uint32_t)spot + stir((uint32_t)(spot >> 32) + key);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = stir(base_r + e);
+    }
+    if constexpr (STATE8) {
+        if (left < 8) {      // what does not exist is no part of a block's largest
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e >= left) m[e] = v[e] = 0.f;
         }
+        float most_m = 0.f;
+        uint32_t most_v = 0;      // (bits of floats >= 0 are in their order, not-a-number above infinity)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            moments(a, factor * in.grad[e], m[e], v[e]);
-            const float x = in.weight[e];
-            // (8-bit states: issue bounds the kernel, and the hardware's root and reciprocal are good to a unit of fp32's last place; a root below 2^-63 would be 0)
-            const float up = STATE8 ? m[e] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(fmaxf(v[e], 0x1p-126f)) + now.eps) : m[e] / (sqrtf(v[e]) + now.eps);
-            w[e] = fmaf(-now.size, up, fmaf(-decay, x, x));
+            most_m = fmaxf(most_m, fabsf(m[e]));
+            most_v = max(most_v, __builtin_bit_cast(uint32_t, v[e]));
         }
-        uint32_t r[8] = {};
-        if (dice) {
-            const int64_t first = place + at;
-            const uint32_t base_r = (uint32_t)first + stir((uint32_t)(first >> 32) + key);
+        most_m = __builtin_bit_cast(float, row_reduce(__builtin_bit_cast(uint32_t, most_m), Most()));
+        most_v = row_reduce(most_v, Most());
+        // (a gradient that is not finite makes v so; a first moment that was not finite before has a block of such)
+        const bool finite = most_v < 0x7f800000u && most_m < INFINITY;
+        const uint32_t bm = block_power<true>(most_m, finite), bv = block_power<false>(__builtin_bit_cast(float, most_v), finite);
+        Codes cm, cv;
+        uint32_t dv[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) r[e] = stir(base_r + e);
+        for (int e = 0; e < 8; ++e) dv[e] = r[e] << 16;
+        encode<true>(m, r, cm, bm, finite);
+        encode<false>(v, dv, cv, bv, finite);
+        cm.store((uint8_t*)base.m + (uint32_t)at, left);
+        cv.store((uint8_t*)base.v + (uint32_t)at, left);
+        if ((threadIdx.x & 15) == 0) {
+            base.m_scale[(uint32_t)at / QEFT_STATE_BLOCK] = (uint8_t)bm;
+            base.v_scale[(uint32_t)at / QEFT_STATE_BLOCK] = (uint8_t)bv;
         }
-        if constexpr (STATE8) {
-            if (left < 8) {      // what does not exist is no part of a block's largest
+    } else {
+        store<true>(base.m, at, left, m);
+        store<true>(base.v, at, left, v);
+    }
+    if (MASTER) store<true>(base.master, at, left, w);
+    if (WEIGHT) {
+        if (!MASTER && a.stochastic) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e >= left) m[e] = v[e] = 0.f;
-            }
-            float most_m = 0.f;
-            uint32_t most_v = 0;      // (bits of floats >= 0 are in their order, not-a-number above infinity)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                most_m = fmaxf(most_m, fabsf(m[e]));
-                most_v = max(most_v, __builtin_bit_cast(uint32_t, v[e]));
-            }
-            most_m = __builtin_bit_cast(float, row_reduce(__builtin_bit_cast(uint32_t, most_m), Most()));
-            most_v = row_reduce(most_v, Most());
-            // (a gradient that is not finite makes v so; a first moment that was not finite before has a block of such)
-            const bool finite = most_v < 0x7f800000u && most_m < INFINITY;
-            const uint32_t bm = block_power<true>(most_m, finite), bv = block_power<false>(__builtin_bit_cast(float, most_v), finite);
-            Codes cm, cv;
-            uint32_t dv[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dv[e] = r[e] << 16;
-            encode<true>(m, r, cm, bm, finite);
-            encode<false>(v, dv, cv, bv, finite);
-            cm.store((uint8_t*)base.m + (uint32_t)at, left);
-            cv.store((uint8_t*)base.v + (uint32_t)at, left);
-            if ((threadIdx.x & 15) == 0) {
-                base.m_scale[(uint32_t)at / QEFT_STATE_BLOCK] = (uint8_t)bm;
-                base.v_scale[(uint32_t)at / QEFT_STATE_BLOCK] = (uint8_t)bv;
-            }
-        } else {
-            store<true>(base.m, at, left, m);
-            store<true>(base.v, at, left, v);
+            for (int e = 0; e < 8; ++e) w[e] = cut_half(w[e], r[e] * 0x5c3c9ccdu >> 19);
         }
-        if (MASTER) store<true>(base.master, at, left, w);
-        if (WEIGHT) {
-            if (!MASTER && a.stochastic) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = cut_half(w[e], r[e] * 0x5c3c9ccdu >> 19);
-            }
-            store<false>(base.weight, at, left, w, STATE8);
-        }
+        store<false>(base.weight, at, left, w, STATE8);
     }
 }
 
-// One partial sum a workgroup, pieces blockIdx.x, + gridDim.x ...
+// One partial sum a workgroup, of every gridDim.x-th bunch of pieces.  A bunch is 64 bytes a thread, so that the chains piece - tensor - gradients of its pieces run at a time
+// (174 million fp16 gradients by 1 / 2 / 4 / 8 pieces 83 / 66 / 59 / 62 us, fp32 ones 115 / 106 / 112 / 117).
 template <bool GRAD32>
 __global__ __launch_bounds__(THREADS) void square_sums_kernel(Tensors t, double* part) {
     __shared__ double slots[16];
+    constexpr int BUNCH = GRAD32 ? 2 : 4;
+    const int at = 8 * threadIdx.x;
     double s = 0.;
-    for (int p = blockIdx.x; p < t.work; p += gridDim.x) {
-        const TensorRecord& rec = t.records[t.piece_of[p]];
-        const int64_t from = (int64_t)(p - rec.first_piece) * t.piece;
-        const int n = (int)min((int64_t)t.piece, rec.n - from);
-        for (int at = 8 * threadIdx.x; at < n; at += STEP) {
-            Raw<GRAD32> g;
-            g.load((const char*)rec.grad + from * (GRAD32 ? 4 : 2), at, n - at);
+    for (int64_t first = (int64_t)blockIdx.x * BUNCH; first < t.work; first += (int64_t)gridDim.x * BUNCH) {
+        const char* from[BUNCH];
+        int left[BUNCH];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s = fma((double)g[e], (double)g[e], s);      // (what does not exist was loaded as 0)
+        for (int i = 0; i < BUNCH; ++i) {
+            const int p = (int)min(first + i, (int64_t)t.work - 1);
+            const TensorRecord& rec = t.records[t.piece_of[p]];
+            const int64_t begin = (int64_t)(p - rec.first_piece) * PIECE;
+            from[i] = scalar((const char*)rec.grad + begin * (GRAD32 ? 4 : 2));
+            left[i] = first + i < t.work ? (int)min((int64_t)PIECE, rec.n - begin) - at : 0;
         }
+        Raw<GRAD32> g[BUNCH];
+#pragma unroll
+        for (int i = 0; i < BUNCH; ++i) g[i].load(from[i], at, left[i]);      // (what does not exist is loaded as 0)
+#pragma unroll
+        for (int i = 0; i < BUNCH; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = fma((double)g[i][e], (double)g[i][e], s);
     }
     s = wave_reduce(s, Sum());
     if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = s;
@@ -316,12 +322,19 @@ __global__ __launch_bounds__(SUM_GROUPS) void norm_finish_kernel(const double* p
     if (steps && finite) *steps += 1;
 }
 
+// Workgroups that a CU runs at a time, by LDS that none of them uses: with more, the rows of memory that so many arrays' streams open push one another out.  174 million weights
+// with 32-bit states (seven streams) by 8 / 6 / 4 / 3 / 2 a CU: 960 / 947 / 921 / 895 / 926 us; without masters 698 / 691 / 662 / 645 / 740; 272 million with 8-bit states and masters (nine, short
+// ones among them) 855 / 847 / 783 / 818 / 1011.  With 8-bit states alone issue needs them all: 480 / 480 / 514 / 608 / 808.
+constexpr int resident_lds(bool state8, bool master) { return !state8 ? 52 * 1024 : master ? 40 * 1024 : 0; }
+constexpr int MOST_WORK = 1 << 23;      // pieces of a launch: a grid has fewer than 2^32 threads
 template <bool GRAD32, bool STATE8>
 void launch(const Tensors& t, const Adamw& a, hipStream_t s) {
-    const unsigned grid = (unsigned)t.work;
-    if (!t.has_master) adamw_kernel<GRAD32, STATE8, true, false><<<grid, THREADS, 0, s>>>(t, a);
-    else if (t.has_weight) adamw_kernel<GRAD32, STATE8, true, true><<<grid, THREADS, 0, s>>>(t, a);
-    else adamw_kernel<GRAD32, STATE8, false, true><<<grid, THREADS, 0, s>>>(t, a);
+    for (int first = 0; first < t.work; first += MOST_WORK) {
+        const unsigned grid = (unsigned)std::min(t.work - first, MOST_WORK);
+        if (!t.has_master) adamw_kernel<GRAD32, STATE8, true, false><<<grid, THREADS, resident_lds(STATE8, false), s>>>(t, a, first);
+        else if (t.has_weight) adamw_kernel<GRAD32, STATE8, true, true><<<grid, THREADS, resident_lds(STATE8, true), s>>>(t, a, first);
+        else adamw_kernel<GRAD32, STATE8, false, true><<<grid, THREADS, resident_lds(STATE8, true), s>>>(t, a, first);
+    }
 }
 
 }  // namespace

@@ -114,35 +114,27 @@ struct Span {
     uintptr_t begin, end;
     bool written;
 };
-struct Counts {
-    int64_t pieces;
-    int piece;
-};
-int count_tensors(const qeft_tensor_t* t, int32_t count, Counts* c) {
-    *c = Counts{0, SMALL_PIECE};
+int count_tensors(const qeft_tensor_t* t, int32_t count, int64_t* pieces) {
+    *pieces = 0;
     if (count < 0 || count > QEFT_MAX_TENSORS) return QEFT_ERR_SHAPE;
     if (count > 0 && !t) return QEFT_ERR_NULL;
     for (int32_t i = 0; i < count; ++i) {
         if (t[i].n < 0 || t[i].n > ((int64_t)1 << 40)) return QEFT_ERR_SHAPE;
-        c->pieces += (t[i].n + SMALL_PIECE - 1) / SMALL_PIECE;
+        *pieces += (t[i].n + PIECE - 1) / PIECE;
     }
-    if (c->pieces <= SMALL_WORK) return QEFT_OK;
-    *c = Counts{0, PIECE};
-    for (int32_t i = 0; i < count; ++i) c->pieces += (t[i].n + PIECE - 1) / PIECE;
-    return c->pieces > ((int64_t)1 << 30) ? QEFT_ERR_SHAPE : QEFT_OK;
+    return *pieces > ((int64_t)1 << 30) ? QEFT_ERR_SHAPE : QEFT_OK;
 }
-size_t plan_bytes(int32_t count, const Counts& c) { return tensors_map_at(count) + (size_t)c.pieces * sizeof(int); }
+size_t plan_bytes(int32_t count, int64_t pieces) { return tensors_map_at(count) + (size_t)pieces * sizeof(int); }
 
 int check_list(const qeft_tensors_t* l, Tensors* t) {
     if (!l) return QEFT_ERR_NULL;
-    if (l->count < 0 || l->count > QEFT_MAX_TENSORS || l->work < 0 || l->work > ((int64_t)1 << 30) || (l->piece != PIECE && l->piece != SMALL_PIECE)) return QEFT_ERR_SHAPE;
+    if (l->count < 0 || l->count > QEFT_MAX_TENSORS || l->work < 0 || l->work > ((int64_t)1 << 30)) return QEFT_ERR_SHAPE;
     if ((l->grad_dtype != QEFT_DTYPE_F16 && l->grad_dtype != QEFT_DTYPE_F32) || (l->state_bits != 8 && l->state_bits != 32)) return QEFT_ERR_UNSUPPORTED;
     if (l->work > 0 && !l->plan) return QEFT_ERR_NULL;
     if (!aligned(l->plan, 16)) return QEFT_ERR_ALIGN;
     t->records = (const TensorRecord*)l->plan;
     t->piece_of = (const int*)((const char*)l->plan + tensors_map_at(l->count));
     t->work = (int)l->work;
-    t->piece = l->piece;
     t->grad_f32 = l->grad_dtype == QEFT_DTYPE_F32;
     t->bits = l->state_bits;
     t->has_weight = l->has_weight != 0;
@@ -295,15 +287,15 @@ int qeft_qk_norm_bwd(const qeft_qk_desc_t* desc, const qeft_qk_bwd_t* a, void* s
 }
 
 size_t qeft_tensors_plan_bytes(const qeft_tensor_t* tensors, int32_t count) {
-    Counts c;
-    return count_tensors(tensors, count, &c) == QEFT_OK ? plan_bytes(count, c) : 0;
+    int64_t pieces;
+    return count_tensors(tensors, count, &pieces) == QEFT_OK ? plan_bytes(count, pieces) : 0;
 }
 int qeft_tensors_plan(const qeft_tensor_t* tensors, int32_t count, int32_t grad_dtype, int32_t state_bits, void* plan, size_t bytes, qeft_tensors_t* list) {
     if (!list) return QEFT_ERR_NULL;
-    Counts c;
-    CHECK(count_tensors(tensors, count, &c));
+    int64_t pieces;
+    CHECK(count_tensors(tensors, count, &pieces));
     if ((grad_dtype != QEFT_DTYPE_F16 && grad_dtype != QEFT_DTYPE_F32) || (state_bits != 8 && state_bits != 32)) return QEFT_ERR_UNSUPPORTED;
-    if (plan_bytes(count, c) > bytes || (bytes > 0 && !plan)) return QEFT_ERR_WORKSPACE;
+    if (plan_bytes(count, pieces) > bytes || (bytes > 0 && !plan)) return QEFT_ERR_WORKSPACE;
     if (!aligned(plan, 8)) return QEFT_ERR_ALIGN;
     // the same arrays for every tensor that has values
     const qeft_tensor_t* one = nullptr;
@@ -349,10 +341,10 @@ int qeft_tensors_plan(const qeft_tensor_t* tensors, int32_t count, int32_t grad_
     for (int32_t i = 0; i < count; ++i) {
         const qeft_tensor_t& t = tensors[i];
         rec[i] = TensorRecord{t.weight, t.master, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.n, block, t.decay, (int32_t)piece};
-        for (const int64_t last = piece + (t.n + c.piece - 1) / c.piece; piece < last; ++piece) map[piece] = i;
+        for (const int64_t last = piece + (t.n + PIECE - 1) / PIECE; piece < last; ++piece) map[piece] = i;
         block += (t.n + QEFT_STATE_BLOCK - 1) / QEFT_STATE_BLOCK;
     }
-    *list = qeft_tensors_t{nullptr, piece, c.piece, count, grad_dtype, state_bits, one && one->weight, one && one->master};
+    *list = qeft_tensors_t{nullptr, piece, count, grad_dtype, state_bits, one && one->weight, one && one->master};
     return QEFT_OK;
 }
 int qeft_adamw_step(const qeft_tensors_t* list, const qeft_adamw_t* a, void* stream) {

@@ -317,12 +317,11 @@ struct TensorRecord {
     float decay;
     int32_t first_piece;     // pieces of work before it
 };
-constexpr int PIECE = 8192, SMALL_PIECE = 2048;  // values of a piece of work, whole blocks; lists of at most SMALL_WORK pieces have small ones
-constexpr int SMALL_WORK = 2048;
+constexpr int PIECE = 2048;  // values of a piece of work, whole blocks
 struct Tensors {
     const TensorRecord* records;
     const int* piece_of;     // [work] the tensor of a piece
-    int work, piece, grad_f32, bits, has_weight, has_master;
+    int work, grad_f32, bits, has_weight, has_master;
 };
 inline size_t tensors_map_at(int count) { return (size_t)count * sizeof(TensorRecord); }
 struct Adamw {

@@ -240,7 +240,7 @@ def test_plans_refuse_what_overlaps():
 def test_plans_say_what_is_where():
     t = rows({}, dict(n=0, grad=0, m=0), dict(n=5000, decay=0.5), dict(n=1), n=2048)
     st, out, data, _ = plan(t)
-    assert st == 0 and out.piece == 2048 and (out.work, out.count, out.grad_dtype, out.state_bits, out.has_weight, out.has_master) == (5, 4, 1, 32, 1, 1) and out.plan is None
+    assert st == 0 and (out.work, out.count, out.grad_dtype, out.state_bits, out.has_weight, out.has_master) == (5, 4, 1, 32, 1, 1) and out.plan is None
     records = [struct.unpack_from("<7QqqfI", data, 80 * i) for i in range(4)]
     assert [r[7] for r in records] == [2048, 0, 5000, 1] and [r[8] for r in records] == [0, 16, 16, 56] and [r[10] for r in records] == [0, 1, 1, 4]
     assert [r[9] for r in records[2:]] == [0.5, pytest.approx(0.1)] and records[2][2] == t[2].grad
@@ -248,17 +248,17 @@ def test_plans_say_what_is_where():
     assert plan(t, bytes_=len(data) - 1)[0] == WORKSPACE and plan(t, where=0)[0] == WORKSPACE and plan(t, where=P + 4)[0] == ALIGN
     assert B.raw.qeft_tensors_plan(None, 1, 1, 32, P, 0, ref(out)) == NULL == B.raw.qeft_tensors_plan(t, 4, 1, 32, P, 0, None)
     assert B.raw.qeft_tensors_plan(t, -1, 1, 32, P, 0, ref(out)) == SHAPE and B.raw.qeft_tensors_plan_bytes(t, -1) == 0
-    big = rows({}, dict(n=2), n=1 << 23)              # (more than 2048 pieces of that size: larger ones)
+    big = rows({}, dict(n=2), n=1 << 23)
     big[0].master, big[0].m, big[0].v, big[0].grad = (i << 40 for i in (1, 2, 3, 4))
     big[0].weight = 5 << 40
     st, out, _, _ = plan(big)
-    assert st == 0 and (out.piece, out.work) == (8192, 1025)
+    assert st == 0 and out.work == 4097
     st, out, data, _ = plan(rows({}), 0)
     assert st == 0 and out.work == 0 and data == b""
 
 
 def slist(**over):
-    return struct_of(B.qeft_tensors_t, dict(plan=P, work=3, piece=8192, count=2, grad_dtype=1, state_bits=32, has_weight=1, has_master=1), over)
+    return struct_of(B.qeft_tensors_t, dict(plan=P, work=3, count=2, grad_dtype=1, state_bits=32, has_weight=1, has_master=1), over)
 
 
 def adamw(**over):
@@ -266,7 +266,7 @@ def adamw(**over):
 
 
 @pytest.mark.parametrize("over,status", [
-    (dict(work=-1), SHAPE), (dict(work=(1 << 30) + 1), SHAPE), (dict(piece=4096), SHAPE), (dict(piece=0), SHAPE), (dict(count=-1), SHAPE), (dict(count=(1 << 20) + 1), SHAPE), (dict(plan=0), NULL), (dict(plan=P + 8), ALIGN),
+    (dict(work=-1), SHAPE), (dict(work=(1 << 30) + 1), SHAPE), (dict(count=-1), SHAPE), (dict(count=(1 << 20) + 1), SHAPE), (dict(plan=0), NULL), (dict(plan=P + 8), ALIGN),
     (dict(grad_dtype=2), UNSUPPORTED), (dict(state_bits=4), UNSUPPORTED)])
 def test_lists_that_are_refused(over, status):
     norm = B.qeft_grad_norm_t(1.0, 1.0, P, 0, P, MUCH)

@@ -65,7 +65,7 @@ CHILD = textwrap.dedent('''
             assert data[0] == data[1]
             n += 1
     for work, count, dt, bits in itertools.product((-1, 0, 1, 2**30, 2**30 + 1, 2**62), (-1, 0, 5, 2**20 + 1, big), (0, 1, 2), (8, 32, 33)):
-        l = B.qeft_tensors_t(P, work, 8192, count, dt, bits, 1, 1)
+        l = B.qeft_tensors_t(P, work, count, dt, bits, 1, 1)
         both("qeft_grad_norm_workspace", C.byref(l))
         if work != 0:
             for b1, step in itertools.product((0.0, 0.9, 1.0, -1.0), (-2**63, 0, 1, 2**30, 2**63 - 1)):
