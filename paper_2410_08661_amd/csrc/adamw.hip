@@ -2,8 +2,9 @@
 //
 //   g = factor grad    m = b1 m + (1 - b1) g    v = b2 v + (1 - b2) g^2    w -= lr decay w + lr r m / (sqrt v + eps q),   q = sqrt(1 - b2^t), r = q / (1 - b1^t)
 //
-// Bytes bound it: every value is read and written once.  A workgroup takes a piece of a tensor, a thread eight values at a time; 16 lanes have a block of an
-// 8-bit state, whose largest value they find without LDS.
+// Bytes bound it: every value is read and written once.  A workgroup takes a piece of a tensor, a thread eight values (two or more in turn, the next loaded ahead: 3 to 5 % slower);
+// 16 lanes have a block of an 8-bit state, whose largest value they find without LDS.  174 million weights with fp32 masters and states 895 us (5.8 TB/s, a large device copy
+// 5.1), 272 million with 8-bit states and stochastic rounding 462 (5.9), 38 thousand 4.
 #include <math.h>
 #include <algorithm>
 #include <type_traits>
@@ -117,12 +118,19 @@ __device__ __forceinline__ void encode(const float (&v)[8], const uint32_t (&r)[
     codes.x = finite ? (uint32_t)w[0] : 0x7f7f7f7fu;
     codes.y = finite ? (uint32_t)w[1] : 0x7f7f7f7fu;
 }
-// x rounded to a value of fp16, up where the bits that are cut and 13 random ones carry: below the smallest binade 2^-14 is added for the time being, so that the same
-// bits are cut everywhere.  Not-a-number stays one.
-__device__ __forceinline__ float cut_half(float x, uint32_t r) {
-    const float a = fabsf(x), base = a < 0x1p-14f ? 0x1p-14f : 0.f;
-    const uint32_t bits = min(__builtin_bit_cast(uint32_t, a + base) + r, 0x7fffe000u) & 0xffffe000u;
-    return copysignf(__builtin_bit_cast(float, bits) - base, x);
+// Eight values rounded to fp16 by the 13 bits that begin 8 below a random word's top: up where the bits that are cut and those carry; as a fixed-point number below the
+// smallest binade (compared with that definition for two million values: the same).
+__device__ __forceinline__ u4 cut_halves(const float (&w)[8], const uint32_t (&r)[8]) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    uint32_t x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        h2 pair = {0, 0};
+        pair = __builtin_amdgcn_cvt_sr_f16_f32(pair, w[2 * i], r[2 * i] << 8, false);
+        pair = __builtin_amdgcn_cvt_sr_f16_f32(pair, w[2 * i + 1], r[2 * i + 1] << 8, true);
+        x[i] = __builtin_bit_cast(uint32_t, pair);
+    }
+    return u4{x[0], x[1], x[2], x[3]};
 }
 
 struct Now {      // what the step's number makes
@@ -158,7 +166,7 @@ struct Base {
     char *weight, *master, *m, *v;
     uint8_t *m_scale, *v_scale;
 };
-// Eight values of everything a step reads.  With 8-bit states loads and stores but the master's go past the caches (272 million weights with masters 839 -> 786 us, without 509 -> 500);
+// Eight values of everything a step reads.  With 8-bit states loads and stores but the master's go past the caches (272 million weights with masters 839 -> 786 us, without, to nearest, 494 -> 454);
 // with 32-bit states that gains nothing (895 both ways).
 template <bool GRAD32, bool STATE8, bool MASTER>
 struct Read {
@@ -266,11 +274,8 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Tensors t, Adamw a, int 
     }
     if (MASTER) store<true>(base.master, at, left, w);
     if (WEIGHT) {
-        if (!MASTER && a.stochastic) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = cut_half(w[e], r[e] * 0x5c3c9ccdu >> 19);
-        }
-        store<false>(base.weight, at, left, w, STATE8);
+        if (!MASTER && a.stochastic) store_halves(base.weight, at, left, cut_halves(w, r), STATE8);
+        else store<false>(base.weight, at, left, w, STATE8);
     }
 }
 
@@ -324,7 +329,7 @@ __global__ __launch_bounds__(SUM_GROUPS) void norm_finish_kernel(const double* p
 
 // Workgroups that a CU runs at a time, by LDS that none of them uses: with more, the rows of memory that so many arrays' streams open push one another out.  174 million weights
 // with 32-bit states (seven streams) by 8 / 6 / 4 / 3 / 2 a CU: 960 / 947 / 921 / 895 / 926 us; without masters 698 / 691 / 662 / 645 / 740; 272 million with 8-bit states and masters (nine, short
-// ones among them) 855 / 847 / 783 / 818 / 1011.  With 8-bit states alone issue needs them all: 480 / 480 / 514 / 608 / 808.
+// ones among them) 855 / 847 / 783 / 818 / 1011.  With 8-bit states alone (six, short ones) many are needed: to nearest 451 / 448 / 492 / 586 / 798.
 constexpr int resident_lds(bool state8, bool master) { return !state8 ? 52 * 1024 : master ? 40 * 1024 : 0; }
 constexpr int MOST_WORK = 1 << 23;      // pieces of a launch: a grid has fewer than 2^32 threads
 template <bool GRAD32, bool STATE8>

@@ -82,6 +82,18 @@ template <> struct Raw<true> {
 };
 typedef Raw<false> Half8;
 
+__device__ __forceinline__ void store_halves(void* row, uint32_t at, int left, u4 v, bool once = false) {
+    char* p = (char*)row + 2 * at;
+    if (left >= 8) {
+        place(p, v, once);
+        return;
+    }
+#pragma unroll 1
+    for (int e = 0; e < left; ++e) {
+        *reinterpret_cast<uint16_t*>(p + 2 * e) = (uint16_t)v.x;
+        v = u4{v.x >> 16 | v.y << 16, v.y >> 16 | v.z << 16, v.z >> 16 | v.w << 16, v.w >> 16};
+    }
+}
 // x goes to the row, rounded to its type (which x then is too)
 template <bool F32>
 __device__ __forceinline__ void store(void* row, uint32_t at, int left, float (&x)[8], bool once = false) {
@@ -107,17 +119,7 @@ __device__ __forceinline__ void store(void* row, uint32_t at, int left, float (&
         h[e] = (_Float16)x[e];
         x[e] = (float)h[e];
     }
-    u4 v = __builtin_bit_cast(u4, h);
-    char* p = (char*)row + 2 * at;
-    if (left >= 8) {
-        place(p, v, once);
-        return;
-    }
-#pragma unroll 1
-    for (int e = 0; e < left; ++e) {
-        *reinterpret_cast<uint16_t*>(p + 2 * e) = (uint16_t)v.x;
-        v = u4{v.x >> 16 | v.y << 16, v.y >> 16 | v.z << 16, v.z >> 16 | v.w << 16, v.w >> 16};
-    }
+    store_halves(row, at, left, __builtin_bit_cast(u4, h), once);
 }
 
 }  // namespace qeft
