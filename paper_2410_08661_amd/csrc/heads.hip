@@ -4,7 +4,8 @@
 //   y = x rs w, rs = 1 / sqrt(mean x^2 + eps)     z = R y:  (a, b) -> (a c - b s, b c + a s),  a = y[j], b = y[j + half], half = rot_dim / 2
 //   g = R^T gz     dx = rs (a - xh mean(a xh)),  a = g w, xh = x rs     dw = sum g xh
 //
-// Bytes bound all three.  A head is L lanes', each with two pieces of VW values half apart, so that pairs meet in a lane and the head's sums stay within a row of lanes
+// Bytes bound all three (4096 tokens of 40 + 40 heads of 128 39 us, 4.4 TB/s, or 33 where the caches hold some of it; the gradient of 4001 tokens of 64 + 8 heads 48, 4.6 TB/s;
+// 8 tokens of 32 + 32 heads into a cache 4.8, of which 3.8 a launch that does nothing).  A head is L lanes', each with two pieces of VW values half apart, so that pairs meet in a lane and the head's sums stay within a row of lanes
 // (no LDS); a wave has 64 / L heads side by side.  Heads of all tokens form one sequence that the grid walks through: no lane waits for a token's last heads.  The
 // gradient's workgroups keep their sums for dw in registers and leave one slab each, summed by a second launch in a fixed order.
 #include "pieces.h"
@@ -16,7 +17,7 @@ namespace {
 
 constexpr int THREADS = 256;
 // Workgroups at most.  Forward: as many as run at a time, five a CU (4096 tokens of 40 + 40 heads 38.8 us; 2048 41.7, 10240 - one head a lane - 38.3, but 4096 tokens of 32 + 1 heads
-// of 40 13.9 -> 16.0).  Gradient: two a CU, each leaves a slab (4001 tokens of 64 + 8 heads with 256 / 512 / 768 / 1024 / 2048: 55 / 45 / 47 / 49 / 59 us).
+// of 40, 20 of them turned, 13.9 -> 16.0; 768 33.3 in place of 33.0 where the caches hold some, 16.2 / 13.9).  The append's grid is the same (41.9, by 768 44.6).  Gradient: two a CU, each leaves a slab (4001 tokens of 64 + 8 heads with 256 / 512 / 768 / 1024 / 2048: 55 / 45 / 47 / 49 / 59 us).
 constexpr int FWD_GROUPS = 1280, BWD_GROUPS = 512;
 
 // Lane's r-th two pieces of a head: the rotated ones, half apart, then what is behind them two by two
@@ -361,7 +362,8 @@ __global__ __launch_bounds__(32 * SHARES) void heads_sum_kernel(Heads a, const f
     *at = a.accumulate ? *at + s : s;
 }
 
-// The widest pieces that both halves of a pair consist of, and the lanes of a head: f.template operator()<VW, R, L>()
+// The widest pieces that both halves of a pair consist of, and the lanes of a head: f.template operator()<VW, R, L>().  Pieces of 16 bytes against 8: 4096 tokens of 40 + 40 heads 33 -> 41 us,
+// gradient 49 -> 64.
 struct Form {
     int vw, lanes;
 };

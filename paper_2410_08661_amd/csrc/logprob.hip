@@ -3,7 +3,9 @@
 //   c = scale log2(e)    K = max z c    s = sum 2^(z c - K)    lse = K ln 2 + ln s    logp = (z_t c - K) ln 2 - ln s    entropy = ln s - ln 2 sum 2^u u / s, u = z c - K
 //   dz_j = scale (p_j (dlse - dlogp - dentropy (log p_j + entropy)) + [j = t] dlogp),   p_j = 2^u / s
 //
-// Bytes bound it: a row is read once into registers, by a workgroup or, the longest, by several whose statistics a second launch joins.
+// Bytes bound it: a row is read once into registers, by a workgroup or, the longest, by several whose statistics a second launch joins.  2003 x 32003 fp32, a third of the entries
+// -infinity, 48 us (5.3 TB/s; a large device copy 5.1); 4096 x 32000 fp16 with the gradient in the same call 85 (5.2), without but with 20 alternatives 62.  Few rows: one of 32000 with 5
+// alternatives 6.2 us, of which 3.8 a launch that does nothing, 57 x 130001 with 20 12.9.
 // z c - K is one multiply-add, K as it was rounded: what rounding K costs is in lse alone.  K is finite where the row is empty, so that -infinity minus it stays what it is.
 #include <math.h>
 #include <algorithm>
@@ -410,9 +412,9 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
 // ---- the gradient alone -------------------------------------------------------------------------------------------------
 constexpr int CHUNK = 8192;      // values of a workgroup
 template <bool F32>
-__global__ __launch_bounds__(256) void logprob_bwd_kernel(Logprob a, int chunks) {
-    const int64_t row = blockIdx.x / chunks;
-    const int from = (int)(blockIdx.x - row * chunks) * CHUNK, n = min(CHUNK, a.n - from);
+__global__ __launch_bounds__(256) void logprob_bwd_kernel(Logprob a, int chunks, int64_t first) {
+    const int64_t row = first + blockIdx.x / chunks;
+    const int from = (int)(blockIdx.x % chunks) * CHUNK, n = min(CHUNK, a.n - from);
     const char* z = row_at(a.z, row, a.ldz, F32) + (size_t)from * (F32 ? 4 : 2);
     char* dz = row_at(a.dz, row, a.lddz, F32) + (size_t)from * (F32 ? 4 : 2);
     const int token = a.token ? a.token[row] : -1;
@@ -435,6 +437,7 @@ struct Plan {
     size_t keys_at, lse_at, bytes;
 };
 constexpr size_t PARTS_BYTES = 64 << 20;      // of a workspace at most: more rows go in rounds
+constexpr int64_t MOST_THREADS = (int64_t)1 << 31;      // of a launch (a grid has fewer than 2^32): more go in rounds too
 constexpr int FINER = 32768, FINER_FROM = 98304, FINER_GROUPS = 256;
 Plan plan_of(int n, bool f32, int64_t m, int top) {
     const int most = f32 ? 8 : 16;      // octets that a thread of 1024 holds beside its work: 64 registers
@@ -447,6 +450,8 @@ Plan plan_of(int n, bool f32, int64_t m, int top) {
     if (n > FINER_FROM && finer > parts && m * finer <= FINER_GROUPS) parts = finer;
     p.parts = parts;
     int per = ceil_div(octets, parts);
+    // As few threads as hold a row in some octets each, where rows are many; where they are few more would be quicker.  With 64 / 256 / 1024 threads 4000 fp16 rows of 500: 5.6 / 7.8 / 22.7 us,
+    // of 2000: 6.3 / 7.8 / 22.9, of 8000: 16.9 / 14.4 / 24.8; 64 rows of 4000 with 5 alternatives 8.1 / 5.4, of 8000 10.4 / 5.8 / 5.4; of 16000 with 256 / 1024 threads 6.7 / 5.9, 4000 of them 24.2 / 30.6.
     const int threads = per <= 256 ? 64 : per <= 2048 ? 256 : 1024;
     int v = 1;
     while (v * threads < per) v *= 2;
@@ -456,7 +461,7 @@ Plan plan_of(int n, bool f32, int64_t m, int top) {
     if (parts == 1) return p;
     p.parts = parts = ceil_div(n, p.len);
     const size_t row = (size_t)parts * (sizeof(Stats) + top * sizeof(uint64_t));
-    p.rows = std::min(m, (int64_t)(PARTS_BYTES / row));
+    p.rows = std::min({m, (int64_t)(PARTS_BYTES / row), MOST_THREADS / 1024 / parts});
     p.keys_at = (size_t)p.rows * parts * sizeof(Stats) + 15 & ~(size_t)15;
     p.lse_at = p.rows < m ? PARTS_BYTES + 16 : p.keys_at + (size_t)p.rows * parts * top * sizeof(uint64_t);
     p.bytes = p.lse_at + (size_t)m * 2 * sizeof(float);
@@ -478,7 +483,8 @@ void launch_rows(const Plan& q, const Logprob& a, const Part& p, hipStream_t s) 
 template <bool F32>
 void launch_bwd(const Logprob& a, hipStream_t s) {
     const int chunks = ceil_div(a.n, CHUNK);
-    logprob_bwd_kernel<F32><<<(unsigned)(a.m * chunks), 256, 0, s>>>(a, chunks);
+    const int64_t most = (MOST_THREADS / 256) / chunks;
+    for (int64_t first = 0; first < a.m; first += most) logprob_bwd_kernel<F32><<<(unsigned)(std::min(most, a.m - first) * chunks), 256, 0, s>>>(a, chunks, first);
 }
 template <bool F32>
 void launch_fwd(const Logprob& a, hipStream_t s) {
