@@ -438,14 +438,15 @@ struct Plan {
 };
 constexpr size_t PARTS_BYTES = 64 << 20;      // of a workspace at most: more rows go in rounds
 constexpr int64_t MOST_THREADS = (int64_t)1 << 31;      // of a launch (a grid has fewer than 2^32): more go in rounds too
-constexpr int FINER = 32768, FINER_FROM = 98304, FINER_GROUPS = 256;
+constexpr int FINER = 32768, FINER_FROM = 65536, FINER_GROUPS = 256;
 Plan plan_of(int n, bool f32, int64_t m, int top) {
     const int most = f32 ? 8 : 16;      // octets that a thread of 1024 holds beside its work: 64 registers
     Plan p{};
     const int octets = ceil_div(n, 8), fit = 1024 * most;
     int parts = ceil_div(octets, fit);
     // A CU takes 9 us for 130000 values (exponentials and sums, 260 KB): where there are CUs for all of them, parts of 32768 values save more than the join's launch
-    // costs.  1 x 130001 with 20 alternatives 15.7 -> 12.5 us, 57 x 130001 16.2 -> 14.4, 16 x 262144 18.7 -> 11.9; 1 x 64000 would go 9.0 -> 11.2.
+    // costs.  1 x 130001 with 20 alternatives 15.7 -> 12.5 us, 57 x 130001 16.2 -> 14.4, 16 x 262144 18.7 -> 11.9, 1 x 68849 13.0 -> 11.3, without alternatives 10.0 -> 8.6 (the gradient
+    // in the same call, then a third launch, 12.9 -> 14.8, at 130001 15.8 -> 14.1); 1 x 50257 would go 8.8 -> 10.4.
     const int finer = ceil_div(n, FINER);
     if (n > FINER_FROM && finer > parts && m * finer <= FINER_GROUPS) parts = finer;
     p.parts = parts;
