@@ -4,7 +4,7 @@
 //
 // Bytes bound it: every value is read and written once.  A workgroup takes a piece of a tensor, a thread eight values (two or more in turn, the next loaded ahead: 3 to 5 % slower);
 // 16 lanes have a block of an 8-bit state, whose largest value they find without LDS.  174 million weights with fp32 masters and states 895 us (5.8 TB/s, a large device copy
-// 5.1), 272 million with 8-bit states and stochastic rounding 462 (5.9), 38 thousand 4.
+// 5.1), 272 million with 8-bit states and stochastic rounding 456 (6.0), 38 thousand 4.
 #include <math.h>
 #include <algorithm>
 #include <type_traits>
@@ -118,7 +118,7 @@ __device__ __forceinline__ void encode(const float (&v)[8], const uint32_t (&r)[
     codes.x = finite ? (uint32_t)w[0] : 0x7f7f7f7fu;
     codes.y = finite ? (uint32_t)w[1] : 0x7f7f7f7fu;
 }
-// Eight values rounded to fp16 by the 13 bits that begin 8 below a random word's top: up where the bits that are cut and those carry; as a fixed-point number below the
+// Eight values rounded to fp16 by the 13 top bits of a random word's product with an odd constant (the word's own ends round the states): up where the bits that are cut and those carry; as a fixed-point number below the
 // smallest binade (compared with that definition for two million values: the same).
 __device__ __forceinline__ u4 cut_halves(const float (&w)[8], const uint32_t (&r)[8]) {
     typedef _Float16 h2 __attribute__((ext_vector_type(2)));
@@ -126,8 +126,8 @@ __device__ __forceinline__ u4 cut_halves(const float (&w)[8], const uint32_t (&r
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         h2 pair = {0, 0};
-        pair = __builtin_amdgcn_cvt_sr_f16_f32(pair, w[2 * i], r[2 * i] << 8, false);
-        pair = __builtin_amdgcn_cvt_sr_f16_f32(pair, w[2 * i + 1], r[2 * i + 1] << 8, true);
+        pair = __builtin_amdgcn_cvt_sr_f16_f32(pair, w[2 * i], r[2 * i] * 0x5c3c9ccdu, false);
+        pair = __builtin_amdgcn_cvt_sr_f16_f32(pair, w[2 * i + 1], r[2 * i + 1] * 0x5c3c9ccdu, true);
         x[i] = __builtin_bit_cast(uint32_t, pair);
     }
     return u4{x[0], x[1], x[2], x[3]};
@@ -166,7 +166,7 @@ struct Base {
     char *weight, *master, *m, *v;
     uint8_t *m_scale, *v_scale;
 };
-// Eight values of everything a step reads.  With 8-bit states loads and stores but the master's go past the caches (272 million weights with masters 839 -> 786 us, without, to nearest, 494 -> 454);
+// Eight values of everything a step reads.  With 8-bit states loads and stores but the master's go past the caches (272 million weights with masters 839 -> 786 us, without 494 -> 454);
 // with 32-bit states that gains nothing (895 both ways).
 template <bool GRAD32, bool STATE8, bool MASTER>
 struct Read {

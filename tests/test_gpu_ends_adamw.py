@@ -58,7 +58,7 @@ def check_step(p, before, lr, step, decays, stochastic=False, seed=0, factor=1.0
         elif not stochastic:
             V.close("weight", p["weights"][i], new, ew, V.HALF)
         else:
-            u = (dice >> 11) % 8192 / 8192.0
+            u = ((dice * 0x5C3C9CCD) % (1 << 32) >> 19).double() / 8192
             got = p["weights"][i].double() * new.sign()
             ok = V.rounded_within(got, new.abs(), ew, u, 2.0 ** -13, 10, 2.0 ** -14) | (new.abs() < ew)
             bad = (~ok).nonzero()[:3, 0]
