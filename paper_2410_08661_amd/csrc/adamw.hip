@@ -257,10 +257,10 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Tensors t, Adamw a, int 
         const bool finite = most_v < 0x7f800000u && most_m < INFINITY;
         const uint32_t bm = block_power<true>(most_m, finite), bv = block_power<false>(__builtin_bit_cast(float, most_v), finite);
         Codes cm, cv;
-        uint32_t dv[8];
+        uint32_t dm[8], dv[8];      // (the instruction would take 20 bits)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dv[e] = r[e] << 16;
-        encode<true>(m, r, cm, bm, finite);
+        for (int e = 0; e < 8; ++e) dm[e] = r[e] & 0xffff0000u, dv[e] = r[e] << 16;
+        encode<true>(m, dm, cm, bm, finite);
         encode<false>(v, dv, cv, bv, finite);
         cm.store((uint8_t*)base.m + (uint32_t)at, left);
         cv.store((uint8_t*)base.v + (uint32_t)at, left);

@@ -79,7 +79,7 @@ def check_step(p, before, lr, step, decays, stochastic=False, seed=0, factor=1.0
             got = V.state_values(p[name][i], p[name + "_scales"][i], name, n) / scale
             got = got * torch.where(x < 0, -1.0, 1.0) if name == "m" else got
             a = x.abs() / scale
-            ok = V.rounded_within(got, a, e / scale, u.double() / 65536, 2.0 ** -16, mant, least)
+            ok = V.rounded_within(got, a, e / scale, u.double() / 65536, 0.0, mant, least)
             if name == "v":
                 ok |= (got == 2.0 ** -16) & (a < 2.0 ** -15)
                 assert bool((got > 0)[x > 0].all())
@@ -139,6 +139,25 @@ def test_zero_states_and_gradients():
         before = [t.clone() for t in w]
         B.qeft_adamw_step(B.TensorList(g, weights=w, **s), 0.1, 1)
         assert all(torch.equal(a, b) for a, b in zip(w, before)) and not any(bool(t.any()) for ts in s.values() for t in ts)
+
+
+def test_8_bit_states_are_rounded_by_16_bits():
+    """From moments that fp32 holds exactly (halves of fp16 gradients and of their squares), every code is the definition's."""
+    n, step, seed = 1 << 21, 3, 11
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    g = (torch.randn(n, generator=gen, device="cuda") * torch.exp2(torch.randint(-8, 3, (n,), generator=gen, device="cuda").float())).half()
+    p = dict(grads=[g], weights=[torch.zeros(n, dtype=torch.float16, device="cuda")])
+    p["m"], p["v"] = ([torch.zeros(n, dtype=torch.uint8, device="cuda")] for _ in range(2))
+    p["m_scales"], p["v_scales"] = ([torch.zeros(n // B.QEFT_STATE_BLOCK, dtype=torch.uint8, device="cuda")] for _ in range(2))
+    B.qeft_adamw_step(B.TensorList(**p), 1e-3, step, beta1=0.5, beta2=0.5, seed=seed)
+    dice, g = V.dice(0, n, step, seed), g.double()
+    for name, x, mant, least, u in (("m", 0.5 * g, 3, 2.0 ** -6, dice >> 16), ("v", 0.5 * g * g, 2, 2.0 ** -14, dice % 65536)):
+        scale = torch.exp2(p[name + "_scales"][0].double() - 127).repeat_interleave(B.QEFT_STATE_BLOCK)
+        want = V.on_grid(x.abs() / scale, u.double() / 65536, mant, least)
+        if name == "v":
+            want = torch.where((want == 0) & (x > 0), 2.0 ** -16, want)
+        got = V.state_values(p[name][0], p[name + "_scales"][0], name, n) / scale
+        assert torch.equal(got.abs(), want) and bool((got * x >= 0).all())
 
 
 def test_8_bit_states_keep_the_mean():
