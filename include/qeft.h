@@ -465,13 +465,14 @@ int qeft_norm_bwd(const qeft_norm_desc_t* desc, const qeft_norm_bwd_t* a, void* 
  * The conventions above hold; tokens, positions, step counts and factors that lie in device memory are clamped or make a row or a step be left out as
  * stated, so that no value leads to an access outside the buffers described. */
 
-/* Log probabilities.  With x = scale * z for logits z [m][ldz] of n entries (fp16 or fp32 by dtype; scale > 0, one over the temperature),
+/* Log probabilities.  With x = scale * z for logits z [m][ldz] of n entries (fp16 or fp32 by dtype; scale > 0, at most 2^126, one over the temperature),
  *     lse = log sum_j exp x_j     logp = x_token - lse     entropy = lse - sum_j p_j x_j, p = exp(x - lse)
  * and the `top` likeliest entries, in order of z, equal ones by index: top_index and their log probabilities top_logp, both [m][ld_top].
  * token int32 [m]; NULL: no logp.  A row whose token is not in 0 .. n - 1 is left out: its logp, lse and entropy are 0, it has no alternatives, and it is
  * not read.  An entry of -infinity has no probability and is no alternative; where there are fewer than `top` others, top_index is -1 and top_logp
  * -infinity.  A row of nothing else: lse and logp -infinity, entropy 0, gradient 0.  Not-a-number and +infinity make their row's lse, logp, entropy, top_logp and
- * gradient not-a-number; top_index counts not-a-number above +infinity.  Sums and exponentials are fp32; scale * z is taken to be below 2^120 in size.  logp, lse, entropy (fp32 [m]) and both top arrays may be
+ * gradient not-a-number; top_index counts not-a-number above +infinity.  Sums and exponentials are fp32, of differences from the row's largest logit, so that logp,
+ * entropy and the alternatives are as exact for large scale * z as for small; lse is infinite where fp32 does not reach, and finite logits count as infinitely far apart from 2^128 on.  logp, lse, entropy (fp32 [m]) and both top arrays may be
  * NULL (top = 0: both must be, and the other way round).
  * qeft_logprob_bwd: with the gradients dlogp, dlse, dentropy (fp32 [m], NULL: 0) of those three, and lse and entropy (needed with dentropy) as the forward gave them,
  *     dz_j = scale * (dlogp ([j = token] - p_j) + dlse p_j - dentropy p_j (log p_j + entropy))

@@ -1,12 +1,14 @@
 // Log probabilities of given tokens, entropies and likeliest tokens from rows of logits, and the gradient of the logits (qeft_logprob_fwd, _bwd, _fwd_bwd).
 //
-//   c = scale log2(e)    K = max z c    s = sum 2^(z c - K)    lse = K ln 2 + ln s    logp = (z_t c - K) ln 2 - ln s    entropy = ln s - ln 2 sum 2^u u / s, u = z c - K
+//   M = max z    u = (z - M) scale log2(e)    s = sum 2^u    lse = scale M + ln s    logp = scale (z_t - M) - ln s    entropy = ln s - ln 2 sum 2^u u / s
 //   dz_j = scale (p_j (dlse - dlogp - dentropy (log p_j + entropy)) + [j = t] dlogp),   p_j = 2^u / s
 //
 // Bytes bound it: a row is read once into registers, by a workgroup or, the longest, by several whose statistics a second launch joins.  2003 x 32003 fp32, a third of the entries
 // -infinity, 48 us (5.3 TB/s; a large device copy 5.1); 4096 x 32000 fp16 with the gradient in the same call 85 (5.2), without but with 20 alternatives 62.  Few rows: one of 32000 with 5
 // alternatives 6.2 us, of which 3.8 a launch that does nothing, 57 x 130001 with 20 12.9.
-// z c - K is one multiply-add, K as it was rounded: what rounding K costs is in lse alone.  K is finite where the row is empty, so that -infinity minus it stays what it is.
+// u is exact to roundings of its own size, 0 for the largest logit, so that what a large scale z costs is in lse alone: one multiply-add z c - K, c = scale log2(e), K = M c as rounded, which
+// leaves all u off by K's error r, known exactly; r goes into the factor that brings a wave's sums to the row's M.  Where K is so large that r would not be small, (z - M) c: an instruction
+// more (4096 x 32000 with 20 alternatives 66 -> 71 us).  M is finite where the row is empty, so that -infinity minus it stays what it is.
 #include <math.h>
 #include <algorithm>
 #include "octets.h"
@@ -17,7 +19,7 @@ namespace qeft {
 namespace {
 
 constexpr float LN2 = 0.693147180559945f, LOG2E = 1.44269504088896f;
-constexpr float LEAST = -3e38f;      // a finite bound of K
+constexpr float LEAST = -3.402823466e38f;      // the lowest finite number: a finite bound of M, which a row of nothing but it reaches
 constexpr float FAR = -200.f;        // 2^u is 0 from here down: u may stop here, where it is a factor beside 2^u
 
 constexpr uint32_t RANK_NEG_INF = 0x007fffffu, RANK_NAN = 0xff800001u;      // (one above +infinity's)
@@ -103,10 +105,16 @@ __device__ __forceinline__ void left_out(const Logprob& a, int64_t row) {
 }
 
 // ---- rows in registers ------------------------------------------------------------------------------------------------
-struct Stats {       // of a part of a row, relative to its own k
-    float k, s, t;
+struct Stats {       // of a part of a row, relative to its own largest logit
+    float most, s, t;
 };
-__device__ __forceinline__ float shrink(float from, float to) { return fmaxf(from - to, FAR); }      // (2^FAR is 0: what is further away adds nothing)
+constexpr float NEAR = 0x1p23f;      // K below which its error is at most 1/2
+// K's error where it is below that
+__device__ __forceinline__ float residue(float most, float c) {
+    const float k = most * c;
+    return fabsf(k) < NEAR ? fmaf(most, c, -k) : 0.f;
+}
+__device__ __forceinline__ float shrink(float from, float to, float c) { return fmaxf((from - to) * c, FAR); }      // (2^FAR is 0: what is further away adds nothing)
 
 // A term of a sum over lanes: rounded for itself.  Joined with the sum's first addition it would be rounded otherwise in the lane that adds it than in the lane it is added
 // to, and the lanes' sums would differ.
@@ -128,19 +136,19 @@ __device__ __forceinline__ float logit_at(const Logprob& a, const char* row, int
 // A row's numbers from its joined statistics, by one thread; zt: the token's logit
 __device__ __forceinline__ void put_row(const Logprob& a, const Part& p, int64_t row, float zt, const Stats& x, float ln_s, float entropy) {
     const bool empty = x.s == 0.f;
-    const float lse = empty ? -INFINITY : fmaf(x.k, LN2, ln_s);
+    const float lse = empty ? -INFINITY : fmaf(x.most, a.scale, ln_s);
     if (a.lse) a.lse[row] = lse;
     if (a.entropy) a.entropy[row] = entropy;
     if (p.lse) {
         p.lse[row] = lse;
         p.entropy[row] = entropy;
     }
-    if (a.logp) a.logp[row] = empty ? -INFINITY : fmaf(fmaf(zt, a.scale * LOG2E, -x.k), LN2, -ln_s);
+    if (a.logp) a.logp[row] = empty ? -INFINITY : fmaf(zt - x.most, a.scale, -ln_s);
 }
-__device__ __forceinline__ void put_top(const Logprob& a, int64_t row, int i, uint64_t key, float k, float ln_s) {
+__device__ __forceinline__ void put_top(const Logprob& a, int64_t row, int i, uint64_t key, float most, float ln_s) {
     const bool there = (uint32_t)(key >> 32) > RANK_NEG_INF;
     a.top_index[row * a.ld_top + i] = there ? (int)~(uint32_t)key : -1;
-    a.top_logp[row * a.ld_top + i] = there ? fmaf(fmaf(value_of(key >> 32), a.scale * LOG2E, -k), LN2, -ln_s) : -INFINITY;
+    a.top_logp[row * a.ld_top + i] = there ? fmaf(value_of(key >> 32) - most, a.scale, -ln_s) : -INFINITY;
 }
 
 // The largest `top` keys of a workgroup, by rounds: each() calls its argument with every key of the thread.  For what the list of candidates does not hold.
@@ -226,7 +234,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     for (int i = 0; i < V; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) mine = fmaxf(mine, v[i][e]);
-    Stats x{fmaxf(wave_reduce(mine, MostFloat()) * c, LEAST), 0.f, 0.f};
+    Stats x{fmaxf(wave_reduce(mine, MostFloat()), LEAST), 0.f, 0.f};
     // (kept as loaded between the steps, not as twice the registers of converted values)
     auto pin = [&] {
 #pragma unroll
@@ -251,25 +259,30 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     const bool wants_t = a.entropy || p.lse || (GRAD && a.dentropy);
     {
         float s[2] = {}, t[2] = {};
+        auto sums = [&](const auto& u_of) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (wants_t) {
+            for (int i = 0; i < V; ++i) {
+                if (wants_t) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float u = fmaf(v[i][e], c, -x.k), y = __builtin_amdgcn_exp2f(u);
-                    s[e & 1] += y;
-                    t[e & 1] = fmaf(y, fmaxf(u, FAR), t[e & 1]);
+                    for (int e = 0; e < 8; ++e) {
+                        const float u = u_of(v[i][e]), y = __builtin_amdgcn_exp2f(u);
+                        s[e & 1] += y;
+                        t[e & 1] = fmaf(y, fmaxf(u, FAR), t[e & 1]);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[e & 1] += __builtin_amdgcn_exp2f(u_of(v[i][e]));
                 }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[e & 1] += __builtin_amdgcn_exp2f(fmaf(v[i][e], c, -x.k));
             }
-        }
+        };
+        const float k = x.most * c;
+        if (fabsf(k) < NEAR) sums([&](float z) { return fmaf(z, c, -k); });
+        else sums([&](float z) { return (z - x.most) * c; });
         x.s = wave_reduce(s[0] + s[1], Sum());
         if (wants_t) x.t = wave_reduce(t[0] + t[1], Sum());
     }
     if (lane == 0) {
-        buf[0][wave] = x.k;
+        buf[0][wave] = x.most;
         buf[1][wave] = x.s;
         buf[2][wave] = x.t;
     }
@@ -278,10 +291,14 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
         const int w = lane & 15;
         const bool there = w < waves;
         const Stats y{there ? buf[0][w] : LEAST, there ? buf[1][w] : 0.f, there ? buf[2][w] : 0.f};
-        x.k = row_reduce(y.k, MostFloat());
-        const float d = shrink(y.k, x.k), f = __builtin_amdgcn_exp2f(d);
+        x.most = row_reduce(y.most, MostFloat());
+        const float d = shrink(y.most, x.most, c) - residue(y.most, c), f = __builtin_amdgcn_exp2f(d);
         x.s = row_reduce(term(y.s, f), Sum());
         x.t = row_reduce(term(f, fmaf(d, y.s, y.t)), Sum());
+    } else {
+        const float d = -residue(x.most, c), f = __builtin_amdgcn_exp2f(d);
+        x.t = f * fmaf(d, x.s, x.t);
+        x.s *= f;
     }
     pin();
     const bool empty = x.s == 0.f;
@@ -295,7 +312,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
         // their values are: the threads are listed, then all look through the listed ones' values, read again.  The few candidates are ordered by comparing each with each.  Rows where
         // many are (equal logits) or with not-a-number, which no maximum shows, go by rounds.
         auto put = [&](int i, uint64_t key) {
-            if (p.parts == 1) put_top(a, row, i, key, x.k, ln_s);
+            if (p.parts == 1) put_top(a, row, i, key, x.most, ln_s);
             else p.keys[(size_t)blockIdx.x * a.top + i] = key;
         };
         uint32_t bound = 0;
@@ -352,7 +369,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     } else {
         char* dz = row_at(a.dz, row, a.lddz, F32);
         if (empty) return zero_row<F32>(dz, a.n);
-        const Slope g = make_slope(a, row, token, x.k + log2f(x.s), entropy);
+        const Slope g = make_slope(a, row, token, fmaf(x.most, c, log2f(x.s)), entropy);
         Raw<F32> x = v[0];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -386,8 +403,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
     if (t == 0) used = 0;
     auto joined = [&](auto v, auto* slots, auto none, const auto& op) { return alone ? wave_reduce(v, op) : group_reduce(v, slots, none, op); };
     Stats x;
-    x.k = joined(y.k, buf[0], LEAST, MostFloat());
-    const float d = shrink(y.k, x.k), f = __builtin_amdgcn_exp2f(d);
+    x.most = joined(y.most, buf[0], LEAST, MostFloat());
+    const float d = shrink(y.most, x.most, a.scale * LOG2E), f = __builtin_amdgcn_exp2f(d);
     x.s = joined(term(y.s, f), buf[1], 0.f, Sum());
     x.t = joined(term(f, fmaf(d, y.s, y.t)), buf[2], 0.f, Sum());
     const float ln_s = logf(x.s), entropy = x.s == 0.f ? 0.f : ln_s - LN2 * (x.t / x.s);
@@ -402,7 +419,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
     }
     __syncthreads();
     const int count = used;
-    auto put = [&](int at, uint64_t key) { put_top(a, row, at, key, x.k, ln_s); };
+    auto put = [&](int at, uint64_t key) { put_top(a, row, at, key, x.most, ln_s); };
     if (count <= CANDIDATES) top_of_list(a.top, list, count, put);
     else top_by_rounds(a.top, slots, [&](auto&& g) {
         for (int j = t; j < total; j += blockDim.x) g(keys[j]);

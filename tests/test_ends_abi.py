@@ -333,3 +333,10 @@ def test_random_numbers_are_spread():
     assert float((same - 0.5).abs().max()) < 5 * s
     flipped = ((h ^ V.stir((x ^ 1) + V.stir(12345) & 0xFFFFFFFF))[:, None] >> torch.arange(32)) & 1
     assert float((flipped.double().mean(0) - 0.5).abs().max()) < 8 * s
+
+
+def test_scales_of_logits():
+    """scale log2 e has to be a finite number."""
+    for scale, status in ((2.0 ** 126, 0), (1e-38, 0), (2.0 ** 126 * (1 + 2.0 ** -23), SHAPE), (3.4e38, SHAPE)):
+        d = B.qeft_logprob_desc_t(100, 0, scale)
+        assert fwd(d, m=0) == bwd(d, m=0) == both(d, f=dict(m=0), m=0) == status
