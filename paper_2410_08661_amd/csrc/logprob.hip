@@ -1,7 +1,7 @@
 // Log probabilities of given tokens, entropies and likeliest tokens from rows of logits, and the gradient of the logits (qeft_logprob_fwd, _bwd, _fwd_bwd).
 //
 //   M = max z    u = (z - M) scale log2(e)    s = sum 2^u    lse = scale M + ln s    logp = scale (z_t - M) - ln s    entropy = ln s - ln 2 sum 2^u u / s
-//   dz_j = scale (p_j (dlse - dlogp - dentropy (log p_j + entropy)) + [j = t] dlogp),   p_j = 2^u / s
+//   dz_j = scale (p_j (dlse - dlogp - dentropy (log p_j + entropy)) + [j = t] dlogp),   p_j = 2^u (1 / s)
 //
 // Bytes bound it: a row is read once into registers, by a workgroup or, the longest, by several whose statistics a second launch joins.  2003 x 32003 fp32, a third of the entries
 // -infinity, 48 us (5.3 TB/s; a large device copy 5.1); 4096 x 32000 fp16 with the gradient in the same call 85 (5.2), without but with 20 alternatives 62.  Few rows: one of 32000 with 5
@@ -53,17 +53,20 @@ struct MostFloat {
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }   // (passes over not-a-number)
 };
 
-// What a row's gradient needs: u = z c - k2, p = 2^u, log p = u ln 2, dz = p (a - dh u), and at_token more at the token
+// What a row's gradient needs: u = (z by - off) c, p = 2^u share, dz = 2^u (a - dh u), and at_token more at the token
 struct Slope {
-    float c, k2, a, dh, at_token;
+    float by, off, c, a, dh, at_token;
     int token;
 };
-__device__ __forceinline__ Slope make_slope(const Logprob& a, int64_t row, int token, float k2, float entropy) {
+// distance: entropy + log share, so that log p + entropy = u ln 2 + distance.  The share stays a factor: as a summand beside the largest logit it would be rounded at that size,
+// and all probabilities be off by one factor.
+__device__ __forceinline__ Slope make_slope(const Logprob& a, int64_t row, int token, float by, float off, float c, float share, float distance) {
     const float dl = a.dlogp ? a.dlogp[row] : 0.f, ds = a.dlse ? a.dlse[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
-    return Slope{a.scale * LOG2E, k2, a.scale * (ds - dl - (dh != 0.f ? dh * entropy : 0.f)), a.scale * dh * LN2, a.scale * dl, a.token ? token : -1};
+    return Slope{by, off, c, a.scale * (ds - dl - (dh != 0.f ? dh * distance : 0.f)) * share, a.scale * dh * LN2 * share, a.scale * dl, a.token ? token : -1};
 }
+__device__ __forceinline__ float u_of(const Slope& g, float z) { return fmaf(z, g.by, -g.off) * g.c; }
 __device__ __forceinline__ float slope_of(const Slope& g, float z) {
-    const float u = fmaf(z, g.c, -g.k2);
+    const float u = u_of(g, z);
     return __builtin_amdgcn_exp2f(u) * fmaf(-g.dh, fmaxf(u, FAR), g.a);      // (p is 0 where u is far, not-a-number where u is)
 }
 template <bool F32>
@@ -75,7 +78,7 @@ __device__ __forceinline__ void put_slopes(const Slope& g, const Raw<F32>& v, ch
         for (int e = 0; e < 8; ++e) x[e] = slope_of(g, v[e]);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(v[e], g.c, -g.k2)) * g.a;
+        for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(u_of(g, v[e])) * g.a;
     }
     if ((uint32_t)(g.token - at) < 8u) {
 #pragma unroll
@@ -259,19 +262,19 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     const bool wants_t = a.entropy || p.lse || (GRAD && a.dentropy);
     {
         float s[2] = {}, t[2] = {};
-        auto sums = [&](const auto& u_of) {
+        auto sums = [&](const auto& far) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 if (wants_t) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float u = u_of(v[i][e]), y = __builtin_amdgcn_exp2f(u);
+                        const float u = far(v[i][e]), y = __builtin_amdgcn_exp2f(u);
                         s[e & 1] += y;
                         t[e & 1] = fmaf(y, fmaxf(u, FAR), t[e & 1]);
                     }
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) s[e & 1] += __builtin_amdgcn_exp2f(u_of(v[i][e]));
+                    for (int e = 0; e < 8; ++e) s[e & 1] += __builtin_amdgcn_exp2f(far(v[i][e]));
                 }
             }
         };
@@ -369,7 +372,8 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     } else {
         char* dz = row_at(a.dz, row, a.lddz, F32);
         if (empty) return zero_row<F32>(dz, a.n);
-        const Slope g = make_slope(a, row, token, fmaf(x.most, c, log2f(x.s)), entropy);
+        const float share = 1.f / x.s;
+        const Slope g = make_slope(a, row, token, 1.f, x.most, c, share, -LN2 * x.t * share);
         Raw<F32> x = v[0];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -438,7 +442,7 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(Logprob a, int chunks,
     if (a.token && (token < 0 || token >= a.n)) return zero_row<F32>(dz, n);
     const float lse = a.lse_in[row];
     if (lse == -INFINITY) return zero_row<F32>(dz, n);
-    const Slope g = make_slope(a, row, token - from, lse * LOG2E, a.entropy_in ? a.entropy_in[row] : 0.f);
+    const Slope g = make_slope(a, row, token - from, a.scale * LOG2E, lse * LOG2E, 1.f, 1.f, a.entropy_in ? a.entropy_in[row] : 0.f);
     Raw<F32> v[CHUNK / 2048];
 #pragma unroll
     for (int i = 0; i < CHUNK / 2048; ++i) v[i].load(z, 8 * threadIdx.x + 2048 * i, n - (int)(8 * threadIdx.x + 2048 * i));

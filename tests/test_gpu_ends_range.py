@@ -118,3 +118,33 @@ def test_rows_of_the_lowest_value_and_of_nothing(n):
             assert abs(float(lse[i]) - (0.5 * x + math.log(n))) <= 2 * U * abs(0.5 * x) and ix[i].tolist() == [0, 1]
             assert torch.equal(lp[i], logp[i].expand(2))
         assert lse[1] == logp[1] == -math.inf and entropy[1] == 0 and ix[1].tolist() == [-1, -1]
+
+
+def some_gradients(m, scale, gen):
+    return [torch.randn(m, generator=gen, device="cuda") * min(1 / scale, 1e30) for _ in range(3)]
+
+
+def check_one_call(f32, offset, std, scale, lowest, m, n):
+    gen = torch.Generator(device="cuda").manual_seed(zlib.crc32(repr((f32, offset, scale, m, n, "g")).encode()))
+    scale = exact32(scale)
+    z = rows(m, n, f32, offset, std, lowest, gen)
+    token = torch.randint(0, n, (m,), generator=gen, device="cuda").int()
+    token[0] = n // 2
+    desc = B.make_logprob_desc(n, z.dtype, scale)
+    _, r = reference(z, token, scale)
+    g = some_gradients(m, scale, gen)
+    want, bound = gradient(r, token, scale, *g)
+    V.close("dz", B.qeft_logprob_fwd_bwd(desc, z, token, *g)[0], want, bound, V.ROUNDING[z.dtype])
+    # a loss moves no row's sum: probabilities and the token's one, however large the logits
+    none = torch.zeros(m, device="cuda")
+    want, bound = gradient(r, token, scale, g[0], none, none)
+    dz = B.qeft_logprob_fwd_bwd(desc, z, token, g[0])[0]
+    V.close("dz of a loss", dz, want, bound, V.ROUNDING[z.dtype])
+    room = bound + V.ROUNDING[z.dtype] * want.abs() + (V.TINY if not f32 else 0.0)
+    assert bool((dz.double().sum(1).abs() <= room.sum(1)).all())
+
+
+@pytest.mark.parametrize("m,n", [(3, 40), (3, 4099), (3, 32000), (200, 65536)])
+@pytest.mark.parametrize("f32,offset,std,scale,lowest", RANGES)
+def test_gradient_in_one_call_of_large_scaled_logits(f32, offset, std, scale, lowest, m, n):
+    check_one_call(f32, offset, std, scale, lowest, m, n)
