@@ -126,12 +126,18 @@ __device__ __forceinline__ float term(float a, float b) {
     return a * b;
 }
 
+// Of a row whose statistics are at hand
+__device__ __forceinline__ Slope make_slope(const Logprob& a, int64_t row, int token, const Stats& x) {
+    const float share = 1.f / x.s;
+    return make_slope(a, row, token, 1.f, x.most, a.scale * LOG2E, share, -LN2 * x.t * share);
+}
+
 // Where a workgroup's part of a row goes: to the call's outputs, or, one of several parts, to the workspace
 struct Part {
     int parts, len;        // parts of a row, values of one
     Stats* stats;          // [m][parts]
     uint64_t* keys;        // [m][parts][top], largest first
-    float *lse, *entropy;  // [m], for a gradient that follows
+    Stats* joined;         // [m] of whole rows, for a gradient that follows
 };
 constexpr int CANDIDATES = 1024;
 
@@ -142,10 +148,7 @@ __device__ __forceinline__ void put_row(const Logprob& a, const Part& p, int64_t
     const float lse = empty ? -INFINITY : fmaf(x.most, a.scale, ln_s);
     if (a.lse) a.lse[row] = lse;
     if (a.entropy) a.entropy[row] = entropy;
-    if (p.lse) {
-        p.lse[row] = lse;
-        p.entropy[row] = entropy;
-    }
+    if (p.joined) p.joined[row] = x;
     if (a.logp) a.logp[row] = empty ? -INFINITY : fmaf(zt - x.most, a.scale, -ln_s);
 }
 __device__ __forceinline__ void put_top(const Logprob& a, int64_t row, int i, uint64_t key, float most, float ln_s) {
@@ -259,7 +262,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
             if (threadIdx.x < 2) used[threadIdx.x] = 0;
         }
     }
-    const bool wants_t = a.entropy || p.lse || (GRAD && a.dentropy);
+    const bool wants_t = a.entropy || a.dentropy;
     {
         float s[2] = {}, t[2] = {};
         auto sums = [&](const auto& far) {
@@ -372,8 +375,7 @@ __global__ __launch_bounds__(1024) void logprob_row_kernel(Logprob a, Part p) {
     } else {
         char* dz = row_at(a.dz, row, a.lddz, F32);
         if (empty) return zero_row<F32>(dz, a.n);
-        const float share = 1.f / x.s;
-        const Slope g = make_slope(a, row, token, 1.f, x.most, c, share, -LN2 * x.t * share);
+        const Slope g = make_slope(a, row, token, x);
         Raw<F32> x = v[0];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -432,17 +434,24 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(Logprob a, Part p) {
 
 // ---- the gradient alone -------------------------------------------------------------------------------------------------
 constexpr int CHUNK = 8192;      // values of a workgroup
-template <bool F32>
-__global__ __launch_bounds__(256) void logprob_bwd_kernel(Logprob a, int chunks, int64_t first) {
+template <bool F32, bool JOINED>
+__global__ __launch_bounds__(256) void logprob_bwd_kernel(Logprob a, const Stats* joined, int chunks, int64_t first) {
     const int64_t row = first + blockIdx.x / chunks;
     const int from = (int)(blockIdx.x % chunks) * CHUNK, n = min(CHUNK, a.n - from);
     const char* z = row_at(a.z, row, a.ldz, F32) + (size_t)from * (F32 ? 4 : 2);
     char* dz = row_at(a.dz, row, a.lddz, F32) + (size_t)from * (F32 ? 4 : 2);
     const int token = a.token ? a.token[row] : -1;
     if (a.token && (token < 0 || token >= a.n)) return zero_row<F32>(dz, n);
-    const float lse = a.lse_in[row];
-    if (lse == -INFINITY) return zero_row<F32>(dz, n);
-    const Slope g = make_slope(a, row, token - from, a.scale * LOG2E, lse * LOG2E, 1.f, 1.f, a.entropy_in ? a.entropy_in[row] : 0.f);
+    Slope g;
+    if constexpr (JOINED) {
+        const Stats x = joined[row];
+        if (x.s == 0.f) return zero_row<F32>(dz, n);
+        g = make_slope(a, row, token - from, x);
+    } else {
+        const float lse = a.lse_in[row];
+        if (lse == -INFINITY) return zero_row<F32>(dz, n);
+        g = make_slope(a, row, token - from, a.scale * LOG2E, lse * LOG2E, 1.f, 1.f, a.entropy_in ? a.entropy_in[row] : 0.f);
+    }
     Raw<F32> v[CHUNK / 2048];
 #pragma unroll
     for (int i = 0; i < CHUNK / 2048; ++i) v[i].load(z, 8 * threadIdx.x + 2048 * i, n - (int)(8 * threadIdx.x + 2048 * i));
@@ -455,7 +464,7 @@ struct Plan {
     int threads, octets;     // of a workgroup, a thread
     int parts, len;          // parts of a row
     int64_t rows;            // that the workspace holds the parts of
-    size_t keys_at, lse_at, bytes;
+    size_t keys_at, joined_at, bytes;
 };
 constexpr size_t PARTS_BYTES = 64 << 20;      // of a workspace at most: more rows go in rounds
 constexpr int64_t MOST_THREADS = (int64_t)1 << 31;      // of a launch (a grid has fewer than 2^32): more go in rounds too
@@ -485,8 +494,8 @@ Plan plan_of(int n, bool f32, int64_t m, int top) {
     const size_t row = (size_t)parts * (sizeof(Stats) + top * sizeof(uint64_t));
     p.rows = std::min({m, (int64_t)(PARTS_BYTES / row), MOST_THREADS / 1024 / parts});
     p.keys_at = (size_t)p.rows * parts * sizeof(Stats) + 15 & ~(size_t)15;
-    p.lse_at = p.rows < m ? PARTS_BYTES + 16 : p.keys_at + (size_t)p.rows * parts * top * sizeof(uint64_t);
-    p.bytes = p.lse_at + (size_t)m * 2 * sizeof(float);
+    p.joined_at = p.rows < m ? PARTS_BYTES + 16 : p.keys_at + (size_t)p.rows * parts * top * sizeof(uint64_t);
+    p.bytes = p.joined_at + (size_t)m * sizeof(Stats);
     return p;
 }
 
@@ -503,15 +512,19 @@ void launch_rows(const Plan& q, const Logprob& a, const Part& p, hipStream_t s) 
     }
 }
 template <bool F32>
-void launch_bwd(const Logprob& a, hipStream_t s) {
+void launch_bwd(const Logprob& a, const Stats* joined, hipStream_t s) {
     const int chunks = ceil_div(a.n, CHUNK);
     const int64_t most = (MOST_THREADS / 256) / chunks;
-    for (int64_t first = 0; first < a.m; first += most) logprob_bwd_kernel<F32><<<(unsigned)(std::min(most, a.m - first) * chunks), 256, 0, s>>>(a, chunks, first);
+    for (int64_t first = 0; first < a.m; first += most) {
+        const unsigned grid = (unsigned)(std::min(most, a.m - first) * chunks);
+        if (joined) logprob_bwd_kernel<F32, true><<<grid, 256, 0, s>>>(a, joined, chunks, first);
+        else logprob_bwd_kernel<F32, false><<<grid, 256, 0, s>>>(a, joined, chunks, first);
+    }
 }
 template <bool F32>
 void launch_fwd(const Logprob& a, hipStream_t s) {
     const Plan q = plan_of(a.n, F32, a.m, a.top);
-    Part p{q.parts, q.len, nullptr, nullptr, nullptr, nullptr};
+    Part p{q.parts, q.len, nullptr, nullptr, nullptr};
     if (q.parts == 1) {
         if (a.dz) launch_rows<F32, true>(q, a, p, s);
         else launch_rows<F32, false>(q, a, p, s);
@@ -519,7 +532,7 @@ void launch_fwd(const Logprob& a, hipStream_t s) {
     }
     p.stats = (Stats*)a.ws;
     p.keys = (uint64_t*)(a.ws + q.keys_at);
-    float* const lse = a.dz ? (float*)(a.ws + q.lse_at) : nullptr;
+    Stats* const joined = a.dz ? (Stats*)(a.ws + q.joined_at) : nullptr;
     for (int64_t from = 0; from < a.m; from += q.rows) {
         Logprob b = a;
         b.m = std::min(q.rows, a.m - from);
@@ -529,16 +542,11 @@ void launch_fwd(const Logprob& a, hipStream_t s) {
         };
         later(b.token, from), later(b.logp, from), later(b.lse, from), later(b.entropy, from);
         later(b.top_logp, from * a.ld_top), later(b.top_index, from * a.ld_top);
-        p.lse = lse ? lse + from : nullptr;
-        p.entropy = lse ? lse + a.m + from : nullptr;
+        p.joined = joined ? joined + from : nullptr;
         launch_rows<F32, false>(q, b, p, s);
         logprob_join_kernel<<<(unsigned)b.m, q.parts <= 64 && a.top == 0 ? 64 : 256, 0, s>>>(b, p);
     }
-    if (!a.dz) return;
-    Logprob b = a;
-    b.lse_in = lse;
-    b.entropy_in = lse + a.m;
-    launch_bwd<F32>(b, s);
+    if (a.dz) launch_bwd<F32>(a, joined, s);
 }
 
 }  // namespace
@@ -556,8 +564,8 @@ hipError_t logprob_fwd(const Logprob& a, hipStream_t s) {
 }
 
 hipError_t logprob_bwd(const Logprob& a, hipStream_t s) {
-    if (a.f32) launch_bwd<true>(a, s);
-    else launch_bwd<false>(a, s);
+    if (a.f32) launch_bwd<true>(a, nullptr, s);
+    else launch_bwd<false>(a, nullptr, s);
     return hipGetLastError();
 }
 

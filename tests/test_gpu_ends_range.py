@@ -148,3 +148,9 @@ def check_one_call(f32, offset, std, scale, lowest, m, n):
 @pytest.mark.parametrize("f32,offset,std,scale,lowest", RANGES)
 def test_gradient_in_one_call_of_large_scaled_logits(f32, offset, std, scale, lowest, m, n):
     check_one_call(f32, offset, std, scale, lowest, m, n)
+
+
+@pytest.mark.parametrize("m,n", [(2, 140001), (300, 132001)])
+@pytest.mark.parametrize("f32,offset,std,scale,lowest", RANGES)
+def test_gradient_in_one_call_of_large_scaled_logits_in_parts(f32, offset, std, scale, lowest, m, n):
+    check_one_call(f32, offset, std, scale, lowest, m, n)
