@@ -476,7 +476,8 @@ int qeft_norm_bwd(const qeft_norm_desc_t* desc, const qeft_norm_bwd_t* a, void* 
  * NULL (top = 0: both must be, and the other way round).
  * qeft_logprob_bwd: with the gradients dlogp, dlse, dentropy (fp32 [m], NULL: 0) of those three, and lse and entropy (needed with dentropy) as the forward gave them,
  *     dz_j = scale * (dlogp ([j = token] - p_j) + dlse p_j - dentropy p_j (log p_j + entropy))
- * of dtype, [m][lddz], which may be z itself; a row that is left out gets zeros.  dlogp needs token.
+ * of dtype, [m][lddz], which may be z itself; a row that is left out gets zeros.  dlogp needs token.  p is exp(x - lse) of the lse given: that lse is rounded to fp32 makes all probabilities
+ * of a row off by up to |lse| 2^-24 of themselves, which qeft_logprob_fwd_bwd's are not.
  * qeft_logprob_fwd_bwd: both in one call, where the gradients are known before: fwd's lse, logp and entropy if asked for (no alternatives: top = 0), and dz; lse
  * and entropy of the bwd struct, and its z and token, are not looked at.  Each row is read once if its n values fit a workgroup's registers (131072 fp16 or 65536 fp32).
  * ws: qeft_logprob_workspace bytes, 16-byte aligned, for fwd and fwd_bwd (0 bytes: NULL will do); what m rows and `top` alternatives need does for fewer of either too.  n at most QEFT_MAX_DIM, top at most QEFT_MAX_TOP and n, m at most QEFT_MAX_ROWS.

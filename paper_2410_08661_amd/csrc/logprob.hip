@@ -1,7 +1,7 @@
 // Log probabilities of given tokens, entropies and likeliest tokens from rows of logits, and the gradient of the logits (qeft_logprob_fwd, _bwd, _fwd_bwd).
 //
 //   M = max z    u = (z - M) scale log2(e)    s = sum 2^u    lse = scale M + ln s    logp = scale (z_t - M) - ln s    entropy = ln s - ln 2 sum 2^u u / s
-//   dz_j = scale (p_j (dlse - dlogp - dentropy (log p_j + entropy)) + [j = t] dlogp),   p_j = 2^u (1 / s)
+//   dz_j = scale (p_j (dlse - dlogp - dentropy (log p_j + entropy)) + [j = t] dlogp),   p_j = 2^u (1 / s), or exp(scale z_j - lse) of a given lse
 //
 // Bytes bound it: a row is read once into registers, by a workgroup or, the longest, by several whose statistics a second launch joins.  2003 x 32003 fp32, a third of the entries
 // -infinity, 48 us (5.3 TB/s; a large device copy 5.1); 4096 x 32000 fp16 with the gradient in the same call 85 (5.2), without but with 20 alternatives 62.  Few rows: one of 32000 with 5
@@ -441,20 +441,23 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(Logprob a, const Stats
     const char* z = row_at(a.z, row, a.ldz, F32) + (size_t)from * (F32 ? 4 : 2);
     char* dz = row_at(a.dz, row, a.lddz, F32) + (size_t)from * (F32 ? 4 : 2);
     const int token = a.token ? a.token[row] : -1;
-    if (a.token && (token < 0 || token >= a.n)) return zero_row<F32>(dz, n);
+    bool none = a.token && (token < 0 || token >= a.n);
     Slope g;
-    if constexpr (JOINED) {
-        const Stats x = joined[row];
-        if (x.s == 0.f) return zero_row<F32>(dz, n);
-        g = make_slope(a, row, token - from, x);
-    } else {
-        const float lse = a.lse_in[row];
-        if (lse == -INFINITY) return zero_row<F32>(dz, n);
-        g = make_slope(a, row, token - from, a.scale * LOG2E, lse * LOG2E, 1.f, 1.f, a.entropy_in ? a.entropy_in[row] : 0.f);
-    }
     Raw<F32> v[CHUNK / 2048];
+    if (!none) {
 #pragma unroll
-    for (int i = 0; i < CHUNK / 2048; ++i) v[i].load(z, 8 * threadIdx.x + 2048 * i, n - (int)(8 * threadIdx.x + 2048 * i));
+        for (int i = 0; i < CHUNK / 2048; ++i) v[i].load(z, 8 * threadIdx.x + 2048 * i, n - (int)(8 * threadIdx.x + 2048 * i));
+        if constexpr (JOINED) {
+            const Stats x = joined[row];
+            none = x.s == 0.f;
+            g = make_slope(a, row, token - from, x);
+        } else {
+            const float lse = a.lse_in[row];
+            none = lse == -INFINITY;
+            g = make_slope(a, row, token - from, a.scale, lse, LOG2E, 1.f, a.entropy_in ? a.entropy_in[row] : 0.f);
+        }
+    }
+    if (none) return zero_row<F32>(dz, n);
 #pragma unroll
     for (int i = 0; i < CHUNK / 2048; ++i) put_slopes(g, v[i], dz, 8 * threadIdx.x + 2048 * i, n - (int)(8 * threadIdx.x + 2048 * i));
 }

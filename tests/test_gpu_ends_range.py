@@ -154,3 +154,42 @@ def test_gradient_in_one_call_of_large_scaled_logits(f32, offset, std, scale, lo
 @pytest.mark.parametrize("f32,offset,std,scale,lowest", RANGES)
 def test_gradient_in_one_call_of_large_scaled_logits_in_parts(f32, offset, std, scale, lowest, m, n):
     check_one_call(f32, offset, std, scale, lowest, m, n)
+
+
+@pytest.mark.parametrize("m,n", [(3, 40), (3, 4099), (3, 32000), (2, 140001)])
+@pytest.mark.parametrize("f32,offset,std,scale,lowest", [r for r in RANGES if max(abs(r[1]), 4 * r[2]) * r[3] <= 1e5])
+def test_gradient_of_large_scaled_logits_by_a_stored_lse(f32, offset, std, scale, lowest, m, n):
+    """As exact as lse is as fp32, which is U of its size."""
+    gen = torch.Generator(device="cuda").manual_seed(zlib.crc32(repr((f32, offset, scale, m, n, "s")).encode()))
+    scale = exact32(scale)
+    z = rows(m, n, f32, offset, std, lowest, gen)
+    token = torch.randint(0, n, (m,), generator=gen, device="cuda").int()
+    desc = B.make_logprob_desc(n, z.dtype, scale)
+    _, lse, entropy, _, _ = B.qeft_logprob_fwd(desc, z, token)
+    _, r = reference(z, token, scale)
+    g = some_gradients(m, scale, gen)
+    kept = torch.expm1((U * r["lse"].abs() + r["eln"])[:, None] + 4 * U * r["logp"].abs())
+    want, bound = gradient(r, token, scale, *g, kept=kept)
+    V.close("dz", B.qeft_logprob_bwd(desc, z, lse, token=token, dlogp=g[0], dlse=g[1], entropy=entropy, dentropy=g[2]), want, bound, V.ROUNDING[z.dtype])
+
+
+@pytest.mark.parametrize("n", [40, 4099, 32000])
+@pytest.mark.parametrize("offset,std,scale", [(0.0, 3.0, 1.0), (1e3, 3.0, 1.0), (1e3, 3.0, 0.7), (3e4, 3.0, 1.3), (-1e6, 3.0, 1.7), (5.8145e6, 20.0, 1.0), (5.8145e6, 20.0, 1 / 3), (1e9, 200.0, 0.9), (0.0, 4.0, 1e5), (1e20, 1e16, 1e-19),
+                                              (0.0, 1e4, 1e25)])
+def test_gradient_of_logits_by_a_given_lse(offset, std, scale, n):
+    """dlse p with p = exp(scale z - lse) of the lse that is given: what the forward's is off by does not grow on the way.  The argument: the factor's two roundings and the multiply-add's (or
+    difference, log2 e and product), 4 U of its distance; the exponential 2 U, its share's 2 U and those of the argument's known error, below 4 U; three products."""
+    gen = torch.Generator(device="cuda").manual_seed(zlib.crc32(repr((offset, scale, n)).encode()))
+    scale = exact32(scale)
+    z = rows(3, n, True, offset, std, 0.0, gen)
+    desc = B.make_logprob_desc(n, torch.float32, scale)
+    lse = (z.double().amax(1) * scale + math.log(n)).float()        # (near the forward's)
+    g = some_gradients(3, scale, gen)[0]
+    x = z.double() * scale - lse.double()[:, None]
+    p = x.exp()
+    want = scale * g.double()[:, None] * p
+    bound = want.abs() * (4 * U * torch.where(p > 0, x, 0.0).abs() + 12 * U) + scale * g.double().abs()[:, None] * 2.0 ** -125
+    dz, want = B.qeft_logprob_bwd(desc, z, lse, dlse=g), finite(want)      # (an lse rounded far below the largest: infinity)
+    inf = want.isinf()
+    assert torch.equal(dz.double()[inf], want[inf])
+    V.close("dz", dz[~inf], want[~inf], bound[~inf], U)
