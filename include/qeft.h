@@ -479,7 +479,8 @@ int qeft_norm_bwd(const qeft_norm_desc_t* desc, const qeft_norm_bwd_t* a, void* 
  * of dtype, [m][lddz], which may be z itself; a row that is left out gets zeros.  dlogp needs token.  p is exp(x - lse) of the lse given: that lse is rounded to fp32 makes all probabilities
  * of a row off by up to |lse| 2^-24 of themselves, which qeft_logprob_fwd_bwd's are not.
  * qeft_logprob_fwd_bwd: both in one call, where the gradients are known before: fwd's lse, logp and entropy if asked for (no alternatives: top = 0), and dz; lse
- * and entropy of the bwd struct, and its z and token, are not looked at.  Each row is read once if its n values fit a workgroup's registers (131072 fp16 or 65536 fp32).
+ * and entropy of the bwd struct, and its z and token, are not looked at.  Each row is read once if its n values fit a workgroup's registers (131072 fp16 or
+ * 65536 fp32), but for a few rows of more than 65536 (256 parts of 32768 values in all), which several workgroups go over twice.
  * ws: qeft_logprob_workspace bytes, 16-byte aligned, for fwd and fwd_bwd (0 bytes: NULL will do); what m rows and `top` alternatives need does for fewer of either too.  n at most QEFT_MAX_DIM, top at most QEFT_MAX_TOP and n, m at most QEFT_MAX_ROWS.
  * Rows of logits and gradients are 16-byte aligned, pitches multiples of 8; those of the alternatives any from `top`. */
 #define QEFT_MAX_TOP 64

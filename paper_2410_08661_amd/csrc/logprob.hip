@@ -478,8 +478,9 @@ Plan plan_of(int n, bool f32, int64_t m, int top) {
     const int octets = ceil_div(n, 8), fit = 1024 * most;
     int parts = ceil_div(octets, fit);
     // A CU takes 9 us for 130000 values (exponentials and sums, 260 KB): where there are CUs for all of them, parts of 32768 values save more than the join's launch
-    // costs.  1 x 130001 with 20 alternatives 15.7 -> 12.5 us, 57 x 130001 16.2 -> 14.4, 16 x 262144 18.7 -> 11.9, 1 x 68849 13.0 -> 11.3, without alternatives 10.0 -> 8.6 (the gradient
-    // in the same call, then a third launch, 12.9 -> 14.8, at 130001 15.8 -> 14.1); 1 x 50257 would go 8.8 -> 10.4.
+    // costs.  1 x 130001 with 20 alternatives 15.7 -> 12.5 us, 57 x 130001 16.2 -> 14.4, 16 x 262144 18.7 -> 11.9, 1 x 68849 13.0 -> 11.3, without alternatives 10.0 -> 8.6; 1 x 50257 would go
+    // 8.8 -> 10.4.  With the gradient in the same call the parts mean a third launch and a second read, and gain all the same: waited for, 1 x 68849 14.6 -> 12.7, 1 x 130001 17.8 -> 12.5,
+    // 60 x 100001 18.6 -> 17.6; behind one another 11.9 -> 12.0, 15.2 -> 12.1, 60 x 115001 17.1 -> 15.6 (60 x 68849 13.3 -> 13.5).
     const int finer = ceil_div(n, FINER);
     if (n > FINER_FROM && finer > parts && m * finer <= FINER_GROUPS) parts = finer;
     p.parts = parts;
