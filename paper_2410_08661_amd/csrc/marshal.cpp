@@ -689,6 +689,9 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t argc) {
         const qeft_tensors_t* l = list_of(c, a[0], a[1]);
         if (!l || !c.ok) return false;
         qeft_adamw_t p{};
+        // (a tensor of a subclass is binding.py's: as a number its value would be asked for, which waits for the GPU and breaks a capture)
+        for (PyObject* o : {a[2], a[3]})
+            if (!PyFloat_Check(o) && !PyLong_Check(o) && !THPVariable_CheckExact(o) && THPVariable_Check(o)) return false;
         if (THPVariable_CheckExact(a[2])) p.lr_at = (const float*)number_at(c, a[2], at::kFloat);
         else p.lr = c.real(a[2]);
         if (THPVariable_CheckExact(a[3])) p.step_at = (const int32_t*)number_at(c, a[3], at::kInt);
