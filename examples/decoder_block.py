@@ -165,7 +165,7 @@ class Tuner:
         return dh, dy
 
     def step(self, h, token, rot, lr, seed=0):
-        """One step on a sequence of embeddings h (fp32) and the tokens to predict (negative: none): the mean loss, and the gradients' norm and factor."""
+        """One step on a sequence of embeddings h (fp32) and the tokens to predict (outside the vocabulary: none): the mean loss, and the gradients' norm and factor."""
         norm, pos = B.make_norm_desc(h.shape[1], torch.float32), torch.arange(h.shape[0], dtype=torch.int32, device="cuda")
         y, saved = None, []
         for i in range(len(self.blocks)):
@@ -173,7 +173,7 @@ class Tuner:
             saved.append(kept)
         h, x = B.qeft_norm_fwd(norm, h, self.w_last, y=y)
         logits = B.qeft_linear_fwd(self.head.desc, self.head.weight, x)
-        count = (token >= 0).sum()
+        count = ((token >= 0) & (token < self.head.desc.out_features)).sum().clamp(min=1)
         weight = (-self.loss_scale / count).expand(token.shape).contiguous().float()
         loss = B.make_logprob_desc(self.head.desc.out_features)
         dz, logp, _, _ = B.qeft_logprob_fwd_bwd(loss, logits, token, weight, dz=logits, entropy=False)
