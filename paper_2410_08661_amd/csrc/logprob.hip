@@ -4,8 +4,8 @@
 //   dz_j = scale (p_j (dlse - dlogp - dentropy (log p_j + entropy)) + [j = t] dlogp),   p_j = 2^u (1 / s), or exp(scale z_j - lse) of a given lse
 //
 // Bytes bound it: a row is read once into registers, by a workgroup or, the longest, by several whose statistics a second launch joins.  2003 x 32003 fp32, a third of the entries
-// -infinity, 48 us (5.3 TB/s; a large device copy 5.1); 4096 x 32000 fp16 with the gradient in the same call 85 (5.2), without but with 20 alternatives 62.  Few rows: one of 32000 with 5
-// alternatives 6.2 us, of which 3.8 a launch that does nothing, 57 x 130001 with 20 12.9.
+// -infinity, 48 us (5.3 TB/s; a large device copy 5.1); 4096 x 32000 fp16 with the gradient in the same call 85 (5.2), without but with entropies and 20 alternatives 66.  Few rows: one of
+// 32000 with 5 alternatives 6.4 us, of which 3.8 a launch that does nothing, 57 x 130001 with 20 13.1.
 // u is exact to roundings of its own size, 0 for the largest logit, so that what a large scale z costs is in lse alone: one multiply-add z c - K, c = scale log2(e), K = M c as rounded, which
 // leaves all u off by K's error r, known exactly; r goes into the factor that brings a wave's sums to the row's M.  Where K is so large that r would not be small, (z - M) c: an instruction
 // more (4096 x 32000 with 20 alternatives 66 -> 71 us).  M is finite where the row is empty, so that -infinity minus it stays what it is.
