@@ -472,12 +472,12 @@ int qeft_norm_bwd(const qeft_norm_desc_t* desc, const qeft_norm_bwd_t* a, void* 
  * not read.  An entry of -infinity has no probability and is no alternative; where there are fewer than `top` others, top_index is -1 and top_logp
  * -infinity.  A row of nothing else: lse and logp -infinity, entropy 0, gradient 0.  Not-a-number and +infinity make their row's lse, logp, entropy, top_logp and
  * gradient not-a-number; top_index counts not-a-number above +infinity.  Sums and exponentials are fp32, of differences from the row's largest logit, so that logp,
- * entropy and the alternatives are as exact for large scale * z as for small; lse is infinite where fp32 does not reach, and finite logits count as infinitely far apart from 2^128 on.  logp, lse, entropy (fp32 [m]) and both top arrays may be
- * NULL (top = 0: both must be, and the other way round).
+ * entropy and the alternatives are as exact for large scale * z as for small; lse is infinite where fp32 does not reach, and finite logits count as infinitely
+ * far apart from 2^128 on.  logp, lse, entropy (fp32 [m]) and both top arrays may be NULL (top = 0: both must be, and the other way round).
  * qeft_logprob_bwd: with the gradients dlogp, dlse, dentropy (fp32 [m], NULL: 0) of those three, and lse and entropy (needed with dentropy) as the forward gave them,
  *     dz_j = scale * (dlogp ([j = token] - p_j) + dlse p_j - dentropy p_j (log p_j + entropy))
- * of dtype, [m][lddz], which may be z itself; a row that is left out gets zeros.  dlogp needs token.  p is exp(x - lse) of the lse given: that lse is rounded to fp32 makes all probabilities
- * of a row off by up to |lse| 2^-24 of themselves, which qeft_logprob_fwd_bwd's are not.
+ * of dtype, [m][lddz], which may be z itself; a row that is left out gets zeros.  dlogp needs token.  p is exp(x - lse) of the
+ * lse given: that lse is rounded to fp32 makes all probabilities of a row off by up to |lse| 2^-24 of themselves, which qeft_logprob_fwd_bwd's are not.
  * qeft_logprob_fwd_bwd: both in one call, where the gradients are known before: fwd's lse, logp and entropy if asked for (no alternatives: top = 0), and dz; lse
  * and entropy of the bwd struct, and its z and token, are not looked at.  Each row is read once if its n values fit a workgroup's registers (131072 fp16 or
  * 65536 fp32), but for a few rows of more than 65536 (256 parts of 32768 values in all), which several workgroups go over twice.
@@ -557,7 +557,7 @@ int qeft_cache_append_norm(const qeft_cache_desc_t* desc, const qeft_cache_t* ca
 
 /* The optimizer: one step of AdamW (Loshchilov and Hutter) over a list of tensors in one launch.  For each value, with gradient g = factor * grad and in step t
  *     m = beta1 m + (1 - beta1) g     v = beta2 v + (1 - beta2) g^2     w = w - lr decay w - lr (m / c1) / (sqrt(v / c2) + eps),  c = 1 - beta^t
- * in fp32.  A tensor is n contiguous values: grad (fp16 or fp32, grad_dtype), the weight fp16 and / or its fp32 copy `master` (at least one; where there are both, master is
+ * in fp32 (with 8-bit states the root and the reciprocal to a unit of its last place).  A tensor is n contiguous values: grad (fp16 or fp32, grad_dtype), the weight fp16 and / or its fp32 copy `master` (at least one; where there are both, master is
  * what is updated and weight its rounding), and the states m, v: fp32, or 8 bits.  All arrays but the scales are 16-byte aligned and none of those that are written may overlap another; all
  * tensors of a list have the same arrays (all a master or none ...).  decay: a tensor's own weight decay.
  * 8-bit states (state_bits == 8): m is n bytes of e4m3 (OCP, finite), v n bytes of e5m2, and m_scale, v_scale one byte e8m0 (2^(byte - 127)) for every QEFT_STATE_BLOCK values, the last
