@@ -465,7 +465,7 @@ int qeft_norm_bwd(const qeft_norm_desc_t* desc, const qeft_norm_bwd_t* a, void* 
  * The conventions above hold; tokens, positions, step counts and factors that lie in device memory are clamped or make a row or a step be left out as
  * stated, so that no value leads to an access outside the buffers described. */
 
-/* Log probabilities.  With x = scale * z for logits z [m][ldz] of n entries (fp16 or fp32 by dtype; scale > 0, at most 2^126, one over the temperature),
+/* Log probabilities.  With x = scale * z for logits z [m][ldz] of n entries (fp16 or fp32 by dtype; scale > 0, below 2^128 ln 2, one over the temperature),
  *     lse = log sum_j exp x_j     logp = x_token - lse     entropy = lse - sum_j p_j x_j, p = exp(x - lse)
  * and the `top` likeliest entries, in order of z, equal ones by index: top_index and their log probabilities top_logp, both [m][ld_top].
  * token int32 [m]; NULL: no logp.  A row whose token is not in 0 .. n - 1 is left out: its logp, lse and entropy are 0, it has no alternatives, and it is

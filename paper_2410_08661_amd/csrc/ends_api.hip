@@ -31,7 +31,7 @@ int check_workspace(const void* ws, size_t have, size_t need) {
 // ---- log probabilities ----
 int check_logprob_desc(const qeft_logprob_desc_t* d) {
     if (!d) return QEFT_ERR_NULL;
-    if (d->n <= 0 || d->n > QEFT_MAX_DIM || !(d->scale > 0.f) || !(d->scale <= 0x1p126f)) return QEFT_ERR_SHAPE;
+    if (d->n <= 0 || d->n > QEFT_MAX_DIM || !(d->scale > 0.f) || !(d->scale * 1.44269504f < INFINITY)) return QEFT_ERR_SHAPE;
     return d->dtype == QEFT_DTYPE_F16 || d->dtype == QEFT_DTYPE_F32 ? QEFT_OK : QEFT_ERR_UNSUPPORTED;
 }
 int check_top(const qeft_logprob_desc_t* d, int64_t m, int32_t top) {

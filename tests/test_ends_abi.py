@@ -337,6 +337,6 @@ def test_random_numbers_are_spread():
 
 def test_scales_of_logits():
     """scale log2 e has to be a finite number."""
-    for scale, status in ((2.0 ** 126, 0), (1e-38, 0), (2.0 ** 126 * (1 + 2.0 ** -23), SHAPE), (3.4e38, SHAPE)):
+    for scale, status in ((2.0 ** 127, 0), (2.3586e38, 0), (1e-38, 0), (2.3587e38, SHAPE), (3.4e38, SHAPE)):
         d = B.qeft_logprob_desc_t(100, 0, scale)
         assert fwd(d, m=0) == bwd(d, m=0) == both(d, f=dict(m=0), m=0) == status
